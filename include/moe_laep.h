@@ -70,7 +70,8 @@ enum {
   MOE_DEV_TOO_FEW_LIVE = 2,  /* a token saw fewer than k live experts */
   MOE_DEV_COUNT_MISMATCH = 3,/* counts disagree with the routing */
   MOE_DEV_WAIT_TIMEOUT = 4,  /* a pipeline wait in a GEMM kernel gave up */
-  MOE_DEV_ROWS_OVERFLOW = 5  /* grouped layout would exceed R rows */
+  MOE_DEV_ROWS_OVERFLOW = 5, /* grouped layout would exceed R rows */
+  MOE_DEV_BAD_OFFSETS = 6    /* seq_offsets descend or leave [0, T] */
 };
 
 /* Library version (major*10000 + minor*100 + patch). */
@@ -146,6 +147,54 @@ int moe_route(const uint16_t *x, const float *w_router, const float *bias,
  */
 int moe_load_stats(const int32_t *topk_idx, int T, int k, int E, int32_t *counts,
                    int accumulate, moe_stream_t stream);
+
+/*
+ * moe_balance_loss - auxiliary losses of a routing and the statistics they are made
+ * of: the load-balance loss (the losses that the paper compares LAEP with, "Mixtral" and
+ * "DeepSeek-V3" in its tables, the latter per sequence), the router z-loss, and per-expert counts.
+ * Sequence s holds tokens [seq_offsets[s], seq_offsets[s+1]); with seq_offsets NULL
+ * (n_seq = 1) one sequence holds all T. A token is valid when it is in a sequence, its
+ * token_mask is nonzero and a live expert's logit is above -inf; what the logits hold of other
+ * tokens and of experts with active_mask 0 does not matter. With E' live experts, n_s valid
+ * tokens in s, M in all, N sequences that have one:
+ *   p[t,:]      = softmax over the live experts of logits[t,:]
+ *   counts[s,e] = #{(t,j) : t valid in s, topk_idx[t,j] == e}
+ *   prob[s,e]   = 1/n_s * sum_t p[t,e]                      (0 in a sequence without valid tokens)
+ *   loss[0]     = coef / N * sum_s sum_e counts[s,e] E' / (k n_s) * prob[s,e]
+ *   loss[1]     = z_coef / M * sum_t lse[t]^2               (both 0 without valid tokens)
+ *   lse[t]      = log sum_e exp(logits[t,e])                (-inf for tokens that are not valid)
+ *   n_tokens    = n_0 .. n_{n_seq-1}, M, N
+ * logits [T,E] fp32 (logits_out of moe_route); topk_idx [T,k] int32; active_mask [E] uint8 or NULL
+ * (all live); token_mask [T] uint8 or NULL (all); seq_offsets [n_seq+1] int32, ascending, inside [0, T]
+ * (else MOE_DEV_BAD_OFFSETS, and the results are undefined), or NULL; loss [2] fp32; counts, prob
+ * [n_seq,E] int32 / fp32; n_tokens [n_seq+2] int32; lse [T] fp32 (all overwritten). ws: of
+ * moe_balance_workspace_size bytes, 16-byte aligned, used until the call's kernels end. Sums over tokens run in a
+ * fixed order: bitwise reproducible. An id outside [0, E) of a valid token is left out and sets
+ * MOE_DEV_BAD_EXPERT. A NaN logit of a live expert makes its sequence's results NaN.
+ * Limits: 1 <= E <= 256, 1 <= k <= min(E, 8), 1 <= n_seq <= 2^20, T >= 0.
+ */
+int moe_balance_loss(const float *logits, const int32_t *topk_idx, const uint8_t *active_mask,
+                     const uint8_t *token_mask, const int32_t *seq_offsets, int n_seq, int T, int E,
+                     int k, float coef, float z_coef, float *loss, int32_t *counts, float *prob,
+                     int32_t *n_tokens, float *lse, void *ws, size_t ws_bytes, moe_stream_t stream);
+
+/* Bytes of `ws` for moe_balance_loss (0 when T < 0, E <= 0 or n_seq <= 0). */
+size_t moe_balance_workspace_size(int T, int E, int n_seq);
+
+/*
+ * moe_balance_loss_bwd - gradient of moe_balance_loss's losses with respect to the logits (the
+ * counts are constants, as in the papers of both losses):
+ *   dz[t,e] = p[t,e] (a_s (f[s,e] - sum_i p[t,i] f[s,i]) + b lse[t]),  f[s,e] = counts[s,e] E' / (k n_s),
+ *   a_s = d_loss[0] coef / (N n_s),  b = 2 d_loss[1] z_coef / M;   0 for tokens that are not valid and
+ *   for experts with active_mask 0
+ * logits, active_mask, seq_offsets, sizes and coefficients as in the forward call; counts,
+ * n_tokens, lse as it wrote them (valid tokens are those with lse > -inf); d_loss [2] fp32 (device) or
+ * NULL (ones); dz [T,E] fp32 (out, overwritten).
+ */
+int moe_balance_loss_bwd(const float *logits, const uint8_t *active_mask, const int32_t *seq_offsets,
+                         int n_seq, int T, int E, int k, float coef, float z_coef,
+                         const int32_t *counts, const int32_t *n_tokens, const float *lse,
+                         const float *d_loss, float *dz, moe_stream_t stream);
 
 /*
  * laep_prune_mask - LAEP expert-pruning decision for one layer (HOST call).
@@ -484,6 +533,30 @@ int moe_grouped_ffn_bwd_wgrad_gather(const uint16_t *d_out_perm, const uint16_t 
 int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
                   const float *d_gate, int T, int d, int E, int k, float *d_logits,
                   float *dw_router, void *ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * moe_route_bwd_dense - moe_route_bwd with a gradient of every logit beside that of the
+ * k selected gates (a loss on the logits, moe_balance_loss_bwd's dz):
+ *   d_logits as in moe_route_bwd;  dZ = dz + d_logits at the selected experts
+ *   dw_router = x^T dZ
+ * dz [T,E] fp32, not scaled or masked here: zero where a logit has no gradient. topk_idx,
+ * topk_gate, d_gate and d_logits may be NULL together (dZ = dz). Other arguments, arithmetic and
+ * limits as in moe_route_bwd. dz's share of the layer input's gradient comes from moe_route_dx.
+ */
+int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
+                        const float *d_gate, const float *dz, int T, int d, int E, int k,
+                        float *d_logits, float *dw_router, void *ws, size_t ws_bytes,
+                        moe_stream_t stream);
+
+/*
+ * moe_route_dx - a dense logit gradient's share of the layer input's gradient:
+ *   dx[t,:] = dx_in[t,:] + sum_e dz[t,e] * w_router[:,e]   (one bf16 rounding)
+ * dz [T,E] fp32; w_router [d,E] fp32; dx_in [T,d] bf16 or NULL (zeros), may be dx itself; dx [T,d]
+ * bf16 (out); both 16-byte aligned. k: the layer's (for the workspace's layout). Limits:
+ * 1 <= E <= 256, 1 <= k <= 8, d % 8 == 0, T >= 0; ws as in moe_route_bwd.
+ */
+int moe_route_dx(const float *dz, const float *w_router, const uint16_t *dx_in, int T, int d, int E,
+                 int k, uint16_t *dx, void *ws, size_t ws_bytes, moe_stream_t stream);
 
 /*
  * moe_permute_bwd - gradient of the layer input (the paper gives no backward;

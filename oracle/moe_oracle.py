@@ -524,3 +524,62 @@ def rearrange(loads, n_groups):
             group_of[e] = g
     return order, group_of, np.array(sums, np.int64)
 
+
+
+# ----------------------------------------------------------------------------
+# Auxiliary losses of the router (the paper's comparison: the load-balance losses that
+# LAEP replaces) and the checkpoints in 8 bits
+# ----------------------------------------------------------------------------
+
+
+def balance_loss(logits, topk_idx, active_mask=None, token_mask=None, seq_offsets=None, coef=1.0,
+                 z_coef=0.0, d_loss=(1.0, 1.0)):
+    """Load-balance loss per sequence, z-loss, their statistics and the gradient of the logits.
+
+    loss[0] = coef / N * sum_s sum_e f[s,e] P[s,e], f[s,e] = counts[s,e] E' / (k n_s), P[s,e] the
+    mean softmax probability over the sequence's n_s valid tokens, N the sequences that have one, E' the
+    live experts; loss[1] = z_coef / M * sum_t lse[t]^2 over all M valid tokens. A token is valid inside a
+    sequence, with a nonzero token_mask and a live logit above -inf. The counts are constants.
+    """
+    z = np.asarray(logits, np.float64).copy()
+    T, E = z.shape
+    k = topk_idx.shape[1]
+    live = np.ones(E, bool) if active_mask is None else np.asarray(active_mask) != 0
+    z[:, ~live] = -np.inf
+    off = [0, T] if seq_offsets is None else [int(v) for v in seq_offsets]
+    S = len(off) - 1
+    ok = ~(z == -np.inf).all(axis=1) if E else np.zeros(T, bool)
+    if token_mask is not None:
+        ok &= np.asarray(token_mask) != 0
+    lse = np.full(T, -np.inf)
+    counts, prob = np.zeros((S, E), np.int64), np.zeros((S, E))
+    p = np.zeros((T, E))
+    members = []
+    for s in range(S):
+        t = np.arange(off[s], off[s + 1])
+        t = t[ok[t]]
+        members.append(t)
+        if len(t) == 0:
+            continue
+        m = z[t].max(axis=1, keepdims=True)
+        ex = np.exp(z[t] - m)
+        lse[t] = (m + np.log(ex.sum(axis=1, keepdims=True)))[:, 0]
+        p[t] = ex / ex.sum(axis=1, keepdims=True)
+        prob[s] = p[t].mean(axis=0)
+        ids = topk_idx[t].reshape(-1)
+        counts[s] = np.bincount(ids[(ids >= 0) & (ids < E)], minlength=E)
+    n = np.array([len(t) for t in members], np.int64)
+    N, M, El = int((n > 0).sum()), int(n.sum()), int(live.sum())
+    loss = np.zeros(2)
+    dz = np.zeros((T, E))
+    for s, t in enumerate(members):
+        if n[s] == 0:
+            continue
+        f = counts[s] * (El / (k * n[s]))
+        loss[0] += coef / N * (f * prob[s]).sum()
+        loss[1] += z_coef / M * (lse[t] ** 2).sum()
+        g = d_loss[0] * coef / (N * n[s]) * f
+        dz[t] = p[t] * (g - (p[t] * g).sum(axis=1, keepdims=True))
+        dz[t] += d_loss[1] * 2 * z_coef / M * lse[t][:, None] * p[t]
+    return {"loss": loss, "counts": counts, "prob": prob, "n_tokens": np.concatenate([n, [M, N]]),
+            "lse": lse, "dz": dz, "p": p, "live": live}

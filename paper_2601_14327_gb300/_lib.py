@@ -20,7 +20,8 @@ MOE_OK = 0
 STATUS_NAMES = {0: "MOE_OK", -1: "MOE_ERR_ARG", -2: "MOE_ERR_UNSUPPORTED", -3: "MOE_ERR_CUDA",
                 -4: "MOE_ERR_INVARIANT", -5: "MOE_ERR_TIMEOUT", -6: "MOE_ERR_WORKSPACE"}
 DEV_NAMES = {0: "MOE_DEV_OK", 1: "MOE_DEV_BAD_EXPERT", 2: "MOE_DEV_TOO_FEW_LIVE",
-             3: "MOE_DEV_COUNT_MISMATCH", 4: "MOE_DEV_WAIT_TIMEOUT", 5: "MOE_DEV_ROWS_OVERFLOW"}
+             3: "MOE_DEV_COUNT_MISMATCH", 4: "MOE_DEV_WAIT_TIMEOUT", 5: "MOE_DEV_ROWS_OVERFLOW",
+             6: "MOE_DEV_BAD_OFFSETS"}
 
 
 class MoEError(RuntimeError):
@@ -34,6 +35,7 @@ I = ctypes.c_int
 I64 = ctypes.c_int64
 SZ = ctypes.c_size_t
 D = ctypes.c_double
+F32 = ctypes.c_float
 
 _SIGS = {
     "moe_version": (I, []),
@@ -67,6 +69,11 @@ _SIGS = {
     "moe_grouped_ffn_bwd_wgrad_gather": (I, [P, P, P, I, P, P, P, P, I, I, I, I64, P, P, P, SZ,
                                              P]),
     "moe_selftest_wait_timeout": (I, [I64, P]),
+    "moe_route_bwd_dense": (I, [P, P, P, P, P, I, I, I, I, P, P, P, SZ, P]),
+    "moe_route_dx": (I, [P, P, P, I, I, I, I, P, P, SZ, P]),
+    "moe_balance_workspace_size": (SZ, [I, I, I]),
+    "moe_balance_loss": (I, [P, P, P, P, P, I, I, I, I, F32, F32, P, P, P, P, P, P, SZ, P]),
+    "moe_balance_loss_bwd": (I, [P, P, P, I, I, I, I, F32, F32, P, P, P, P, P, P]),
 }
 
 
@@ -302,6 +309,19 @@ def moe_route_bwd(x, topk_idx, topk_gate, d_gate, T, d, E, k, d_logits, dw_route
         _ptr(dw_router), _ptr(ws), ws_bytes, _stream(stream)))
 
 
+def moe_route_bwd_dense(x, topk_idx, topk_gate, d_gate, dz, T, d, E, k, d_logits, dw_router, ws,
+                        ws_bytes, stream=None):
+    _check("moe_route_bwd_dense", load().moe_route_bwd_dense(
+        _ptr(x), _ptr(topk_idx), _ptr(topk_gate), _ptr(d_gate), _ptr(dz), T, d, E, k,
+        _ptr(d_logits), _ptr(dw_router), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_route_dx(dz, w_router, dx_in, T, d, E, k, dx, ws, ws_bytes, stream=None):
+    _check("moe_route_dx", load().moe_route_dx(
+        _ptr(dz), _ptr(w_router), _ptr(dx_in), T, d, E, k, _ptr(dx), _ptr(ws), ws_bytes,
+        _stream(stream)))
+
+
 def moe_permute_map(topk_idx, counts, T, E, k, rows_cap, group_offsets, group_counts,
                     row_of_assignment, token_of_row, ws, ws_bytes, stream=None):
     _check("moe_permute_map", load().moe_permute_map(
@@ -340,6 +360,25 @@ def moe_permute_bwd(dx_perm, row_of_assignment, topk_idx, d_logits, w_router, T,
     _check("moe_permute_bwd", load().moe_permute_bwd(
         _ptr(dx_perm), _ptr(row_of_assignment), _ptr(topk_idx), _ptr(d_logits), _ptr(w_router),
         T, d, E, k, _ptr(dx), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_balance_workspace_size(T, E, n_seq=1):
+    return int(load().moe_balance_workspace_size(T, E, n_seq))
+
+
+def moe_balance_loss(logits, topk_idx, active_mask, token_mask, seq_offsets, n_seq, T, E, k, coef,
+                     z_coef, loss, counts, prob, n_tokens, lse, ws, ws_bytes, stream=None):
+    _check("moe_balance_loss", load().moe_balance_loss(
+        _ptr(logits), _ptr(topk_idx), _ptr(active_mask), _ptr(token_mask), _ptr(seq_offsets),
+        n_seq, T, E, k, coef, z_coef, _ptr(loss), _ptr(counts), _ptr(prob), _ptr(n_tokens),
+        _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_balance_loss_bwd(logits, active_mask, seq_offsets, n_seq, T, E, k, coef, z_coef, counts,
+                         n_tokens, lse, d_loss, dz, stream=None):
+    _check("moe_balance_loss_bwd", load().moe_balance_loss_bwd(
+        _ptr(logits), _ptr(active_mask), _ptr(seq_offsets), n_seq, T, E, k, coef, z_coef,
+        _ptr(counts), _ptr(n_tokens), _ptr(lse), _ptr(d_loss), _ptr(dz), _stream(stream)))
 
 
 def moe_selftest_wait_timeout(limit_ns, stream=None):

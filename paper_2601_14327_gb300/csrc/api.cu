@@ -150,11 +150,12 @@ int moe_device_error(int *code, int clear) {
   if (!code) return moe::set_error(MOE_ERR_ARG, "moe_device_error: null code");
   int st = moe::cuda_status(cudaDeviceSynchronize(), "moe_device_error: synchronize");
   if (st) return st;
-  int c0 = 0, c1 = 0, c2 = 0;
+  int c0 = 0, c1 = 0, c2 = 0, c3 = 0;
   if ((st = moe::route_dev_error(clear, &c0))) return st;
   if ((st = moe::permute_dev_error(clear, &c1))) return st;
   if ((st = moe::gemm_dev_error(clear, &c2))) return st;
-  *code = c0 ? c0 : (c1 ? c1 : c2);
+  if ((st = moe::balance_dev_error(clear, &c3))) return st;
+  *code = c0 ? c0 : (c1 ? c1 : (c2 ? c2 : c3));
   return MOE_OK;
 }
 

@@ -62,6 +62,7 @@ void timing_end(const char *name, cudaEvent_t begin, cudaStream_t s);
 int route_dev_error(int clear, int *code);
 int permute_dev_error(int clear, int *code);
 int gemm_dev_error(int clear, int *code);
+int balance_dev_error(int clear, int *code);
 
 }  // namespace moe
 

@@ -593,12 +593,13 @@ __global__ void load_stats_kernel(const int32_t *__restrict__ topk_idx, int64_t 
 // and dZ (the [T, E] logit gradient, zero off the selected experts) as three bf16
 // terms, K-major for the tensor cores: dz3[s][e][t] for e < NP, t < Tp (tokens padded
 // to 64; the padding is zero). One thread per token and 16 experts (blockIdx.y); the
-// y = 0 blocks also write d_logits.
+// y = 0 blocks also write d_logits. DENSE: dz [T, E] is added to dZ, and topk_idx may be null.
 constexpr int kDzExperts = 16;
+template <bool DENSE>
 __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
                                     const float *__restrict__ gate, const float *__restrict__ dgate,
-                                    int T, int Tp, int k, int NP, float *__restrict__ d_logits,
-                                    uint16_t *__restrict__ dz3) {
+                                    const float *__restrict__ dz, int T, int Tp, int E, int k, int NP,
+                                    float *__restrict__ d_logits, uint16_t *__restrict__ dz3) {
   pdl_start();
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
   if (t >= Tp) return;
@@ -609,7 +610,7 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
     g[j] = 0.f;
     dg[j] = 0.f;
     ei[j] = -1;
-    if (j < k && t < T) {
+    if (j < k && t < T && (!DENSE || topk_idx != nullptr)) {
       g[j] = gate[size_t(t) * k + j];
       dg[j] = dgate[size_t(t) * k + j];
       ei[j] = topk_idx[size_t(t) * k + j];
@@ -619,7 +620,7 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     g[j] = g[j] * (dg[j] - s);
-    if (blockIdx.y == 0 && j < k && t < T) d_logits[size_t(t) * k + j] = g[j];
+    if (blockIdx.y == 0 && j < k && t < T && (!DENSE || topk_idx != nullptr)) d_logits[size_t(t) * k + j] = g[j];
   }
   const size_t plane = size_t(NP) * Tp;
   const int e0 = blockIdx.y * kDzExperts;
@@ -628,6 +629,7 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (ei[j] == e) v = g[j];  // the k selected experts of a token are distinct
+    if (DENSE && t < T && e < E) v += dz[size_t(t) * E + e];
     const __nv_bfloat16 hi = __float2bfloat16_rn(v);
     const float r1 = v - __bfloat162float(hi);
     const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
@@ -675,6 +677,43 @@ __global__ void route_dw_reduce_kernel(const float *__restrict__ partial, int sp
 __global__ void zero_f32_kernel(float *p, int n) {
   pdl_start();
   for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = 0.f;
+}
+
+// dx = bf16(dx_in + dz W^T): 64 tokens x 64 columns per block, 4 x 4 per thread.
+constexpr int kDxTile = 64;
+__global__ void __launch_bounds__(256) route_dx_kernel(const float *__restrict__ dz, const float *__restrict__ w,
+                                                       const uint16_t *dx_in, int T, int d, int E, uint16_t *dx) {
+  __shared__ float s_z[16][kDxTile + 4], s_w[16][kDxTile + 4];
+  pdl_start();
+  const int t0 = blockIdx.x * kDxTile, i0 = blockIdx.y * kDxTile;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float acc[4][4] = {};
+  for (int e0 = 0; e0 < E; e0 += 16) {
+    for (int r = ty; r < kDxTile; r += 16) {
+      const int e = e0 + tx;
+      s_z[tx][r] = t0 + r < T && e < E ? dz[size_t(t0 + r) * E + e] : 0.f;
+      s_w[tx][r] = i0 + r < d && e < E ? w[size_t(i0 + r) * E + e] : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(s_z[e][ty * 4 + a], s_w[e][tx * 4 + b], acc[a][b]);
+    __syncthreads();
+  }
+  const int c = i0 + tx * 4;
+  if (c >= d) return;  // (d is a multiple of 8)
+  for (int a = 0; a < 4; ++a) {
+    const int t = t0 + ty * 4 + a;
+    if (t >= T) break;
+    uint2 v = make_uint2(0, 0);
+    if (dx_in != nullptr) v = *reinterpret_cast<const uint2 *>(dx_in + size_t(t) * d + c);
+    v.x = pack_bf16x2(acc[a][0] + bf16_lo(v.x), acc[a][1] + bf16_hi(v.x));
+    v.y = pack_bf16x2(acc[a][2] + bf16_lo(v.y), acc[a][3] + bf16_hi(v.y));
+    *reinterpret_cast<uint2 *>(dx + size_t(t) * d + c) = v;
+  }
 }
 
 template <bool DW, int G, bool AHEAD = false>
@@ -868,29 +907,29 @@ int launch_route_dw(const uint16_t *x, const uint16_t *dz3, int T, int d, int E,
 
 extern "C" {
 
-int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
-                  const float *d_gate, int T, int d, int E, int k, float *d_logits,
-                  float *dw_router, void *ws, size_t ws_bytes, moe_stream_t stream) {
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+static int route_bwd(const char *fn, const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
+                     const float *d_gate, const float *dz, int T, int d, int E, int k, float *d_logits,
+                     float *dw_router, void *ws, size_t ws_bytes, cudaStream_t s) {
   if (E < 1 || E > 256 || k < 1 || k > 8 || k > E || T < 0 || d <= 0 || d % 8)
-    return moe::set_error(MOE_ERR_ARG, "moe_route_bwd: sizes");
-  if (!dw_router || (T > 0 && (!x || !topk_idx || !topk_gate || !d_gate || !d_logits || !ws)))
-    return moe::set_error(MOE_ERR_ARG, "moe_route_bwd: null pointer");
+    return moe::set_error(MOE_ERR_ARG, "%s: sizes", fn);
+  const bool gates = dz == nullptr || topk_idx || topk_gate || d_gate || d_logits;
+  if (!dw_router || (T > 0 && (!x || !ws || (gates && (!topk_idx || !topk_gate || !d_gate || !d_logits)))))
+    return moe::set_error(MOE_ERR_ARG, "%s: null pointer", fn);
   if ((x && !moe::aligned16(x)) || (ws && !moe::aligned16(ws)))
-    return moe::set_error(MOE_ERR_ARG, "moe_route_bwd: alignment");
+    return moe::set_error(MOE_ERR_ARG, "%s: alignment", fn);
   if (T == 0) {
     const int n = d * E;
     MOE_LAUNCH("zero_dw_router", s, moe::launch_dep(zero_f32_kernel, std::min((n + 255) / 256, 1024), 256, 0, s, dw_router, n));
     return moe::launch_status("moe_route_bwd: zero");
   }
   const moe::WsLayout L = moe::ws_layout(T, d, E, k, 0);
-  if (ws_bytes < L.total) return moe::set_error(MOE_ERR_WORKSPACE, "moe_route_bwd: workspace");
+  if (ws_bytes < L.total) return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace", fn);
   uint16_t *dz3 = reinterpret_cast<uint16_t *>(static_cast<char *>(ws) + L.route_dz3);
   float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + L.route_dw_partial);
   const int NP = route_tc_np(E), Tp = route_tokens_padded(T);
   dim3 zgrid((Tp + 255) / 256, (NP + kDzExperts - 1) / kDzExperts);
-  MOE_LAUNCH("route_bwd_dz", s, moe::launch_dep(route_bwd_dz_kernel, zgrid, 256, 0, s,
-                                    topk_idx, topk_gate, d_gate, T, Tp, k, NP, d_logits, dz3));
+  MOE_LAUNCH("route_bwd_dz", s, moe::launch_dep(dz ? route_bwd_dz_kernel<true> : route_bwd_dz_kernel<false>, zgrid, 256, 0,
+                                    s, topk_idx, topk_gate, d_gate, dz, T, Tp, E, k, NP, d_logits, dz3));
   if (int st = moe::launch_status("moe_route_bwd: dz")) return st;
   int splits = 0;
   if (int st = launch_route_dw(x, dz3, T, d, E, partial, &splits, s)) return st;
@@ -898,6 +937,38 @@ int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_
   MOE_LAUNCH("route_bwd_reduce", s, moe::launch_dep(route_dw_reduce_kernel, std::min((n + 255) / 256, 4 * moe::num_sms()), 256, 0, s,
                                         partial, splits, d, E, route_dw_stride(E), dw_router));
   return moe::launch_status("moe_route_bwd: reduce");
+}
+
+int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
+                  const float *d_gate, int T, int d, int E, int k, float *d_logits,
+                  float *dw_router, void *ws, size_t ws_bytes, moe_stream_t stream) {
+  return route_bwd("moe_route_bwd", x, topk_idx, topk_gate, d_gate, nullptr, T, d, E, k, d_logits, dw_router, ws,
+                   ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
+                        const float *d_gate, const float *dz, int T, int d, int E, int k,
+                        float *d_logits, float *dw_router, void *ws, size_t ws_bytes,
+                        moe_stream_t stream) {
+  if (T > 0 && !dz) return moe::set_error(MOE_ERR_ARG, "moe_route_bwd_dense: null dz");
+  return route_bwd("moe_route_bwd_dense", x, topk_idx, topk_gate, d_gate, dz, T, d, E, k, d_logits, dw_router, ws,
+                   ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int moe_route_dx(const float *dz, const float *w_router, const uint16_t *dx_in, int T, int d, int E,
+                 int k, uint16_t *dx, void *ws, size_t ws_bytes, moe_stream_t stream) {
+  const char *fn = "moe_route_dx";
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (E < 1 || E > 256 || k < 1 || k > 8 || T < 0 || d <= 0 || d % 8) return moe::set_error(MOE_ERR_ARG, "%s: sizes", fn);
+  if (T == 0) return MOE_OK;
+  if (!dz || !w_router || !dx || !ws) return moe::set_error(MOE_ERR_ARG, "%s: null pointer", fn);
+  if (!moe::aligned16(dx) || (dx_in && !moe::aligned16(dx_in)) || !moe::aligned16(ws))
+    return moe::set_error(MOE_ERR_ARG, "%s: alignment", fn);
+  const moe::WsLayout L = moe::ws_layout(T, d, E, k, 0);
+  if (ws_bytes < L.total) return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace", fn);
+  dim3 grid((T + kDxTile - 1) / kDxTile, (d + kDxTile - 1) / kDxTile);
+  MOE_LAUNCH("route_dx", s, moe::launch_dep(route_dx_kernel, grid, 256, 0, s, dz, w_router, dx_in, T, d, E, dx));
+  return moe::launch_status("moe_route_dx: launch");
 }
 
 }  // extern "C"

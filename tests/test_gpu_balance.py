@@ -1,0 +1,331 @@
+"""Balance loss, its gradient, and the products that carry it on, against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import moe_oracle as O
+from paper_2601_14327_gb300 import _lib as L
+
+pytestmark = pytest.mark.gpu
+
+F32, I32 = torch.float32, torch.int32
+
+
+@pytest.fixture(autouse=True)
+def _clean_device_error():
+    L.moe_device_error(clear=True)
+    yield
+    assert L.moe_device_error(clear=True) == 0
+
+
+def _inputs(T, E, k, S, masked=0, padded=0.0, seed=0, scale=2.0):
+    rng = np.random.default_rng(seed + 7 * T + E)
+    z = (rng.standard_normal((T, E)) * scale).astype(np.float32)
+    z -= np.log1p(rng.permutation(E)).astype(np.float32)
+    mask = None
+    if masked:
+        mask = np.ones(E, np.uint8)
+        mask[rng.permutation(E)[:masked]] = 0
+        z[:, mask == 0] = -np.inf
+    idx = np.argsort(-z, axis=1, kind="stable")[:, :k].astype(np.int32)
+    off = None
+    if S:
+        off = np.concatenate([[0], np.sort(rng.integers(0, T + 1, S))]).astype(np.int32)
+        off[-1] = max(off[-2], T - T // 16)
+    tok = (rng.random(T) >= padded).astype(np.uint8) if padded else None
+    return z, idx, mask, tok, off
+
+
+def _dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+class Balance:
+    """The two calls with buffers of their own, filled with what must not be left there."""
+
+    def __init__(self, T, E, k, S):
+        self.T, self.E, self.k, self.S = T, E, k, max(1, S)
+        nan = float("nan")
+        self.loss = torch.full((2,), nan, device="cuda")
+        self.counts = torch.full((self.S, E), -7, dtype=I32, device="cuda")
+        self.prob = torch.full((self.S, E), nan, device="cuda")
+        self.n_tokens = torch.full((self.S + 2,), -7, dtype=I32, device="cuda")
+        self.lse = torch.full((T,), nan, device="cuda")
+        self.dz = torch.full((T, E), nan, device="cuda")
+        self.ws = torch.full((L.moe_balance_workspace_size(T, E, self.S),), 255, dtype=torch.uint8, device="cuda")
+
+    def __call__(self, z, idx, mask, tok, off, coef, z_coef, d_loss=None, stream=None):
+        L.moe_balance_loss(z, idx, mask, tok, off, self.S, self.T, self.E, self.k, coef, z_coef, self.loss,
+                           self.counts, self.prob, self.n_tokens, self.lse, self.ws, self.ws.numel(), stream)
+        L.moe_balance_loss_bwd(z, mask, off, self.S, self.T, self.E, self.k, coef, z_coef, self.counts,
+                               self.n_tokens, self.lse, d_loss, self.dz, stream)
+        return {n: getattr(self, n).cpu().numpy() for n in ("loss", "counts", "prob", "n_tokens", "lse", "dz")}
+
+
+def _check(got, ref, coef, z_coef, d_loss, k):
+    assert (got["counts"] == ref["counts"]).all()
+    assert (got["n_tokens"] == ref["n_tokens"]).all()
+    ok = ref["lse"] > -np.inf
+    assert (np.isneginf(got["lse"]) == ~ok).all()
+    # exp 2 ulp (2^-22), its argument's rounding weighted by p (|x| e^-|x| summed: < ln 256 * 2^-24), 13
+    # additions, log 1 ulp, the final addition
+    err = np.abs(got["lse"][ok] - ref["lse"][ok])
+    assert (err <= 2e-6 + 2 ** -23 * np.abs(ref["lse"][ok])).all(), err.max()
+    # p: 2^-22 + |z - m| 2^-24 (|z - m| <= 88: 5.3e-6) and the quotient; < 80 additions of 2^-24 each
+    np.testing.assert_allclose(got["prob"], ref["prob"], rtol=1.2e-5, atol=1e-36)
+    np.testing.assert_allclose(got["loss"], ref["loss"], rtol=1.2e-5, atol=1e-36)
+    # gradient: p as above twice (its own and the weights of the mean), a, b, f - 1 and the sums' roundings,
+    # relative to the sizes of its terms
+    T, E = ref["dz"].shape
+    scale = np.zeros((T, E))
+    off = ref["off"]
+    N, M, El = ref["n_tokens"][-1], ref["n_tokens"][-2], ref["live"].sum()
+    for s in range(len(off) - 1):
+        t = np.arange(off[s], off[s + 1])
+        t = t[ok[t]]
+        if len(t):
+            f = np.abs(ref["counts"][s] * (El / (k * len(t))) - 1)
+            p = ref["p"][t]
+            scale[t] = p * (abs(d_loss[0]) * coef / (N * len(t)) * (f + (p * f).sum(1, keepdims=True))
+                            + abs(d_loss[1]) * 2 * z_coef / M * np.abs(ref["lse"][t])[:, None])
+    bad = np.abs(got["dz"] - ref["dz"]) > 2e-5 * scale + 1e-37
+    assert not bad.any(), (bad.sum(), np.abs(got["dz"] - ref["dz"])[bad].max())
+    assert (got["dz"][~ok] == 0).all() and (got["dz"][:, ~ref["live"]] == 0).all()
+
+
+CASES = [
+    # T, E, k, sequences (0: no offsets), pruned, padded
+    (1, 1, 1, 0, 0, 0.0), (1, 256, 8, 0, 0, 0.0), (3, 5, 2, 2, 1, 0.0),
+    # experts at the edges of the lanes per token
+    (130, 16, 2, 3, 0, 0.2), (131, 17, 3, 0, 4, 0.0), (100, 32, 4, 1, 0, 0.0), (257, 33, 4, 5, 7, 0.3),
+    (77, 64, 6, 2, 0, 0.0), (300, 65, 8, 0, 20, 0.0), (201, 128, 8, 4, 0, 0.5), (99, 129, 8, 1, 0, 0.0),
+    (515, 171, 8, 7, 30, 0.1), (90, 192, 7, 2, 0, 0.0), (64, 193, 8, 0, 0, 0.0), (1000, 256, 8, 33, 85, 0.1),
+    # a chunk per 8 tokens up to 4864, then longer ones; more sequences than tokens
+    (4864, 64, 8, 3, 0, 0.0), (4865, 24, 4, 11, 3, 0.05), (20001, 96, 6, 40, 0, 0.0), (50, 12, 3, 200, 0, 0.2),
+    # every token masked
+    (40, 20, 2, 3, 0, 1.0)]
+
+
+@pytest.mark.parametrize("T,E,k,S,masked,padded", CASES)
+def test_balance_against_oracle(T, E, k, S, masked, padded):
+    z, idx, mask, tok, off = _inputs(T, E, k, S, masked, padded)
+    coef, z_coef, d = 0.013, 0.002, (0.6, 1.7)
+    ref = O.balance_loss(z, idx, mask, tok, off, coef, z_coef, d)
+    ref["off"] = [0, T] if off is None else off
+    b = Balance(T, E, k, S)
+    got = b(_dev(z), _dev(idx), _dev(mask), _dev(tok), _dev(off), coef, z_coef, torch.tensor(d, device="cuda"))
+    _check(got, ref, coef, z_coef, d, k)
+    # twice the same inputs through the same workspace: the same bits
+    again = b(_dev(z), _dev(idx), _dev(mask), _dev(tok), _dev(off), coef, z_coef, torch.tensor(d, device="cuda"))
+    assert all((got[n] == again[n]).all() for n in got)
+    # d_loss NULL: ones
+    one = b(_dev(z), _dev(idx), _dev(mask), _dev(tok), _dev(off), coef, z_coef)
+    _check(one, {**O.balance_loss(z, idx, mask, tok, off, coef, z_coef), "off": ref["off"]}, coef, z_coef, (1, 1), k)
+
+
+def test_balance_without_tokens():
+    E, k, S = 10, 2, 3
+    got = Balance(0, E, k, S)(None, None, None, None, torch.zeros(S + 1, dtype=I32, device="cuda"), 1.0, 1.0)
+    assert (got["loss"] == 0).all() and (got["counts"] == 0).all() and (got["prob"] == 0).all()
+    assert (got["n_tokens"] == 0).all()
+
+
+def test_balance_large_logits_and_masked_rubbish():
+    """Logits near 1000 (their sum's rounding is common to a token's probabilities), masked tokens and
+    pruned experts that hold infinities and NaN, rows without a live logit, rows behind the last sequence."""
+    T, E, k = 200, 40, 4
+    z, idx, mask, tok, off = _inputs(T, E, k, 3, masked=6, padded=0.2)
+    z[np.ix_(np.arange(0, T, 3), mask != 0)] += 1000
+    z[5, :] = -np.inf
+    z[17, :] = -np.inf
+    coef, z_coef, d = 0.01, 1e-4, (1, 1)
+    ref = O.balance_loss(z, idx, mask, tok, off, coef, z_coef)
+    ref["off"] = off
+    dirty = z.copy()
+    dirty[:, mask == 0] = np.nan
+    dirty[tok == 0] = np.inf
+    dirty[off[-1]:] = np.nan
+    bad_idx = idx.copy()
+    bad_idx[tok == 0] = -1
+    bad_idx[off[-1]:] = 9999
+    bad_idx[[5, 17]] = E
+    got = Balance(T, E, k, 3)(_dev(dirty), _dev(bad_idx), _dev(mask), _dev(tok), _dev(off), coef, z_coef)
+    _check(got, ref, coef, z_coef, d, k)
+
+
+def test_balance_nan_reaches_its_sequence_only():
+    T, E, k = 64, 8, 2
+    z, idx, _, _, _ = _inputs(T, E, k, 0)
+    off = np.array([0, 30, 64], np.int32)
+    z[40, 3] = np.nan
+    got = Balance(T, E, k, 2)(_dev(z), _dev(idx), None, None, _dev(off), 1.0, 0.0)
+    assert np.isnan(got["loss"][0]) and np.isfinite(got["prob"][0]).all() and np.isnan(got["prob"][1]).any()
+    assert np.isfinite(got["dz"][:30]).all() and np.isnan(got["dz"][40]).all()
+    assert np.isfinite(np.delete(got["lse"], 40)).all()
+
+
+def test_balance_flags_bad_ids_and_offsets():
+    T, E, k = 50, 6, 2
+    z, idx, _, _, _ = _inputs(T, E, k, 0)
+    idx[7, 1] = E
+    idx[9, 0] = -1
+    got = Balance(T, E, k, 0)(_dev(z), _dev(idx), None, None, None, 1.0, 0.0)
+    assert L.moe_device_error(clear=True) == 1  # MOE_DEV_BAD_EXPERT
+    assert (got["counts"] == O.balance_loss(z, idx)["counts"]).all()
+    idx = np.clip(idx, 0, E - 1)
+    for off in ([0, 30, 20], [-1, 30, 50], [0, 20, T + 1]):
+        Balance(T, E, k, 2)(_dev(z), _dev(idx), None, None, _dev(np.array(off, np.int32)), 1.0, 0.0)
+        assert L.moe_device_error(clear=True) == 6, off  # MOE_DEV_BAD_OFFSETS
+
+
+def test_balance_in_a_graph_and_on_another_stream():
+    """Captured once and replayed on new inputs; two graphs with workspaces of their own."""
+    T, E, k, S = 700, 48, 4, 5
+    z, idx, mask, tok, off = _inputs(T, E, k, S, 5, 0.1)
+    z2, idx2, _, tok2, _ = _inputs(T, E, k, S, 0, 0.1, seed=1)
+    z2[:, mask == 0] = -np.inf
+    idx2 = np.argsort(-z2, axis=1, kind="stable")[:, :k].astype(np.int32)
+    bufs = [_dev(z), _dev(idx), _dev(mask), _dev(tok), _dev(off)]
+    b, e = Balance(T, E, k, S), Balance(T, E, k, S)
+    want = [e(*bufs, 0.01, 0.001), e(_dev(z2), _dev(idx2), bufs[2], _dev(tok2), bufs[4], 0.01, 0.001)]
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+
+    def calls(stream):
+        L.moe_balance_loss(*bufs, S, T, E, k, 0.01, 0.001, b.loss, b.counts, b.prob, b.n_tokens, b.lse, b.ws,
+                           b.ws.numel(), stream)
+        L.moe_balance_loss_bwd(bufs[0], bufs[2], bufs[4], S, T, E, k, 0.01, 0.001, b.counts, b.n_tokens, b.lse, None,
+                               b.dz, stream)
+
+    calls(st)
+    st.synchronize()
+    with torch.cuda.graph(g, stream=st):
+        calls(torch.cuda.current_stream())
+    for i, new in ((0, None), (1, (z2, idx2, tok2)), (0, (z, idx, tok))):
+        if new is not None:
+            for at, v in zip((0, 1, 3), new):
+                bufs[at].copy_(_dev(v))
+        g.replay()
+        torch.cuda.synchronize()
+        for n, v in want[i].items():
+            assert (getattr(b, n).cpu().numpy() == v).all(), (i, n)
+
+
+# ---------------------------------------------------------------- into the router's weight and the input
+
+
+def _router_inputs(T, d, E, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, d, generator=g).to(torch.bfloat16)
+    w = torch.randn(d, E, generator=g) / d ** 0.5
+    z = torch.randn(T, E, generator=g)
+    idx = torch.argsort(z, dim=1, descending=True)[:, :k].to(I32).contiguous()
+    gate = torch.softmax(torch.gather(z, 1, idx.long()), 1).contiguous()
+    dg = torch.randn(T, k, generator=g)
+    dz = torch.randn(T, E, generator=g) * torch.softmax(3 * z, 1)
+    dx_in = (0.1 * torch.randn(T, d, generator=g)).to(torch.bfloat16)
+    return x, w, idx, gate, dg, dz, dx_in
+
+
+ROUTER = [(1, 8, 1, 1), (3, 72, 5, 2), (130, 136, 13, 2), (257, 256, 17, 4), (333, 200, 64, 6), (128, 512, 128, 8),
+          (1000, 384, 100, 4), (515, 776, 171, 8), (129, 1024, 256, 8), (2500, 264, 48, 3), (4097, 2048, 33, 8)]
+
+
+@pytest.mark.parametrize("T,d,E,k", ROUTER)
+def test_dense_router_backward_against_oracle(T, d, E, k):
+    x, w, idx, gate, dg, dz, _ = _router_inputs(T, d, E, k, T + E)
+    n = L.moe_workspace_size(T, d, E, k, 128)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    dl = torch.full((T, k), float("nan"), device="cuda")
+    dw = torch.full((d, E), float("nan"), device="cuda")
+    L.moe_route_bwd_dense(x.cuda(), idx.cuda(), gate.cuda(), dg.cuda(), dz.cuda(), T, d, E, k, dl, dw, ws, n)
+    dl_ref, dw_ref = O.router_backward(x.double().numpy(), idx.numpy(), gate.double().numpy(),
+                                       dg.double().numpy(), E)
+    xd, zd = x.double().numpy(), dz.double().numpy()
+    dw_ref = dw_ref + xd.T @ zd
+    g64, dg64 = gate.double().numpy(), dg.double().numpy()
+    zs = np.abs(g64) * (np.abs(dg64) + np.sum(np.abs(g64 * dg64), axis=1, keepdims=True))
+    assert (np.abs(dl.cpu().numpy() - dl_ref) <= 2e-6 * zs + 1e-30).all()
+    size = np.abs(zd)
+    np.put_along_axis(size, idx.numpy().astype(np.int64),
+                      np.take_along_axis(size, idx.numpy().astype(np.int64), 1) + zs, 1)
+    # as moe_route_bwd: dZ carried to 2^-24, exact products, fp32 sums over the tokens
+    assert (np.abs(dw.cpu().double().numpy() - dw_ref) <= 1e-5 * (np.abs(xd).T @ size) + 1e-30).all()
+    # without the gates' part, and with a zero dz the same bits as moe_route_bwd
+    only = torch.full_like(dw, float("nan"))
+    L.moe_route_bwd_dense(x.cuda(), None, None, None, dz.cuda(), T, d, E, k, None, only, ws, n)
+    assert (np.abs(only.cpu().double().numpy() - xd.T @ zd) <= 1e-5 * (np.abs(xd).T @ np.abs(zd)) + 1e-30).all()
+    none, plain, dl2 = torch.empty_like(dw), torch.empty_like(dw), torch.empty_like(dl)
+    L.moe_route_bwd_dense(x.cuda(), idx.cuda(), gate.cuda(), dg.cuda(), torch.zeros(T, E, device="cuda"), T, d, E, k,
+                          dl, none, ws, n)
+    L.moe_route_bwd(x.cuda(), idx.cuda(), gate.cuda(), dg.cuda(), T, d, E, k, dl2, plain, ws, n)
+    assert torch.equal(none, plain) and torch.equal(dl, dl2)
+
+
+def test_dense_router_backward_without_tokens():
+    dw = torch.full((64, 6), float("nan"), device="cuda")
+    n = L.moe_workspace_size(0, 64, 6, 2, 128)
+    L.moe_route_bwd_dense(None, None, None, None, None, 0, 64, 6, 2, None, dw,
+                          torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    assert (dw == 0).all()
+    L.moe_route_dx(None, None, None, 0, 64, 6, 2, None, None, 0)
+
+
+def _dx(dz, w, dx_in, k, out=None):
+    T, E = dz.shape
+    d = w.shape[0]
+    n = L.moe_workspace_size(T, d, E, k, 128)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full((T, d), float("nan"), dtype=torch.bfloat16, device="cuda") if out is None else out
+    L.moe_route_dx(dz.cuda(), w.cuda(), dx_in, T, d, E, k, out, ws, n)
+    torch.cuda.synchronize()
+    return out
+
+
+def _dx_bound(ref, size):
+    # the result's rounding to bf16 (2^-8); both factors in half precision (2^-11 each, powers of two
+    # taken out), products exact, up to 256 fp32 additions (2^-24 each)
+    return 2 ** -8 * np.abs(ref) + (2 ** -10 + 2 ** -16) * (1 + 2 ** -8) * size + 1e-37
+
+
+@pytest.mark.parametrize("T,d,E,k", ROUTER)
+def test_route_dx_against_64_bits(T, d, E, k):
+    _, w, _, _, _, dz, dx_in = _router_inputs(T, d, E, k, T + E + 1)
+    prod, size = dz.double().numpy() @ w.double().numpy().T, dz.abs().double().numpy() @ w.abs().double().numpy().T
+    got = _dx(dz, w, None, k).double().cpu().numpy()
+    assert (np.abs(got - prod) <= _dx_bound(prod, size)).all()
+    ref = prod + dx_in.double().numpy()
+    out = _dx(dz, w, dx_in.cuda(), k)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= _dx_bound(ref, size)).all()
+    # in place: the same bits; no token's gradient: dx_in
+    buf = dx_in.cuda()
+    assert torch.equal(_dx(dz, w, buf, k, out=buf), out)
+    assert torch.equal(_dx(torch.zeros(T, E), w, dx_in.cuda(), k), dx_in.cuda())
+
+
+def test_route_dx_wide_ranges():
+    """Rows and columns of very different sizes: each row of the result is as near as its own size asks."""
+    T, d, E, k = 300, 272, 60, 4
+    _, w, _, _, _, dz, _ = _router_inputs(T, d, E, k, 5)
+    dz = dz * torch.exp2(torch.arange(T)[:, None] % 61 - 50.0)
+    w = w * torch.exp2(torch.arange(d)[:, None] % 41 - 30.0)
+    dz[7] = 0
+    w[9] = 0
+    # smaller than the row's largest by up to 2^20
+    dz[:, ::3] *= 2.0 ** -20
+    prod, size = dz.double().numpy() @ w.double().numpy().T, dz.abs().double().numpy() @ w.abs().double().numpy().T
+    got = _dx(dz, w, None, k).double().cpu().numpy()
+    assert (np.abs(got - prod) <= _dx_bound(prod, size)).all()
+    assert (got[7] == 0).all() and (got[:, 9] == 0).all()
+
+
+def test_route_dx_infinities_stay_in_their_row():
+    T, d, E, k = 140, 136, 20, 2
+    _, w, _, _, _, dz, dx_in = _router_inputs(T, d, E, k, 6)
+    clean = _dx(dz, w, dx_in.cuda(), k)
+    dz[3, 4], dz[100, 0] = float("nan"), float("inf")
+    got = _dx(dz, w, dx_in.cuda(), k)
+    keep = [t for t in range(T) if t not in (3, 100)]
+    assert torch.equal(got[keep], clean[keep])
+    assert torch.isnan(got[3]).all() and not torch.isfinite(got[100]).any()
