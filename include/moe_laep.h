@@ -517,6 +517,77 @@ int moe_grouped_ffn_bwd_wgrad_gather(const uint16_t *d_out_perm, const uint16_t 
                                      void *ws, size_t ws_bytes, moe_stream_t stream);
 
 /*
+ * Activation checkpoints in 8 bits (no counterpart in the paper). What a layer keeps from its forward
+ * to its backward pass, besides the routing: its input x and the pre-activations [A|B]. X_perm and H, the
+ * other operands of the backward, are made again from them. At T=65536, d=7168, F=2048, top-8 that is 2.8 GB a layer
+ * instead of 15.5 GB.
+ * Format: 32 consecutive values of a row (a row's last block may be shorter) share the scale 2^(s - 127),
+ * the smallest power of two with which the largest of them is at most 448 (s >= 1); each value is
+ * the E4M3 code nearest to value / scale, ties to even: off by at most 2^-4 of itself, or by 2^-10 scales
+ * below 2^-6 scales. A block with an infinity or a NaN reads back as NaN (s = 255).
+ */
+
+/*
+ * moe_ckpt_pack / moe_ckpt_unpack - rows of bf16 into 8 bits and back.
+ * x [rows, cols] bf16, 16-byte aligned; q [rows, cols] uint8 codes, 8-byte aligned; scale
+ * [rows, ceil(cols/32)] uint8, the s of each block. Limits: cols % 8 == 0, 0 <= rows < 2^31.
+ */
+int moe_ckpt_pack(const uint16_t *x, int64_t rows, int cols, uint8_t *q, uint8_t *scale,
+                  moe_stream_t stream);
+int moe_ckpt_unpack(const uint8_t *q, const uint8_t *scale, int64_t rows, int cols, uint16_t *x,
+                    moe_stream_t stream);
+
+/*
+ * moe_ckpt_permute - moe_permute's row copy from a packed x: x_perm[row_of_assignment[t,j], :] =
+ * the unpacked row t, padding rows of the groups zeroed (rows at or past group_offsets[E] are not
+ * written); x [T,d] bf16 receives the unpacked rows themselves unless NULL (the router's backward reads
+ * them). q, scale as moe_ckpt_pack wrote them for T rows of d columns; group_offsets, group_counts,
+ * row_of_assignment from moe_permute (entries outside [0, rows_cap) are left out). Limits as in
+ * moe_permute.
+ */
+int moe_ckpt_permute(const uint8_t *q, const uint8_t *scale, const int32_t *row_of_assignment,
+                     const int32_t *group_offsets, const int32_t *group_counts, int T, int d, int E,
+                     int k, int64_t rows_cap, uint16_t *x, uint16_t *x_perm, moe_stream_t stream);
+
+/*
+ * moe_grouped_ffn_fwd_ckpt - moe_grouped_ffn_fwd that keeps [A|B] in 8 bits instead of ab_saved:
+ * the gate/up GEMM's epilogue packs its fp32 accumulators. h and out_perm are moe_grouped_ffn_fwd's, bit for bit.
+ * ab_q: rows_cap*2F bytes, codes of the [rows, 2F] matrix [A|B] in 32-row blocks, element (r, c) at
+ * ((r/32)*(2F/16) + c/16)*512 + (r%32)*16 + c%16; ab_scale: rows_cap*2F/32 bytes, the s of row r and
+ * columns 32 b .. 32 b + 31 at ((r/32)*(2F/32) + b)*32 + r%32; both 16-byte aligned. Other arguments and
+ * limits as in moe_grouped_ffn_fwd.
+ */
+int moe_grouped_ffn_fwd_ckpt(const uint16_t *x_perm, const int32_t *group_offsets, int E, int d,
+                             int F, int64_t rows_cap, const uint16_t *w_gate_up,
+                             const uint16_t *w_down, uint8_t *ab_q, uint8_t *ab_scale, uint16_t *h,
+                             uint16_t *out_perm, void *ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * moe_grouped_ffn_bwd_dgrad_ckpt - moe_grouped_ffn_bwd_dgrad from [A|B] kept in 8 bits: the dH
+ * GEMM's epilogue unpacks them, and writes H = silu(A) * B [rows_cap,F] bf16, which moe_grouped_ffn_bwd_wgrad
+ * reads, to h (rows below group_offsets[E]). Its results are those of moe_grouped_ffn_bwd_dgrad on
+ * moe_ckpt_unpack_ab's ab_saved. Other arguments and limits as there.
+ */
+int moe_grouped_ffn_bwd_dgrad_ckpt(const uint16_t *d_out_perm, const uint8_t *ab_q,
+                                   const uint8_t *ab_scale, const int32_t *group_offsets, int E,
+                                   int d, int F, int64_t rows_cap, const uint16_t *w_gate_up,
+                                   const uint16_t *w_down, const float *topk_gate,
+                                   const float *d_gate, const int32_t *row_of_assignment,
+                                   const float *w_router, int T, int k, float *d_gate_out,
+                                   uint16_t *h, uint16_t *d_ab, uint16_t *dx_perm, void *ws,
+                                   size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * moe_ckpt_unpack_ab - [A|B] kept in 8 bits back into ab_saved (bf16, the layout of
+ * moe_grouped_ffn_fwd) and H = silu(A) * B into h [rows_cap,F], for callers of the other backward entry
+ * points. Either output may be NULL, not both. Rows below group_offsets[E] are written. All pointers but
+ * group_offsets 16-byte aligned. Limits: 1 <= E <= 256, F % 128 == 0, 128 <= rows_cap < 2^31.
+ */
+int moe_ckpt_unpack_ab(const uint8_t *ab_q, const uint8_t *ab_scale, const int32_t *group_offsets,
+                       int E, int F, int64_t rows_cap, uint16_t *ab_saved, uint16_t *h,
+                       moe_stream_t stream);
+
+/*
  * moe_route_bwd - backward of the router's softmax over the selected experts
  * (the routing scores of Sec. 3.2 as a trainable linear router):
  *   d_logits[t,j] = g[t,j] * (d_gate[t,j] - sum_i g[t,i] * d_gate[t,i])

@@ -583,3 +583,26 @@ def balance_loss(logits, topk_idx, active_mask=None, token_mask=None, seq_offset
         dz[t] += d_loss[1] * 2 * z_coef / M * lse[t][:, None] * p[t]
     return {"loss": loss, "counts": counts, "prob": prob, "n_tokens": np.concatenate([n, [M, N]]),
             "lse": lse, "dz": dz, "p": p, "live": live}
+
+
+def ckpt_round(x):
+    """Rows in 8 bits: 32 consecutive values of a row share 2^(s - 127), the smallest power of two (s >= 1)
+    with which the largest is at most 448; each becomes the nearest E4M3 value (4 significant bits down to
+    2^-6, steps of 2^-9 below; ties to even) times it; a block with an infinity or a NaN becomes NaN
+    (s = 255). Returns (values, s)."""
+    x = np.asarray(x, np.float64)
+    rows, cols = x.shape
+    nblk = -(-cols // 32)
+    b = np.zeros((rows, nblk * 32))
+    b[:, :cols] = x
+    b = b.reshape(rows, nblk, 32)
+    bad = ~np.isfinite(b).all(axis=2)
+    b = np.where(bad[:, :, None], 0.0, b)
+    m, e = np.frexp(np.abs(b).max(axis=2) / 448.0)     # max / 448 = m 2^e, m in [0.5, 1)
+    e = np.where(m == 0.5, e - 1, e)                    # a power of two needs no more
+    e = np.maximum(np.where(m == 0, -126, e), -126)
+    y = np.ldexp(b, -e[:, :, None])
+    step = np.ldexp(1.0, np.maximum(np.frexp(y)[1] - 1, -6) - 3)
+    v = np.ldexp(np.round(y / step) * step, e[:, :, None])
+    v[bad] = np.nan
+    return v.reshape(rows, -1)[:, :cols], np.where(bad, 255, e + 127).astype(np.uint8)

@@ -69,6 +69,13 @@ _SIGS = {
     "moe_grouped_ffn_bwd_wgrad_gather": (I, [P, P, P, I, P, P, P, P, I, I, I, I64, P, P, P, SZ,
                                              P]),
     "moe_selftest_wait_timeout": (I, [I64, P]),
+    "moe_ckpt_pack": (I, [P, I64, I, P, P, P]),
+    "moe_ckpt_unpack": (I, [P, P, I64, I, P, P]),
+    "moe_ckpt_permute": (I, [P, P, P, P, P, I, I, I, I, I64, P, P, P]),
+    "moe_ckpt_unpack_ab": (I, [P, P, P, I, I, I64, P, P, P]),
+    "moe_grouped_ffn_fwd_ckpt": (I, [P, P, I, I, I, I64, P, P, P, P, P, P, P, SZ, P]),
+    "moe_grouped_ffn_bwd_dgrad_ckpt": (I, [P, P, P, P, I, I, I, I64, P, P, P, P, P, P, I, I, P, P,
+                                           P, P, P, SZ, P]),
     "moe_route_bwd_dense": (I, [P, P, P, P, P, I, I, I, I, P, P, P, SZ, P]),
     "moe_route_dx": (I, [P, P, P, I, I, I, I, P, P, SZ, P]),
     "moe_balance_workspace_size": (SZ, [I, I, I]),
@@ -307,6 +314,47 @@ def moe_route_bwd(x, topk_idx, topk_gate, d_gate, T, d, E, k, d_logits, dw_route
     _check("moe_route_bwd", load().moe_route_bwd(
         _ptr(x), _ptr(topk_idx), _ptr(topk_gate), _ptr(d_gate), T, d, E, k, _ptr(d_logits),
         _ptr(dw_router), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_ckpt_pack(x, rows, cols, q, scale, stream=None):
+    _check("moe_ckpt_pack", load().moe_ckpt_pack(_ptr(x), rows, cols, _ptr(q), _ptr(scale),
+                                                 _stream(stream)))
+
+
+def moe_ckpt_unpack(q, scale, rows, cols, x, stream=None):
+    _check("moe_ckpt_unpack", load().moe_ckpt_unpack(_ptr(q), _ptr(scale), rows, cols, _ptr(x),
+                                                     _stream(stream)))
+
+
+def moe_ckpt_permute(q, scale, row_of_assignment, group_offsets, group_counts, T, d, E, k, rows_cap,
+                     x, x_perm, stream=None):
+    _check("moe_ckpt_permute", load().moe_ckpt_permute(
+        _ptr(q), _ptr(scale), _ptr(row_of_assignment), _ptr(group_offsets), _ptr(group_counts), T,
+        d, E, k, rows_cap, _ptr(x), _ptr(x_perm), _stream(stream)))
+
+
+def moe_ckpt_unpack_ab(ab_q, ab_scale, group_offsets, E, F, rows_cap, ab_saved, h, stream=None):
+    _check("moe_ckpt_unpack_ab", load().moe_ckpt_unpack_ab(
+        _ptr(ab_q), _ptr(ab_scale), _ptr(group_offsets), E, F, rows_cap, _ptr(ab_saved), _ptr(h),
+        _stream(stream)))
+
+
+def moe_grouped_ffn_fwd_ckpt(x_perm, group_offsets, E, d, F, rows_cap, w_gate_up, w_down, ab_q,
+                             ab_scale, h, out_perm, ws, ws_bytes, stream=None):
+    _check("moe_grouped_ffn_fwd_ckpt", load().moe_grouped_ffn_fwd_ckpt(
+        _ptr(x_perm), _ptr(group_offsets), E, d, F, rows_cap, _ptr(w_gate_up), _ptr(w_down),
+        _ptr(ab_q), _ptr(ab_scale), _ptr(h), _ptr(out_perm), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_grouped_ffn_bwd_dgrad_ckpt(d_out_perm, ab_q, ab_scale, group_offsets, E, d, F, rows_cap,
+                                   w_gate_up, w_down, topk_gate, d_gate, row_of_assignment,
+                                   w_router, T, k, d_gate_out, h, d_ab, dx_perm, ws, ws_bytes,
+                                   stream=None):
+    _check("moe_grouped_ffn_bwd_dgrad_ckpt", load().moe_grouped_ffn_bwd_dgrad_ckpt(
+        _ptr(d_out_perm), _ptr(ab_q), _ptr(ab_scale), _ptr(group_offsets), E, d, F, rows_cap,
+        _ptr(w_gate_up), _ptr(w_down), _ptr(topk_gate), _ptr(d_gate), _ptr(row_of_assignment),
+        _ptr(w_router), T, k, _ptr(d_gate_out), _ptr(h), _ptr(d_ab), _ptr(dx_perm), _ptr(ws),
+        ws_bytes, _stream(stream)))
 
 
 def moe_route_bwd_dense(x, topk_idx, topk_gate, d_gate, dz, T, d, E, k, d_logits, dw_router, ws,

@@ -28,6 +28,7 @@
 #include <cuda.h>
 #include <stdlib.h>
 
+#include "ckpt.cuh"
 #include "common.cuh"
 #include "tc_ptx.cuh"
 #include "tmap.cuh"
@@ -105,6 +106,8 @@ struct GemmParams {
   uint16_t *out;   // primary output
   uint16_t *out2;  // kGateUp: pre-activations [A|B] (32-row blocked, see ab_block_index)
   const uint16_t *aux;  // kDgradDown: saved pre-activations [rows, 2F]
+  // Kernels with CK: the pre-activations kept in 8 bits (ckpt.cuh) in the place of out2 / aux.
+  uint8_t *ab_q, *ab_scale;
   // Gathered operand (kGateUp: A, kWgradGateUp: B): grouped row r reads row
   // token_of_row[r] of x [T, d] instead of row r of X_perm (nullptr: X_perm).
   const int32_t *token_of_row;
@@ -149,20 +152,6 @@ struct Tile {
 __device__ __forceinline__ void fail(volatile int *abort_flag) {
   dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
   *abort_flag = 1;
-}
-
-// sigmoid(a) = 1 / (1 + e^-a) with the fast reciprocal-based divide (2 ulp; the
-// results are rounded to bf16). For very negative a, e^-a overflows to +inf and
-// the quotient is 0, the limit of the function.
-__device__ __forceinline__ float sigmoid_f(float a) { return __fdividef(1.f, 1.f + __expf(-a)); }
-__device__ __forceinline__ float silu_f(float a) { return a * sigmoid_f(a); }
-
-// Saved pre-activations [A|B] are stored in 32-row blocks: element (r, c) of the
-// [rows, 2F] matrix lives at ((r/32)*(2F/8) + c/8)*256 + (r%32)*8 + c%8, so the
-// 32 rows a warp owns in the epilogue touch 512 contiguous bytes per 8 columns
-// (one coalesced warp access in the forward's store and the backward's load).
-__device__ __forceinline__ size_t ab_block_index(size_t row, int col, int F) {
-  return ((row >> 5) * size_t(2 * F / 8) + size_t(col >> 3)) * 256 + (row & 31) * 8 + (col & 7);
 }
 
 // Epilogue of one accumulator tile for the 32 rows and the column half (`half`) this
@@ -210,8 +199,32 @@ __device__ __forceinline__ void pack32(const uint32_t (&r)[32], uint4 (&v)[4]) {
   }
 }
 
-template <int MODE, int BN>
-__device__ __forceinline__ void epilogue_tile(const GemmParams &p, const CUtensorMap *tmO,
+// Keeps 32 consecutive values of this lane's row, columns col .. col + 31 of [A|B], in 8 bits, from the
+// fp32 accumulators: one rounding (through bf16 first, one value in 32 would go to the other
+// neighbour). ~110 instructions per 32 values, where storing bf16 takes ~30, and half the bytes.
+__device__ __forceinline__ void keep_8bit(const GemmParams &p, size_t row, int col, const uint32_t (&r)[32]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) m = max(m, r[i] & 0x7fffffffu);
+  const uint32_t s = ckpt::scale_byte(m);
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = ckpt::kNanCodes;
+  if (s != 255u) {
+    const float inv = ckpt::scale_inverse(s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      w[i] = ckpt::codes4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]),
+                          __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]), inv);
+  }
+  uint8_t *dst = p.ab_q + ckpt::ab_code_index(row, col, p.F);
+  stg_v4(dst, make_uint4(w[0], w[1], w[2], w[3]));
+  stg_v4(dst + 512, make_uint4(w[4], w[5], w[6], w[7]));
+  p.ab_scale[ckpt::ab_scale_index(row, col, p.F)] = uint8_t(s);
+}
+
+template <int MODE, int BN, bool CK>
+__device__ __forceinline__ void epilogue_tile(const GemmParams &p, const CUtensorMap *tmO, const CUtensorMap *tmH,
                                               uint32_t stage, int lane, uint32_t tb, size_t row,
                                               int out_row, int e, int nt, int half) {
   using Tr = Traits<MODE>;
@@ -236,8 +249,14 @@ __device__ __forceinline__ void epilogue_tile(const GemmParams &p, const CUtenso
         }
         const int col = nt * 128 + c + v * 8;
         vh[v] = pack8(fh);
-        stg_v4(p.out2 + ab_block_index(row, col, F), pack8(fa));
-        stg_v4(p.out2 + ab_block_index(row, F + col, F), pack8(fb));
+        if (!CK) {
+          stg_v4(p.out2 + ab_block_index(row, col, F), pack8(fa));
+          stg_v4(p.out2 + ab_block_index(row, F + col, F), pack8(fb));
+        }
+      }
+      if (CK) {
+        keep_8bit(p, row, nt * 128 + c, ra);
+        keep_8bit(p, row, F + nt * 128 + c, rb);
       }
       stage_and_store(tmO, stage, lane, vh, nt * 128 + c, trow);
     }
@@ -249,21 +268,42 @@ __device__ __forceinline__ void epilogue_tile(const GemmParams &p, const CUtenso
 #pragma unroll 1
     for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 32) {
       if (f0 + c >= F) break;  // a cut last tile
+      // CK: 32 codes and a scale of each of A and B in va[0..1], vb[0..1], and H for dW_down besides
       uint4 va[4], vb[4];
+      float sa = 0.f, sb = 0.f;
+      if (CK) {
+        const uint8_t *qa = p.ab_q + ckpt::ab_code_index(row, f0 + c, F), *qb = p.ab_q + ckpt::ab_code_index(row, F + f0 + c, F);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        va[v] = ldg_nc_v4(p.aux + ab_block_index(row, f0 + c + v * 8, F));
-        vb[v] = ldg_nc_v4(p.aux + ab_block_index(row, F + f0 + c + v * 8, F));
+        for (int v = 0; v < 2; ++v) {
+          va[v] = ldg_nc_v4(qa + 512 * v);
+          vb[v] = ldg_nc_v4(qb + 512 * v);
+        }
+        sa = ckpt::scale_value(__ldg(p.ab_scale + ckpt::ab_scale_index(row, f0 + c, F)));
+        sb = ckpt::scale_value(__ldg(p.ab_scale + ckpt::ab_scale_index(row, F + f0 + c, F)));
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          va[v] = ldg_nc_v4(p.aux + ab_block_index(row, f0 + c + v * 8, F));
+          vb[v] = ldg_nc_v4(p.aux + ab_block_index(row, F + f0 + c + v * 8, F));
+        }
       }
       uint32_t r[32];
       tc::tmem_ld_32x32b_x32(tb + c, r);
       tc::tmem_ld_wait();
-      uint4 vda[4], vdb[4];
+      uint4 vda[4], vdb[4], vh[4];
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        float fa[8], fb[8], da[8], db[8];
-        unpack8(va[v], fa);
-        unpack8(vb[v], fb);
+        float fa[8], fb[8], da[8], db[8], fh[8];
+        if (CK) {
+          const uint4 &qa = va[v / 2], &qb = vb[v / 2];
+          ckpt::values4(v % 2 ? qa.z : qa.x, sa, fa);
+          ckpt::values4(v % 2 ? qa.w : qa.y, sa, fa + 4);
+          ckpt::values4(v % 2 ? qb.z : qb.x, sb, fb);
+          ckpt::values4(v % 2 ? qb.w : qb.y, sb, fb + 4);
+        } else {
+          unpack8(va[v], fa);
+          unpack8(vb[v], fb);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float dh = __uint_as_float(r[v * 8 + i]);
@@ -271,12 +311,15 @@ __device__ __forceinline__ void epilogue_tile(const GemmParams &p, const CUtenso
           da[i] = dh * fb[i] * (sg * (1.f + fa[i] * (1.f - sg)));
           db[i] = dh * fa[i] * sg;
           gsum = fmaf(db[i], fb[i], gsum);  // dh * silu(a) * b = dH * H
+          if (CK) fh[i] = fa[i] * sg * fb[i];
         }
         vda[v] = pack8(da);
         vdb[v] = pack8(db);
+        if (CK) vh[v] = pack8(fh);
       }
       stage_and_store(tmO, stage, lane, vda, f0 + c, trow);
       stage_and_store(tmO, stage, lane, vdb, F + f0 + c, trow);
+      if (CK) stage_and_store(tmH, stage, lane, vh, f0 + c, trow);
       if (BN == 256 && c == half * 128 + 32) {
         gsum0 = gsum;
         gsum = 0.f;
@@ -417,11 +460,12 @@ __device__ __forceinline__ int ctas_with_one_tile(const int *s_key, const int *s
   return best_i * per_e;
 }
 
-template <int MODE, int BN>
+template <int MODE, int BN, bool CK>
 __global__ void __launch_bounds__(kThreads, 1)
     grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                         const __grid_constant__ CUtensorMap tmB,
-                        const __grid_constant__ CUtensorMap tmO, const GemmParams p) {
+                        const __grid_constant__ CUtensorMap tmO,
+                        const __grid_constant__ CUtensorMap tmH, const GemmParams p) {
   using Tr = Traits<MODE>;
   using Sh = Shape<BN>;
   constexpr int STAGES = Sh::STAGES;
@@ -660,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::fence_after_sync();
       const uint32_t tb = tmem_base + (uint32_t(q * 32) << 16) + a * BN;
 
-      epilogue_tile<MODE, BN>(p, &tmO, stage, lane, tb,
+      epilogue_tile<MODE, BN, CK>(p, &tmO, &tmH, stage, lane, tb,
                               size_t(t.goff) + size_t(t.mt) * BM + r_in_tile,
                               t.mt * BM + r_in_tile, t.e, t.nt, half);
       tc::fence_before_sync();
@@ -757,11 +801,14 @@ __device__ __forceinline__ int4 ld_rows4(const int32_t *p) {
 // GB300 at T=16384, d=4096, 48 live experts: both GEMMs take ~3.3x as long as with
 // X_perm tile loads (each k-block needs 32 gathers of 4 x 128 bytes where one tile
 // load moves 128 rows; the per-instruction cost of the gathers sets the pace).
-template <int MODE, int BN, bool GATHER>
+// CK (kGateUp, kDgradDown): the pre-activations are kept in 8 bits, and kDgradDown stores H (map
+// tmH), which dW_down needs, besides [dA|dB].
+template <int MODE, int BN, bool GATHER, bool CK>
 __global__ void __launch_bounds__(kThreads, 1)
     grouped_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA,
                              const __grid_constant__ CUtensorMap tmB,
-                             const __grid_constant__ CUtensorMap tmO, const GemmParams p) {
+                             const __grid_constant__ CUtensorMap tmO,
+                             const __grid_constant__ CUtensorMap tmH, const GemmParams p) {
   using Tr = Traits<MODE>;
   constexpr int KB = GATHER ? 64 : 128;
   using Sh = PairShape<BN, KB>;
@@ -1278,7 +1325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           continue;
         }
         if (mine) {
-          epilogue_tile<MODE, BN>(p, &tmO, stage, lane, tb,
+          epilogue_tile<MODE, BN, CK>(p, &tmO, &tmH, stage, lane, tb,
                                   size_t(t.goff) + size_t(mt) * BM + r_in_tile,
                                   mt * BM + r_in_tile, t.e, t.nt, half);
         }
@@ -1349,27 +1396,27 @@ int use_sched_ws(GemmParams &p, void *ws, size_t ws_bytes, const char *fn) {
   return MOE_OK;
 }
 
-template <int MODE, int BN>
-int launch_one(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o,
+template <int MODE, int BN, bool CK>
+int launch_one(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &h,
                const GemmParams &p, cudaStream_t s, const char *what) {
   using Sh = Shape<BN>;
   static bool attr = false;
   if (!attr) {
-    cudaError_t e = cudaFuncSetAttribute(grouped_gemm_kernel<MODE, BN>,
+    cudaError_t e = cudaFuncSetAttribute(grouped_gemm_kernel<MODE, BN, CK>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, int(Sh::SMEM));
     if (e != cudaSuccess) return moe::cuda_status(e, what);
     attr = true;
   }
-  MOE_LAUNCH(kGemmName[MODE], s, moe::launch_dep(grouped_gemm_kernel<MODE, BN>, moe::num_sms(), kThreads, Sh::SMEM, s,
-                                                 a, b, o, p));
+  MOE_LAUNCH(kGemmName[MODE], s, moe::launch_dep(grouped_gemm_kernel<MODE, BN, CK>, moe::num_sms(), kThreads, Sh::SMEM, s,
+                                                 a, b, o, h, p));
   return moe::launch_status(what);
 }
 
-template <int MODE, int BN, bool GATHER>
-int launch_pair(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o,
+template <int MODE, int BN, bool GATHER, bool CK>
+int launch_pair(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &h,
                 const GemmParams &p, cudaStream_t s, const char *what) {
   using Sh = PairShape<BN, GATHER ? 64 : 128>;
-  auto kern = grouped_gemm_pair_kernel<MODE, BN, GATHER>;
+  auto kern = grouped_gemm_pair_kernel<MODE, BN, GATHER, CK>;
   cudaLaunchAttribute at[3];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = 2;
@@ -1405,7 +1452,7 @@ int launch_pair(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o
   }
   cfg.gridDim = dim3(2 * nclusters);
   cfg.numAttrs = 3;
-  MOE_LAUNCH(kGemmName[MODE], s, cudaLaunchKernelEx(&cfg, kern, a, b, o, p));
+  MOE_LAUNCH(kGemmName[MODE], s, cudaLaunchKernelEx(&cfg, kern, a, b, o, h, p));
   return moe::launch_status(what);
 }
 
@@ -1502,26 +1549,27 @@ GemmPlan wgrad_plan(int N, int m_tiles, int64_t rows_cap, int E, bool gather) {
 
 // Builds the tensor maps for one GEMM and launches it. A: [a_rows, a_cols] row-major
 // bf16; B likewise. N = output columns (for kGateUp: 2F, in tiles of 128 gate + 128 up).
-// The output p.out is [o_rows, o_cols] row-major bf16.
-template <int MODE>
+// The output p.out is [o_rows, o_cols] row-major bf16. CK: see grouped_gemm_pair_kernel; h is
+// then kDgradDown's second output [o_rows, F].
+template <int MODE, bool CK = false>
 int run_gemm_out(int N, const void *a_base, uint64_t a_rows, uint64_t a_cols, const void *b_base,
                  uint64_t b_rows, uint64_t b_cols, const void *o_base, uint64_t o_rows,
-                 uint64_t o_cols, GemmParams p, cudaStream_t s, const char *what);
+                 uint64_t o_cols, GemmParams p, cudaStream_t s, const char *what, const void *h = nullptr);
 
-template <int MODE>
+template <int MODE, bool CK = false>
 int run_gemm(int N, const void *a_base, uint64_t a_rows, uint64_t a_cols, const void *b_base,
              uint64_t b_rows, uint64_t b_cols, uint64_t o_rows, uint64_t o_cols, GemmParams p,
-             cudaStream_t s, const char *what) {
-  return run_gemm_out<MODE>(N, a_base, a_rows, a_cols, b_base, b_rows, b_cols, p.out, o_rows,
-                            o_cols, p, s, what);
+             cudaStream_t s, const char *what, const void *h = nullptr) {
+  return run_gemm_out<MODE, CK>(N, a_base, a_rows, a_cols, b_base, b_rows, b_cols, p.out, o_rows,
+                                o_cols, p, s, what, h);
 }
 
 // As run_gemm, with the output tensor map built over o_base (p.out may be nullptr when
 // the epilogue stores no output tile).
-template <int MODE>
+template <int MODE, bool CK>
 int run_gemm_out(int N, const void *a_base, uint64_t a_rows, uint64_t a_cols, const void *b_base,
                  uint64_t b_rows, uint64_t b_cols, const void *o_base, uint64_t o_rows,
-                 uint64_t o_cols, GemmParams p, cudaStream_t s, const char *what) {
+                 uint64_t o_cols, GemmParams p, cudaStream_t s, const char *what, const void *h) {
   using Tr = Traits<MODE>;
   if (!Tr::WGRAD) p.dynamic = 0;  // equal-cost tiles: fixed stride, no counter to reset
   const bool gather = p.token_of_row != nullptr;
@@ -1554,33 +1602,35 @@ int run_gemm_out(int N, const void *a_base, uint64_t a_rows, uint64_t a_cols, co
     return st;
   CUtensorMap mo;  // the epilogue's output, in 32 x 32 chunks
   if ((st = make_map(&mo, o_base, o_rows, o_cols, 32, 32, what, CU_TENSOR_MAP_SWIZZLE_64B))) return st;
+  CUtensorMap mh = mo;
+  if (h != nullptr && (st = make_map(&mh, h, o_rows, uint64_t(p.F), 32, 32, what, CU_TENSOR_MAP_SWIZZLE_64B))) return st;
   if (pair) {
-    if constexpr (MODE == kGateUp || MODE == kWgradGateUp) {
+    if constexpr ((MODE == kGateUp || MODE == kWgradGateUp) && !CK) {
       if (gather)
-        return BN == 256 ? launch_pair<MODE, 256, true>(ma, mb, mo, p, s, what)
-                         : launch_pair<MODE, 128, true>(ma, mb, mo, p, s, what);
+        return BN == 256 ? launch_pair<MODE, 256, true, false>(ma, mb, mo, mh, p, s, what)
+                         : launch_pair<MODE, 128, true, false>(ma, mb, mo, mh, p, s, what);
     }
     if (Tr::WGRAD || !split_rows(a_rows))
-      return BN == 256 ? launch_pair<MODE, 256, false>(ma, mb, mo, p, s, what)
-                       : launch_pair<MODE, 128, false>(ma, mb, mo, p, s, what);
+      return BN == 256 ? launch_pair<MODE, 256, false, CK>(ma, mb, mo, mh, p, s, what)
+                       : launch_pair<MODE, 128, false, CK>(ma, mb, mo, mh, p, s, what);
     // Activation GEMMs on many rows: a group's last block of an odd number of 128-row
     // blocks would be half of a 256-row pair tile whose other half is computed and dropped;
     // the one-SM kernel (128-row tiles) takes those blocks in a second launch.
     GemmParams q = p;
     q.rows_split = 1;
-    if ((st = BN == 256 ? launch_pair<MODE, 256, false>(ma, mb, mo, q, s, what)
-                        : launch_pair<MODE, 128, false>(ma, mb, mo, q, s, what)))
+    if ((st = BN == 256 ? launch_pair<MODE, 256, false, CK>(ma, mb, mo, mh, q, s, what)
+                        : launch_pair<MODE, 128, false, CK>(ma, mb, mo, mh, q, s, what)))
       return st;
     CUtensorMap mb1;  // the one-SM kernel's B boxes
     if ((st = Tr::B_MN ? make_map(&mb1, b_base, b_rows, b_cols, 64, BK, what)
                        : make_map(&mb1, b_base, b_rows, b_cols, BK, 128, what)))
       return st;
     q.rows_split = 2;
-    return BN == 256 ? launch_one<MODE, 256>(ma, mb1, mo, q, s, what)
-                     : launch_one<MODE, 128>(ma, mb1, mo, q, s, what);
+    return BN == 256 ? launch_one<MODE, 256, CK>(ma, mb1, mo, mh, q, s, what)
+                     : launch_one<MODE, 128, CK>(ma, mb1, mo, mh, q, s, what);
   }
-  return BN == 256 ? launch_one<MODE, 256>(ma, mb, mo, p, s, what)
-                   : launch_one<MODE, 128>(ma, mb, mo, p, s, what);
+  return BN == 256 ? launch_one<MODE, 256, CK>(ma, mb, mo, mh, p, s, what)
+                   : launch_one<MODE, 128, CK>(ma, mb, mo, mh, p, s, what);
 }
 
 int check_common(int E, int d, int F, int64_t rows_cap, const char *fn) {
@@ -1742,36 +1792,57 @@ int moe_selftest_wait_timeout(int64_t limit_ns, moe_stream_t stream) {
   return moe::launch_status("moe_selftest_wait_timeout");
 }
 
-int moe_grouped_ffn_fwd(const uint16_t *x_perm, const int32_t *group_offsets, int E, int d, int F,
-                        int64_t rows_cap, const uint16_t *w_gate_up, const uint16_t *w_down,
-                        uint16_t *ab_saved, uint16_t *h, uint16_t *out_perm, void *ws,
-                        size_t ws_bytes, moe_stream_t stream) {
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (int st = check_common(E, d, F, rows_cap, "moe_grouped_ffn_fwd")) return st;
-  const void *ptrs[] = {x_perm, group_offsets, w_gate_up, w_down, ab_saved, h, out_perm};
+// moe_grouped_ffn_fwd, and with the pre-activations kept in 8 bits (ab_q, ab_scale) in the place of ab_saved.
+static int ffn_fwd(const char *fn, const uint16_t *x_perm, const int32_t *group_offsets, int E, int d, int F,
+                   int64_t rows_cap, const uint16_t *w_gate_up, const uint16_t *w_down, bool keep8,
+                   uint16_t *ab_saved, uint8_t *ab_q, uint8_t *ab_scale, uint16_t *h, uint16_t *out_perm,
+                   void *ws, size_t ws_bytes, cudaStream_t s) {
+  if (int st = check_common(E, d, F, rows_cap, fn)) return st;
+  const void *ptrs[] = {x_perm, group_offsets, w_gate_up, w_down, keep8 ? static_cast<const void *>(ab_q) : ab_saved,
+                        keep8 ? static_cast<const void *>(ab_scale) : ab_saved, h, out_perm};
   for (const void *q : ptrs)
-    if (!q || !moe::aligned16(q)) return moe::set_error(MOE_ERR_ARG, "moe_grouped_ffn_fwd: null or unaligned pointer");
+    if (!q || !moe::aligned16(q)) return moe::set_error(MOE_ERR_ARG, "%s: null or unaligned pointer", fn);
   const uint64_t R = uint64_t(rows_cap);
   GemmParams p{};
-  if (int st = use_sched_ws(p, ws, ws_bytes, "moe_grouped_ffn_fwd")) return st;
+  if (int st = use_sched_ws(p, ws, ws_bytes, fn)) return st;
   p.group_offsets = group_offsets;
   p.E = E; p.d = d; p.F = F;
   // [A | B] = X W_gate_up^T, H = silu(A) * B
   p.nkb = d / BK;
   p.out = h;
   p.out2 = ab_saved;
-  if (int st = run_gemm<kGateUp>(2 * F, x_perm, R, d, w_gate_up, uint64_t(E) * 2 * F, d, R, F, p,
-                                 s, "moe_grouped_ffn_fwd: gate/up GEMM"))
+  p.ab_q = ab_q;
+  p.ab_scale = ab_scale;
+  const char *what = "moe_grouped_ffn_fwd: gate/up GEMM";
+  const uint64_t wr = uint64_t(E) * 2 * F;
+  if (int st = keep8 ? run_gemm<kGateUp, true>(2 * F, x_perm, R, d, w_gate_up, wr, d, R, F, p, s, what)
+                     : run_gemm<kGateUp>(2 * F, x_perm, R, d, w_gate_up, wr, d, R, F, p, s, what))
     return st;
   // O = H W_down^T
   GemmParams q{};
-  use_sched_ws(q, ws, ws_bytes, "moe_grouped_ffn_fwd");
+  use_sched_ws(q, ws, ws_bytes, fn);
   q.group_offsets = group_offsets;
   q.E = E; q.d = d; q.F = F;
   q.nkb = F / BK;
   q.out = out_perm;
   return run_gemm<kDown>(d, h, R, F, w_down, uint64_t(E) * d, F, R, d, q, s,
                          "moe_grouped_ffn_fwd: down GEMM");
+}
+
+int moe_grouped_ffn_fwd(const uint16_t *x_perm, const int32_t *group_offsets, int E, int d, int F,
+                        int64_t rows_cap, const uint16_t *w_gate_up, const uint16_t *w_down,
+                        uint16_t *ab_saved, uint16_t *h, uint16_t *out_perm, void *ws,
+                        size_t ws_bytes, moe_stream_t stream) {
+  return ffn_fwd("moe_grouped_ffn_fwd", x_perm, group_offsets, E, d, F, rows_cap, w_gate_up, w_down, false, ab_saved,
+                 nullptr, nullptr, h, out_perm, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int moe_grouped_ffn_fwd_ckpt(const uint16_t *x_perm, const int32_t *group_offsets, int E, int d, int F,
+                             int64_t rows_cap, const uint16_t *w_gate_up, const uint16_t *w_down,
+                             uint8_t *ab_q, uint8_t *ab_scale, uint16_t *h, uint16_t *out_perm, void *ws,
+                             size_t ws_bytes, moe_stream_t stream) {
+  return ffn_fwd("moe_grouped_ffn_fwd_ckpt", x_perm, group_offsets, E, d, F, rows_cap, w_gate_up, w_down, true, nullptr,
+                 ab_q, ab_scale, h, out_perm, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int moe_grouped_ffn_fwd_combine(const uint16_t *x_perm, const int32_t *group_offsets, int E, int d,
@@ -1879,17 +1950,17 @@ int moe_grouped_ffn_fwd_gather(const uint16_t *x, const int32_t *token_of_row, i
                          "moe_grouped_ffn_fwd_gather: down GEMM");
 }
 
-int moe_grouped_ffn_bwd_dgrad(const uint16_t *d_out_perm, const uint16_t *ab_saved,
-                              const int32_t *group_offsets, int E, int d, int F, int64_t rows_cap,
-                              const uint16_t *w_gate_up, const uint16_t *w_down,
-                              const float *topk_gate, const float *d_gate,
-                              const int32_t *row_of_assignment, const float *w_router, int T,
-                              int k, float *d_gate_out, uint16_t *d_ab, uint16_t *dx_perm,
-                              void *ws, size_t ws_bytes, moe_stream_t stream) {
-  const char *fn = "moe_grouped_ffn_bwd_dgrad";
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+// moe_grouped_ffn_bwd_dgrad, and with the pre-activations kept in 8 bits (then H is written to h).
+static int ffn_dgrad(const char *fn, const uint16_t *d_out_perm, bool keep8, const uint16_t *ab_saved,
+                     const uint8_t *ab_q, const uint8_t *ab_scale, const int32_t *group_offsets, int E, int d, int F,
+                     int64_t rows_cap, const uint16_t *w_gate_up, const uint16_t *w_down,
+                     const float *topk_gate, const float *d_gate, const int32_t *row_of_assignment,
+                     const float *w_router, int T, int k, float *d_gate_out, uint16_t *h, uint16_t *d_ab,
+                     uint16_t *dx_perm, void *ws, size_t ws_bytes, cudaStream_t s) {
   if (int st = check_common(E, d, F, rows_cap, fn)) return st;
-  const void *ptrs[] = {d_out_perm, ab_saved, group_offsets, w_gate_up, w_down, d_ab, dx_perm};
+  const void *ptrs[] = {d_out_perm, keep8 ? static_cast<const void *>(ab_q) : ab_saved,
+                        keep8 ? static_cast<const void *>(ab_scale) : ab_saved,
+                        keep8 ? static_cast<const void *>(h) : ab_saved, group_offsets, w_gate_up, w_down, d_ab, dx_perm};
   for (const void *q : ptrs)
     if (!q || !moe::aligned16(q)) return moe::set_error(MOE_ERR_ARG, "%s: null or unaligned pointer", fn);
   const uint64_t R = uint64_t(rows_cap);
@@ -1924,11 +1995,14 @@ int moe_grouped_ffn_bwd_dgrad(const uint16_t *d_out_perm, const uint16_t *ab_sav
   p.nkb = d / BK;
   p.out = d_ab;
   p.aux = ab_saved;
+  p.ab_q = const_cast<uint8_t *>(ab_q);  // (read only)
+  p.ab_scale = const_cast<uint8_t *>(ab_scale);
   if (gate) p.gate_partial = reinterpret_cast<float *>(static_cast<char *>(ws) + L.gate_partial);
   float *row_dz = router ? reinterpret_cast<float *>(static_cast<char *>(ws) + L.row_dz) : nullptr;
   p.zero_dz = row_dz;
-  if ((st = run_gemm<kDgradDown>(F, d_out_perm, R, d, w_down, uint64_t(E) * d, F, R, 2 * F, p,
-                                 s, "moe_grouped_ffn_bwd: dH GEMM")))
+  const char *what = "moe_grouped_ffn_bwd: dH GEMM";
+  if ((st = keep8 ? run_gemm<kDgradDown, true>(F, d_out_perm, R, d, w_down, uint64_t(E) * d, F, R, 2 * F, p, s, what, h)
+                  : run_gemm<kDgradDown>(F, d_out_perm, R, d, w_down, uint64_t(E) * d, F, R, 2 * F, p, s, what)))
     return st;
   if (T > 0 && (gate || router)) {
     const float *part = p.gate_partial;
@@ -1956,6 +2030,30 @@ int moe_grouped_ffn_bwd_dgrad(const uint16_t *d_out_perm, const uint16_t *ab_sav
   p.aux = nullptr;
   return run_gemm<kDgradGateUp>(d, d_ab, R, 2 * F, w_gate_up, uint64_t(E) * 2 * F, d, R, d, p,
                                 s, "moe_grouped_ffn_bwd: dX GEMM");
+}
+
+int moe_grouped_ffn_bwd_dgrad(const uint16_t *d_out_perm, const uint16_t *ab_saved,
+                              const int32_t *group_offsets, int E, int d, int F, int64_t rows_cap,
+                              const uint16_t *w_gate_up, const uint16_t *w_down,
+                              const float *topk_gate, const float *d_gate,
+                              const int32_t *row_of_assignment, const float *w_router, int T,
+                              int k, float *d_gate_out, uint16_t *d_ab, uint16_t *dx_perm,
+                              void *ws, size_t ws_bytes, moe_stream_t stream) {
+  return ffn_dgrad("moe_grouped_ffn_bwd_dgrad", d_out_perm, false, ab_saved, nullptr, nullptr, group_offsets, E, d, F,
+                   rows_cap, w_gate_up, w_down, topk_gate, d_gate, row_of_assignment, w_router, T, k, d_gate_out,
+                   nullptr, d_ab, dx_perm, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int moe_grouped_ffn_bwd_dgrad_ckpt(const uint16_t *d_out_perm, const uint8_t *ab_q, const uint8_t *ab_scale,
+                                   const int32_t *group_offsets, int E, int d, int F, int64_t rows_cap,
+                                   const uint16_t *w_gate_up, const uint16_t *w_down,
+                                   const float *topk_gate, const float *d_gate,
+                                   const int32_t *row_of_assignment, const float *w_router, int T,
+                                   int k, float *d_gate_out, uint16_t *h, uint16_t *d_ab,
+                                   uint16_t *dx_perm, void *ws, size_t ws_bytes, moe_stream_t stream) {
+  return ffn_dgrad("moe_grouped_ffn_bwd_dgrad_ckpt", d_out_perm, true, nullptr, ab_q, ab_scale, group_offsets, E, d, F,
+                   rows_cap, w_gate_up, w_down, topk_gate, d_gate, row_of_assignment, w_router, T, k, d_gate_out,
+                   h, d_ab, dx_perm, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int moe_grouped_ffn_bwd_wgrad(const uint16_t *d_out_perm, const uint16_t *x_perm,

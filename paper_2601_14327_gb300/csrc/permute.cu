@@ -221,22 +221,7 @@ __global__ void __launch_bounds__(kThreads) pad_token_kernel(const int32_t *__re
   for (int r = r0 + threadIdx.x; r < r1; r += kThreads) token_of_row[r] = 0;
 }
 
-// Zeroes the padding rows [group_offsets[e] + group_counts[e], group_offsets[e+1]) of expert
-// b / kPadSplit, share b % kPadSplit. The first E * kPadSplit blocks of the kernels that
-// write a grouped tensor do this beside the token rows (as a launch of its own it took
-// 8 us of a 240 us dispatch at T=16384, d=4096, 64 experts, and 2-3 us of a small one).
-constexpr int kPadSplit = 8;
-__device__ __forceinline__ void zero_pad_rows(int b, const int32_t *__restrict__ group_offsets,
-                                              const int32_t *__restrict__ group_counts, int d,
-                                              int64_t rows_cap, uint16_t *__restrict__ buf) {
-  const int e = b / kPadSplit;
-  const int r0 = group_offsets[e] + group_counts[e];
-  const int r1 = int(min((long long)group_offsets[e + 1], (long long)rows_cap));
-  const int nv = d / 8;
-  const uint4 z = make_uint4(0, 0, 0, 0);
-  for (int r = r0 + (b % kPadSplit) * kWarps + int(threadIdx.x >> 5); r < r1; r += kPadSplit * kWarps)
-    for (int c = threadIdx.x & 31; c < nv; c += 32) stg_v4(buf + size_t(r) * d + c * 8, z);
-}
+using moe::kPadSplit;
 
 // Token and column segment of a warp: nseg warps share a token, warp `seg` taking its 16-byte
 // vectors lane + 32 (seg + nseg i) (see token_segments). False past the last token.
@@ -257,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) perm_gather_kernel(
     const int32_t *__restrict__ group_counts, uint16_t *__restrict__ x_perm) {
   pdl_start();
   if (int(blockIdx.x) < pad_blocks) {
-    zero_pad_rows(blockIdx.x, group_offsets, group_counts, d, rows_cap, x_perm);
+    moe::zero_pad_rows<kWarps>(blockIdx.x, group_offsets, group_counts, d, rows_cap, x_perm);
     return;
   }
   const int lane = threadIdx.x & 31;
@@ -337,7 +322,7 @@ __global__ void __launch_bounds__(kThreads) combine_bwd_kernel(
     float *__restrict__ d_gate) {
   pdl_start();
   if (DOUT && int(blockIdx.x) < pad_blocks) {
-    zero_pad_rows(blockIdx.x, group_offsets, group_counts, d, rows_cap, d_out_perm);
+    moe::zero_pad_rows<kWarps>(blockIdx.x, group_offsets, group_counts, d, rows_cap, d_out_perm);
     return;
   }
   const int lane = threadIdx.x & 31;

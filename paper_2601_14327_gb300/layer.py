@@ -26,6 +26,59 @@ class LayerShape:
         return L.moe_perm_rows_max(self.T, self.k, self.E)
 
 
+@dataclasses.dataclass
+class BalanceLoss:
+    """Auxiliary losses of a layer's router (moe_balance_loss): the load-balance loss over the batch, or per
+    packed sequence with seq_offsets [n + 1] int32, and the z-loss. token_mask [T] uint8: 0 for padding."""
+    coef: float
+    z_coef: float = 0.0
+    token_mask: Optional[torch.Tensor] = None
+    seq_offsets: Optional[torch.Tensor] = None
+
+    @property
+    def n_seq(self) -> int:
+        return 1 if self.seq_offsets is None else self.seq_offsets.numel() - 1
+
+
+def _alloc_routing(o, s: LayerShape, dev, balance_seqs: int):
+    """What the backward needs of a routing, as attributes of o (balance_seqs: most sequences of a
+    BalanceLoss, 0: none)."""
+    f32, i32 = torch.float32, torch.int32
+    o.topk_idx = torch.empty(s.T, s.k, dtype=i32, device=dev)
+    o.topk_gate = torch.empty(s.T, s.k, dtype=f32, device=dev)
+    o.counts = torch.empty(s.E, dtype=i32, device=dev)
+    o.group_offsets = torch.empty(s.E + 1, dtype=i32, device=dev)
+    o.group_counts = torch.empty(s.E, dtype=i32, device=dev)
+    o.row_of_assignment = torch.empty(s.T, s.k, dtype=i32, device=dev)
+    o.balance = o.balance_mask = None  # the forward's BalanceLoss and mask, kept for the backward
+    o.balance_seqs = balance_seqs
+    if balance_seqs:
+        o.loss = torch.empty(2, dtype=f32, device=dev)
+        o.balance_counts = torch.empty(balance_seqs, s.E, dtype=i32, device=dev)
+        o.balance_prob = torch.empty(balance_seqs, s.E, dtype=f32, device=dev)
+        o.balance_tokens = torch.empty(balance_seqs + 2, dtype=i32, device=dev)
+        o.lse = torch.empty(s.T, dtype=f32, device=dev)
+
+
+class MoECheckpoint:
+    """What one layer keeps from its forward to its backward, with the activations in 8 bits: the routing,
+    x and the pre-activations [A|B] (T*d + 2*F*rows_cap bytes and 1/32 of that in scales; with
+    balance_seqs also the fp32 logits). Pass it to forward() and backward(); the MoELayerBuffers
+    (ckpt=True) of the calls may serve other layers in between."""
+
+    def __init__(self, shape: LayerShape, device="cuda", balance_seqs: int = 0):
+        s, dev, u8 = shape, torch.device(device), torch.uint8
+        if s.d % 128 or s.F % 128:
+            raise ValueError("d_model and d_ff must be multiples of 128")
+        self.shape = s
+        _alloc_routing(self, s, dev, balance_seqs)
+        self.logits = torch.empty(s.T, s.E, dtype=torch.float32, device=dev) if balance_seqs else None
+        self.x_q = torch.empty(s.T, s.d, dtype=u8, device=dev)
+        self.x_scale = torch.empty(s.T, s.d // 32, dtype=u8, device=dev)
+        self.ab_q = torch.empty(s.rows_cap, 2 * s.F, dtype=u8, device=dev)
+        self.ab_scale = torch.empty(s.rows_cap, 2 * s.F // 32, dtype=u8, device=dev)
+
+
 class MoELayerBuffers:
     """Device buffers of one layer step (activations, grouped layout, grads).
 
@@ -38,16 +91,25 @@ class MoELayerBuffers:
 
     fused_combine=True: the combine runs in the down GEMM's epilogue
     (moe_grouped_ffn_fwd_combine, fp32 atomics into y_acc; the last bits of y can
-    change from run to run); O is then stored only when a backward follows."""
+    change from run to run); O is then stored only when a backward follows.
+
+    balance_seqs=n: buffers for a BalanceLoss over up to n sequences (forward's balance argument).
+
+    ckpt=True: for calls with a MoECheckpoint only, which keeps what a layer's backward needs; one
+    object then serves any number of layers of the shape (ab is not allocated)."""
 
     def __init__(self, shape: LayerShape, device="cuda", backward: bool = True,
-                 gather: bool = False, fused_combine: bool = False):
+                 gather: bool = False, fused_combine: bool = False, balance_seqs: int = 0,
+                 ckpt: bool = False):
         s = shape
         self.shape = s
         self.gather = gather
         self.fused_combine = fused_combine
         if fused_combine and gather:
             raise ValueError("fused_combine reads X_perm: use it with gather=False")
+        self.ckpt = ckpt
+        if ckpt and (gather or fused_combine):
+            raise ValueError("the checkpointed forward has neither gather nor fused_combine")
         self.x = None  # the forward's input, kept for the backward
         R = s.rows_cap
         dev = torch.device(device)
@@ -55,19 +117,17 @@ class MoELayerBuffers:
         self.ws_bytes = max(L.moe_workspace_size(s.T, s.d, s.E, s.k, s.F), 256)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
         self.logits = torch.empty(s.T, s.E, dtype=f32, device=dev)
-        self.topk_idx = torch.empty(s.T, s.k, dtype=i32, device=dev)
-        self.topk_gate = torch.empty(s.T, s.k, dtype=f32, device=dev)
-        self.counts = torch.empty(s.E, dtype=i32, device=dev)
-        self.group_offsets = torch.empty(s.E + 1, dtype=i32, device=dev)
-        self.group_counts = torch.empty(s.E, dtype=i32, device=dev)
-        self.row_of_assignment = torch.empty(s.T, s.k, dtype=i32, device=dev)
+        _alloc_routing(self, s, dev, balance_seqs)
+        if balance_seqs:
+            self.balance_ws = torch.empty(L.moe_balance_workspace_size(s.T, s.E, balance_seqs), dtype=torch.uint8,
+                                          device=dev)
         if gather:
             self.token_of_row = torch.empty(R, dtype=i32, device=dev)
             self.x_perm = None
         else:
             self.token_of_row = None
             self.x_perm = torch.empty(R, s.d, dtype=bf16, device=dev)
-        self.ab = torch.empty(R, 2 * s.F, dtype=bf16, device=dev)
+        self.ab = None if ckpt else torch.empty(R, 2 * s.F, dtype=bf16, device=dev)
         self.h = torch.empty(R, s.F, dtype=bf16, device=dev)
         self.out_perm = (torch.empty(R, s.d, dtype=bf16, device=dev)
                          if backward or not fused_combine else None)
@@ -83,6 +143,8 @@ class MoELayerBuffers:
             self.d_logits = torch.empty(s.T, s.k, dtype=f32, device=dev)
             self.dw_router = torch.empty(s.d, s.E, dtype=f32, device=dev)
             self.dx = torch.empty(s.T, s.d, dtype=bf16, device=dev)
+            self.dz = torch.empty(s.T, s.E, dtype=f32, device=dev) if balance_seqs else None
+            self.x_back = torch.empty(s.T, s.d, dtype=bf16, device=dev) if ckpt else None
             # second stream: the router backward and the unpermute-sum run beside
             # the grouped GEMMs (whose CTAs leave registers and threads free)
             self.side = torch.cuda.Stream(device=dev) if dev.type == "cuda" else None
@@ -90,20 +152,57 @@ class MoELayerBuffers:
 
 def route(b: MoELayerBuffers, x, w_router, bias, active_mask=None, logits_in=None,
           keep_logits: bool = False, stream=None):
+    _route(b, b, b.logits if keep_logits else None, x, w_router, bias, active_mask, logits_in, stream)
+
+
+def _route(b, kept, logits, x, w_router, bias, active_mask, logits_in, stream):
     s = b.shape
-    L.moe_route(x, w_router, bias, active_mask, s.T, s.d, s.E, s.k, logits_in,
-                b.logits if keep_logits else None, b.topk_idx, b.topk_gate, b.counts, b.ws,
-                b.ws_bytes, stream)
+    L.moe_route(x, w_router, bias, active_mask, s.T, s.d, s.E, s.k, logits_in, logits, kept.topk_idx,
+                kept.topk_gate, kept.counts, b.ws, b.ws_bytes, stream)
+
+
+def _kept(b: MoELayerBuffers, ckpt: Optional[MoECheckpoint]):
+    """What holds the routing: b, or the layer's checkpoint."""
+    if (ckpt is not None) != b.ckpt:
+        raise ValueError("buffers made with ckpt=True go with a MoECheckpoint, others without")
+    if ckpt is not None and ckpt.shape != b.shape:
+        raise ValueError("the checkpoint is of another shape")
+    return b if ckpt is None else ckpt
 
 
 def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mask=None,
-            logits_in=None, keep_logits: bool = False, stream=None):
+            logits_in=None, keep_logits: bool = False, stream=None,
+            balance: Optional[BalanceLoss] = None, ckpt: Optional[MoECheckpoint] = None):
     """route -> permute -> grouped SwiGLU FFN -> combine (in the down GEMM's epilogue
-    when b.fused_combine). Returns b.y."""
+    when b.fused_combine). Returns b.y.
+
+    balance: adds the router's auxiliary losses; loss [2] (balance, z), balance_counts, balance_prob
+    [sequences, E] are then in b (in ckpt, when given), and backward() adds their gradient.
+    ckpt: the layer's checkpoint (for b with ckpt=True): receives the routing (in the place of b's
+    attributes), x and the pre-activations in 8 bits."""
     s = b.shape
     R = s.rows_cap
+    kept = _kept(b, ckpt)
+    if balance is not None and not 1 <= balance.n_seq <= min(kept.balance_seqs, b.balance_seqs):
+        raise ValueError(f"balance over {balance.n_seq} sequences: more than the buffers' balance_seqs")
     stream = L.stream_handle(stream)  # once for all calls
-    route(b, x, w_router, bias, active_mask, logits_in, keep_logits, stream)
+    logits = kept.logits if balance is not None else b.logits if keep_logits else None
+    _route(b, kept, logits, x, w_router, bias, active_mask, logits_in, stream)
+    kept.balance, kept.balance_mask = balance, active_mask
+    if balance is not None:
+        L.moe_balance_loss(logits, kept.topk_idx, active_mask, balance.token_mask, balance.seq_offsets,
+                           balance.n_seq, s.T, s.E, s.k, balance.coef, balance.z_coef, kept.loss,
+                           kept.balance_counts, kept.balance_prob, kept.balance_tokens, kept.lse,
+                           b.balance_ws, b.balance_ws.numel(), stream)
+    if ckpt is not None:
+        L.moe_permute(x, kept.topk_idx, kept.counts, s.T, s.d, s.E, s.k, R, kept.group_offsets,
+                      kept.group_counts, kept.row_of_assignment, b.x_perm, b.ws, b.ws_bytes, stream)
+        L.moe_ckpt_pack(x, s.T, s.d, ckpt.x_q, ckpt.x_scale, stream)
+        L.moe_grouped_ffn_fwd_ckpt(b.x_perm, kept.group_offsets, s.E, s.d, s.F, R, w_gate_up, w_down,
+                                   ckpt.ab_q, ckpt.ab_scale, b.h, b.out_perm, b.ws, b.ws_bytes, stream)
+        L.moe_unpermute_combine(b.out_perm, kept.row_of_assignment, kept.topk_gate, s.T, s.d, s.k, b.y,
+                                stream)
+        return b.y
     b.x = x
     if b.gather:
         L.moe_permute_map(b.topk_idx, b.counts, s.T, s.E, s.k, R, b.group_offsets,
@@ -129,7 +228,8 @@ def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mas
 
 
 def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
-             overlap: bool = False, active_mask=None):
+             overlap: bool = False, active_mask=None, d_loss=None,
+             ckpt: Optional[MoECheckpoint] = None):
     """combine bwd -> grouped FFN dgrad (with the gate gradient and the router's term of dx)
     -> router bwd -> permute bwd -> grouped FFN wgrad.
 
@@ -143,9 +243,14 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
     default is one stream: on GB300 at T=65536, d_model=7168 the step is power-capped,
     and running those memory-bound kernels beside the GEMMs slowed the GEMMs by more
     than it hid (96.1-96.7 against 97.0-97.3 ms per step).
+
+    After a forward with balance, dw_router and dx hold the auxiliary losses' gradient too; d_loss [2]
+    fp32 on the device: the gradient of the losses (None: ones).
+    ckpt: the layer's checkpoint, as in forward(): X_perm, x and H come from its 8 bits.
     Returns (dx, dw_gate_up, dw_down, dw_router)."""
     s = b.shape
     R = s.rows_cap
+    kept = _kept(b, ckpt)
     if overlap:
         main = torch.cuda.current_stream() if stream is None else stream
         side = b.side
@@ -153,29 +258,49 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
         main = side = L.stream_handle(stream)  # once for all calls
     # d_out_perm = g * dy; the gate gradient comes from the dH GEMM (below), so the combine
     # backward does not read out_perm
-    L.moe_unpermute_combine_bwd(dy, None, b.row_of_assignment, b.topk_gate,
-                                b.group_offsets, b.group_counts, s.T, s.d, s.E, s.k,
+    L.moe_unpermute_combine_bwd(dy, None, kept.row_of_assignment, kept.topk_gate,
+                                kept.group_offsets, kept.group_counts, s.T, s.d, s.E, s.k,
                                 b.d_out_perm, None, main)
     # dH (+ the gate gradient into b.d_gate), dX with the router's term of dx added to the
     # grouped rows in its epilogue
-    L.moe_grouped_ffn_bwd_dgrad(b.d_out_perm, b.ab, b.group_offsets, s.E, s.d, s.F, R,
-                                w_gate_up, w_down, b.topk_gate, None, b.row_of_assignment,
-                                w_router, s.T, s.k, b.d_gate, b.d_ab, b.dx_perm, b.ws,
-                                b.ws_bytes, main)
+    if ckpt is not None:
+        x = b.x_back
+        L.moe_ckpt_permute(ckpt.x_q, ckpt.x_scale, ckpt.row_of_assignment, ckpt.group_offsets,
+                           ckpt.group_counts, s.T, s.d, s.E, s.k, R, x, b.x_perm, main)
+        L.moe_grouped_ffn_bwd_dgrad_ckpt(b.d_out_perm, ckpt.ab_q, ckpt.ab_scale, ckpt.group_offsets, s.E,
+                                         s.d, s.F, R, w_gate_up, w_down, ckpt.topk_gate, None,
+                                         ckpt.row_of_assignment, w_router, s.T, s.k, b.d_gate, b.h,
+                                         b.d_ab, b.dx_perm, b.ws, b.ws_bytes, main)
+    else:
+        x = b.x
+        L.moe_grouped_ffn_bwd_dgrad(b.d_out_perm, b.ab, b.group_offsets, s.E, s.d, s.F, R,
+                                    w_gate_up, w_down, b.topk_gate, None, b.row_of_assignment,
+                                    w_router, s.T, s.k, b.d_gate, b.d_ab, b.dx_perm, b.ws,
+                                    b.ws_bytes, main)
     if overlap:
         ev = torch.cuda.Event()
         ev.record(main)
         side.wait_event(ev)
-    L.moe_route_bwd(b.x, b.topk_idx, b.topk_gate, b.d_gate, s.T, s.d, s.E, s.k, b.d_logits,
-                    b.dw_router, b.ws, b.ws_bytes, side)
-    L.moe_permute_bwd(b.dx_perm, b.row_of_assignment, b.topk_idx, None, None, s.T, s.d, s.E,
+    bal = kept.balance
+    if bal is not None:
+        L.moe_balance_loss_bwd(kept.logits, kept.balance_mask, bal.seq_offsets, bal.n_seq, s.T, s.E,
+                               s.k, bal.coef, bal.z_coef, kept.balance_counts, kept.balance_tokens,
+                               kept.lse, d_loss, b.dz, side)
+        L.moe_route_bwd_dense(x, kept.topk_idx, kept.topk_gate, b.d_gate, b.dz, s.T, s.d, s.E, s.k,
+                              b.d_logits, b.dw_router, b.ws, b.ws_bytes, side)
+    else:
+        L.moe_route_bwd(x, kept.topk_idx, kept.topk_gate, b.d_gate, s.T, s.d, s.E, s.k, b.d_logits,
+                        b.dw_router, b.ws, b.ws_bytes, side)
+    L.moe_permute_bwd(b.dx_perm, kept.row_of_assignment, kept.topk_idx, None, None, s.T, s.d, s.E,
                       s.k, b.dx, b.ws, b.ws_bytes, side)
+    if bal is not None:
+        L.moe_route_dx(b.dz, w_router, b.dx, s.T, s.d, s.E, s.k, b.dx, b.ws, b.ws_bytes, side)
     if b.gather:
         L.moe_grouped_ffn_bwd_wgrad_gather(b.d_out_perm, b.x, b.token_of_row, s.T, b.h, b.d_ab,
                                            b.group_offsets, active_mask, s.E, s.d, s.F, R,
                                            b.dw_gate_up, b.dw_down, b.ws, b.ws_bytes, main)
     else:
-        L.moe_grouped_ffn_bwd_wgrad(b.d_out_perm, b.x_perm, b.h, b.d_ab, b.group_offsets,
+        L.moe_grouped_ffn_bwd_wgrad(b.d_out_perm, b.x_perm, b.h, b.d_ab, kept.group_offsets,
                                     active_mask, s.E, s.d, s.F, R, b.dw_gate_up, b.dw_down, b.ws,
                                     b.ws_bytes, main)
     if overlap:

@@ -45,7 +45,7 @@ def test_oracle_gradient_against_autograd_and_differences(T, E, k, S, masked, pa
         f = np.bincount(idx[t].reshape(-1), minlength=E)[live] * live.sum() / (k * len(t))
         lose = lose + 0.3 / len(seqs) * (torch.tensor(f) * torch.softmax(zt[t], 1).mean(0)).sum()
         zl = zl + 0.2 * (torch.logsumexp(zt[t], 1) ** 2).sum() / ref["n_tokens"][-2]
-    np.testing.assert_allclose(ref["loss"], [float(lose), float(zl)], rtol=1e-12)
+    np.testing.assert_allclose(ref["loss"], [lose.item(), zl.item()], rtol=1e-12)
     (0.7 * lose + 1.9 * zl).backward()
     np.testing.assert_allclose(ref["dz"][:, live], zt.grad.numpy(), rtol=1e-10, atol=1e-14)
     assert (ref["dz"][:, ~live] == 0).all()
