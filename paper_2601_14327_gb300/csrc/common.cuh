@@ -41,6 +41,7 @@ struct WsLayout {
   size_t row_dz;        // fp32  [rows_cap]        moe_grouped_ffn_bwd_dgrad router logit gradient per grouped row
   size_t gate_partial;  // fp32  [rows_cap, F/64]  moe_grouped_ffn_bwd_dgrad per-row dH * H sums (gate gradient)
   size_t route_partial; // fp32  [splits, T, NE]   moe_route split-reduction partial logits
+  size_t route_dx;      // fp16, fp32              moe_route_dx's factors in half precision and their scales
   size_t route_w3;      // bf16  [3, NP, d]        moe_route router weight as three bf16 terms
   size_t total;
 };
@@ -49,6 +50,7 @@ size_t route_partial_bytes(int T, int d, int E);
 size_t route_w3_bytes(int d, int E);
 size_t route_dz3_bytes(int T, int E);
 size_t route_dw_partial_bytes(int T, int d, int E);
+size_t route_dx_bytes(int T, int d, int E);
 constexpr int kPermChunk = 4096;  // assignments per block in the permutation
 constexpr int kGroupPad = 128;    // rows per group are padded to this
 

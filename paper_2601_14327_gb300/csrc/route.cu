@@ -4,6 +4,7 @@
 // Routing indicator E[i,j,l] and per-expert token number: Sec. 3.2, Eq. 1 and
 // Algorithm 1 Step 1 of the LAEP paper. Pruned experts receive no token
 // (Sec. 4, Table 5): their logit is -inf before the top-k.
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -679,41 +680,344 @@ __global__ void zero_f32_kernel(float *p, int n) {
   for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = 0.f;
 }
 
-// dx = bf16(dx_in + dz W^T): 64 tokens x 64 columns per block, 4 x 4 per thread.
-constexpr int kDxTile = 64;
-__global__ void __launch_bounds__(256) route_dx_kernel(const float *__restrict__ dz, const float *__restrict__ w,
-                                                       const uint16_t *dx_in, int T, int d, int E, uint16_t *dx) {
-  __shared__ float s_z[16][kDxTile + 4], s_w[16][kDxTile + 4];
+// ---- dx = bf16(dx_in + dz W^T) on the tensor cores ------------------------------
+// Both factors in half precision: a row of dz [T, E] and a row of W [d, E] (one output column) are each
+// scaled by the power of two that brings their largest value into [2^14, 2^15), so that a value keeps 11
+// significant bits down to 2^-29 of its row's largest and has an absolute step below. The products are
+// exact, their sum is fp32, and the two powers of two are taken out of it exactly: what is lost is 2^-11 per
+// factor, beside the 2^-8 with which the result is rounded to bf16 (2-norm error of the result against
+// 64 bits: 1.01 times that of the rounding alone). One product instead of the six of bf16 pairs
+// or half the rate of tf32, and half the operand bytes.
+//
+// HBM-bound (dx_in read, dx written: 4 bytes per 2 E operations). A persistent CTA takes
+// consecutive 128-token x 256-column tiles, columns first, so that a token block's operand stays in shared memory
+// for its whole row of tiles and W's (a few MB) comes from L2. Warp 0 issues the operand loads, warp 1
+// the MMAs, into two accumulators; warps 2..9 add dx_in. Each of those has its own ring of three 32-row x 64-column
+// pieces of dx: a piece is loaded by TMA two pieces ahead, gets the products added in place, and is
+// stored by TMA from there. No piece is touched by two warps, so dx_in may be dx.
+constexpr int kDxBN = 256;
+constexpr int kDxEpiWarps = 8;
+constexpr int kDxThreads = 64 + 32 * kDxEpiWarps;
+constexpr int kDxSlots = 3;
+constexpr uint32_t kDxABlock = kRtBM * kRtBK * 2, kDxBStage = kDxBN * kRtBK * 2, kDxSlotBytes = 32 * 64 * 2;
+
+struct RouteDxParams {
+  int T, d, NP;  // NP: experts rounded up to 16
+  int nkb;       // 64-wide k-blocks
+  int n_tiles, tiles, stages;
+  int has_in;    // dx_in given
+  const float *row_scale, *col_scale;  // what the factors' rows were divided by (col_scale padded to 64)
+};
+
+int route_dx_stages(int nkb) {
+  const int64_t rest = kRtMaxSmem - 2048 - int64_t(nkb) * kDxABlock - int64_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes;
+  return int(std::min<int64_t>(4, rest / kDxBStage));  // 2 with four k-blocks, 3 with one
+}
+size_t route_dx_smem(int nkb, int stages) {
+  return 1024 + size_t(nkb) * kDxABlock + size_t(stages) * kDxBStage + size_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes +
+         size_t(2 * stages + 8 + kDxEpiWarps * kDxSlots) * 8 + 16;
+}
+
+// Rows of W, then rows of dz (E fp32 values each) -> half precision [rows][NP] and their scales.
+__global__ void __launch_bounds__(256) route_dx_split_kernel(const float *__restrict__ w, const float *__restrict__ dz,
+                                                             int d, int d_pad, int T, int E, int NP,
+                                                             __half *__restrict__ w16, float *__restrict__ col_scale,
+                                                             __half *__restrict__ z16, float *__restrict__ row_scale) {
   pdl_start();
-  const int t0 = blockIdx.x * kDxTile, i0 = blockIdx.y * kDxTile;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (int e0 = 0; e0 < E; e0 += 16) {
-    for (int r = ty; r < kDxTile; r += 16) {
-      const int e = e0 + tx;
-      s_z[tx][r] = t0 + r < T && e < E ? dz[size_t(t0 + r) * E + e] : 0.f;
-      s_w[tx][r] = i0 + r < d && e < E ? w[size_t(i0 + r) * E + e] : 0.f;
+  const int lane = threadIdx.x & 31;
+  for (int64_t r = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); r < int64_t(d_pad) + T; r += int64_t(gridDim.x) * 8) {
+    const bool is_w = r < d_pad;
+    if (is_w && r >= d) {  // the columns that round d up to whole pieces
+      if (lane == 0) col_scale[r] = 0.f;
+      continue;
     }
-    __syncthreads();
+    const int64_t i = is_w ? r : r - d_pad;
+    const float *src = (is_w ? w : dz) + size_t(i) * E;
+    float v[8];
+    uint32_t m = 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
+    for (int u = 0; u < 8; ++u) {
+      const int e = lane + 32 * u;
+      v[u] = e < E ? src[e] : 0.f;
+      m = max(m, __float_as_uint(v[u]) & 0x7fffffffu);
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    // exponent of the largest value (of a row with an infinity or NaN: as it is; below 2^-112: as 2^-112)
+    int e = int(m >> 23);
+    e = e == 255 ? 141 : max(e, 15);
+    const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
+    __half *dst = (is_w ? w16 : z16) + size_t(i) * NP;
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(s_z[e][ty * 4 + a], s_w[e][tx * 4 + b], acc[a][b]);
-    __syncthreads();
+    for (int u = 0; u < 8; ++u)
+      if (lane + 32 * u < NP) dst[lane + 32 * u] = __float2half_rn(v[u] * up);
+    if (lane == 0) (is_w ? col_scale : row_scale)[i] = __uint_as_float(uint32_t(e - 14) << 23);
   }
-  const int c = i0 + tx * 4;
-  if (c >= d) return;  // (d is a multiple of 8)
-  for (int a = 0; a < 4; ++a) {
-    const int t = t0 + ty * 4 + a;
-    if (t >= T) break;
-    uint2 v = make_uint2(0, 0);
-    if (dx_in != nullptr) v = *reinterpret_cast<const uint2 *>(dx_in + size_t(t) * d + c);
-    v.x = pack_bf16x2(acc[a][0] + bf16_lo(v.x), acc[a][1] + bf16_hi(v.x));
-    v.y = pack_bf16x2(acc[a][2] + bf16_lo(v.y), acc[a][3] + bf16_hi(v.y));
-    *reinterpret_cast<uint2 *>(dx + size_t(t) * d + c) = v;
+}
+
+__global__ void __launch_bounds__(kDxThreads, 1)
+    route_dx_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmW,
+                    const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmOut,
+                    const RouteDxParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+  const int S = p.stages;
+  const uint32_t sA = raw + pad, sB = sA + uint32_t(p.nkb) * kDxABlock, sSlots = sB + uint32_t(S) * kDxBStage;
+  const uint32_t bars_off = pad + uint32_t(p.nkb) * kDxABlock + uint32_t(S) * kDxBStage + kDxEpiWarps * kDxSlots * kDxSlotBytes;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem_raw + bars_off);
+  int *misc = reinterpret_cast<int *>(bars + 2 * S + 8 + kDxEpiWarps * kDxSlots);
+  volatile int *abort_flag = misc + 1;
+  volatile int no_abort = 0;
+  const uint32_t bar0 = tc::smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * S + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * S + 2 + a); };
+  const uint32_t afull_bar = bar0 + 8u * (2 * S + 4), aempty_bar = bar0 + 8u * (2 * S + 5);
+  const uint32_t drain_bar = bar0 + 8u * (2 * S + 6);
+  auto slot_bar = [&](int w, int s) { return bar0 + 8u * (2 * S + 8 + w * kDxSlots + s); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr uint32_t IDESC = tc::idesc_f16_f32(kRtBM, kDxBN);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      tc::mbar_init(full_bar(s), 1);
+      tc::mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      tc::mbar_init(tfull_bar(a), 1);
+      tc::mbar_init(tempty_bar(a), kDxEpiWarps);
+    }
+    tc::mbar_init(afull_bar, 1);
+    tc::mbar_init(aempty_bar, 1);
+    tc::mbar_init(drain_bar, 1);
+    for (int w = 0; w < kDxEpiWarps; ++w)
+      for (int s = 0; s < kDxSlots; ++s) tc::mbar_init(slot_bar(w, s), 1);
+    tc::fence_mbar_init();
+    misc[1] = 0;
   }
+  if (warp == 1) {
+    tc::tmem_alloc(tc::smem_u32(misc), 2 * kDxBN);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem_base = static_cast<uint32_t>(misc[0]);
+  pdl_start();
+  const int tile0 = int(int64_t(p.tiles) * blockIdx.x / gridDim.x), tile1 = int(int64_t(p.tiles) * (blockIdx.x + 1) / gridDim.x);
+  auto fail = [&]() {
+    dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
+    *abort_flag = 1;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0, blocks = 0;
+      int m_now = -1;
+      bool ok = true;
+      for (int tile = tile0; tile < tile1 && ok; ++tile) {
+        const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
+        if (m != m_now) {
+          if (blocks > 0 && !tc::mbar_wait(aempty_bar, (blocks - 1) & 1u, kRtWaitNs, abort_flag)) { fail(); break; }
+          tc::mbar_arrive_expect_tx(afull_bar, uint32_t(p.nkb) * kDxABlock);
+          for (int kb = 0; kb < p.nkb; ++kb) tc::tma_load_2d(sA + kb * kDxABlock, &tmZ, afull_bar, kb * kRtBK, m * kRtBM);
+          ++blocks;
+          m_now = m;
+        }
+        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
+          const int s = it % S;
+          if (!tc::mbar_wait(empty_bar(s), ((it / S) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
+          tc::mbar_arrive_expect_tx(full_bar(s), kDxBStage);
+          tc::tma_load_2d(sB + s * kDxBStage, &tmW, full_bar(s), kb * kRtBK, n * kDxBN);
+        }
+      }
+      // every issued load lands before the CTA may exit
+      for (int s = 0; s < S; ++s)
+        if (it > uint32_t(s) && !tc::mbar_wait(full_bar(s), ((it - 1 - s) / S) & 1u, kRtWaitNs, &no_abort)) fail();
+      if (blocks > 0 && !tc::mbar_wait(afull_bar, (blocks - 1) & 1u, kRtWaitNs, &no_abort)) fail();
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t it = 0, blocks = 0, tcount = 0;
+      int m_now = -1;
+      bool ok = true, issued = false;
+      for (int tile = tile0; tile < tile1 && ok; ++tile, ++tcount) {
+        const int m = tile / p.n_tiles;
+        const uint32_t a = tcount & 1u;
+        if (m != m_now) {
+          if (!tc::mbar_wait(afull_bar, blocks & 1u, kRtWaitNs, abort_flag)) { fail(); break; }
+          ++blocks;
+          m_now = m;
+        }
+        if (!tc::mbar_wait(tempty_bar(a), ((tcount >> 1) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); break; }
+        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
+          const int s = it % S;
+          if (!tc::mbar_wait(full_bar(s), (it / S) & 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
+          tc::fence_after_sync();
+          const uint64_t ad = tc::smem_desc_sw128(sA + kb * kDxABlock, 16, 1024), bd = tc::smem_desc_sw128(sB + s * kDxBStage, 16, 1024);
+          const int steps = min(4, (p.NP - kb * kRtBK) / 16);
+          for (int kk = 0; kk < steps; ++kk)  // (a descriptor's address counts 16 bytes)
+            tc::mma_bf16(tmem_base + a * kDxBN, ad + uint64_t(2 * kk), bd + uint64_t(2 * kk), IDESC, (kb | kk) != 0);
+          tc::mma_commit(empty_bar(s));
+          issued = true;
+        }
+        if (!ok) break;
+        tc::mma_commit(tfull_bar(a));
+        if ((tile + 1) / p.n_tiles != m) tc::mma_commit(aempty_bar);  // the token block's last tile
+      }
+      if (issued) {
+        tc::mma_commit(drain_bar);
+        if (!tc::mbar_wait(drain_bar, 0, kRtWaitNs, &no_abort)) fail();
+      }
+    }
+  } else {
+    const int w = warp - 2, q = warp & 3, half = w / 4;
+    const uint32_t slots = sSlots + uint32_t(w) * (kDxSlots * kDxSlotBytes);
+    // This warp's pieces: (tile, c), c = 0 or 1, column c * 64 of its half of the tile; those that lie
+    // wholly past dx are left out. Piece n is in slot n % 3.
+    struct Piece {
+      int tile, c;
+    };
+    auto row_of = [&](const Piece &x) { return x.tile / p.n_tiles * kRtBM + q * 32; };
+    auto col_of = [&](const Piece &x) { return x.tile % p.n_tiles * kDxBN + half * 128 + x.c * 64; };
+    auto inside = [&](const Piece &x) { return row_of(x) < p.T && col_of(x) < p.d; };
+    auto next = [&](Piece &x) {  // the piece that follows (tile == tile1: none)
+      do {
+        x.c ^= 1;
+        if (x.c == 0) ++x.tile;
+      } while (x.tile < tile1 && !inside(x));
+    };
+    Piece ahead{tile0 - 1, 1};
+    next(ahead);
+    uint32_t loads = 0, done = 0;
+    auto load = [&]() {  // lane 0: the next piece's dx_in into its slot, which its last store has left
+      if (p.has_in && ahead.tile < tile1) {
+        const uint32_t s = loads % kDxSlots;
+        tc::mbar_arrive_expect_tx(slot_bar(w, s), kDxSlotBytes);
+        tc::tma_load_2d(slots + s * kDxSlotBytes, &tmIn, slot_bar(w, s), col_of(ahead), row_of(ahead));
+        next(ahead);
+        ++loads;
+      }
+    };
+    if (lane == 0) {
+      load();
+      load();
+    }
+    bool ok = true;
+    uint32_t tcount = 0;
+    for (int tile = tile0; tile < tile1 && ok; ++tile, ++tcount) {
+      const uint32_t a = tcount & 1u;
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(tfull_bar(a), (tcount >> 1) & 1u, kRtWaitNs, abort_flag));
+      if (!ok) { fail(); break; }
+      tc::fence_after_sync();
+      const int row = tile / p.n_tiles * kRtBM + q * 32 + lane;
+      const float rs = row < p.T ? p.row_scale[row] : 0.f;
+      for (int c = 0; c < 2; ++c) {
+        const Piece x{tile, c};
+        if (!inside(x)) continue;
+        const uint32_t s = done % kDxSlots, slot = slots + s * kDxSlotBytes;
+        uint32_t r[64];
+        const uint32_t tb = tmem_base + (uint32_t(q * 32) << 16) + a * kDxBN + half * 128 + c * 64;
+        tc::tmem_ld_32x32b_x32(tb, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
+        tc::tmem_ld_32x32b_x32(tb + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
+        tc::tmem_ld_wait();
+        if (p.has_in) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(slot_bar(w, s), (done / kDxSlots) & 1u, kRtWaitNs, abort_flag));
+          if (!ok) { fail(); break; }
+        } else {
+          if (lane == 0) tc::bulk_wait_read<kDxSlots - 1>();  // the slot's last store has read it
+          __syncwarp();
+        }
+        const float *cs = p.col_scale + col_of(x);
+        const uint32_t mine = slot + uint32_t(lane) * 128u;
+#pragma unroll
+        for (uint32_t v = 0; v < 8; ++v) {
+          const uint32_t at = mine + ((v ^ (uint32_t(lane) & 7u)) << 4);  // the 128-byte swizzle
+          float f[8];
+          if (p.has_in) {
+            unpack8(tc::ld_shared_v4(at), f);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = 0.f;
+          }
+          const float4 c0 = __ldg(reinterpret_cast<const float4 *>(cs + 8 * v)), c1 = __ldg(reinterpret_cast<const float4 *>(cs + 8 * v + 4));
+          const float sc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = fmaf(__uint_as_float(r[8 * v + i]) * rs, sc[i], f[i]);
+          tc::st_shared_v4(at, pack8(f));
+        }
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tc::tma_store_2d(&tmOut, slot, col_of(x), row_of(x));
+          tc::bulk_commit();
+          if (p.has_in) {
+            tc::bulk_wait_read<1>();  // the store before this one, from the slot that is loaded now
+            load();
+          }
+        }
+        ++done;
+      }
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(tempty_bar(a));
+    }
+    if (lane == 0) {
+      for (uint32_t n = done; n < loads; ++n)  // (after an abort: loads nothing read)
+        if (!tc::mbar_wait(slot_bar(w, n % kDxSlots), (n / kDxSlots) & 1u, kRtWaitNs, &no_abort)) fail();
+      tc::bulk_wait0();
+    }
+    __syncwarp();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem_base, 2 * kDxBN);
+  }
+}
+
+// The regions of route_dx_bytes: W's and dz's rows in half precision, their scales.
+int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int T, int d, int E, uint16_t *dx, char *ws,
+                    cudaStream_t s) {
+  const int NP = route_tc_np(E), d_pad = (d + 63) / 64 * 64;
+  __half *w16 = reinterpret_cast<__half *>(ws), *z16 = w16 + size_t(d_pad) * NP;
+  float *col_scale = reinterpret_cast<float *>(z16 + size_t(T) * NP), *row_scale = col_scale + d_pad;
+  const char *what = "moe_route_dx: factors";
+  const int64_t rows = int64_t(d_pad) + T;
+  const int grid0 = int(std::min<int64_t>((rows + 7) / 8, int64_t(moe::num_sms()) * 32));
+  MOE_LAUNCH("route_dx_split", s, moe::launch_dep(route_dx_split_kernel, grid0, 256, 0, s, w, dz, d, d_pad, T, E, NP, w16,
+                                                  col_scale, z16, row_scale));
+  if (int st = moe::launch_status(what)) return st;
+  what = "moe_route_dx: product";
+  RouteDxParams p{};
+  p.T = T;
+  p.d = d;
+  p.NP = NP;
+  p.nkb = (NP + kRtBK - 1) / kRtBK;
+  p.n_tiles = (d + kDxBN - 1) / kDxBN;
+  p.tiles = (T + kRtBM - 1) / kRtBM * p.n_tiles;
+  p.stages = route_dx_stages(p.nkb);
+  p.has_in = dx_in != nullptr;
+  p.row_scale = row_scale;
+  p.col_scale = col_scale;
+  CUtensorMap mz, mw, mi, mo;
+  int st;
+  if ((st = moe::make_map(&mz, z16, uint64_t(T), uint64_t(NP), kRtBK, kRtBM, "router dx dz"))) return st;
+  if ((st = moe::make_map(&mw, w16, uint64_t(d), uint64_t(NP), kRtBK, kDxBN, "router dx w"))) return st;
+  if ((st = moe::make_map(&mo, dx, uint64_t(T), uint64_t(d), 64, 32, "router dx"))) return st;
+  mi = mo;
+  if (dx_in != nullptr && (st = moe::make_map(&mi, dx_in, uint64_t(T), uint64_t(d), 64, 32, "router dx_in"))) return st;
+  static bool attr_set = false;
+  if (!attr_set) {
+    cudaError_t e = cudaFuncSetAttribute(route_dx_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    attr_set = true;
+  }
+  const int grid = std::min(p.tiles, moe::num_sms());
+  MOE_LAUNCH("route_dx", s, moe::launch_dep(route_dx_kernel, grid, kDxThreads, route_dx_smem(p.nkb, p.stages), s, mz, mw, mi, mo, p));
+  return moe::launch_status(what);
 }
 
 template <bool DW, int G, bool AHEAD = false>
@@ -808,6 +1112,10 @@ size_t route_partial_bytes(int T, int d, int E) {
 size_t route_w3_bytes(int d, int E) { return size_t(3) * route_tc_np(E) * size_t(d) * 2; }
 size_t route_dz3_bytes(int T, int E) {
   return size_t(3) * route_tc_np(E) * size_t(route_tokens_padded(T)) * 2;
+}
+size_t route_dx_bytes(int T, int d, int E) {
+  const size_t rows = size_t(std::max(T, 0)) + size_t((d + 63) / 64 * 64);
+  return rows * (size_t(route_tc_np(E)) * 2 + 4);
 }
 size_t route_dw_partial_bytes(int T, int d, int E) {
   if (T <= 0) return 0;
@@ -966,9 +1274,7 @@ int moe_route_dx(const float *dz, const float *w_router, const uint16_t *dx_in, 
     return moe::set_error(MOE_ERR_ARG, "%s: alignment", fn);
   const moe::WsLayout L = moe::ws_layout(T, d, E, k, 0);
   if (ws_bytes < L.total) return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace", fn);
-  dim3 grid((T + kDxTile - 1) / kDxTile, (d + kDxTile - 1) / kDxTile);
-  MOE_LAUNCH("route_dx", s, moe::launch_dep(route_dx_kernel, grid, 256, 0, s, dz, w_router, dx_in, T, d, E, dx));
-  return moe::launch_status("moe_route_dx: launch");
+  return launch_route_dx(dz, w_router, dx_in, T, d, E, dx, static_cast<char *>(ws) + L.route_dx, s);
 }
 
 }  // extern "C"
