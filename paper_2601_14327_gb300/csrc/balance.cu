@@ -29,12 +29,12 @@ MOE_DEV_ERR_DECL
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kMaxWarps = 24;  // of a block: 80 registers a thread, one block per SM
 constexpr int kMaxSeqs = 1 << 20;
 
-// Tokens per chunk: four chunks per SM of a GB300 (152), at least a token per warp.
-int chunk_tokens(int T) { return std::max(kWarps, (T + 607) / 608); }
+// Tokens per chunk: one block for each of a GB300's 152 SMs, and few rows of partial sums for
+// the second kernel; at least eight, the tokens of one warp or two.
+int chunk_tokens(int T) { return std::max(8, (T + 151) / 152); }
 int chunk_count(int T) { return (T + chunk_tokens(T) - 1) / chunk_tokens(T); }
 int expert_groups(int E) { return (E + 31) / 32; }
 
@@ -43,9 +43,9 @@ struct BalanceWs {
   size_t prob;   // fp32 [rows, E]  sums of p
   size_t count;  // int32 [rows, E] assignments
   size_t n;      // int32 [rows]    valid tokens
-  size_t zsq;    // fp64 [rows]     sums of lse^2
-  size_t part;   // fp64 [n_seq, groups of 32 experts] sums of f P
-  size_t zseq;   // fp64 [n_seq]    sums of lse^2
+  size_t zsq;    // fp32 [rows]     sums of lse^2
+  size_t part;   // fp32 [n_seq, groups of 32 experts] sums of f P
+  size_t zseq;   // fp32 [n_seq]    sums of lse^2
   size_t total;
 };
 BalanceWs balance_ws(int T, int E, int n_seq) {
@@ -60,11 +60,11 @@ BalanceWs balance_ws(int T, int E, int n_seq) {
   w.n = off;
   off += up(rows * 4);
   w.zsq = off;
-  off += up(rows * 8);
+  off += up(rows * 4);
   w.part = off;
-  off += up(size_t(n_seq) * expert_groups(E) * 8);
+  off += up(size_t(n_seq) * expert_groups(E) * 4);
   w.zseq = off;
-  off += up(size_t(n_seq) * 8);
+  off += up(size_t(n_seq) * 4);
   w.total = off;
   return w;
 }
@@ -80,7 +80,7 @@ struct BalanceParams {
   int *ticket;
   float *w_prob;
   int32_t *w_count, *w_n;
-  double *w_zsq, *w_part, *w_zseq;
+  float *w_zsq, *w_part, *w_zseq;
   // outputs
   float *loss, *prob, *lse;
   int32_t *counts, *n_tokens;
@@ -91,108 +91,178 @@ __device__ __forceinline__ void sequence_range(const int32_t *off, int s, int T,
   *a = off == nullptr ? 0 : min(max(off[s], 0), T);
   *b = off == nullptr ? T : min(max(off[s + 1], 0), T);
 }
-// The first sequence that ends behind token t (n_seq: none).
-__device__ __forceinline__ int first_sequence(const int32_t *off, int n_seq, int T, int t) {
+// The first sequence that ends behind token t (n_seq: none), by a whole warp: 32 offsets a step (a
+// binary search's dependent loads were ~1.3 us of a 4 us kernel at 24 sequences).
+__device__ __forceinline__ int first_sequence(const int32_t *off, int n_seq, int t, int lane) {
   if (off == nullptr) return 0;
-  int lo = 0, hi = n_seq;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid + 1] > t) hi = mid;
-    else lo = mid + 1;
+  int lo = 0, len = n_seq;
+  while (len > 0) {
+    const int step = (len + 31) / 32, last = (lane + 1) * step - 1;  // of this lane's share
+    const unsigned behind = __ballot_sync(0xffffffffu, last >= len || off[lo + last + 1] > t);
+    if (behind == 0) return lo + len;
+    const int skip = (__ffs(behind) - 1) * step;
+    lo += skip;
+    len = min(step - 1, len - skip);
   }
   return lo;
 }
 
+// The larger value, NaN if either is one.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 template <int LPT> __device__ __forceinline__ float group_max(float v) {
 #pragma unroll
-  for (int h = LPT / 2; h > 0; h >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, h));
+  for (int h = LPT / 2; h > 0; h >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, h));
   return v;
 }
+// 2^x, 2 ulp; results below 2^-126 are zero.
+__device__ __forceinline__ float exp2_quick(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.44269504088896341f;
 template <int LPT> __device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
   for (int h = LPT / 2; h > 0; h >>= 1) v += __shfl_xor_sync(0xffffffffu, v, h);
   return v;
 }
 
-// Log-sum-exp of every token and the partial sums of its chunk. LPT lanes share a token, lane q
-// holding the logits of experts q + LPT i.
-template <int LPT, int NI>
-__global__ void __launch_bounds__(kThreads) balance_stats_kernel(const BalanceParams p) {
-  __shared__ float s_prob[kWarps][256];
+// Expert of logit i of lane q, LPT lanes sharing a token's row: VEC, runs of four (rows of whole 16-byte
+// vectors); else every LPT-th expert.
+template <int LPT, bool VEC> __device__ __forceinline__ int expert_of(int q, int i) {
+  return VEC ? 4 * (q + LPT * (i / 4)) + i % 4 : q + LPT * i;
+}
+// Bit i: logit i of lane q is a live expert's.
+template <int LPT, int NI, bool VEC>
+__device__ __forceinline__ unsigned live_bits(const uint8_t *active_mask, int E, int q) {
+  unsigned live = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int e = expert_of<LPT, VEC>(q, i);
+    if (e < E && (active_mask == nullptr || active_mask[e] != 0)) live |= 1u << i;
+  }
+  return live;
+}
+// A token's logits of lane q (not `mine`, or past E: not read, and z is left as it is).
+template <int LPT, int NI, bool VEC>
+__device__ __forceinline__ void load_row(const float *__restrict__ row, int E, int q, bool mine, float (&z)[NI]) {
+#pragma unroll
+  for (int i = 0; i < NI; i += VEC ? 4 : 1) {
+    const int e = expert_of<LPT, VEC>(q, i);
+    if (!mine || e >= E) continue;
+    if (VEC) {
+      const float4 v = __ldg(reinterpret_cast<const float4 *>(row + e));
+      z[i] = v.x;
+      z[i + 1] = v.y;
+      z[i + 2] = v.z;
+      z[i + 3] = v.w;
+    } else {
+      z[i] = __ldg(row + e);
+    }
+  }
+}
+// Lanes' live experts of 32.
+__device__ __forceinline__ int count_live(const uint8_t *active_mask, int E, int lane) {
+  int n = 0;
+  for (int e = lane; e < E; e += 32) n += active_mask == nullptr || active_mask[e] != 0;
+  return __reduce_add_sync(0xffffffffu, n);
+}
+
+// Log-sum-exp of every token and the partial sums of its chunk. LPT lanes share a token, so that a
+// shuffle step serves 32 / LPT of them; the next tokens' logits load while these are summed. What
+// counts is instructions per logit (five: the largest, the exponent's argument, 2^x, two sums; 17 with expf,
+// a select per logit for masked ones and a NaN test were 27 us of issue at T=65536, 256 experts,
+// where the loads take 10): a row is masked only where some expert is (or E leaves lanes over), and what a
+// token that does not count holds is computed with and not added.
+// The argument's product with log2 e is fused with the subtraction of the largest logit's; that one's
+// rounding is common to the row, so it cancels in p and adds |m| 2^-24 to the log-sum-exp.
+template <int LPT, int NI, bool VEC>
+__global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_stats_kernel(const BalanceParams p) {
+  __shared__ float s_prob[kMaxWarps][256];
   __shared__ int s_hist[256];
-  __shared__ int s_n[kWarps];
-  __shared__ float s_z[kWarps];
-  __shared__ int s_first;
+  __shared__ int s_n[kMaxWarps];
+  __shared__ float s_z[kMaxWarps];
   constexpr int TPW = 32 / LPT;  // tokens per warp
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, q = lane % LPT;
-  for (int e = tid; e < 256; e += kThreads) s_hist[e] = 0;
+  const int threads = blockDim.x, warps = threads >> 5;
+  for (int e = tid; e < 256; e += threads) s_hist[e] = 0;
   pdl_start();
   if (blockIdx.x == 0 && tid == 0) *p.ticket = 0;
   const int t0 = blockIdx.x * p.chunk, t1 = min(p.T, t0 + p.chunk);
   if (t0 >= t1) return;  // (no tokens at all)
-  if (tid == 0) s_first = first_sequence(p.seq_offsets, p.n_seq, p.T, t0);
-  bool live[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int e = q + LPT * i;
-    live[i] = e < p.E && (p.active_mask == nullptr || p.active_mask[e] != 0);
-  }
+  const unsigned live = live_bits<LPT, NI, VEC>(p.active_mask, p.E, q);
+  const bool masked = __any_sync(0xffffffffu, live != (1u << NI) - 1u);
   __syncthreads();
   int cur = t0;
-  for (int s = s_first; s < p.n_seq && cur < t1; ++s) {
+  for (int s = first_sequence(p.seq_offsets, p.n_seq, t0, lane); s < p.n_seq && cur < t1; ++s) {
     int a, b;
     sequence_range(p.seq_offsets, s, p.T, &a, &b);
     if (a >= t1) break;
     a = max(a, cur);
     b = min(b, t1);
-    for (int t = cur + tid; t < a; t += kThreads) p.lse[t] = -INFINITY;  // between sequences
+    for (int t = cur + tid; t < a; t += threads) p.lse[t] = -INFINITY;  // between sequences
     cur = max(cur, a);
     if (a >= b) continue;
     float acc[NI] = {};
     float zs = 0.f;
     int n = 0;
+    int t = a + warp * TPW + lane / LPT;
+    bool mine = t < b && (p.token_mask == nullptr || p.token_mask[t] != 0);
+    float next[NI] = {};
+    load_row<LPT, NI, VEC>(p.logits + size_t(t) * p.E, p.E, q, mine, next);
     // (whole warps stay in the loop: the sums are warp-wide)
-    for (int tb = a + warp * TPW; tb < b; tb += kWarps * TPW) {
-      const int t = tb + lane / LPT;
-      const bool mine = t < b && (p.token_mask == nullptr || p.token_mask[t] != 0);
-      float z[NI], m = -INFINITY;
+    for (int tb = a + warp * TPW; tb < b; tb += warps * TPW) {
+      const bool now = mine;
+      const int tn = t;
+      float z[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) z[i] = next[i];
+      t += warps * TPW;
+      mine = t < b && (p.token_mask == nullptr || p.token_mask[t] != 0);
+      load_row<LPT, NI, VEC>(p.logits + size_t(t) * p.E, p.E, q, mine, next);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) z[i] = live >> i & 1 ? z[i] : -INFINITY;
+      }
+      float m[4], den[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NI; ++i) m[i % 4] = i < 4 ? z[i] : max_nan(m[i % 4], z[i]);
+      m[0] = group_max<LPT>(max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])));
+      const float c = -m[0] * kLog2e;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        z[i] = mine && live[i] ? p.logits[size_t(t) * p.E + q + LPT * i] : -INFINITY;
+        z[i] = exp2_quick(fmaf(z[i], kLog2e, c));
+        den[i % 4] += z[i];
       }
-#pragma unroll
-      for (int i = 0; i < NI; ++i) m = z[i] != z[i] ? INFINITY : fmaxf(m, z[i]);  // a NaN stays one in the sum
-      m = group_max<LPT>(m);
-      float den = 0.f;
-      const bool some = m > -INFINITY;
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        z[i] = some ? expf(z[i] - m) : 0.f;
-        den += z[i];
-      }
-      den = group_sum<LPT>(den);
-      const float lse = some ? m + logf(den) : -INFINITY;
-      if (q == 0 && t < b) p.lse[t] = lse;
+      den[0] = group_sum<LPT>((den[0] + den[1]) + (den[2] + den[3]));
+      const bool some = now && !(m[0] == -INFINITY);
       if (some) {
-        const float r = 1.f / den;
+        const float r = __fdividef(1.f, den[0]), lse = m[0] + logf(den[0]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) acc[i] = fmaf(z[i], r, acc[i]);
         if (q == 0) {
+          p.lse[tn] = lse;
           zs = fmaf(lse, lse, zs);
           ++n;
         }
         for (int j = q; j < p.k; j += LPT) {
-          const int e = p.topk_idx[size_t(t) * p.k + j];
+          const int e = p.topk_idx[size_t(tn) * p.k + j];
           if (e >= 0 && e < p.E) atomicAdd(&s_hist[e], 1);
           else dev_flag(&g_dev_err, MOE_DEV_BAD_EXPERT);
         }
+      } else if (q == 0 && tn < b) {
+        p.lse[tn] = -INFINITY;
       }
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
 #pragma unroll
       for (int h = LPT; h < 32; h <<= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], h);
-      if (lane < LPT) s_prob[warp][q + LPT * i] = acc[i];
+      if (lane < LPT) s_prob[warp][expert_of<LPT, VEC>(q, i)] = acc[i];
     }
     zs = group_sum<32>(zs);
     n = __reduce_add_sync(0xffffffffu, n);
@@ -202,38 +272,37 @@ __global__ void __launch_bounds__(kThreads) balance_stats_kernel(const BalancePa
     }
     __syncthreads();
     const size_t row = size_t(blockIdx.x) + s;
-    for (int e = tid; e < p.E; e += kThreads) {
+    for (int e = tid; e < p.E; e += threads) {
       float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += s_prob[w][e];
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) v += s_prob[w][e];
       p.w_prob[row * p.E + e] = v;
       p.w_count[row * p.E + e] = s_hist[e];
       s_hist[e] = 0;
     }
-    if (tid == 0) {
-      double z = 0.0;
-      int m = 0;
-      for (int w = 0; w < kWarps; ++w) {
-        z += double(s_z[w]);
-        m += s_n[w];
+    if (warp == 0) {
+      zs = group_sum<32>(lane < warps ? s_z[lane] : 0.f);
+      n = __reduce_add_sync(0xffffffffu, lane < warps ? s_n[lane] : 0);
+      if (lane == 0) {
+        p.w_zsq[row] = zs;
+        p.w_n[row] = n;
       }
-      p.w_zsq[row] = z;
-      p.w_n[row] = m;
     }
     __syncthreads();
     cur = b;
   }
-  for (int t = cur + tid; t < t1; t += kThreads) p.lse[t] = -INFINITY;  // behind the last sequence
+  for (int t = cur + tid; t < t1; t += threads) p.lse[t] = -INFINITY;  // behind the last sequence
 }
 
 // Sums of one sequence's rows for 32 experts (blockIdx.x = sequence * groups + group; a warp
 // takes every (blockDim.x / 32)th row), its counts, mean probabilities and share of the loss. The
-// last block to finish adds the shares, always in the same order.
+// last block to finish adds the shares, always in the same order. (Sums of few terms are fp32: a chain of
+// fp64 additions and quotients took ~10 us here, whatever the size.)
 __global__ void __launch_bounds__(1024) balance_reduce_kernel(const BalanceParams p) {
   __shared__ float s_p[32][33];
   __shared__ int s_c[32][33];
-  __shared__ int s_n[32];
-  __shared__ double s_d[32], s_z[32];
+  __shared__ int s_n[32], s_m[32];
+  __shared__ float s_d[32], s_z[32];
   __shared__ int s_last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   pdl_start();
@@ -244,57 +313,49 @@ __global__ void __launch_bounds__(1024) balance_reduce_kernel(const BalanceParam
   if (p.seq_offsets != nullptr && threadIdx.x == 0 &&
       (p.seq_offsets[s] < 0 || p.seq_offsets[s + 1] < p.seq_offsets[s] || p.seq_offsets[s + 1] > p.T))
     dev_flag(&g_dev_err, MOE_DEV_BAD_OFFSETS);
+  const int live_all = warp == 0 ? count_live(p.active_mask, p.E, lane) : 0;
   const int c0 = a / p.chunk, c1 = a < b ? (b - 1) / p.chunk : c0 - 1;  // its chunks
-  float v = 0.f;
+  float v = 0.f, zs = 0.f;
   int c = 0, n = 0;
-  double zs = 0.0;
-  for (int i = c0 + warp; i <= c1; i += warps) {
-    const size_t row = size_t(i) + s;
-    if (e < p.E) {
-      v += p.w_prob[row * p.E + e];
-      c += p.w_count[row * p.E + e];
-    }
-    if (lane == 0) {
-      n += p.w_n[row];
-      zs += p.w_zsq[row];
+  for (int i = c0 + int(threadIdx.x); i <= c1; i += blockDim.x) {
+    n += p.w_n[size_t(i) + s];
+    zs += p.w_zsq[size_t(i) + s];
+  }
+  if (e < p.E) {
+#pragma unroll 8
+    for (int i = c0 + warp; i <= c1; i += warps) {
+      const size_t at = (size_t(i) + s) * p.E + e;
+      v += p.w_prob[at];
+      c += p.w_count[at];
     }
   }
   s_p[warp][lane] = v;
   s_c[warp][lane] = c;
+  n = __reduce_add_sync(0xffffffffu, n);
+  zs = group_sum<32>(zs);
   if (lane == 0) {
     s_n[warp] = n;
     s_z[warp] = zs;
   }
-  int live_all = 0;
-  for (int i = threadIdx.x; i < p.E; i += blockDim.x)
-    live_all += p.active_mask == nullptr || p.active_mask[i] != 0;
-  live_all = __reduce_add_sync(0xffffffffu, live_all);
-  if (lane == 0) s_last = 0;
-  __syncthreads();
-  if (lane == 0) atomicAdd(&s_last, live_all);
-  __syncthreads();
-  live_all = s_last;
   __syncthreads();
   if (warp == 0) {
     v = 0.f;
     c = 0;
-    n = 0;
-    zs = 0.0;
+#pragma unroll 8
     for (int w = 0; w < warps; ++w) {
       v += s_p[w][lane];
       c += s_c[w][lane];
-      n += s_n[w];
-      zs += s_z[w];
     }
+    n = __reduce_add_sync(0xffffffffu, lane < warps ? s_n[lane] : 0);
+    zs = group_sum<32>(lane < warps ? s_z[lane] : 0.f);
     const float prob = n > 0 ? v / float(n) : 0.f;
-    double part = 0.0;
+    float part = 0.f;
     if (e < p.E) {
       p.counts[size_t(s) * p.E + e] = c;
       p.prob[size_t(s) * p.E + e] = prob;
-      if (n > 0) part = double(c) * live_all / (double(p.k) * n) * double(prob);
+      if (n > 0) part = float(int64_t(c) * live_all) / float(int64_t(p.k) * n) * prob;
     }
-#pragma unroll
-    for (int h = 16; h > 0; h >>= 1) part += __shfl_xor_sync(0xffffffffu, part, h);
+    part = group_sum<32>(part);
     if (lane == 0) {
       p.w_part[size_t(s) * groups + grp] = part;
       if (grp == 0) {
@@ -308,80 +369,64 @@ __global__ void __launch_bounds__(1024) balance_reduce_kernel(const BalanceParam
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  double part = 0.0;
-  zs = 0.0;
+  double part = 0.0, zq = 0.0;  // (up to 2^23 terms)
   int m = 0, seqs = 0;
-  for (int i = threadIdx.x; i < p.n_seq * groups; i += blockDim.x) part += __ldcg(p.w_part + i);
+  for (int i = threadIdx.x; i < p.n_seq * groups; i += blockDim.x) part += double(__ldcg(p.w_part + i));
   for (int i = threadIdx.x; i < p.n_seq; i += blockDim.x) {
     const int ni = __ldcg(p.n_tokens + i);
     m += ni;
     seqs += ni > 0;
-    zs += __ldcg(p.w_zseq + i);
+    zq += double(__ldcg(p.w_zseq + i));
   }
-#pragma unroll
-  for (int h = 16; h > 0; h >>= 1) {
-    part += __shfl_xor_sync(0xffffffffu, part, h);
-    zs += __shfl_xor_sync(0xffffffffu, zs, h);
-  }
+  const float wpart = group_sum<32>(float(part)), wz = group_sum<32>(float(zq));
   m = __reduce_add_sync(0xffffffffu, m);
   seqs = __reduce_add_sync(0xffffffffu, seqs);
   if (lane == 0) {
-    s_d[warp] = part;
-    s_z[warp] = zs;
+    s_d[warp] = wpart;
+    s_z[warp] = wz;
     s_n[warp] = m;
-    s_c[0][warp] = seqs;
+    s_m[warp] = seqs;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    part = 0.0;
-    zs = 0.0;
-    m = 0;
-    seqs = 0;
-    for (int w = 0; w < warps; ++w) {
-      part += s_d[w];
-      zs += s_z[w];
-      m += s_n[w];
-      seqs += s_c[0][w];
+  if (warp == 0) {
+    const float d = group_sum<32>(lane < warps ? s_d[lane] : 0.f), z = group_sum<32>(lane < warps ? s_z[lane] : 0.f);
+    m = __reduce_add_sync(0xffffffffu, lane < warps ? s_n[lane] : 0);
+    seqs = __reduce_add_sync(0xffffffffu, lane < warps ? s_m[lane] : 0);
+    if (lane == 0) {
+      p.loss[0] = seqs > 0 ? p.coef * (d / float(seqs)) : 0.f;
+      p.loss[1] = m > 0 ? p.z_coef * (z / float(m)) : 0.f;
+      p.n_tokens[p.n_seq] = m;
+      p.n_tokens[p.n_seq + 1] = seqs;
     }
-    p.loss[0] = seqs > 0 ? float(double(p.coef) * part / seqs) : 0.f;
-    p.loss[1] = m > 0 ? float(double(p.z_coef) * zs / m) : 0.f;
-    p.n_tokens[p.n_seq] = m;
-    p.n_tokens[p.n_seq + 1] = seqs;
   }
 }
 
 // dz, from the kept log-sum-exp. Its rounding (of a number that may be much larger than one) is
 // common to a token's probabilities: dividing by their sum takes it out. A warp walks the sequences of
 // its tokens by itself, with the sequence's f - 1 of its experts in registers.
-template <int LPT, int NI>
-__global__ void __launch_bounds__(kThreads) balance_bwd_kernel(
+template <int LPT, int NI, bool VEC>
+__global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_bwd_kernel(
     const float *__restrict__ logits, const uint8_t *__restrict__ active_mask,
     const int32_t *__restrict__ seq_offsets, int n_seq, int T, int E, int k, int chunk, float coef, float z_coef,
     const int32_t *__restrict__ counts, const int32_t *__restrict__ n_tokens,
     const float *__restrict__ lse, const float *__restrict__ d_loss, float *__restrict__ dz) {
   constexpr int TPW = 32 / LPT;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane % LPT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, q = lane % LPT;
   pdl_start();
   const int t0 = blockIdx.x * chunk, t1 = min(T, t0 + chunk);
   if (t0 >= t1) return;
-  int live_all = 0;
-  for (int e = lane; e < E; e += 32) live_all += active_mask == nullptr || active_mask[e] != 0;
-  live_all = __reduce_add_sync(0xffffffffu, live_all);
-  bool live[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int e = q + LPT * i;
-    live[i] = e < E && (active_mask == nullptr || active_mask[e] != 0);
-  }
+  const int live_all = count_live(active_mask, E, lane);
+  const unsigned live = live_bits<LPT, NI, VEC>(active_mask, E, q);
+  const bool masked = __any_sync(0xffffffffu, live != (1u << NI) - 1u);
   const int m = n_tokens[n_seq], seqs = n_tokens[n_seq + 1];
   const float g0 = d_loss != nullptr ? d_loss[0] : 1.f, g1 = d_loss != nullptr ? d_loss[1] : 1.f;
   const float bz = m > 0 ? 2.f * z_coef * g1 / float(m) : 0.f;
   auto zero = [&](int a, int b) {  // rows of tokens in no sequence
-    for (int t = a + warp; t < b; t += kWarps)
+    for (int t = a + warp; t < b; t += warps)
       for (int e = lane; e < E; e += 32) dz[size_t(t) * E + e] = 0.f;
   };
   int cur = t0;
-  for (int s = first_sequence(seq_offsets, n_seq, T, t0); s < n_seq && cur < t1; ++s) {
+  for (int s = first_sequence(seq_offsets, n_seq, t0, lane); s < n_seq && cur < t1; ++s) {
     int a, b;
     sequence_range(seq_offsets, s, T, &a, &b);
     if (a >= t1) break;
@@ -390,39 +435,56 @@ __global__ void __launch_bounds__(kThreads) balance_bwd_kernel(
     zero(cur, a);
     cur = max(cur, a);
     if (a >= b) continue;
+    int t = a + warp * TPW + lane / LPT;
+    float l = t < b ? lse[t] : -INFINITY;
+    float next[NI] = {};
+    load_row<LPT, NI, VEC>(logits + size_t(t) * E, E, q, t < b, next);
     const int n = n_tokens[s];
     const float as = n > 0 && seqs > 0 ? coef * g0 / (float(seqs) * float(n)) : 0.f;
     float f[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       f[i] = 0.f;
-      if (live[i] && n > 0) {
-        const int64_t all = int64_t(k) * n, c = counts[size_t(s) * E + q + LPT * i];
+      if ((live >> i & 1) && n > 0) {
+        const int64_t all = int64_t(k) * n, c = counts[size_t(s) * E + expert_of<LPT, VEC>(q, i)];
         f[i] = float(c * live_all - all) / float(all);
       }
     }
-    for (int tb = a + warp * TPW; tb < b; tb += kWarps * TPW) {
-      const int t = tb + lane / LPT;
-      const float l = t < b ? lse[t] : -INFINITY;
-      const bool some = !(l == -INFINITY);
-      float z[NI], s0 = 0.f, s1 = 0.f;
+    for (int tb = a + warp * TPW; tb < b; tb += warps * TPW) {
+      const int tn = t;
+      const float ln = l;
+      float z[NI], s0[2] = {0.f, 0.f}, s1[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NI; ++i) z[i] = some && live[i] ? logits[size_t(t) * E + q + LPT * i] : -INFINITY;
+      for (int i = 0; i < NI; ++i) z[i] = next[i];
+      t += warps * TPW;
+      l = t < b ? lse[t] : -INFINITY;
+      load_row<LPT, NI, VEC>(logits + size_t(t) * E, E, q, t < b, next);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) z[i] = live >> i & 1 ? z[i] : -INFINITY;
+      }
+      const float c = -ln * kLog2e;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        z[i] = some ? expf(z[i] - l) : 0.f;
-        s0 += z[i];
-        s1 = fmaf(z[i], f[i], s1);
+        z[i] = exp2_quick(fmaf(z[i], kLog2e, c));
+        s0[i % 2] += z[i];
+        s1[i % 2] = fmaf(z[i], f[i], s1[i % 2]);
       }
-      s0 = group_sum<LPT>(s0);
-      s1 = group_sum<LPT>(s1);
-      if (t < b) {
-        const float r = some ? 1.f / s0 : 0.f, base = some ? fmaf(bz, l, -as * (s1 * r)) : 0.f;
+      s0[0] = group_sum<LPT>(s0[0] + s0[1]);
+      s1[0] = group_sum<LPT>(s1[0] + s1[1]);
+      if (tn >= b) continue;
+      // p (a f + base), p = z / s0; a token that does not count gets zeros whatever it holds
+      const float r = __fdividef(1.f, s0[0]), ar = as * r, base = r * fmaf(bz, ln, -as * (s1[0] * r));
+      const bool some = !(ln == -INFINITY);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int e = q + LPT * i;
-          if (e < E) dz[size_t(t) * E + e] = z[i] * r * fmaf(as, f[i], base);
-        }
+      for (int i = 0; i < NI; ++i) z[i] = some ? z[i] * fmaf(ar, f[i], base) : 0.f;
+      float *dst = dz + size_t(tn) * E;
+#pragma unroll
+      for (int i = 0; i < NI; i += VEC ? 4 : 1) {
+        const int e = expert_of<LPT, VEC>(q, i);
+        if (e >= E) continue;
+        if (VEC) *reinterpret_cast<float4 *>(dst + e) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
+        else dst[e] = z[i];
       }
     }
     cur = b;
@@ -430,15 +492,25 @@ __global__ void __launch_bounds__(kThreads) balance_bwd_kernel(
   zero(cur, t1);
 }
 
-// Lanes per token and logits per lane for E experts.
-template <typename F> void with_lanes(int E, F f) {
-  if (E <= 16) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-  else if (E <= 32) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
-  else if (E <= 64) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
-  else if (E <= 128) f(std::integral_constant<int, 32>(), std::integral_constant<int, 4>());
-  else if (E <= 192) f(std::integral_constant<int, 32>(), std::integral_constant<int, 6>());
-  else f(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
+// Lanes per token and logits per lane for E experts; whether a row of logits is whole 16-byte vectors.
+template <typename F> void with_lanes(int E, bool vec, F f) {
+  auto pick = [&](auto v) {
+    using std::integral_constant;
+    if (E <= 16) f(integral_constant<int, 4>(), integral_constant<int, 4>(), v);
+    else if (E <= 64) f(integral_constant<int, 8>(), integral_constant<int, 8>(), v);
+    else if (E <= 128) f(integral_constant<int, 16>(), integral_constant<int, 8>(), v);
+    else if (E <= 192) f(integral_constant<int, 16>(), integral_constant<int, 12>(), v);
+    else f(integral_constant<int, 16>(), integral_constant<int, 16>(), v);
+  };
+  if (vec) pick(std::true_type());
+  else pick(std::false_type());
 }
+// Warps of a block: enough for its chunk's tokens at once, up to what an SM holds.
+int block_warps(int T, int E) {
+  const int tpw = E <= 16 ? 8 : E <= 64 ? 4 : 2;
+  return std::min(kMaxWarps, (chunk_tokens(T) + tpw - 1) / tpw);
+}
+bool whole_vectors(int E, const void *a, const void *b) { return E % 4 == 0 && moe::aligned16(a) && moe::aligned16(b); }
 
 int check_sizes(const char *fn, int T, int E, int k, int n_seq, const void *seq_offsets, float coef, float z_coef) {
   if (E < 1 || E > 256) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: E=%d not in [1,256]", fn, E);
@@ -493,21 +565,22 @@ int moe_balance_loss(const float *logits, const int32_t *topk_idx, const uint8_t
   p.w_prob = reinterpret_cast<float *>(base + w.prob);
   p.w_count = reinterpret_cast<int32_t *>(base + w.count);
   p.w_n = reinterpret_cast<int32_t *>(base + w.n);
-  p.w_zsq = reinterpret_cast<double *>(base + w.zsq);
-  p.w_part = reinterpret_cast<double *>(base + w.part);
-  p.w_zseq = reinterpret_cast<double *>(base + w.zseq);
+  p.w_zsq = reinterpret_cast<float *>(base + w.zsq);
+  p.w_part = reinterpret_cast<float *>(base + w.part);
+  p.w_zseq = reinterpret_cast<float *>(base + w.zseq);
   p.loss = loss;
   p.prob = prob;
   p.lse = lse;
   p.counts = counts;
   p.n_tokens = n_tokens;
-  const int grid = std::max(1, chunk_count(T));
-  with_lanes(E, [&](auto lpt, auto ni) {
-    MOE_LAUNCH("balance_stats", s, moe::launch_dep(balance_stats_kernel<lpt.value, ni.value>, grid, kThreads, 0, s, p));
+  const int grid = std::max(1, chunk_count(T)), stat_threads = 32 * block_warps(T, E);
+  with_lanes(E, whole_vectors(E, logits, logits), [&](auto lpt, auto ni, auto vec) {
+    MOE_LAUNCH("balance_stats", s,
+               moe::launch_dep(balance_stats_kernel<lpt.value, ni.value, vec.value>, grid, stat_threads, 0, s, p));
   });
   if (int st = moe::launch_status("moe_balance_loss: token sums")) return st;
-  // few sequences: many warps for a sequence's rows; many: few rows each
-  const int threads = n_seq <= 32 ? 1024 : 128;
+  // a warp per ~4 of a sequence's rows, about
+  const int rows = chunk_count(T) / n_seq + 1, threads = 32 * std::max(4, std::min(32, rows / 4));
   MOE_LAUNCH("balance_reduce", s, moe::launch_dep(balance_reduce_kernel, n_seq * expert_groups(E), threads, 0, s, p));
   return moe::launch_status("moe_balance_loss: reduction");
 }
@@ -522,10 +595,11 @@ int moe_balance_loss_bwd(const float *logits, const uint8_t *active_mask, const 
   if (T == 0) return MOE_OK;
   if (!logits || !counts || !n_tokens || !lse || !dz) return moe::set_error(MOE_ERR_ARG, "%s: null pointer", fn);
   const int chunk = chunk_tokens(T);
-  with_lanes(E, [&](auto lpt, auto ni) {
-    MOE_LAUNCH("balance_bwd", s, moe::launch_dep(balance_bwd_kernel<lpt.value, ni.value>, chunk_count(T), kThreads, 0, s,
-                                                 logits, active_mask, seq_offsets, n_seq, T, E, k, chunk, coef, z_coef, counts,
-                                                 n_tokens, lse, d_loss, dz));
+  with_lanes(E, whole_vectors(E, logits, dz), [&](auto lpt, auto ni, auto vec) {
+    MOE_LAUNCH("balance_bwd", s,
+               moe::launch_dep(balance_bwd_kernel<lpt.value, ni.value, vec.value>, chunk_count(T), 32 * block_warps(T, E), 0, s, logits,
+                               active_mask, seq_offsets, n_seq, T, E, k, chunk, coef, z_coef, counts, n_tokens, lse, d_loss,
+                               dz));
   });
   return moe::launch_status("moe_balance_loss_bwd: launch");
 }
