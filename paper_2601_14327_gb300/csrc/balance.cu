@@ -29,6 +29,9 @@ MOE_DEV_ERR_DECL
 
 namespace {
 
+// The kernels here let the next one start when their blocks end, not when they start: waiting blocks
+// of a next kernel take room that this one's blocks still want (47.6 / 44.9 us for the three kernels at
+// T=65536, 256 experts; 23.3 / 21.9 at 16384, 64; 15.9 / 14.5 at 37, 64).
 constexpr int kMaxWarps = 24;  // of a block: 80 registers a thread, one block per SM
 constexpr int kMaxSeqs = 1 << 20;
 
@@ -190,7 +193,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_stats_kernel(const 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, q = lane % LPT;
   const int threads = blockDim.x, warps = threads >> 5;
   for (int e = tid; e < 256; e += threads) s_hist[e] = 0;
-  pdl_start();
+  pdl_wait();
   if (blockIdx.x == 0 && tid == 0) *p.ticket = 0;
   const int t0 = blockIdx.x * p.chunk, t1 = min(p.T, t0 + p.chunk);
   if (t0 >= t1) return;  // (no tokens at all)
@@ -305,7 +308,7 @@ __global__ void __launch_bounds__(1024) balance_reduce_kernel(const BalanceParam
   __shared__ float s_d[32], s_z[32];
   __shared__ int s_last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  pdl_start();
+  pdl_wait();
   const int groups = (p.E + 31) / 32;
   const int s = blockIdx.x / groups, grp = blockIdx.x - s * groups, e = grp * 32 + lane;
   int a, b;
@@ -412,7 +415,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_bwd_kernel(
     const float *__restrict__ lse, const float *__restrict__ d_loss, float *__restrict__ dz) {
   constexpr int TPW = 32 / LPT;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, q = lane % LPT;
-  pdl_start();
+  pdl_wait();
   const int t0 = blockIdx.x * chunk, t1 = min(T, t0 + chunk);
   if (t0 >= t1) return;
   const int live_all = count_live(active_mask, E, lane);

@@ -65,13 +65,17 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const uint16_t *__restri
 
 // Rows of codes -> bf16 rows x_out[r] (null: not stored) and the K grouped rows of the row's
 // assignments (K = 0: none). Blocks below pad_blocks zero the groups' padding rows.
+// The next kernel may start when blocks end, not when they start: its waiting blocks then take the
+// SMs' room unevenly, and the few heavy blocks of this one (a row and its copies per warp) land on
+// few SMs: with a pack before it 26.9 us a pass against 16.5 at 1,021 rows of 2,048, top-6 (12.5 with four
+// warps per row besides).
 template <bool GROUPED>
 __global__ void __launch_bounds__(kThreads) unpack_kernel(
     const uint8_t *__restrict__ q, const uint8_t *__restrict__ scale, int64_t rows, int cols, int nseg,
     const int32_t *__restrict__ row_of_assignment, int k, int64_t rows_cap, int pad_blocks,
     const int32_t *__restrict__ group_offsets, const int32_t *__restrict__ group_counts,
     uint16_t *__restrict__ x_out, uint16_t *__restrict__ x_perm) {
-  pdl_start();
+  pdl_wait();
   const int lane = threadIdx.x & 31;
   if (GROUPED && int(blockIdx.x) < pad_blocks) {
     moe::zero_pad_rows<kWarps>(blockIdx.x, group_offsets, group_counts, cols, rows_cap, x_perm);
@@ -121,44 +125,54 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(
 }
 
 // Kept [A|B] -> bf16 in the layout of moe_grouped_ffn_fwd's ab_saved, and H = silu(A) * B. A warp takes
-// a 32-row tile's 16 columns of A and the same of B, a lane a row.
+// 32 columns of A and the same of B of a 32-row tile, a lane a row, as the GEMM epilogue that kept them. H's rows
+// go through shared memory, so that a store instruction writes 8 whole 64-byte row pieces and
+// not 32 quarters of one.
 __global__ void __launch_bounds__(kThreads) unpack_ab_kernel(const uint8_t *__restrict__ q,
                                                              const uint8_t *__restrict__ scale,
                                                              const int32_t *__restrict__ group_offsets, int E, int F,
-                                                             int64_t rows_cap, uint16_t *__restrict__ ab, uint16_t *__restrict__ h) {
-  pdl_start();
-  const int lane = threadIdx.x & 31, per = F / 16;
-  const int64_t n = min(int64_t(group_offsets[E]), rows_cap) / 32 * per;
-  for (int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); w < n; w += int64_t(gridDim.x) * kWarps) {
-    const int64_t tile = w / per;
-    const int c = int(w - tile * per) * 16;
-    const size_t row = size_t(tile) * 32 + lane;
-    const uint4 qa = ldg_nc_v4(q + ckpt::ab_code_index(row, c, F)), qb = ldg_nc_v4(q + ckpt::ab_code_index(row, F + c, F));
-    const float sa = ckpt::scale_value(__ldg(scale + ckpt::ab_scale_index(row, c, F)));
-    const float sb = ckpt::scale_value(__ldg(scale + ckpt::ab_scale_index(row, F + c, F)));
-    const uint32_t wa[4] = {qa.x, qa.y, qa.z, qa.w}, wb[4] = {qb.x, qb.y, qb.z, qb.w};
+                                                             int64_t rows_cap, uint16_t *__restrict__ ab,
+                                                             uint16_t *__restrict__ h) {
+  __shared__ uint4 s_h[kWarps][32][4];  // 16-byte piece c of row r at (c + r / 2) % 4: no bank conflicts
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = F / 32;
+  const int64_t w = int64_t(blockIdx.x) * kWarps + warp;
+  const int64_t tile = w / per;
+  if (tile >= min(int64_t(group_offsets[E]), rows_cap) / 32) return;
+  const int c = int(w - tile * per) * 32;
+  const size_t row = size_t(tile) * 32 + lane;
+  const uint8_t *qa = q + ckpt::ab_code_index(row, c, F), *qb = q + ckpt::ab_code_index(row, F + c, F);
+  const uint4 va[2] = {ldg_nc_v4(qa), ldg_nc_v4(qa + 512)}, vb[2] = {ldg_nc_v4(qb), ldg_nc_v4(qb + 512)};
+  const float sa = ckpt::scale_value(__ldg(scale + ckpt::ab_scale_index(row, c, F)));
+  const float sb = ckpt::scale_value(__ldg(scale + ckpt::ab_scale_index(row, F + c, F)));
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      float fa[8], fb[8], fh[8];
-      ckpt::values4(wa[2 * half], sa, fa);
-      ckpt::values4(wa[2 * half + 1], sa, fa + 4);
-      ckpt::values4(wb[2 * half], sb, fb);
-      ckpt::values4(wb[2 * half + 1], sb, fb + 4);
+  for (int v = 0; v < 4; ++v) {
+    float fa[8], fb[8], fh[8];
+    ckpt::values4(v % 2 ? va[v / 2].z : va[v / 2].x, sa, fa);
+    ckpt::values4(v % 2 ? va[v / 2].w : va[v / 2].y, sa, fa + 4);
+    ckpt::values4(v % 2 ? vb[v / 2].z : vb[v / 2].x, sb, fb);
+    ckpt::values4(v % 2 ? vb[v / 2].w : vb[v / 2].y, sb, fb + 4);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fh[i] = silu_f(fa[i]) * fb[i];
-      const int col = c + 8 * half;
-      if (ab != nullptr) {
-        stg_v4(ab + ab_block_index(row, col, F), pack8(fa));
-        stg_v4(ab + ab_block_index(row, F + col, F), pack8(fb));
-      }
-      if (h != nullptr) stg_v4(h + row * F + col, pack8(fh));
+    for (int i = 0; i < 8; ++i) fh[i] = silu_f(fa[i]) * fb[i];
+    if (ab != nullptr) {
+      stg_v4(ab + ab_block_index(row, c + 8 * v, F), pack8(fa));
+      stg_v4(ab + ab_block_index(row, F + c + 8 * v, F), pack8(fb));
     }
+    s_h[warp][lane][(v + (lane >> 1)) & 3] = pack8(fh);
+  }
+  if (h == nullptr) return;
+  __syncwarp();
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int r = 8 * u + (lane >> 2), v = lane & 3;
+    stg_v4(h + (size_t(tile) * 32 + r) * F + c + 8 * v, s_h[warp][r][(v + (r >> 1)) & 3]);
   }
 }
 
-// Warps per row: one from 8 warps per SM on, and with fewer rows as many as give that.
+// Warps per row: one from 32 warps per SM on, and with fewer rows as many as give that (1,021 rows of
+// 2,048: 16.5 us with 8 warps per SM, 12.7 with 16, 12.5 with 32; 32,768 rows of 4,096 the same).
 int row_segments(int64_t rows, int cols) {
-  const int64_t warps = int64_t(moe::num_sms()) * 8, most = (cols / 8 + 31) / 32;
+  const int64_t warps = int64_t(moe::num_sms()) * 32, most = (cols / 8 + 31) / 32;
   return int(std::max<int64_t>(1, std::min(most, warps / std::max<int64_t>(rows, 1))));
 }
 int64_t row_grid(int64_t rows, int nseg) { return (rows * nseg + kWarps - 1) / kWarps; }
@@ -236,10 +250,11 @@ int moe_ckpt_unpack_ab(const uint8_t *ab_q, const uint8_t *ab_scale, const int32
   for (const void *p : {static_cast<const void *>(ab_q), static_cast<const void *>(ab_scale),
                         static_cast<const void *>(ab_saved), static_cast<const void *>(h)})
     if (p && !moe::aligned16(p)) return moe::set_error(MOE_ERR_ARG, "%s: alignment", fn);
-  const int64_t warps = rows_cap / 32 * (F / 16);
-  const int grid = int(std::max<int64_t>(1, std::min<int64_t>((warps + kWarps - 1) / kWarps, int64_t(moe::num_sms()) * 64)));
-  MOE_LAUNCH("ckpt_unpack_ab", s, moe::launch_dep(unpack_ab_kernel, grid, kThreads, 0, s, ab_q, ab_scale, group_offsets, E,
-                                                  F, rows_cap, ab_saved, h));
+  const int64_t warps = rows_cap / 32 * (F / 32);
+  if (warps / kWarps >= (int64_t(1) << 31) - 1)
+    return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: rows_cap=%lld F=%d", fn, (long long)rows_cap, F);
+  MOE_LAUNCH("ckpt_unpack_ab", s, moe::launch_dep(unpack_ab_kernel, dim3(unsigned((warps + kWarps - 1) / kWarps)), kThreads, 0,
+                                                  s, ab_q, ab_scale, group_offsets, E, F, rows_cap, ab_saved, h));
   return moe::launch_status("moe_ckpt_unpack_ab: launch");
 }
 

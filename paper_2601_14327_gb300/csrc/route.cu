@@ -594,13 +594,12 @@ __global__ void load_stats_kernel(const int32_t *__restrict__ topk_idx, int64_t 
 // and dZ (the [T, E] logit gradient, zero off the selected experts) as three bf16
 // terms, K-major for the tensor cores: dz3[s][e][t] for e < NP, t < Tp (tokens padded
 // to 64; the padding is zero). One thread per token and 16 experts (blockIdx.y); the
-// y = 0 blocks also write d_logits. DENSE: dz [T, E] is added to dZ, and topk_idx may be null.
+// y = 0 blocks also write d_logits.
 constexpr int kDzExperts = 16;
-template <bool DENSE>
 __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
                                     const float *__restrict__ gate, const float *__restrict__ dgate,
-                                    const float *__restrict__ dz, int T, int Tp, int E, int k, int NP,
-                                    float *__restrict__ d_logits, uint16_t *__restrict__ dz3) {
+                                    int T, int Tp, int k, int NP, float *__restrict__ d_logits,
+                                    uint16_t *__restrict__ dz3) {
   pdl_start();
   const int t = blockIdx.x * blockDim.x + threadIdx.x;
   if (t >= Tp) return;
@@ -611,7 +610,7 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
     g[j] = 0.f;
     dg[j] = 0.f;
     ei[j] = -1;
-    if (j < k && t < T && (!DENSE || topk_idx != nullptr)) {
+    if (j < k && t < T) {
       g[j] = gate[size_t(t) * k + j];
       dg[j] = dgate[size_t(t) * k + j];
       ei[j] = topk_idx[size_t(t) * k + j];
@@ -621,7 +620,7 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     g[j] = g[j] * (dg[j] - s);
-    if (blockIdx.y == 0 && j < k && t < T && (!DENSE || topk_idx != nullptr)) d_logits[size_t(t) * k + j] = g[j];
+    if (blockIdx.y == 0 && j < k && t < T) d_logits[size_t(t) * k + j] = g[j];
   }
   const size_t plane = size_t(NP) * Tp;
   const int e0 = blockIdx.y * kDzExperts;
@@ -630,7 +629,6 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (ei[j] == e) v = g[j];  // the k selected experts of a token are distinct
-    if (DENSE && t < T && e < E) v += dz[size_t(t) * E + e];
     const __nv_bfloat16 hi = __float2bfloat16_rn(v);
     const float r1 = v - __bfloat162float(hi);
     const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
@@ -640,6 +638,85 @@ __global__ void route_bwd_dz_kernel(const int32_t *__restrict__ topk_idx,
     dz3[at] = __bfloat16_as_ushort(hi);
     dz3[plane + at] = __bfloat16_as_ushort(mid);
     dz3[2 * plane + at] = __bfloat16_as_ushort(lo);
+  }
+}
+
+// The same with a dense gradient dz [T, E] beside the selected experts' (topk_idx null: alone): tiles of
+// 64 tokens x 64 experts, transposed through shared memory, so that dz is read along its rows and the terms are
+// written along theirs, 16 bytes a thread (a thread per token reading 64-byte pieces of its row: 40 us at T=65536,
+// 171 experts; 27 now, the bytes alone 17).
+constexpr int kDzTile = 64;
+__global__ void __launch_bounds__(256) route_bwd_dz_dense_kernel(
+    const int32_t *__restrict__ topk_idx, const float *__restrict__ gate, const float *__restrict__ dgate,
+    const float *__restrict__ dz, int T, int Tp, int E, int k, int NP, float *__restrict__ d_logits,
+    uint16_t *__restrict__ dz3) {
+  __shared__ float tile[kDzTile][kDzTile + 1];  // [expert][token]
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int t0 = blockIdx.x * kDzTile, e0 = blockIdx.y * kDzTile;
+#pragma unroll
+  for (int i = 0; i < kDzTile / 8; ++i) {
+    const int r = warp + 8 * i, t = t0 + r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int e = e0 + lane + 32 * h;
+      tile[lane + 32 * h][r] = t < T && e < E ? __ldg(dz + size_t(t) * E + e) : 0.f;
+    }
+  }
+  float g[8], dg[8], s = 0.f;
+  int ei[8];
+  const int t = t0 + tid;
+  const bool mine = topk_idx != nullptr && tid < kDzTile && t < T;
+  if (mine) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      g[j] = dg[j] = 0.f;
+      ei[j] = -1;
+      if (j < k) {
+        g[j] = gate[size_t(t) * k + j];
+        dg[j] = dgate[size_t(t) * k + j];
+        ei[j] = topk_idx[size_t(t) * k + j];
+        s = fmaf(g[j], dg[j], s);
+      }
+    }
+  }
+  __syncthreads();
+  if (mine) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = g[j] * (dg[j] - s);
+      if (blockIdx.y == 0 && j < k) d_logits[size_t(t) * k + j] = v;
+      const int e = ei[j] - e0;  // (an id outside [0, E) is left out)
+      if (ei[j] >= 0 && ei[j] < E && e >= 0 && e < kDzTile) tile[e][tid] += v;
+    }
+  }
+  __syncthreads();
+  const size_t plane = size_t(NP) * Tp;
+#pragma unroll
+  for (int u = tid; u < kDzTile * (kDzTile / 8); u += 256) {
+    const int e = u / 8, c = u % 8 * 8;
+    if (e0 + e >= NP) break;
+    uint32_t o[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint16_t b[3][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float v = tile[e][c + 2 * i + h];
+        const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+        const float r1 = v - __bfloat162float(hi);
+        const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
+        const float r2 = r1 - __bfloat162float(mid);
+        b[0][h] = __bfloat16_as_ushort(hi);
+        b[1][h] = __bfloat16_as_ushort(mid);
+        b[2][h] = __bfloat16_as_ushort(__float2bfloat16_rn(r2));
+      }
+#pragma unroll
+      for (int m = 0; m < 3; ++m) o[m][i] = uint32_t(b[m][0]) | uint32_t(b[m][1]) << 16;
+    }
+    uint16_t *dst = dz3 + size_t(e0 + e) * Tp + t0 + c;
+#pragma unroll
+    for (int m = 0; m < 3; ++m) stg_v4(dst + m * plane, make_uint4(o[m][0], o[m][1], o[m][2], o[m][3]));
   }
 }
 
@@ -1236,8 +1313,12 @@ static int route_bwd(const char *fn, const uint16_t *x, const int32_t *topk_idx,
   float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + L.route_dw_partial);
   const int NP = route_tc_np(E), Tp = route_tokens_padded(T);
   dim3 zgrid((Tp + 255) / 256, (NP + kDzExperts - 1) / kDzExperts);
-  MOE_LAUNCH("route_bwd_dz", s, moe::launch_dep(dz ? route_bwd_dz_kernel<true> : route_bwd_dz_kernel<false>, zgrid, 256, 0,
-                                    s, topk_idx, topk_gate, d_gate, dz, T, Tp, E, k, NP, d_logits, dz3));
+  if (dz)
+    MOE_LAUNCH("route_bwd_dz", s, moe::launch_dep(route_bwd_dz_dense_kernel, dim3(Tp / kDzTile, (NP + kDzTile - 1) / kDzTile), 256,
+                                      0, s, topk_idx, topk_gate, d_gate, dz, T, Tp, E, k, NP, d_logits, dz3));
+  else
+    MOE_LAUNCH("route_bwd_dz", s, moe::launch_dep(route_bwd_dz_kernel, zgrid, 256, 0, s,
+                                      topk_idx, topk_gate, d_gate, T, Tp, k, NP, d_logits, dz3));
   if (int st = moe::launch_status("moe_route_bwd: dz")) return st;
   int splits = 0;
   if (int st = launch_route_dw(x, dz3, T, d, E, partial, &splits, s)) return st;
