@@ -720,6 +720,226 @@ __global__ void __launch_bounds__(256) route_bwd_dz_dense_kernel(
   }
 }
 
+// x^T dZ of the dense router backward on CTA pairs. The tensor core adds to its fp32 accumulator with
+// truncation: over the ~2,500 additions of a long split route_tc_kernel's sums come out 4e-5 too small (2-norm,
+// T=65536, d=7168, 171 experts; an fp32 product by the library is 5e-6 off), more than the rounding of a dense
+// loss gradient may be. Here an accumulator takes kDwFlush k-blocks, while the epilogue warps add the one before to
+// their registers, rounding to nearest: 8.8e-7 off, whatever T is. The tensor pipe sets the time: 275 us there,
+// 263 at its measured rate (route_tc_kernel: 291, by shared memory; a pair's M=256 MMA reads each SM's own 128
+// features and half of dZ's rows). Two terms of dZ would take 230 us and be 2.5e-6 off, ten times
+// what an fp32 product is over 1,000 tokens. Roles as in the grouped GEMMs' pair kernel: warp 0 of each
+// CTA loads (its features of x, its half of the terms' rows), one thread of the even CTA issues the MMAs, warps
+// 2..9 of each own a TMEM lane quarter and half of the experts.
+constexpr int kDwFlush = 4;
+constexpr int kDwThreads = 64 + 32 * 8;
+struct RouteDwParams {
+  int M, NP, NE;         // d, experts rounded up to 16, row stride of the partial sums
+  int nkb, kb_per_split; // 64-token k-blocks
+  int G;                 // terms per MMA: 3 (each with its own columns) or 1
+  int stages;
+  uint32_t buf_cols;     // TMEM columns of an accumulator
+  float *partial;
+};
+uint32_t route_dwp_stage_bytes(int NP) { return kRtBM * kRtBK * 2 + 3u * uint32_t(NP / 2) * 128u; }
+int route_dwp_group(int NP) { return 3 * NP <= 256 ? 3 : 1; }
+size_t route_dwp_smem(int NP, int stages) {
+  return 1024 + size_t(stages) * route_dwp_stage_bytes(NP) + size_t(2 * stages + 5) * 8 + 16;
+}
+int route_dwp_stages(int NP) { return int(std::min<int64_t>(8, (kRtMaxSmem - 2048) / route_dwp_stage_bytes(NP))); }
+
+__global__ void __launch_bounds__(kDwThreads, 1)
+    route_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmZ,
+                         const RouteDwParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+  constexpr uint32_t a_bytes = kRtBM * kRtBK * 2;
+  const uint32_t half_rows = uint32_t(p.NP / 2), b_term = half_rows * 128u;  // a multiple of 1024
+  const uint32_t stage_bytes = a_bytes + 3u * b_term;
+  const int S = p.stages;
+  const uint32_t s0 = raw + pad;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem_raw + pad + size_t(S) * stage_bytes);
+  int *misc = reinterpret_cast<int *>(bars + 2 * S + 5);
+  volatile int *abort_flag = misc + 1;
+  volatile int no_abort = 0;
+  const uint32_t bar0 = tc::smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * S + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * S + 2 + a); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * S + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_ctarank();
+  const bool leader = rank == 0;
+  const int feature0 = int(blockIdx.x) * kRtBM;  // this CTA's features (the pair's are consecutive)
+  const int split = blockIdx.y, kb0 = split * p.kb_per_split, nk = min(p.nkb, kb0 + p.kb_per_split) - kb0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      tc::mbar_init(full_bar(s), 1);
+      tc::mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      tc::mbar_init(tfull_bar(a), 1);
+      tc::mbar_init(tempty_bar(a), 16);  // the epilogue warps of both CTAs
+    }
+    tc::mbar_init(drain_bar, 1);
+    tc::fence_mbar_init();
+    misc[1] = 0;
+  }
+  if (warp == 1) {
+    tc::tmem_alloc_pair(tc::smem_u32(misc), 2 * p.buf_cols);
+    tc::tmem_relinquish_pair();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync();  // barriers of both CTAs initialized before any remote use
+  tc::fence_after_sync();
+  const uint32_t tmem_base = static_cast<uint32_t>(misc[0]);
+  pdl_wait();
+  auto fail = [&]() {
+    dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
+    *abort_flag = 1;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t full_leader = tc::mapa(full_bar(0), 0);
+      uint32_t it = 0;
+      for (; int(it) < nk; ++it) {
+        const int s = it % S, k0 = (kb0 + int(it)) * kRtBK;
+        if (!tc::mbar_wait(empty_bar(s), ((it / S) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); break; }
+        if (leader) tc::mbar_arrive_expect_tx(full_bar(s), 2 * stage_bytes);
+        const uint32_t a = s0 + s * stage_bytes, b = a + a_bytes, fb = full_leader + 8u * s;
+        // x^T: two 64-feature x 64-token boxes
+        tc::tma_load_2d_pair(a, &tmX, fb, feature0, k0);
+        tc::tma_load_2d_pair(a + 8192, &tmX, fb, feature0 + 64, k0);
+        // the pair's N rows are the even CTA's, then the odd one's: of all three terms, or of each
+        if (p.G == 3) {
+          tc::tma_load_2d_pair(b, &tmZ, fb, k0, int(rank * 3u * half_rows));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            tc::tma_load_2d_pair(b + j * b_term, &tmZ, fb, k0, j * p.NP + int(rank * half_rows));
+        }
+      }
+      if (leader)  // its full barriers count the loads of both CTAs
+        for (int s = 0; s < S; ++s)
+          if (it > uint32_t(s) && !tc::mbar_wait(full_bar(s), ((it - 1 - s) / S) & 1u, kRtWaitNs, &no_abort)) fail();
+    }
+  } else if (warp == 1) {
+    if (leader && lane == 0) {
+      const uint32_t idesc = tc::idesc_bf16_f32(2 * kRtBM, p.G * p.NP, true, false);
+      uint32_t it = 0;
+      bool ok = true, issued = false;
+      for (uint32_t f = 0; int(it) < nk && ok; ++f) {
+        const uint32_t a = f & 1u, d = tmem_base + a * p.buf_cols;
+        if (!tc::mbar_wait(tempty_bar(a), ((f >> 1) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); break; }
+        tc::fence_after_sync();
+        for (int b = 0; b < kDwFlush && int(it) < nk; ++b, ++it) {
+          const int s = it % S;
+          if (!tc::mbar_wait(full_bar(s), (it / S) & 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
+          tc::fence_after_sync();
+          const uint32_t a_s = s0 + s * stage_bytes;
+          const uint64_t a0 = tc::smem_desc_sw128(a_s, 8192, 1024), b0 = tc::smem_desc_sw128(a_s + a_bytes, 16, 1024);
+#pragma unroll
+          for (int kk = 0; kk < kRtBK / 16; ++kk) {  // (a descriptor's address counts 16 bytes)
+            tc::mma_bf16_pair(d, a0 + uint64_t(kk * 128), b0 + uint64_t(kk * 2), idesc, (b | kk) != 0 ? 1u : 0u);
+            if (p.G == 1) {
+              tc::mma_bf16_pair(d, a0 + uint64_t(kk * 128), b0 + uint64_t(kk * 2) + uint64_t(b_term >> 4), idesc, 1u);
+              tc::mma_bf16_pair(d, a0 + uint64_t(kk * 128), b0 + uint64_t(kk * 2) + 2 * uint64_t(b_term >> 4), idesc, 1u);
+            }
+          }
+          tc::mma_commit_pair_mc(empty_bar(s), 0x3);
+          issued = true;
+        }
+        if (!ok) break;
+        tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
+      }
+      if (issued) {
+        tc::mma_commit_pair(drain_bar);
+        if (!tc::mbar_wait(drain_bar, 0, kRtWaitNs, &no_abort)) fail();
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) / 4;
+    const uint32_t tempty_leader = tc::mapa(tempty_bar(0), 0);
+    float acc[128];  // this lane's feature, experts half * NP/2 + c
+#pragma unroll
+    for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+    bool ok = true;
+    const uint32_t flushes = uint32_t(nk + kDwFlush - 1) / kDwFlush;
+    for (uint32_t f = 0; f < flushes; ++f) {
+      const uint32_t a = f & 1u;
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(tfull_bar(a), (f >> 1) & 1u, kRtWaitNs, abort_flag));
+      if (!ok) { fail(); break; }
+      tc::fence_after_sync();
+      const uint32_t tb = tmem_base + (uint32_t(q * 32) << 16) + a * p.buf_cols + uint32_t(half) * half_rows;
+      // (8 columns at a time: with 16 the 168 registers that ten warps leave a thread do not hold them)
+#pragma unroll
+      for (int c = 0; c < 128; c += 8) {
+        if (uint32_t(c) < half_rows) {
+          uint32_t r[8];
+          tc::tmem_ld_32x32b_x8(tb + c, r);
+          if (p.G == 3) {
+            uint32_t r1[8], r2[8];
+            tc::tmem_ld_32x32b_x8(tb + c + p.NP, r1);
+            tc::tmem_ld_32x32b_x8(tb + c + 2 * p.NP, r2);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              acc[c + i] += __uint_as_float(r[i]) + (__uint_as_float(r1[i]) + __uint_as_float(r2[i]));
+          } else {
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[c + i] += __uint_as_float(r[i]);
+          }
+        }
+      }
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * a);
+    }
+    const int row = feature0 + q * 32 + lane;
+    if (ok && row < p.M) {
+      float *dst = p.partial + (size_t(split) * p.M + row) * p.NE + half * half_rows;
+#pragma unroll
+      for (int c = 0; c < 128; c += 4)
+        if (uint32_t(c) < half_rows) *reinterpret_cast<float4 *>(dst + c) = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+    }
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync();  // no CTA leaves while its peer may still signal it
+  if (warp == 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc_pair(tmem_base, 2 * p.buf_cols);
+  }
+}
+
+// Splits of the reduction over nkb k-blocks for d features: the least estimated time (ns), a pair's k-block
+// in its MMAs, its shared-memory traffic or its share of the HBM rate for x, whole rounds of the 76 pairs with ~3 us of
+// filling and draining each, and a split's partial sums written and read. A function of (d, nkb, NP) alone.
+int route_dwp_splits(int M, int nkb, int NP) {
+  const int64_t tiles = (M + 2 * kRtBM - 1) / (2 * kRtBM), pairs = kRtSms / 2;
+  const int64_t a = kRtBM * kRtBK * 2, b = 3 * int64_t(NP / 2) * 128, reads = route_dwp_group(NP) == 3 ? 1 : 3;
+  // (MMA: 3 terms x 4 steps of 256 x NP x 16 at a pair's 8,192 multiply-adds a clock, 1.9 GHz)
+  const int64_t kb_ns = std::max<int64_t>({a * 1000 / 44700, (a + b + reads * a + b) * 1000 / 243000, int64_t(NP) * 6000 / 1900});
+  const int64_t ne = (NP + 31) / 32 * 32;
+  int best = 1;
+  int64_t best_ns = INT64_MAX;
+  for (int r = 1; r <= 8; ++r) {  // the splits that fill r rounds
+    const int want = int(std::max<int64_t>(1, std::min<int64_t>({r * pairs / tiles, nkb, kRtDwSplits})));
+    const int per = (nkb + want - 1) / want, s = (nkb + per - 1) / per;  // every split gets at least one k-block
+    const int64_t ns = (tiles * s + pairs - 1) / pairs * (per * kb_ns + 3000) + s * int64_t(M) * ne * 8 / 4000;
+    if (ns < best_ns) {
+      best_ns = ns;
+      best = s;
+    }
+  }
+  return best;
+}
+
 // dw_router[i, e] = sum over the splits, in order, of partial[split][i][e]; four experts per thread,
 // four partials in flight.
 __global__ void route_dw_reduce_kernel(const float *__restrict__ partial, int splits, int d,
@@ -1196,7 +1416,9 @@ size_t route_dx_bytes(int T, int d, int E) {
 }
 size_t route_dw_partial_bytes(int T, int d, int E) {
   if (T <= 0) return 0;
-  const int splits = route_dw_plan(d, route_tokens_padded(T), route_tc_np(E)).splits;
+  const int NP = route_tc_np(E), Tp = route_tokens_padded(T);
+  int splits = route_dw_plan(d, Tp, NP).splits;
+  if (E <= 256) splits = std::max(splits, route_dwp_splits(d, Tp / kRtBK, NP));  // (moe_route_bwd_dense)
   return size_t(splits) * size_t(d) * size_t(route_dw_stride(E)) * 4;
 }
 }  // namespace moe
@@ -1288,6 +1510,53 @@ int launch_route_dw(const uint16_t *x, const uint16_t *dz3, int T, int d, int E,
     default: return launch_route_mma<true, 3>("route_bwd_dw", grid, smem, mx, mz, p, s, what);
   }
 }
+
+// As launch_route_dw, on CTA pairs (see route_dw_pair_kernel).
+int launch_route_dw_pair(const uint16_t *x, const uint16_t *dz3, int T, int d, int E, float *partial,
+                         int *splits_out, cudaStream_t s) {
+  const int NP = route_tc_np(E), Tp = route_tokens_padded(T);
+  const char *what = "moe_route_bwd_dense: weight gradient";
+  RouteDwParams p{};
+  p.M = d;
+  p.NP = NP;
+  p.NE = route_dw_stride(E);
+  p.nkb = Tp / kRtBK;
+  const int splits = route_dwp_splits(d, p.nkb, NP);
+  p.kb_per_split = (p.nkb + splits - 1) / splits;
+  p.G = route_dwp_group(NP);
+  p.stages = route_dwp_stages(NP);
+  const uint32_t cols = uint32_t(p.G * NP);
+  p.buf_cols = cols <= 32 ? 32u : cols <= 64 ? 64u : cols <= 128 ? 128u : 256u;
+  p.partial = partial;
+  CUtensorMap mx, mz;
+  int st;
+  if ((st = moe::make_map(&mx, x, uint64_t(T), uint64_t(d), 64, kRtBK, "router bwd x"))) return st;
+  if ((st = moe::make_map(&mz, dz3, uint64_t(3 * NP), uint64_t(Tp), kRtBK, uint32_t(p.G * NP / 2), "router bwd dz")))
+    return st;
+  static bool attr_set = false;
+  if (!attr_set) {
+    cudaError_t e = cudaFuncSetAttribute(route_dw_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    attr_set = true;
+  }
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see moe::launch_dep
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * ((d + 2 * kRtBM - 1) / (2 * kRtBM)), splits);
+  cfg.blockDim = dim3(kDwThreads);
+  cfg.dynamicSmemBytes = route_dwp_smem(NP, p.stages);
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  *splits_out = splits;
+  MOE_LAUNCH("route_bwd_dw", s, cudaLaunchKernelEx(&cfg, route_dw_pair_kernel, mx, mz, p));
+  return moe::launch_status(what);
+}
 }  // namespace
 
 extern "C" {
@@ -1321,7 +1590,9 @@ static int route_bwd(const char *fn, const uint16_t *x, const int32_t *topk_idx,
                                       topk_idx, topk_gate, d_gate, T, Tp, k, NP, d_logits, dz3));
   if (int st = moe::launch_status("moe_route_bwd: dz")) return st;
   int splits = 0;
-  if (int st = launch_route_dw(x, dz3, T, d, E, partial, &splits, s)) return st;
+  if (int st = dz ? launch_route_dw_pair(x, dz3, T, d, E, partial, &splits, s)
+                  : launch_route_dw(x, dz3, T, d, E, partial, &splits, s))
+    return st;
   const int n = d * (route_dw_stride(E) / 4);
   MOE_LAUNCH("route_bwd_reduce", s, moe::launch_dep(route_dw_reduce_kernel, std::min((n + 255) / 256, 4 * moe::num_sms()), 256, 0, s,
                                         partial, splits, d, E, route_dw_stride(E), dw_router));
