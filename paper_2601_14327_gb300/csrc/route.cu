@@ -986,17 +986,22 @@ __global__ void zero_f32_kernel(float *p, int n) {
 // 64 bits: 1.01 times that of the rounding alone). One product instead of the six of bf16 pairs
 // or half the rate of tf32, and half the operand bytes.
 //
-// HBM-bound (dx_in read, dx written: 4 bytes per 2 E operations). A persistent CTA takes
-// consecutive 128-token x 256-column tiles, columns first, so that a token block's operand stays in shared memory
-// for its whole row of tiles and W's (a few MB) comes from L2. Warp 0 issues the operand loads, warp 1
-// the MMAs, into two accumulators; warps 2..9 add dx_in. Each of those has its own ring of three 32-row x 64-column
-// pieces of dx: a piece is loaded by TMA two pieces ahead, gets the products added in place, and is
-// stored by TMA from there. No piece is touched by two warps, so dx_in may be dx.
+// HBM-bound (dx_in read, dx written: 4 bytes per 2 E operations). A persistent CTA pair takes
+// consecutive 256-token x 256-column tiles, columns first, so that a token block's operand stays in shared memory
+// for its whole row of tiles and W's (a few MB) comes from L2, half to each CTA. Warp 0 of each CTA
+// issues its operand loads, one thread of the even CTA the MMAs, into two accumulators; warps 2..17 add dx_in. Each
+// of those has its own ring of three 32-row x 32-column pieces of dx: a piece is loaded by TMA two pieces
+// ahead, gets the products added in place, and is stored by TMA from there. No piece is touched by two warps, so
+// dx_in may be dx.
+// T=65536, d=7168, in and out of place: 307 us at 171 experts (6.1 TB/s; a copy of dx takes 275), 306 at
+// 32, 332 at 256. Single SMs, which load all of W's operand through two 32 KB stages: 317, 299, 400. Eight
+// adding warps with pieces of 64 columns: 318, 315, 340; 128-column tiles: 416 at 171; four pieces a warp
+// and a shorter operand ring: 315, 307, 399.
 constexpr int kDxBN = 256;
-constexpr int kDxEpiWarps = 8;
+constexpr int kDxEpiWarps = 16;
 constexpr int kDxThreads = 64 + 32 * kDxEpiWarps;
 constexpr int kDxSlots = 3;
-constexpr uint32_t kDxABlock = kRtBM * kRtBK * 2, kDxBStage = kDxBN * kRtBK * 2, kDxSlotBytes = 32 * 64 * 2;
+constexpr uint32_t kDxABlock = kRtBM * kRtBK * 2, kDxBStage = kDxBN / 2 * kRtBK * 2, kDxSlotBytes = 32 * 32 * 2;
 
 struct RouteDxParams {
   int T, d, NP;  // NP: experts rounded up to 16
@@ -1008,7 +1013,7 @@ struct RouteDxParams {
 
 int route_dx_stages(int nkb) {
   const int64_t rest = kRtMaxSmem - 2048 - int64_t(nkb) * kDxABlock - int64_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes;
-  return int(std::min<int64_t>(4, rest / kDxBStage));  // 2 with four k-blocks, 3 with one
+  return int(std::min<int64_t>(6, rest / kDxBStage));  // 4 with four k-blocks
 }
 size_t route_dx_smem(int nkb, int stages) {
   return 1024 + size_t(nkb) * kDxABlock + size_t(stages) * kDxBStage + size_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes +
@@ -1074,7 +1079,9 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   const uint32_t drain_bar = bar0 + 8u * (2 * S + 6);
   auto slot_bar = [&](int w, int s) { return bar0 + 8u * (2 * S + 8 + w * kDxSlots + s); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr uint32_t IDESC = tc::idesc_f16_f32(kRtBM, kDxBN);
+  constexpr uint32_t IDESC = tc::idesc_f16_f32(2 * kRtBM, kDxBN);
+  const uint32_t rank = tc::cluster_ctarank();
+  const bool leader = rank == 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
@@ -1083,7 +1090,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     }
     for (int a = 0; a < 2; ++a) {
       tc::mbar_init(tfull_bar(a), 1);
-      tc::mbar_init(tempty_bar(a), kDxEpiWarps);
+      tc::mbar_init(tempty_bar(a), 2 * kDxEpiWarps);  // of both CTAs
     }
     tc::mbar_init(afull_bar, 1);
     tc::mbar_init(aempty_bar, 1);
@@ -1094,15 +1101,17 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     misc[1] = 0;
   }
   if (warp == 1) {
-    tc::tmem_alloc(tc::smem_u32(misc), 2 * kDxBN);
-    tc::tmem_relinquish();
+    tc::tmem_alloc_pair(tc::smem_u32(misc), 2 * kDxBN);
+    tc::tmem_relinquish_pair();
   }
   tc::fence_before_sync();
   __syncthreads();
+  tc::cluster_sync();  // barriers of both CTAs initialized before any remote use
   tc::fence_after_sync();
   const uint32_t tmem_base = static_cast<uint32_t>(misc[0]);
   pdl_start();
-  const int tile0 = int(int64_t(p.tiles) * blockIdx.x / gridDim.x), tile1 = int(int64_t(p.tiles) * (blockIdx.x + 1) / gridDim.x);
+  const int pair = int(blockIdx.x / 2), pairs = int(gridDim.x / 2);
+  const int tile0 = int(int64_t(p.tiles) * pair / pairs), tile1 = int(int64_t(p.tiles) * (pair + 1) / pairs);
   auto fail = [&]() {
     dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
     *abort_flag = 1;
@@ -1110,6 +1119,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
 
   if (warp == 0) {
     if (lane == 0) {
+      const uint32_t full_leader = tc::mapa(full_bar(0), 0), afull_leader = tc::mapa(afull_bar, 0);
       uint32_t it = 0, blocks = 0;
       int m_now = -1;
       bool ok = true;
@@ -1117,25 +1127,28 @@ __global__ void __launch_bounds__(kDxThreads, 1)
         const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
         if (m != m_now) {
           if (blocks > 0 && !tc::mbar_wait(aempty_bar, (blocks - 1) & 1u, kRtWaitNs, abort_flag)) { fail(); break; }
-          tc::mbar_arrive_expect_tx(afull_bar, uint32_t(p.nkb) * kDxABlock);
-          for (int kb = 0; kb < p.nkb; ++kb) tc::tma_load_2d(sA + kb * kDxABlock, &tmZ, afull_bar, kb * kRtBK, m * kRtBM);
+          if (leader) tc::mbar_arrive_expect_tx(afull_bar, 2 * uint32_t(p.nkb) * kDxABlock);
+          for (int kb = 0; kb < p.nkb; ++kb)
+            tc::tma_load_2d_pair(sA + kb * kDxABlock, &tmZ, afull_leader, kb * kRtBK, (2 * m + int(rank)) * kRtBM);
           ++blocks;
           m_now = m;
         }
         for (int kb = 0; kb < p.nkb; ++kb, ++it) {
           const int s = it % S;
           if (!tc::mbar_wait(empty_bar(s), ((it / S) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
-          tc::mbar_arrive_expect_tx(full_bar(s), kDxBStage);
-          tc::tma_load_2d(sB + s * kDxBStage, &tmW, full_bar(s), kb * kRtBK, n * kDxBN);
+          if (leader) tc::mbar_arrive_expect_tx(full_bar(s), 2 * kDxBStage);
+          tc::tma_load_2d_pair(sB + s * kDxBStage, &tmW, full_leader + 8u * s, kb * kRtBK, n * kDxBN + int(rank) * (kDxBN / 2));
         }
       }
-      // every issued load lands before the CTA may exit
-      for (int s = 0; s < S; ++s)
-        if (it > uint32_t(s) && !tc::mbar_wait(full_bar(s), ((it - 1 - s) / S) & 1u, kRtWaitNs, &no_abort)) fail();
-      if (blocks > 0 && !tc::mbar_wait(afull_bar, (blocks - 1) & 1u, kRtWaitNs, &no_abort)) fail();
+      // every issued load lands before the CTAs may exit (the even CTA's barriers count both CTAs')
+      if (leader) {
+        for (int s = 0; s < S; ++s)
+          if (it > uint32_t(s) && !tc::mbar_wait(full_bar(s), ((it - 1 - s) / S) & 1u, kRtWaitNs, &no_abort)) fail();
+        if (blocks > 0 && !tc::mbar_wait(afull_bar, (blocks - 1) & 1u, kRtWaitNs, &no_abort)) fail();
+      }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (leader && lane == 0) {
       uint32_t it = 0, blocks = 0, tcount = 0;
       int m_now = -1;
       bool ok = true, issued = false;
@@ -1155,29 +1168,30 @@ __global__ void __launch_bounds__(kDxThreads, 1)
           const uint64_t ad = tc::smem_desc_sw128(sA + kb * kDxABlock, 16, 1024), bd = tc::smem_desc_sw128(sB + s * kDxBStage, 16, 1024);
           const int steps = min(4, (p.NP - kb * kRtBK) / 16);
           for (int kk = 0; kk < steps; ++kk)  // (a descriptor's address counts 16 bytes)
-            tc::mma_bf16(tmem_base + a * kDxBN, ad + uint64_t(2 * kk), bd + uint64_t(2 * kk), IDESC, (kb | kk) != 0);
-          tc::mma_commit(empty_bar(s));
+            tc::mma_bf16_pair(tmem_base + a * kDxBN, ad + uint64_t(2 * kk), bd + uint64_t(2 * kk), IDESC, (kb | kk) != 0);
+          tc::mma_commit_pair_mc(empty_bar(s), 0x3);
           issued = true;
         }
         if (!ok) break;
-        tc::mma_commit(tfull_bar(a));
-        if ((tile + 1) / p.n_tiles != m) tc::mma_commit(aempty_bar);  // the token block's last tile
+        tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
+        if ((tile + 1) / p.n_tiles != m) tc::mma_commit_pair_mc(aempty_bar, 0x3);  // the token block's last tile
       }
       if (issued) {
-        tc::mma_commit(drain_bar);
+        tc::mma_commit_pair(drain_bar);
         if (!tc::mbar_wait(drain_bar, 0, kRtWaitNs, &no_abort)) fail();
       }
     }
   } else {
-    const int w = warp - 2, q = warp & 3, half = w / 4;
+    const int w = warp - 2, q = warp & 3, part = w / 4;
+    const uint32_t tempty_leader = tc::mapa(tempty_bar(0), 0);
     const uint32_t slots = sSlots + uint32_t(w) * (kDxSlots * kDxSlotBytes);
-    // This warp's pieces: (tile, c), c = 0 or 1, column c * 64 of its half of the tile; those that lie
+    // This warp's pieces: (tile, c), c = 0 or 1, column c * 32 of its quarter of the tile; those that lie
     // wholly past dx are left out. Piece n is in slot n % 3.
     struct Piece {
       int tile, c;
     };
-    auto row_of = [&](const Piece &x) { return x.tile / p.n_tiles * kRtBM + q * 32; };
-    auto col_of = [&](const Piece &x) { return x.tile % p.n_tiles * kDxBN + half * 128 + x.c * 64; };
+    auto row_of = [&](const Piece &x) { return (x.tile / p.n_tiles * 2 + int(rank)) * kRtBM + q * 32; };
+    auto col_of = [&](const Piece &x) { return x.tile % p.n_tiles * kDxBN + part * 64 + x.c * 32; };
     auto inside = [&](const Piece &x) { return row_of(x) < p.T && col_of(x) < p.d; };
     auto next = [&](Piece &x) {  // the piece that follows (tile == tile1: none)
       do {
@@ -1208,16 +1222,14 @@ __global__ void __launch_bounds__(kDxThreads, 1)
       ok = __all_sync(0xffffffffu, tc::mbar_wait(tfull_bar(a), (tcount >> 1) & 1u, kRtWaitNs, abort_flag));
       if (!ok) { fail(); break; }
       tc::fence_after_sync();
-      const int row = tile / p.n_tiles * kRtBM + q * 32 + lane;
+      const int row = (tile / p.n_tiles * 2 + int(rank)) * kRtBM + q * 32 + lane;
       const float rs = row < p.T ? p.row_scale[row] : 0.f;
       for (int c = 0; c < 2; ++c) {
         const Piece x{tile, c};
         if (!inside(x)) continue;
         const uint32_t s = done % kDxSlots, slot = slots + s * kDxSlotBytes;
-        uint32_t r[64];
-        const uint32_t tb = tmem_base + (uint32_t(q * 32) << 16) + a * kDxBN + half * 128 + c * 64;
-        tc::tmem_ld_32x32b_x32(tb, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
-        tc::tmem_ld_32x32b_x32(tb + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
+        uint32_t r[32];
+        tc::tmem_ld_32x32b_x32(tmem_base + (uint32_t(q * 32) << 16) + a * kDxBN + part * 64 + c * 32, r);
         tc::tmem_ld_wait();
         if (p.has_in) {
           ok = __all_sync(0xffffffffu, tc::mbar_wait(slot_bar(w, s), (done / kDxSlots) & 1u, kRtWaitNs, abort_flag));
@@ -1227,10 +1239,10 @@ __global__ void __launch_bounds__(kDxThreads, 1)
           __syncwarp();
         }
         const float *cs = p.col_scale + col_of(x);
-        const uint32_t mine = slot + uint32_t(lane) * 128u;
+        const uint32_t mine = slot + uint32_t(lane) * 64u, sw = (uint32_t(lane) >> 1) & 3u;
 #pragma unroll
-        for (uint32_t v = 0; v < 8; ++v) {
-          const uint32_t at = mine + ((v ^ (uint32_t(lane) & 7u)) << 4);  // the 128-byte swizzle
+        for (uint32_t v = 0; v < 4; ++v) {
+          const uint32_t at = mine + ((v ^ sw) << 4);  // the 64-byte swizzle
           float f[8];
           if (p.has_in) {
             unpack8(tc::ld_shared_v4(at), f);
@@ -1258,7 +1270,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
       }
       tc::fence_before_sync();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(tempty_bar(a));
+      if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * a);
     }
     if (lane == 0) {
       for (uint32_t n = done; n < loads; ++n)  // (after an abort: loads nothing read)
@@ -1269,9 +1281,10 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   }
   tc::fence_before_sync();
   __syncthreads();
+  tc::cluster_sync();  // no CTA leaves while its peer may still signal it
   if (warp == 1) {
     tc::fence_after_sync();
-    tc::tmem_dealloc(tmem_base, 2 * kDxBN);
+    tc::tmem_dealloc_pair(tmem_base, 2 * kDxBN);
   }
 }
 
@@ -1294,7 +1307,7 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
   p.NP = NP;
   p.nkb = (NP + kRtBK - 1) / kRtBK;
   p.n_tiles = (d + kDxBN - 1) / kDxBN;
-  p.tiles = (T + kRtBM - 1) / kRtBM * p.n_tiles;
+  p.tiles = (T + 2 * kRtBM - 1) / (2 * kRtBM) * p.n_tiles;
   p.stages = route_dx_stages(p.nkb);
   p.has_in = dx_in != nullptr;
   p.row_scale = row_scale;
@@ -1302,18 +1315,40 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
   CUtensorMap mz, mw, mi, mo;
   int st;
   if ((st = moe::make_map(&mz, z16, uint64_t(T), uint64_t(NP), kRtBK, kRtBM, "router dx dz"))) return st;
-  if ((st = moe::make_map(&mw, w16, uint64_t(d), uint64_t(NP), kRtBK, kDxBN, "router dx w"))) return st;
-  if ((st = moe::make_map(&mo, dx, uint64_t(T), uint64_t(d), 64, 32, "router dx"))) return st;
+  if ((st = moe::make_map(&mw, w16, uint64_t(d), uint64_t(NP), kRtBK, kDxBN / 2, "router dx w"))) return st;
+  if ((st = moe::make_map(&mo, dx, uint64_t(T), uint64_t(d), 32, 32, "router dx", CU_TENSOR_MAP_SWIZZLE_64B))) return st;
   mi = mo;
-  if (dx_in != nullptr && (st = moe::make_map(&mi, dx_in, uint64_t(T), uint64_t(d), 64, 32, "router dx_in"))) return st;
-  static bool attr_set = false;
-  if (!attr_set) {
+  if (dx_in != nullptr &&
+      (st = moe::make_map(&mi, dx_in, uint64_t(T), uint64_t(d), 32, 32, "router dx_in", CU_TENSOR_MAP_SWIZZLE_64B)))
+    return st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see moe::launch_dep
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kDxThreads);
+  cfg.stream = s;
+  cfg.attrs = at;
+  static int pairs = 0;  // that fit at once (one CTA per SM, whatever the sizes)
+  if (!pairs) {
     cudaError_t e = cudaFuncSetAttribute(route_dx_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
-    attr_set = true;
+    cfg.gridDim = dim3(2 * (moe::num_sms() / 2));
+    cfg.dynamicSmemBytes = kRtMaxSmem;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, route_dx_kernel, &cfg);
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    if (n <= 0) return moe::set_error(MOE_ERR_CUDA, "%s: no co-resident CTA pair fits", what);
+    pairs = n;
   }
-  const int grid = std::min(p.tiles, moe::num_sms());
-  MOE_LAUNCH("route_dx", s, moe::launch_dep(route_dx_kernel, grid, kDxThreads, route_dx_smem(p.nkb, p.stages), s, mz, mw, mi, mo, p));
+  cfg.gridDim = dim3(2 * std::min(p.tiles, pairs));
+  cfg.dynamicSmemBytes = route_dx_smem(p.nkb, p.stages);
+  cfg.numAttrs = 2;
+  MOE_LAUNCH("route_dx", s, cudaLaunchKernelEx(&cfg, route_dx_kernel, mz, mw, mi, mo, p));
   return moe::launch_status(what);
 }
 

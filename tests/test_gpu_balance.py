@@ -102,6 +102,9 @@ CASES = [
     (515, 171, 8, 7, 30, 0.1), (90, 192, 7, 2, 0, 0.0), (64, 193, 8, 0, 0, 0.0), (1000, 256, 8, 33, 85, 0.1),
     # a chunk per 8 tokens up to 4864, then longer ones; more sequences than tokens
     (4864, 64, 8, 3, 0, 0.0), (4865, 24, 4, 11, 3, 0.05), (20001, 96, 6, 40, 0, 0.0), (50, 12, 3, 200, 0, 0.2),
+    # one block: at most three sequences and four rounds of tokens, and just more than that
+    (200, 64, 6, 3, 3, 0.1), (200, 64, 6, 4, 0, 0.1), (384, 60, 4, 0, 0, 0.0), (385, 60, 4, 0, 0, 0.0),
+    (192, 250, 8, 2, 9, 0.0), (193, 250, 8, 2, 9, 0.0),
     # every token masked
     (40, 20, 2, 3, 0, 1.0)]
 
