@@ -103,7 +103,7 @@ int64_t moe_perm_rows_max(int T, int k, int E);
  * moe_grouped_ffn_* entry points need a ws of at least 256 bytes (16-byte
  * aligned), and two weight-gradient calls whose kernels may overlap on the GPU
  * need separate workspaces. The other calls use disjoint regions after them, so the router
- * backward and the unpermute-sum may share one workspace with GEMM calls running
+ * backward (moe_route_bwd, moe_route_bwd_dense, moe_route_dx) and the unpermute-sum may share one workspace with GEMM calls running
  * beside them on another stream. */
 size_t moe_workspace_size(int T, int d, int E, int k, int F);
 
@@ -171,7 +171,7 @@ int moe_load_stats(const int32_t *topk_idx, int T, int k, int E, int32_t *counts
  * moe_balance_workspace_size bytes, 16-byte aligned, used until the call's kernels end. Sums over tokens run in a
  * fixed order: bitwise reproducible. An id outside [0, E) of a valid token is left out and sets
  * MOE_DEV_BAD_EXPERT. A NaN logit of a live expert makes its sequence's results NaN.
- * Limits: 1 <= E <= 256, 1 <= k <= min(E, 8), 1 <= n_seq <= 2^20, T >= 0.
+ * Limits: 1 <= E <= 256, 1 <= k <= min(E, 8), 1 <= n_seq <= 2^20, 0 <= T <= 2^30.
  */
 int moe_balance_loss(const float *logits, const int32_t *topk_idx, const uint8_t *active_mask,
                      const uint8_t *token_mask, const int32_t *seq_offsets, int n_seq, int T, int E,
@@ -611,8 +611,11 @@ int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_
  *   d_logits as in moe_route_bwd;  dZ = dz + d_logits at the selected experts
  *   dw_router = x^T dZ
  * dz [T,E] fp32, not scaled or masked here: zero where a logit has no gradient. topk_idx,
- * topk_gate, d_gate and d_logits may be NULL together (dZ = dz). Other arguments, arithmetic and
- * limits as in moe_route_bwd. dz's share of the layer input's gradient comes from moe_route_dx.
+ * topk_gate, d_gate and d_logits may be NULL together (dZ = dz). An id outside [0, E) is left out of dZ; one
+ * that a token has twice counts twice. dZ is carried as in moe_route_bwd, and the sums over the tokens are
+ * added up in fp32, rounding to nearest, every 256 tokens (the tensor cores truncate): dw_router
+ * is ~1e-6 off in the 2-norm whatever T is. Bitwise reproducible. Other arguments, ws and limits as in moe_route_bwd.
+ * dz's share of the layer input's gradient comes from moe_route_dx.
  */
 int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,
                         const float *d_gate, const float *dz, int T, int d, int E, int k,
@@ -623,7 +626,9 @@ int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float 
  * moe_route_dx - a dense logit gradient's share of the layer input's gradient:
  *   dx[t,:] = dx_in[t,:] + sum_e dz[t,e] * w_router[:,e]   (one bf16 rounding)
  * dz [T,E] fp32; w_router [d,E] fp32; dx_in [T,d] bf16 or NULL (zeros), may be dx itself; dx [T,d]
- * bf16 (out); both 16-byte aligned. k: the layer's (for the workspace's layout). Limits:
+ * bf16 (out); both 16-byte aligned. The product's factors are rounded to 11 significant bits (half precision, a
+ * power of two taken out of each row of dz and of w_router), its sums are fp32. An infinity or NaN in
+ * a row of dz or w_router stays in that row or column of dx. k: the layer's (for the workspace's layout). Limits:
  * 1 <= E <= 256, 1 <= k <= 8, d % 8 == 0, T >= 0; ws as in moe_route_bwd.
  */
 int moe_route_dx(const float *dz, const float *w_router, const uint16_t *dx_in, int T, int d, int E,

@@ -43,6 +43,11 @@ int num_sms() {
   return cached[dev];
 }
 
+int device_slot() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64 ? dev : 63;
+}
+
 // ---- kernel timing registry ----
 namespace {
 struct TimingRec {
@@ -118,14 +123,16 @@ WsLayout ws_layout(int T, int d, int E, int k, int F) {
   off += align256(size_t(moe_perm_rows_max(T, k, E)) * 8);
   w.row_dz = off;
   off += align256(size_t(moe_perm_rows_max(T, k, E)) * 4);
+  // (from here on the offsets depend on F, which the router's entry points do not know: what they use
+  // beside GEMM calls on another stream stands before)
+  w.route_dx = off;
+  off += align256(route_dx_bytes(T, d, E));
   w.gate_partial = off;
   off += align256(size_t(moe_perm_rows_max(T, k, E)) * size_t(std::max(F, 0) / 64) * 4);
   w.route_partial = off;
   off += align256(route_partial_bytes(T, d, E));
   w.route_w3 = off;
   off += align256(route_w3_bytes(d, E));
-  w.route_dx = off;
-  off += align256(route_dx_bytes(T, d, E));
   w.total = off;
   return w;
 }

@@ -34,6 +34,7 @@ namespace {
 // T=65536, 256 experts; 23.3 / 21.9 at 16384, 64; 15.9 / 14.5 at 37, 64).
 constexpr int kMaxWarps = 24;  // of a block: 80 registers a thread, one block per SM
 constexpr int kMaxSeqs = 1 << 20;
+constexpr int kMaxTokens = 1 << 30;  // (a chunk's last token plus a round of tokens stays an int)
 
 // Tokens per chunk: one block for each of a GB300's 152 SMs, and few rows of partial sums for
 // the second kernel; at least eight, the tokens of one warp or two.
@@ -652,7 +653,7 @@ bool whole_vectors(int E, const void *a, const void *b) { return E % 4 == 0 && m
 int check_sizes(const char *fn, int T, int E, int k, int n_seq, const void *seq_offsets, float coef, float z_coef) {
   if (E < 1 || E > 256) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: E=%d not in [1,256]", fn, E);
   if (k < 1 || k > 8 || k > E) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: k=%d", fn, k);
-  if (T < 0 || n_seq < 1 || n_seq > kMaxSeqs)
+  if (T < 0 || T > kMaxTokens || n_seq < 1 || n_seq > kMaxSeqs)
     return moe::set_error(MOE_ERR_ARG, "%s: T=%d n_seq=%d", fn, T, n_seq);
   if (n_seq > 1 && !seq_offsets) return moe::set_error(MOE_ERR_ARG, "%s: n_seq=%d without seq_offsets", fn, n_seq);
   if (!isfinite(coef) || !isfinite(z_coef)) return moe::set_error(MOE_ERR_ARG, "%s: coefficients", fn);

@@ -25,6 +25,8 @@ int launch_status(const char *what);
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int num_sms();
+// The calling thread's current device, as an index below 64 into what is kept per device (others share one).
+int device_slot();
 
 // The first bytes of every workspace belong to the grouped GEMMs' tile scheduler
 // (their entry points know neither T nor k, so the region has a fixed offset and size).
@@ -39,9 +41,9 @@ struct WsLayout {
   size_t w_router_t;    // fp32  [E, d]            moe_permute_bwd transposed router
   size_t combine_rows;  // int32 + fp32 [rows_cap] moe_grouped_ffn_fwd_combine token and gate of each row
   size_t row_dz;        // fp32  [rows_cap]        moe_grouped_ffn_bwd_dgrad router logit gradient per grouped row
+  size_t route_dx;      // fp16, fp32              moe_route_dx's factors in half precision and their scales
   size_t gate_partial;  // fp32  [rows_cap, F/64]  moe_grouped_ffn_bwd_dgrad per-row dH * H sums (gate gradient)
   size_t route_partial; // fp32  [splits, T, NE]   moe_route split-reduction partial logits
-  size_t route_dx;      // fp16, fp32              moe_route_dx's factors in half precision and their scales
   size_t route_w3;      // bf16  [3, NP, d]        moe_route router weight as three bf16 terms
   size_t total;
 };

@@ -1332,7 +1332,8 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
   cfg.blockDim = dim3(kDxThreads);
   cfg.stream = s;
   cfg.attrs = at;
-  static int pairs = 0;  // that fit at once (one CTA per SM, whatever the sizes)
+  static int fit[64] = {};  // pairs at once on each device (one CTA per SM, whatever the sizes)
+  int &pairs = fit[moe::device_slot()];
   if (!pairs) {
     cudaError_t e = cudaFuncSetAttribute(route_dx_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
@@ -1568,11 +1569,12 @@ int launch_route_dw_pair(const uint16_t *x, const uint16_t *dz3, int T, int d, i
   if ((st = moe::make_map(&mx, x, uint64_t(T), uint64_t(d), 64, kRtBK, "router bwd x"))) return st;
   if ((st = moe::make_map(&mz, dz3, uint64_t(3 * NP), uint64_t(Tp), kRtBK, uint32_t(p.G * NP / 2), "router bwd dz")))
     return st;
-  static bool attr_set = false;
-  if (!attr_set) {
+  static bool attr_set[64] = {};
+  bool &set = attr_set[moe::device_slot()];
+  if (!set) {
     cudaError_t e = cudaFuncSetAttribute(route_dw_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
-    attr_set = true;
+    set = true;
   }
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;

@@ -170,6 +170,17 @@ def _kept(b: MoELayerBuffers, ckpt: Optional[MoECheckpoint]):
     return b if ckpt is None else ckpt
 
 
+def _check_balance(b, kept, balance: BalanceLoss):
+    if not 1 <= balance.n_seq <= min(kept.balance_seqs, b.balance_seqs):
+        raise ValueError(f"balance over {balance.n_seq} sequences: more than the buffers' balance_seqs")
+    off, tok = balance.seq_offsets, balance.token_mask
+    if off is not None and (off.dtype != torch.int32 or not off.is_contiguous()):
+        raise ValueError("seq_offsets: a contiguous int32 tensor")
+    if tok is not None and (tok.dtype not in (torch.uint8, torch.bool) or not tok.is_contiguous()
+                            or tok.numel() != b.shape.T):
+        raise ValueError("token_mask: a contiguous uint8 or bool tensor of T values")
+
+
 def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mask=None,
             logits_in=None, keep_logits: bool = False, stream=None,
             balance: Optional[BalanceLoss] = None, ckpt: Optional[MoECheckpoint] = None):
@@ -183,8 +194,8 @@ def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mas
     s = b.shape
     R = s.rows_cap
     kept = _kept(b, ckpt)
-    if balance is not None and not 1 <= balance.n_seq <= min(kept.balance_seqs, b.balance_seqs):
-        raise ValueError(f"balance over {balance.n_seq} sequences: more than the buffers' balance_seqs")
+    if balance is not None:
+        _check_balance(b, kept, balance)
     stream = L.stream_handle(stream)  # once for all calls
     logits = kept.logits if balance is not None else b.logits if keep_logits else None
     _route(b, kept, logits, x, w_router, bias, active_mask, logits_in, stream)

@@ -86,7 +86,7 @@ def _bwd(**kw):
 @pytest.mark.parametrize("call", [_loss, _bwd])
 @pytest.mark.parametrize("bad,status", [
     ({"E": 0}, -2), ({"E": 257}, -2), ({"k": 0}, -2), ({"k": 9}, -2), ({"k": 8, "E": 7}, -2), ({"T": -1}, -1),
-    ({"n_seq": 0}, -1), ({"n_seq": -3}, -1), ({"n_seq": 2}, -1), ({"n_seq": (1 << 20) + 1, "seq_offsets": 16}, -1),
+    ({"T": (1 << 30) + 1}, -1), ({"n_seq": 0}, -1), ({"n_seq": -3}, -1), ({"n_seq": 2}, -1), ({"n_seq": (1 << 20) + 1, "seq_offsets": 16}, -1),
     ({"coef": float("nan")}, -1), ({"z_coef": float("inf")}, -1), ({"logits": None}, -1), ({"lse": None}, -1),
     ({"counts": None}, -1), ({"n_tokens": None}, -1)])
 def test_balance_refusals(call, bad, status):
@@ -112,7 +112,7 @@ def test_balance_backward_refuses_no_output():
 
 def test_balance_workspace_sizes():
     # per chunk or sequence a row of E fp32 sums and E counts
-    assert L.moe_balance_workspace_size(65536, 256, 1) >= 600 * 256 * 8
+    assert L.moe_balance_workspace_size(65536, 256, 1) >= 152 * 256 * 8
     assert L.moe_balance_workspace_size(0, 8, 1) > 0
     assert L.moe_balance_workspace_size(16, 8, 1000) >= 1000 * 8 * 8
     for bad in ((-1, 8, 1), (8, 0, 1), (8, 8, 0)):

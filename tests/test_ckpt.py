@@ -140,3 +140,8 @@ def test_layer_refuses_mixed_buffers():
                     (layer.MoELayerBuffers(s, "cpu", balance_seqs=3, ckpt=True), c)):
         with pytest.raises(ValueError):  # three sequences
             layer.forward(b, None, None, None, None, None, balance=layer.BalanceLoss(0.1, seq_offsets=off), ckpt=ckpt)
+    b = layer.MoELayerBuffers(s, "cpu", balance_seqs=3)
+    for bad in ({"seq_offsets": off.long()}, {"seq_offsets": torch.zeros(8, dtype=torch.int32)[::2]},
+                {"seq_offsets": off[:1]}, {"token_mask": torch.ones(8)}, {"token_mask": torch.ones(7, dtype=torch.uint8)}):
+        with pytest.raises(ValueError):
+            layer.forward(b, None, None, None, None, None, balance=layer.BalanceLoss(0.1, **bad))

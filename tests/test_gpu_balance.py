@@ -167,6 +167,24 @@ def test_balance_nan_reaches_its_sequence_only():
     assert np.isfinite(np.delete(got["lse"], 40)).all()
 
 
+@pytest.mark.parametrize("T,E", [(40, 64), (9000, 64), (700, 256)])
+def test_balance_unaligned_rows_and_late_first_sequence(T, E):
+    """Rows of whole 16-byte vectors that start off a 16-byte boundary; rows before the first sequence."""
+    k = 4
+    z, idx, mask, tok, _ = _inputs(T, E, k, 0, masked=3, padded=0.1)
+    off = np.array([T // 8, T // 8, T // 2, T - 3], np.int32)
+    ref = O.balance_loss(z, idx, mask, tok, off, 0.02, 0.003)
+    ref["off"] = off
+    b = Balance(T, E, k, 3)
+    args = [_dev(idx), _dev(mask), _dev(tok), _dev(off), 0.02, 0.003]
+    aligned = b(_dev(z), *args)
+    _check(aligned, ref, 0.02, 0.003, (1, 1), k)
+    shifted = torch.empty(T * E + 1, device="cuda")[1:].view(T, E)
+    shifted.copy_(_dev(z))
+    b.dz = torch.full((T * E + 3,), float("nan"), device="cuda")[3:].view(T, E)
+    _check(b(shifted, *args), ref, 0.02, 0.003, (1, 1), k)
+
+
 def test_balance_flags_bad_ids_and_offsets():
     T, E, k = 50, 6, 2
     z, idx, _, _, _ = _inputs(T, E, k, 0)
@@ -285,6 +303,70 @@ def test_dense_router_backward_over_many_tokens(T, d, E):
     ref = x.double().T @ dz.double()
     assert torch.equal(dw, again)
     assert float((dw.double() - ref).norm() / ref.norm()) < 2.9e-6
+
+
+def test_dense_router_backward_ids_twice_and_outside():
+    T, d, E, k = 100, 64, 10, 3
+    x, w, idx, gate, dg, dz, _ = _router_inputs(T, d, E, k, 9)
+    idx[:, 1] = idx[:, 0]
+    idx[::5, 2] = E
+    idx[1::5, 2] = -1
+    n = L.moe_workspace_size(T, d, E, k, 128)
+    dl, dw = torch.empty(T, k, device="cuda"), torch.empty(d, E, device="cuda")
+    L.moe_route_bwd_dense(x.cuda(), idx.cuda(), gate.cuda(), dg.cuda(), dz.cuda(), T, d, E, k, dl, dw,
+                          torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    g64, dg64 = gate.double().numpy(), dg.double().numpy()
+    dl_ref = g64 * (dg64 - (g64 * dg64).sum(1, keepdims=True))
+    zz = dz.double().numpy().copy()
+    for j in range(k):
+        t = np.flatnonzero((idx[:, j].numpy() >= 0) & (idx[:, j].numpy() < E))
+        np.add.at(zz, (t, idx[t, j].numpy()), dl_ref[t, j])
+    assert np.abs(dl.cpu().numpy() - dl_ref).max() < 1e-5
+    size = np.abs(x.double().numpy()).T @ (np.abs(dz.double().numpy()) + 3 * np.abs(dl_ref).max())
+    assert (np.abs(dw.cpu().double().numpy() - x.double().numpy().T @ zz) <= 1e-5 * size).all()
+
+
+def test_router_dx_beside_the_experts_backward():
+    """moe_route_dx on a second stream beside moe_grouped_ffn_bwd_dgrad with one workspace: both as alone."""
+    T, d, E, k, F = 4000, 512, 16, 4, 1024
+    g = torch.Generator(device="cuda").manual_seed(1)
+    R = L.moe_perm_rows_max(T, k, E)
+
+    def rnd(*n, dtype=torch.bfloat16, s=1.0):
+        return (s * torch.randn(*n, generator=g, device="cuda")).to(dtype)
+
+    idx = torch.argsort(rnd(T, E, dtype=F32), dim=1)[:, :k].to(I32).contiguous()
+    gate, n = torch.full((T, k), 1 / k, device="cuda"), L.moe_workspace_size(T, d, E, k, F)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    off, cnt = torch.empty(E + 1, dtype=I32, device="cuda"), torch.empty(E, dtype=I32, device="cuda")
+    row, xp = torch.empty(T, k, dtype=I32, device="cuda"), torch.zeros(R, d, dtype=torch.bfloat16, device="cuda")
+    L.moe_permute(rnd(T, d), idx, None, T, d, E, k, R, off, cnt, row, xp, ws, n)
+    ab, wu, wd = rnd(R, 2 * F), rnd(E, 2 * F, d, s=0.02), rnd(E, d, F, s=0.02)
+    dz, w, dx_in = rnd(T, E, dtype=F32), rnd(d, E, dtype=F32), rnd(T, d)
+    dab, dx = torch.empty(R, 2 * F, dtype=torch.bfloat16, device="cuda"), torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+    dxp, dg = torch.zeros(R, d, dtype=torch.bfloat16, device="cuda"), torch.empty(T, k, device="cuda")
+    side = torch.cuda.Stream()
+
+    def dgrad():
+        L.moe_grouped_ffn_bwd_dgrad(xp, ab, off, E, d, F, R, wu, wd, gate, None, row, None, T, k, dg, dab, dxp, ws, n)
+
+    def route(stream=None):
+        L.moe_route_dx(dz, w, dx_in, T, d, E, k, dx, ws, n, stream)
+
+    dgrad()
+    route()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (dx, dg, dxp)]
+    for _ in range(20):
+        for t in (dx, dg, dxp):
+            t.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            dgrad()
+            route(side)
+        torch.cuda.synchronize()
+        for a, b in zip((dx, dg, dxp), want):
+            assert torch.equal(a, b)
 
 
 def test_dense_router_backward_without_tokens():
