@@ -190,7 +190,22 @@ __device__ __forceinline__ int count_live(const uint8_t *active_mask, int E, int
 // where the loads take 10): a row is masked only where some expert is (or E leaves lanes over), and what a
 // token that does not count holds is computed with and not added.
 // The argument's product with log2 e is fused with the subtraction of the largest logit's; that one's
-// rounding is common to the row, so it cancels in p and adds |m| 2^-24 to the log-sum-exp.
+// rounding is common to the row, so it cancels in p and adds |m| 2^-24 to the log-sum-exp. (Not where the largest
+// is so large that this would be no small part of an exponent, a row of the type's lowest value, say: see
+// exponents.)
+template <int NI> __device__ __forceinline__ void exponents(float (&z)[NI], float m) {  // 2^((z - m) log2 e)
+  const bool far = __any_sync(0xffffffffu, fabsf(m) > 65536.f);
+  const float c = -m * kLog2e;
+  if (far) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) z[i] = (z[i] - m) * kLog2e;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) z[i] = fmaf(z[i], kLog2e, c);
+  }
+#pragma unroll
+  for (int i = 0; i < NI; ++i) z[i] = exp2_quick(z[i]);
+}
 template <int LPT, int NI, bool VEC> struct TokenSums {
   static constexpr int TPW = 32 / LPT;               // tokens per warp
   static constexpr int IDS = LPT >= 8 ? 1 : 8 / LPT;  // experts of a token per lane
@@ -240,12 +255,9 @@ template <int LPT, int NI, bool VEC> struct TokenSums {
 #pragma unroll
       for (int i = 0; i < NI; ++i) m[i % 4] = i < 4 ? z[i] : max_nan(m[i % 4], z[i]);
       m[0] = group_max<LPT>(max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])));
-      const float c = -m[0] * kLog2e;
+      exponents(z, m[0]);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        z[i] = exp2_quick(fmaf(z[i], kLog2e, c));
-        den[i % 4] += z[i];
-      }
+      for (int i = 0; i < NI; ++i) den[i % 4] += z[i];
       den[0] = group_sum<LPT>((den[0] + den[1]) + (den[2] + den[3]));
       if (valid && !(m[0] == -INFINITY)) {
         const float r = __fdividef(1.f, den[0]), lse = m[0] + logf(den[0]);
@@ -411,7 +423,7 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_one_block_kernel(co
   for (int t = cur + tid; t < p.T; t += threads) p.lse[t] = -INFINITY;  // behind the last sequence
   if (tid == 0) {
     p.loss[0] = seqs > 0 ? p.coef * (part / float(seqs)) : 0.f;
-    p.loss[1] = all > 0 ? p.z_coef * (zsum / float(all)) : 0.f;
+    p.loss[1] = all > 0 && p.z_coef != 0.f ? p.z_coef * (zsum / float(all)) : 0.f;
     p.n_tokens[p.n_seq] = all;
     p.n_tokens[p.n_seq + 1] = seqs;
   }
@@ -517,7 +529,7 @@ __global__ void __launch_bounds__(1024) balance_reduce_kernel(const BalanceParam
     seqs = __reduce_add_sync(0xffffffffu, lane < warps ? s_m[lane] : 0);
     if (lane == 0) {
       p.loss[0] = seqs > 0 ? p.coef * (d / float(seqs)) : 0.f;
-      p.loss[1] = m > 0 ? p.z_coef * (z / float(m)) : 0.f;
+      p.loss[1] = m > 0 && p.z_coef != 0.f ? p.z_coef * (z / float(m)) : 0.f;
       p.n_tokens[p.n_seq] = m;
       p.n_tokens[p.n_seq + 1] = seqs;
     }
@@ -597,10 +609,9 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_bwd_kernel(
 #pragma unroll
         for (int i = 0; i < NI; ++i) z[i] = live >> i & 1 ? z[i] : -INFINITY;
       }
-      const float c = -ln * kLog2e;
+      exponents(z, ln);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        z[i] = exp2_quick(fmaf(z[i], kLog2e, c));
         s0[i % 2] += z[i];
         s1[i % 2] = fmaf(z[i], f[i], s1[i % 2]);
       }

@@ -156,6 +156,38 @@ def test_balance_large_logits_and_masked_rubbish():
     _check(got, ref, coef, z_coef, d, k)
 
 
+@pytest.mark.parametrize("T", [60, 3000])
+def test_balance_rows_of_the_lowest_value(T):
+    """Masks as the type's lowest value: such a logit has no probability beside an ordinary one; a row of nothing
+    else is a row of equal logits. Also very large ones."""
+    E, k = 20, 3
+    z, idx, _, _, _ = _inputs(T, E, k, 0)
+    low = np.finfo(np.float32).min
+    z[:, 4] = low
+    z[1::7] = low
+    z[2::7, 3] = -low
+    z[3::7] += 3e9
+    z[4::7, 5:] *= 1e5
+    idx = np.argsort(-z, axis=1, kind="stable")[:, :k].astype(np.int32)
+    off = np.array([0, T // 2, T], np.int32)
+    ref = O.balance_loss(z, idx, None, None, off, 0.5, 0.0)
+    ref["off"] = off
+    got = Balance(T, E, k, 2)(_dev(z), _dev(idx), None, None, _dev(off), 0.5, 0.0)
+    assert got["loss"][1] == 0 and (ref["p"][1] == 1 / E).all()
+    # a log-sum-exp this large has no room for the sum of exponentials: the log-sum-exp itself, and
+    # then p (from it) only where it is exact, near logits of ordinary size, or from the sums of p
+    # (2e-6 + 2^-23 |lse| as in _check: where m + log(sum) cancels, the roundings of m, up to 8 here, and of the
+    # logarithm stay, 8 * 2^-24 + 2^-22)
+    np.testing.assert_allclose(got["lse"], ref["lse"], rtol=2 ** -23, atol=2e-6)
+    np.testing.assert_allclose(got["prob"], ref["prob"], rtol=1.2e-5, atol=1e-36)
+    np.testing.assert_allclose(got["loss"], ref["loss"], rtol=1.2e-5)
+    assert np.isfinite(got["dz"]).all()
+    few = np.abs(ref["lse"]) < 100
+    assert (np.abs(got["dz"] - ref["dz"])[few] <= 2e-5 * np.abs(ref["dz"][few]).max()).all()
+    # rows of equal logits: p is divided by its sum, so their rounding does not matter
+    np.testing.assert_allclose(got["dz"][1::7], ref["dz"][1::7], rtol=2e-5, atol=2e-5 * np.abs(ref["dz"]).max())
+
+
 def test_balance_nan_reaches_its_sequence_only():
     T, E, k = 64, 8, 2
     z, idx, _, _, _ = _inputs(T, E, k, 0)
