@@ -467,3 +467,40 @@ def test_route_dx_infinities_stay_in_their_row():
     keep = [t for t in range(T) if t not in (3, 100)]
     assert torch.equal(got[keep], clean[keep])
     assert torch.isnan(got[3]).all() and not torch.isfinite(got[100]).any()
+
+
+def test_balance_and_router_past_32_bits():
+    """More than 2^31 logits; the last rows against 64 bits."""
+    T, E, k, d = 8_500_000, 256, 1, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn(T, E, generator=g, device="cuda")
+    idx = z.argmax(1, keepdim=True).to(I32)
+    b = Balance(T, E, k, 0)
+    L.moe_balance_loss(z, idx, None, None, None, 1, T, E, k, 1.0, 0.5, b.loss, b.counts, b.prob, b.n_tokens, b.lse, b.ws,
+                       b.ws.numel())
+    L.moe_balance_loss_bwd(z, None, None, 1, T, E, k, 1.0, 0.5, b.counts, b.n_tokens, b.lse, None, b.dz)
+    assert T * E > 2 ** 31 and int(b.counts.sum()) == T
+    zt = z[-500:].double()
+    lse = torch.logsumexp(zt, 1)
+    assert ((b.lse[-500:].double() - lse).abs() <= 2e-6 + 2 ** -23 * lse.abs()).all()
+    p, f = torch.exp(zt - lse[:, None]), b.counts[0].double() * E / T - 1
+    dz = p * ((f - (p * f).sum(1, keepdim=True)) / T + lse[:, None] / T)
+    size = p * ((f.abs() + (p * f.abs()).sum(1, keepdim=True)) / T + lse[:, None].abs() / T)
+    assert ((b.dz[-500:].double() - dz).abs() <= 2e-5 * size).all()
+    del z
+    n = L.moe_workspace_size(T, d, E, k, 128)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    w = torch.randn(d, E, generator=g, device="cuda")
+    b.dz *= T
+    out = torch.full((T, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    L.moe_route_dx(b.dz, w, None, T, d, E, k, out, ws, n)
+    ref, size = b.dz[-500:].double() @ w.double().T, b.dz[-500:].double().abs() @ w.double().abs().T
+    err = (out[-500:].double() - ref).abs().cpu().numpy()
+    assert (err <= _dx_bound(ref.cpu().numpy(), size.cpu().numpy())).all()
+    # x^T dZ over the last rows alone: the others' x is zero
+    x = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    x[-500:] = torch.randn(500, d, generator=g, device="cuda").to(torch.bfloat16)
+    dw = torch.empty(d, E, device="cuda")
+    L.moe_route_bwd_dense(x, None, None, None, b.dz, T, d, E, k, None, dw, ws, n)
+    xt, zt = x[-500:].double(), b.dz[-500:].double()
+    assert ((dw.double() - xt.T @ zt).abs() <= 1e-5 * (xt.abs().T @ zt.abs()) + 1e-30).all()

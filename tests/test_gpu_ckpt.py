@@ -424,3 +424,45 @@ def test_graph_of_a_checkpointed_step_replays():
         torch.cuda.synchronize()
         for got, ref in zip(list(out) + [c.loss], want[i]):
             assert torch.equal(got, ref)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 codes in rows and in the kept [A|B]: the last rows are as a small call has them."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rows, cols = 263000, 8200
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    tail = torch.randn(40, cols, generator=g, device="cuda").to(BF16)
+    x[-40:] = tail
+    q, s = torch.empty(rows, cols, dtype=U8, device="cuda"), torch.empty(rows, -(-cols // 32), dtype=U8, device="cuda")
+    L.moe_ckpt_pack(x, rows, cols, q, s)
+    q2, s2 = _pack(tail.cpu())
+    assert rows * cols > 2 ** 31 and torch.equal(q[-40:], q2) and torch.equal(s[-40:], s2)
+    x.fill_(7)
+    L.moe_ckpt_unpack(q, s, rows, cols, x)
+    assert _same(x[-40:].double().cpu().numpy(), O.ckpt_round(tail.double().cpu().numpy())[0])
+    assert (x[:-40:997] == 0).all()
+    del x, q, s
+    # the experts: one group of 263,040 rows, the last 128 of which hold values; 8,192 columns of [A|B]
+    d, E, F, R = 128, 1, 4096, 263040
+    xp = torch.zeros(R, d, dtype=BF16, device="cuda")
+    xp[-128:] = torch.randn(128, d, generator=g, device="cuda").to(BF16)
+    wu = (0.1 * torch.randn(E, 2 * F, d, generator=g, device="cuda")).to(BF16)
+    wd = (0.1 * torch.randn(E, d, F, generator=g, device="cuda")).to(BF16)
+    ws = torch.empty(256, dtype=U8, device="cuda")
+
+    def run(xs):
+        n = xs.shape[0]
+        off = torch.tensor([0, n], dtype=I32, device="cuda")
+        q, s = torch.empty(n, 2 * F, dtype=U8, device="cuda"), torch.empty(n, 2 * F // 32, dtype=U8, device="cuda")
+        h, out = torch.empty(n, F, dtype=BF16, device="cuda"), torch.empty(n, d, dtype=BF16, device="cuda")
+        L.moe_grouped_ffn_fwd_ckpt(xs, off, E, d, F, n, wu, wd, q, s, h, out, ws, 256)
+        h8, dab, dx = torch.empty_like(h), torch.empty(n, 2 * F, dtype=BF16, device="cuda"), torch.empty_like(out)
+        L.moe_grouped_ffn_bwd_dgrad_ckpt(xs, q, s, off, E, d, F, n, wu, wd, None, None, None, None, 0, 1, None, h8, dab,
+                                         dx, ws, 256)
+        ab = torch.empty(n, 2 * F, dtype=BF16, device="cuda")
+        L.moe_ckpt_unpack_ab(q, s, off, E, F, n, ab, None)
+        return [t[-128:].clone() for t in (q, s, h, out, h8, dab, dx, ab)]
+
+    assert R * 2 * F > 2 ** 31
+    for a, b in zip(run(xp), run(xp[-128:].contiguous())):
+        assert torch.equal(a, b)
