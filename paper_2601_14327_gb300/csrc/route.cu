@@ -739,6 +739,8 @@ struct RouteDwParams {
   int stages;
   uint32_t buf_cols;     // TMEM columns of an accumulator
   float *partial;
+  float *dw;             // [M, E], written at once where there is one split (else nullptr)
+  int E;
 };
 uint32_t route_dwp_stage_bytes(int NP) { return kRtBM * kRtBK * 2 + 3u * uint32_t(NP / 2) * 128u; }
 int route_dwp_group(int NP) { return 3 * NP <= 256 ? 3 : 1; }
@@ -901,7 +903,21 @@ __global__ void __launch_bounds__(kDwThreads, 1)
       if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * a);
     }
     const int row = feature0 + q * 32 + lane;
-    if (ok && row < p.M) {
+    if (p.dw != nullptr) {
+      // The rows go out whole: through the operands' shared memory, which the last MMA has read (an odd
+      // stride: a lane owns a row). After an abort nothing is written.
+      const int stride = p.E | 1;
+      float *s_dw = reinterpret_cast<float *>(smem_raw + pad);
+      const int n = min(int(half_rows), p.E - half * int(half_rows));
+#pragma unroll
+      for (int c = 0; c < 128; ++c)
+        if (ok && c < n) s_dw[(q * 32 + lane) * stride + half * half_rows + c] = acc[c];
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      for (int r = warp - 2; r < kRtBM; r += 8) {
+        if (!ok || feature0 + r >= p.M) break;
+        for (int e = lane; e < p.E; e += 32) p.dw[size_t(feature0 + r) * p.E + e] = s_dw[r * stride + e];
+      }
+    } else if (ok && row < p.M) {
       float *dst = p.partial + (size_t(split) * p.M + row) * p.NE + half * half_rows;
 #pragma unroll
       for (int c = 0; c < 128; c += 4)
@@ -920,7 +936,12 @@ __global__ void __launch_bounds__(kDwThreads, 1)
 // Splits of the reduction over nkb k-blocks for d features: the least estimated time (ns), a pair's k-block
 // in its MMAs, its shared-memory traffic or its share of the HBM rate for x, whole rounds of the 76 pairs with ~3 us of
 // filling and draining each, and a split's partial sums written and read. A function of (d, nkb, NP) alone.
+// One k-block, or up to kDwFlush of more than 64 experts: one split, which writes the gradient itself; the launch that
+// adds the splits costs more than their k-blocks. moe_route_bwd_dense and moe_route_dx, splits / one: 17.2 / 15.6 us at
+// 5 tokens, d 424, 8 experts, 19.5 / 18.6 at 60, 7168, 64, 30.6 / 24.2 at 250, 7168, 171, 27.3 / 26.5 at 200, 2872, 225;
+// 18.4 / 19.2 at 256, 512, 64, 18.2 / 18.8 at 125, 4280, 8.
 int route_dwp_splits(int M, int nkb, int NP) {
+  if (nkb == 1 || (nkb <= kDwFlush && NP > 64)) return 1;
   const int64_t tiles = (M + 2 * kRtBM - 1) / (2 * kRtBM), pairs = kRtSms / 2;
   const int64_t a = kRtBM * kRtBK * 2, b = 3 * int64_t(NP / 2) * 128, reads = route_dwp_group(NP) == 3 ? 1 : 3;
   // (MMA: 3 terms x 4 steps of 256 x NP x 16 at a pair's 8,192 multiply-adds a clock, 1.9 GHz)
@@ -1549,7 +1570,7 @@ int launch_route_dw(const uint16_t *x, const uint16_t *dz3, int T, int d, int E,
 
 // As launch_route_dw, on CTA pairs (see route_dw_pair_kernel).
 int launch_route_dw_pair(const uint16_t *x, const uint16_t *dz3, int T, int d, int E, float *partial,
-                         int *splits_out, cudaStream_t s) {
+                         float *dw_router, int *splits_out, cudaStream_t s) {
   const int NP = route_tc_np(E), Tp = route_tokens_padded(T);
   const char *what = "moe_route_bwd_dense: weight gradient";
   RouteDwParams p{};
@@ -1564,6 +1585,8 @@ int launch_route_dw_pair(const uint16_t *x, const uint16_t *dz3, int T, int d, i
   const uint32_t cols = uint32_t(p.G * NP);
   p.buf_cols = cols <= 32 ? 32u : cols <= 64 ? 64u : cols <= 128 ? 128u : 256u;
   p.partial = partial;
+  p.dw = splits == 1 ? dw_router : nullptr;
+  p.E = E;
   CUtensorMap mx, mz;
   int st;
   if ((st = moe::make_map(&mx, x, uint64_t(T), uint64_t(d), 64, kRtBK, "router bwd x"))) return st;
@@ -1627,9 +1650,10 @@ static int route_bwd(const char *fn, const uint16_t *x, const int32_t *topk_idx,
                                       topk_idx, topk_gate, d_gate, T, Tp, k, NP, d_logits, dz3));
   if (int st = moe::launch_status("moe_route_bwd: dz")) return st;
   int splits = 0;
-  if (int st = dz ? launch_route_dw_pair(x, dz3, T, d, E, partial, &splits, s)
+  if (int st = dz ? launch_route_dw_pair(x, dz3, T, d, E, partial, dw_router, &splits, s)
                   : launch_route_dw(x, dz3, T, d, E, partial, &splits, s))
     return st;
+  if (dz && splits == 1) return MOE_OK;  // written at once
   const int n = d * (route_dw_stride(E) / 4);
   MOE_LAUNCH("route_bwd_reduce", s, moe::launch_dep(route_dw_reduce_kernel, std::min((n + 255) / 256, 4 * moe::num_sms()), 256, 0, s,
                                         partial, splits, d, E, route_dw_stride(E), dw_router));

@@ -504,3 +504,18 @@ def test_balance_and_router_past_32_bits():
     L.moe_route_bwd_dense(x, None, None, None, b.dz, T, d, E, k, None, dw, ws, n)
     xt, zt = x[-500:].double(), b.dz[-500:].double()
     assert ((dw.double() - xt.T @ zt).abs() <= 1e-5 * (xt.abs().T @ zt.abs()) + 1e-30).all()
+
+
+@pytest.mark.parametrize("T,d,E", [(64, 136, 256), (63, 264, 1), (65, 128, 65), (256, 384, 80), (250, 1032, 171), (256, 136, 240),
+                                   (257, 384, 100), (1, 8, 33)])
+def test_dense_router_backward_in_one_split(T, d, E):
+    """One k-block, and up to four of more than 64 experts, are written without partial sums; just more are not."""
+    g = torch.Generator().manual_seed(T * d + E)
+    x, dz = torch.randn(T, d, generator=g).to(torch.bfloat16), torch.randn(T, E, generator=g)
+    n = L.moe_workspace_size(T, d, E, 1, 128)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    dw = torch.full((d + 1, E), 7.0, device="cuda")
+    L.moe_route_bwd_dense(x.cuda(), None, None, None, dz.cuda(), T, d, E, 1, None, dw, ws, n)
+    xd, zd = x.double().numpy(), dz.double().numpy()
+    assert (np.abs(dw[:d].cpu().double().numpy() - xd.T @ zd) <= 1e-5 * (np.abs(xd).T @ np.abs(zd)) + 1e-30).all()
+    assert (dw[d] == 7).all()  # nothing behind the last row
