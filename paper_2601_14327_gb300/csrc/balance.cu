@@ -192,13 +192,13 @@ __device__ __forceinline__ int count_live(const uint8_t *active_mask, int E, int
 // The argument's product with log2 e is fused with the subtraction of the largest logit's; that one's
 // rounding is common to the row, so it cancels in p and adds |m| 2^-24 to the log-sum-exp. (Not where the largest
 // is so large that this would be no small part of an exponent, a row of the type's lowest value, say: see
-// exponents.)
+// exponents. Which of the two a token gets is its own row's matter, not its neighbours' in the warp.)
 template <int NI> __device__ __forceinline__ void exponents(float (&z)[NI], float m) {  // 2^((z - m) log2 e)
-  const bool far = __any_sync(0xffffffffu, fabsf(m) > 65536.f);
+  const bool far = fabsf(m) > 65536.f && m != -INFINITY;  // (-inf: no token, nothing of it is used)
   const float c = -m * kLog2e;
-  if (far) {
+  if (__any_sync(0xffffffffu, far)) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) z[i] = (z[i] - m) * kLog2e;
+    for (int i = 0; i < NI; ++i) z[i] = far ? (z[i] - m) * kLog2e : fmaf(z[i], kLog2e, c);
   } else {
 #pragma unroll
     for (int i = 0; i < NI; ++i) z[i] = fmaf(z[i], kLog2e, c);

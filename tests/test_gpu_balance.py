@@ -188,6 +188,31 @@ def test_balance_rows_of_the_lowest_value(T):
     np.testing.assert_allclose(got["dz"][1::7], ref["dz"][1::7], rtol=2e-5, atol=2e-5 * np.abs(ref["dz"]).max())
 
 
+@pytest.mark.parametrize("T,E", [(60, 64), (61, 13), (3001, 64), (3000, 250)])
+def test_balance_bits_do_not_depend_on_other_tokens(T, E):
+    """What masked tokens, tokens behind the last sequence and pruned experts hold, and which tokens share a warp with
+    one, changes no bit of the results."""
+    z, idx, mask, tok, off = _inputs(T, E, 2, 2, masked=3, padded=0.3)
+    d = torch.tensor((0.6, 1.7), device="cuda")
+    got = []
+    for fill in (0.0, 1e30, np.inf, -3e38):
+        y = z.copy()
+        y[tok == 0] = fill
+        y[off[-1]:] = fill
+        y[:, mask == 0] = fill
+        got.append(Balance(T, E, 2, 2)(_dev(y), _dev(idx), _dev(mask), _dev(tok), _dev(off), 0.013, 0.002, d))
+    for g in got[1:]:
+        assert all((g[n] == got[0][n]).all() for n in g)
+    # a token with a logit of 1e5 (a log-sum-exp of its own kind) beside the others: their bits stay, but for the
+    # sequence's means in dz
+    y = z.copy()
+    t = int(np.flatnonzero(tok[:off[1]])[0]) if tok[:off[1]].any() else 0
+    y[t, np.flatnonzero(mask)[0]] = 1e5
+    far = Balance(T, E, 2, 2)(_dev(y), _dev(idx), _dev(mask), _dev(tok), _dev(off), 0.013, 0.002, d)
+    same = np.arange(T) != t
+    assert (far["lse"][same] == got[0]["lse"][same]).all() and (far["dz"][same] == got[0]["dz"][same]).all()
+
+
 def test_balance_nan_reaches_its_sequence_only():
     T, E, k = 64, 8, 2
     z, idx, _, _, _ = _inputs(T, E, k, 0)
