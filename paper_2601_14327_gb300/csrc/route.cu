@@ -1065,15 +1065,17 @@ __global__ void __launch_bounds__(256) route_dx_split_kernel(const float *__rest
       m = max(m, __float_as_uint(v[u]) & 0x7fffffffu);
     }
     m = __reduce_max_sync(0xffffffffu, m);
-    // exponent of the largest value (of a row with an infinity or NaN: as it is; below 2^-112: as 2^-112)
+    // exponent of the largest value (of a row with an infinity or NaN: as it is; below 2^-111: as 2^-111)
     int e = int(m >> 23);
-    e = e == 255 ? 141 : max(e, 15);
+    e = e == 255 ? 141 : max(e, 16);
     const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
     __half *dst = (is_w ? w16 : z16) + size_t(i) * NP;
 #pragma unroll
     for (int u = 0; u < 8; ++u)
       if (lane + 32 * u < NP) dst[lane + 32 * u] = __float2half_rn(v[u] * up);
-    if (lane == 0) (is_w ? col_scale : row_scale)[i] = __uint_as_float(uint32_t(e - 14) << 23);
+    // (2^24 from one scale to the other: a sum, below 2^38, times dz's alone then stays finite for any dz; a row of W
+    // from 2^118 on gets an infinite scale)
+    if (lane == 0) (is_w ? col_scale : row_scale)[i] = __uint_as_float(uint32_t(e - 14) << 23) * (is_w ? 0x1p24f : 0x1p-24f);
   }
 }
 

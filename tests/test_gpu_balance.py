@@ -483,6 +483,18 @@ def test_route_dx_wide_ranges():
     assert (got[7] == 0).all() and (got[:, 9] == 0).all()
 
 
+def test_route_dx_largest_and_smallest_factors():
+    """Gradients up to fp32's largest beside weights that bring the product back, and the other way round."""
+    T, d, E, k = 280, 136, 40, 2
+    _, w, _, _, _, dz, _ = _router_inputs(T, d, E, k, 8)
+    dz, w = dz / dz.abs().max(), w / w.abs().max()
+    for a, b in ((2.0 ** 127, 2.0 ** -60), (2.0 ** 127, 2.0 ** -100), (2.0 ** -80, 2.0 ** 117), (2.0 ** -100, 2.0 ** 60)):
+        y, v = dz * a, w * b
+        prod, size = y.double().numpy() @ v.double().numpy().T, y.abs().double().numpy() @ v.abs().double().numpy().T
+        got = _dx(y, v, None, k).double().cpu().numpy()
+        assert (np.abs(got - prod) <= _dx_bound(prod, size)).all(), (a, b)
+
+
 def test_route_dx_infinities_stay_in_their_row():
     T, d, E, k = 140, 136, 20, 2
     _, w, _, _, _, dz, dx_in = _router_inputs(T, d, E, k, 6)
