@@ -165,20 +165,28 @@ def _kept(b: MoELayerBuffers, ckpt: Optional[MoECheckpoint]):
     """What holds the routing: b, or the layer's checkpoint."""
     if (ckpt is not None) != b.ckpt:
         raise ValueError("buffers made with ckpt=True go with a MoECheckpoint, others without")
-    if ckpt is not None and ckpt.shape != b.shape:
-        raise ValueError("the checkpoint is of another shape")
+    if ckpt is not None and (ckpt.shape != b.shape or ckpt.topk_idx.device != b.h.device):
+        raise ValueError("the checkpoint is of another shape or device")
     return b if ckpt is None else ckpt
 
 
 def _check_balance(b, kept, balance: BalanceLoss):
     if not 1 <= balance.n_seq <= min(kept.balance_seqs, b.balance_seqs):
         raise ValueError(f"balance over {balance.n_seq} sequences: more than the buffers' balance_seqs")
-    off, tok = balance.seq_offsets, balance.token_mask
-    if off is not None and (off.dtype != torch.int32 or not off.is_contiguous()):
-        raise ValueError("seq_offsets: a contiguous int32 tensor")
+    off, tok, dev = balance.seq_offsets, balance.token_mask, kept.topk_idx.device
+    if off is not None and (off.dtype != torch.int32 or not off.is_contiguous() or off.device != dev):
+        raise ValueError("seq_offsets: a contiguous int32 tensor on the layer's device")
     if tok is not None and (tok.dtype not in (torch.uint8, torch.bool) or not tok.is_contiguous()
-                            or tok.numel() != b.shape.T):
-        raise ValueError("token_mask: a contiguous uint8 or bool tensor of T values")
+                            or tok.numel() != b.shape.T or tok.device != dev):
+        raise ValueError("token_mask: a contiguous uint8 or bool tensor of T values on the layer's device")
+
+
+def _check_d_loss(kept, d_loss):
+    if kept.balance is None:
+        raise ValueError("d_loss: the forward had no balance")
+    if (d_loss.dtype != torch.float32 or d_loss.numel() != 2 or not d_loss.is_contiguous()
+            or d_loss.device != kept.topk_idx.device):
+        raise ValueError("d_loss: two contiguous fp32 values on the layer's device")
 
 
 def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mask=None,
@@ -262,6 +270,8 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
     s = b.shape
     R = s.rows_cap
     kept = _kept(b, ckpt)
+    if d_loss is not None:
+        _check_d_loss(kept, d_loss)
     if overlap:
         main = torch.cuda.current_stream() if stream is None else stream
         side = b.side

@@ -145,3 +145,21 @@ def test_layer_refuses_mixed_buffers():
                 {"seq_offsets": off[:1]}, {"token_mask": torch.ones(8)}, {"token_mask": torch.ones(7, dtype=torch.uint8)}):
         with pytest.raises(ValueError):
             layer.forward(b, None, None, None, None, None, balance=layer.BalanceLoss(0.1, **bad))
+
+
+def test_layer_refuses_tensors_of_another_device_and_other_d_loss():
+    s = layer.LayerShape(8, 128, 4, 2, 128)
+    b = layer.MoELayerBuffers(s, "cpu", balance_seqs=1)
+    for bad in ({"seq_offsets": torch.empty(2, dtype=torch.int32, device="meta")},
+                {"token_mask": torch.empty(8, dtype=torch.uint8, device="meta")}):
+        with pytest.raises(ValueError):
+            layer.forward(b, None, None, None, None, None, balance=layer.BalanceLoss(0.1, **bad))
+    with pytest.raises(ValueError):
+        layer.forward(layer.MoELayerBuffers(s, "cpu", ckpt=True), None, None, None, None, None,
+                      ckpt=layer.MoECheckpoint(s, "meta"))
+    with pytest.raises(ValueError):  # no forward with a balance loss came before
+        layer.backward(b, None, None, None, None, d_loss=torch.ones(2))
+    b.balance = layer.BalanceLoss(0.1)
+    for bad in (torch.ones(1), torch.ones(2, dtype=torch.float64), torch.ones(4)[::2], torch.empty(2, device="meta")):
+        with pytest.raises(ValueError):
+            layer.backward(b, None, None, None, None, d_loss=bad)
