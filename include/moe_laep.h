@@ -524,7 +524,8 @@ int moe_grouped_ffn_bwd_wgrad_gather(const uint16_t *d_out_perm, const uint16_t 
  * Format: 32 consecutive values of a row (a row's last block may be shorter) share the scale 2^(s - 127),
  * the smallest power of two with which the largest of them is at most 448 (s >= 1); each value is
  * the E4M3 code nearest to value / scale, ties to even: off by at most 2^-4 of itself, or by 2^-10 scales
- * below 2^-6 scales. A block with an infinity or a NaN reads back as NaN (s = 255).
+ * below 2^-6 scales. A block with an infinity or a NaN reads back as NaN (s = 255); a value from 1.9375 * 2^127
+ * on, whose code stands for 2^128, as an infinity.
  */
 
 /*

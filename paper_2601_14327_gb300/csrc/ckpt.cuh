@@ -3,7 +3,7 @@
 // value is the E4M3 code nearest to v / scale (ties to even). Powers of two make the division and the
 // product exact, so a code is off by its own rounding only: 2^-4 of a value down to 2^-14 of the
 // block's largest, an absolute step below. A block that holds an infinity or a NaN becomes all NaN
-// (s = 255), as its gradients would. Scales below 2^-126 are not used (s >= 1).
+// (s = 255), as its gradients would; values from 1.9375 * 2^127 on round to 2^128, an infinity. Scales below 2^-126 are not used (s >= 1).
 #pragma once
 
 #include <cuda_fp8.h>
