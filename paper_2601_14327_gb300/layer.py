@@ -29,7 +29,9 @@ class LayerShape:
 @dataclasses.dataclass
 class BalanceLoss:
     """Auxiliary losses of a layer's router (moe_balance_loss): the load-balance loss over the batch, or per
-    packed sequence with seq_offsets [n + 1] int32, and the z-loss. token_mask [T] uint8: 0 for padding."""
+    packed sequence with seq_offsets [n + 1] int32, and the z-loss. token_mask [T] uint8: 0 for padding.
+    forward() keeps the fields' values of the moment for its backward(), so the object may be set anew and used
+    again in between; the tensors are not copied and stay as they are until that backward."""
     coef: float
     z_coef: float = 0.0
     token_mask: Optional[torch.Tensor] = None
@@ -50,7 +52,8 @@ def _alloc_routing(o, s: LayerShape, dev, balance_seqs: int):
     o.group_offsets = torch.empty(s.E + 1, dtype=i32, device=dev)
     o.group_counts = torch.empty(s.E, dtype=i32, device=dev)
     o.row_of_assignment = torch.empty(s.T, s.k, dtype=i32, device=dev)
-    o.balance = o.balance_mask = None  # the forward's BalanceLoss and mask, kept for the backward
+    # of the forward, for the backward: its BalanceLoss (a copy), number of sequences and mask
+    o.balance, o.balance_n, o.balance_mask = None, 0, None
     o.balance_seqs = balance_seqs
     if balance_seqs:
         o.loss = torch.empty(2, dtype=f32, device=dev)
@@ -207,8 +210,10 @@ def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mas
     stream = L.stream_handle(stream)  # once for all calls
     logits = kept.logits if balance is not None else b.logits if keep_logits else None
     _route(b, kept, logits, x, w_router, bias, active_mask, logits_in, stream)
-    kept.balance, kept.balance_mask = balance, active_mask
+    kept.balance = None
     if balance is not None:
+        balance = dataclasses.replace(balance)  # the caller's object may change before the backward
+        kept.balance, kept.balance_n, kept.balance_mask = balance, balance.n_seq, active_mask
         L.moe_balance_loss(logits, kept.topk_idx, active_mask, balance.token_mask, balance.seq_offsets,
                            balance.n_seq, s.T, s.E, s.k, balance.coef, balance.z_coef, kept.loss,
                            kept.balance_counts, kept.balance_prob, kept.balance_tokens, kept.lse,
@@ -304,7 +309,7 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
         side.wait_event(ev)
     bal = kept.balance
     if bal is not None:
-        L.moe_balance_loss_bwd(kept.logits, kept.balance_mask, bal.seq_offsets, bal.n_seq, s.T, s.E,
+        L.moe_balance_loss_bwd(kept.logits, kept.balance_mask, bal.seq_offsets, kept.balance_n, s.T, s.E,
                                s.k, bal.coef, bal.z_coef, kept.balance_counts, kept.balance_tokens,
                                kept.lse, d_loss, b.dz, side)
         L.moe_route_bwd_dense(x, kept.topk_idx, kept.topk_gate, b.d_gate, b.dz, s.T, s.d, s.E, s.k,
