@@ -277,6 +277,8 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
     kept = _kept(b, ckpt)
     if d_loss is not None:
         _check_d_loss(kept, d_loss)
+    if kept.balance is not None and getattr(b, "dz", None) is None:
+        raise ValueError("the forward had a balance loss: its backward needs buffers made with balance_seqs")
     if overlap:
         main = torch.cuda.current_stream() if stream is None else stream
         side = b.side

@@ -83,3 +83,17 @@ def test_backward_takes_the_forwards_number_of_sequences(calls):
     calls.clear()
     _backward(b)
     assert _args(calls, "moe_balance_loss_bwd")["n_seq"] == 2
+
+
+@pytest.mark.parametrize("kw", [{}, {"balance_seqs": 1, "backward": False}])
+def test_backward_refuses_buffers_without_room_for_the_losses_gradient(calls, kw):
+    """The checkpoint's forward had a balance loss, the backward's buffers have no dz (or no backward at all): refused
+    before the first launch."""
+    c = layer.MoECheckpoint(S, "cpu", 1)
+    _forward(layer.MoELayerBuffers(S, "cpu", balance_seqs=1, ckpt=True), layer.BalanceLoss(0.1), c)
+    calls.clear()
+    with pytest.raises(ValueError):
+        _backward(layer.MoELayerBuffers(S, "cpu", ckpt=True, **kw), c)
+    assert not calls
+    _backward(layer.MoELayerBuffers(S, "cpu", balance_seqs=1, ckpt=True), c)
+    assert calls
