@@ -198,6 +198,7 @@ def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mas
     """route -> permute -> grouped SwiGLU FFN -> combine (in the down GEMM's epilogue
     when b.fused_combine). Returns b.y.
 
+    keep_logits: b.logits [T, E] receives the masked logits.
     balance: adds the router's auxiliary losses; loss [2] (balance, z), balance_counts, balance_prob
     [sequences, E] are then in b (in ckpt, when given), and backward() adds their gradient.
     ckpt: the layer's checkpoint (for b with ckpt=True): receives the routing (in the place of b's
@@ -210,6 +211,8 @@ def forward(b: MoELayerBuffers, x, w_router, bias, w_gate_up, w_down, active_mas
     stream = L.stream_handle(stream)  # once for all calls
     logits = kept.logits if balance is not None else b.logits if keep_logits else None
     _route(b, kept, logits, x, w_router, bias, active_mask, logits_in, stream)
+    if keep_logits and logits is not b.logits:  # (the routing of these logits is the same one)
+        _route(b, kept, b.logits, x, w_router, bias, active_mask, logits, stream)
     kept.balance = None
     if balance is not None:
         balance = dataclasses.replace(balance)  # the caller's object may change before the backward

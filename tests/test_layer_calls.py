@@ -97,3 +97,22 @@ def test_backward_refuses_buffers_without_room_for_the_losses_gradient(calls, kw
     assert not calls
     _backward(layer.MoELayerBuffers(S, "cpu", balance_seqs=1, ckpt=True), c)
     assert calls
+
+
+@pytest.mark.parametrize("balance", [False, True])
+@pytest.mark.parametrize("ckpt", [False, True])
+def test_kept_logits_are_in_the_buffers(calls, balance, ckpt):
+    """keep_logits: the last call that writes b.logits makes them this routing's, also where a checkpoint keeps the
+    logits for the balance loss."""
+    b = layer.MoELayerBuffers(S, "cpu", balance_seqs=1, ckpt=ckpt)
+    c = layer.MoECheckpoint(S, "cpu", 1) if ckpt else None
+    _forward(b, layer.BalanceLoss(0.1) if balance else None, c, mask=5, keep_logits=True, logits_in=7)
+    routes = [a for n, a in calls if n == "moe_route"]
+    assert routes[-1]["logits_out"] is b.logits and all(a["active_mask"] == 5 for a in routes)
+    # a second call has the first one's logits, so it writes the same routing
+    assert routes[0]["logits_in"] == 7 and all(a["logits_in"] is c.logits for a in routes[1:])
+    if balance:
+        assert any(a["logits_out"] is (c or b).logits for a in routes)
+    calls.clear()
+    _forward(b, layer.BalanceLoss(0.1) if balance else None, c, logits_in=7)
+    assert len([n for n, _ in calls if n == "moe_route"]) == 1
