@@ -1404,12 +1404,13 @@ template <int MODE, int BN, bool CK>
 int launch_one(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &h,
                const GemmParams &p, cudaStream_t s, const char *what) {
   using Sh = Shape<BN>;
-  static bool attr = false;
-  if (!attr) {
+  static bool attr[64] = {};  // of each device
+  bool &set = attr[moe::device_slot()];
+  if (!set) {
     cudaError_t e = cudaFuncSetAttribute(grouped_gemm_kernel<MODE, BN, CK>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize, int(Sh::SMEM));
     if (e != cudaSuccess) return moe::cuda_status(e, what);
-    attr = true;
+    set = true;
   }
   MOE_LAUNCH(kGemmName[MODE], s, moe::launch_dep(grouped_gemm_kernel<MODE, BN, CK>, moe::num_sms(), kThreads, Sh::SMEM, s,
                                                  a, b, o, h, p));
@@ -1443,7 +1444,8 @@ int launch_pair(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  static int nclusters = 0;
+  static int fit[64] = {};  // co-resident pairs on each device
+  int &nclusters = fit[moe::device_slot()];
   if (!nclusters) {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(Sh::SMEM));
     if (e != cudaSuccess) return moe::cuda_status(e, what);

@@ -1379,11 +1379,12 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
 template <bool DW, int G, bool AHEAD = false>
 int launch_route_mma(const char *name, dim3 grid, size_t smem, const CUtensorMap &a, const CUtensorMap &b,
                        const RouteTcParams &p, cudaStream_t s, const char *what) {
-  static bool attr_set = false;
-  if (!attr_set) {
+  static bool attr_set[64] = {};
+  bool &set = attr_set[moe::device_slot()];
+  if (!set) {
     cudaError_t e = cudaFuncSetAttribute(route_tc_kernel<DW, G, AHEAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
-    attr_set = true;
+    set = true;
   }
   MOE_LAUNCH(name, s, moe::launch_dep(route_tc_kernel<DW, G, AHEAD>, grid, kRtThreads, smem, s, a, b, p));
   return moe::launch_status(what);
