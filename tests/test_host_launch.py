@@ -91,3 +91,25 @@ def test_every_entry_point_launches_on_a_second_device(fake, first, second):
     assert len(rows) == 3 and rows[0][0] > 60
     for launches, pairs, room in rows:
         assert launches == rows[0][0] and pairs <= room, rows
+
+
+def test_first_calls_from_two_threads(fake):
+    """The first look-up of the driver's tensor-map call, still under way in another thread."""
+    out = _child(fake, CALLS + """
+    fake.fake_entry_point_ms(300)
+    failed, gate = [], threading.Barrier(4)
+
+    def call():
+        try:
+            gate.wait()
+            L.moe_grouped_ffn_fwd(N, N, 4, 128, 128, 1024, N, N, N, N, N, **WS)
+        except Exception as e:
+            failed.append(repr(e))
+
+    L.load()
+    threads = [threading.Thread(target=call) for _ in range(4)]
+    for t in threads: t.start()
+    for t in threads: t.join()
+    print(failed)
+    """)
+    assert out.strip() == "[]"
