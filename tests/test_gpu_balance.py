@@ -556,3 +556,63 @@ def test_dense_router_backward_in_one_split(T, d, E):
     xd, zd = x.double().numpy(), dz.double().numpy()
     assert (np.abs(dw[:d].cpu().double().numpy() - xd.T @ zd) <= 1e-5 * (np.abs(xd).T @ np.abs(zd)) + 1e-30).all()
     assert (dw[d] == 7).all()  # nothing behind the last row
+
+
+def _sums_64(z, idx, off, k):
+    """counts, prob and sum of lse^2 of each sequence, in 64 bits and slices."""
+    E, out = z.shape[1], []
+    for a, b in zip(off[:-1], off[1:]):
+        p, q = torch.zeros(E, dtype=torch.float64, device="cuda"), 0.0
+        for t in range(a, b, 1 << 20):
+            y = z[t:min(b, t + (1 << 20))].double()
+            lse = torch.logsumexp(y, 1)
+            p += torch.exp(y - lse[:, None]).sum(0)
+            q += float((lse * lse).sum())
+        c = torch.bincount(idx[a:b].reshape(-1).long(), minlength=E)
+        out.append((c, p / max(1, b - a), q))
+    return out
+
+
+def _check_sums(z, idx, off, k):
+    T, E = z.shape
+    S = len(off) - 1
+    b = Balance(T, E, k, S)
+    coef, z_coef = 0.7, 0.3
+    L.moe_balance_loss(z, idx, None, None, None if S == 1 else torch.tensor(off, dtype=I32, device="cuda"), S, T, E, k,
+                       coef, z_coef, b.loss, b.counts, b.prob, b.n_tokens, b.lse, b.ws, b.ws.numel())
+    ref = _sums_64(z, idx, off, k)
+    N, M = sum(hi > lo for lo, hi in zip(off[:-1], off[1:])), off[-1] - off[0]
+    loss = 0.0
+    for s, (c, p, _) in enumerate(ref):
+        n = off[s + 1] - off[s]
+        assert int(b.n_tokens[s]) == n and torch.equal(b.counts[s].long(), c)
+        # fp32 additions one after another: 80 of a lane, 3 of a warp's tokens, 24 warps, then rows of chunks
+        # (64 and T / 2^20 at most) and 32 warps, 2^-24 each; p itself: exp and the quotient 2^-22 each, the exponent's
+        # argument |z - m| 2^-23 (|z - m| < 16)
+        tol = (80 + 3 + 24 + 64 + T / 2 ** 20 + 32 + 4) * 2 ** -24 + 2 ** -21 + 2 ** -19
+        assert ((b.prob[s].double() - p).abs() <= tol * p).all(), float(((b.prob[s].double() - p).abs() / p).max())
+        if n:
+            loss += coef / N * float((c.double() * E / (k * n) * p).sum())
+    # (a few more roundings: the quotients, the products, the sums over experts and sequences)
+    tol += 24 * 2 ** -24
+    assert abs(float(b.loss[0]) - loss) <= tol * loss
+    lz = z_coef * sum(r[2] for r in ref) / M
+    assert abs(float(b.loss[1]) - lz) <= tol * lz, (float(b.loss[1]), lz)
+
+
+def test_balance_sums_of_many_equal_tokens():
+    """Equal addends round the same way: sums of one after another would be off by more the more tokens there are."""
+    T, E, k = 1 << 26, 4, 1
+    row = torch.log(torch.tensor([0.8694458658865812, 0.06, 0.04, 0.0305541341134188], dtype=torch.float64)) + 1.3
+    z = row.float().cuda().expand(T, E).contiguous()
+    _check_sums(z, torch.zeros(T, k, dtype=I32, device="cuda"), [0, T], k)
+
+
+@pytest.mark.parametrize("T,E,k,S", [(1_500_000, 96, 4, 5), (4_000_000, 16, 2, 1), (2_400_000, 40, 8, 300)])
+def test_balance_sums_of_many_tokens(T, E, k, S):
+    """More chunks than SMs: sums of probabilities and squares against 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(T + E)
+    z = torch.randn(T, E, generator=g, device="cuda") - torch.log1p(torch.arange(E, device="cuda").float())
+    idx = torch.randint(0, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    cut = torch.sort(torch.randint(0, T + 1, (S - 1,), generator=g, device="cuda"))[0].tolist()
+    _check_sums(z, idx, [0] + cut + [T], k)
