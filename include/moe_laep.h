@@ -615,8 +615,8 @@ int moe_route_bwd(const uint16_t *x, const int32_t *topk_idx, const float *topk_
  * dz [T,E] fp32, not scaled or masked here: zero where a logit has no gradient. topk_idx,
  * topk_gate, d_gate and d_logits may be NULL together (dZ = dz). An id outside [0, E) is left out of dZ; one
  * that a token has twice counts twice. dZ is carried as in moe_route_bwd, and the sums over the tokens are
- * added up in fp32, rounding to nearest, every 256 tokens (the tensor cores truncate): dw_router
- * is ~1e-6 off in the 2-norm whatever T is. Bitwise reproducible. Other arguments, ws and limits as in moe_route_bwd.
+ * added up in fp32, rounding to nearest, every 256 tokens (the tensor cores truncate): dw_router is 8.8e-7 off in the
+ * 2-norm at T=65536, and at most (200 + T/256) 2^-24 of sum_t |x[t,:]| |dZ[t,:]| anywhere. Bitwise reproducible. Other arguments, ws and limits as in moe_route_bwd.
  * dz's share of the layer input's gradient comes from moe_route_dx.
  */
 int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float *topk_gate,

@@ -724,7 +724,8 @@ __global__ void __launch_bounds__(256) route_bwd_dz_dense_kernel(
 // truncation: over the ~2,500 additions of a long split route_tc_kernel's sums come out 4e-5 too small (2-norm,
 // T=65536, d=7168, 171 experts; an fp32 product by the library is 5e-6 off), more than the rounding of a dense
 // loss gradient may be. Here an accumulator takes kDwFlush k-blocks, while the epilogue warps add the one before to
-// their registers, rounding to nearest: 8.8e-7 off, whatever T is. The tensor pipe sets the time: 275 us there,
+// their registers, rounding to nearest: 8.8e-7 off. (What is left to grow with T is a chain of T / 256 fp32 additions over
+// the number of splits: 2^-24 each of a sum that keeps its sign, 32 at this size.) The tensor pipe sets the time: 275 us there,
 // 263 at its measured rate (route_tc_kernel: 291, by shared memory; a pair's M=256 MMA reads each SM's own 128
 // features and half of dZ's rows). Two terms of dZ would take 230 us and be 2.5e-6 off, ten times
 // what an fp32 product is over 1,000 tokens. Roles as in the grouped GEMMs' pair kernel: warp 0 of each

@@ -616,3 +616,24 @@ def test_balance_sums_of_many_tokens(T, E, k, S):
     idx = torch.randint(0, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
     cut = torch.sort(torch.randint(0, T + 1, (S - 1,), generator=g, device="cuda"))[0].tolist()
     _check_sums(z, idx, [0] + cut + [T], k)
+
+
+@pytest.mark.parametrize("T,d,E", [(1 << 22, 64, 20), ((1 << 20) + 77, 136, 171), (65536, 256, 64)])
+def test_dense_router_backward_of_many_tokens_of_one_sign(T, d, E):
+    """Sums that grow all along, so that every addition rounds in the size of the result: against 64 bits in slices."""
+    g = torch.Generator(device="cuda").manual_seed(T + E)
+    x = (1 + 0.1 * torch.randn(T, d, generator=g, device="cuda")).to(torch.bfloat16)
+    dz = 1 + 0.1 * torch.rand(T, E, generator=g, device="cuda")
+    n = L.moe_workspace_size(T, d, E, 8, 128)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    dw = torch.empty(d, E, device="cuda")
+    L.moe_route_bwd_dense(x, None, None, None, dz, T, d, E, 8, None, dw, ws, n)
+    ref = torch.zeros(d, E, dtype=torch.float64, device="cuda")
+    for t in range(0, T, 1 << 18):
+        ref += x[t:t + (1 << 18)].double().T @ dz[t:t + (1 << 18)].double()
+    # (up to 256 features: 64 splits.) dZ carried to 2^-24; 48 truncated additions of 2^-23 in an accumulator, one
+    # rounded addition per 256 tokens of a split, two of the terms, one per split
+    kb = -(-T // 64)
+    chain = -(-(-(-kb // 64)) // 4)
+    tol = (1 + 2 * 48 + chain + 2 + 64) * 2 ** -24
+    assert ((dw.double() - ref).abs() <= tol * ref).all(), float(((dw.double() - ref).abs() / ref).max())
