@@ -466,3 +466,27 @@ def test_offsets_past_32_bits():
     assert R * 2 * F > 2 ** 31
     for a, b in zip(run(xp), run(xp[-128:].contiguous())):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,d,E,k", [(37, 2048, 64, 6), (700, 72, 16, 4)])
+def test_ckpt_permute_leaves_out_rows_out_of_range(T, d, E, k):
+    """Entries outside [0, rows_cap): their rows stay as they were, and so does what lies before and behind x_perm."""
+    R, rim = L.moe_perm_rows_max(T, k, E), 40
+    idx = _routing(T, E, k, T)
+    off, cnt, row = _layout(idx, E, R)
+    q, s = _pack(_values(T, d, T + d))
+
+    def run(r):
+        whole = torch.full((rim + R + rim, d), 9.0, dtype=BF16, device="cuda")
+        L.moe_ckpt_permute(q, s, r, off, cnt, T, d, E, k, R, None, whole[rim:rim + R])
+        return whole
+
+    want, bad = run(row), row.clone()
+    dropped = []
+    for i, (t, j) in enumerate([(0, 0), (T - 1, k - 1), (T // 2, 1), (3, 2), (5, 0)]):
+        dropped.append(rim + int(row[t, j]))
+        bad[t, j] = (R, -1, R + rim - 1, -rim, R + 1)[i]
+    got = run(bad)
+    differ = (got != want).any(dim=1).nonzero().flatten().tolist()
+    assert differ == sorted(dropped)
+    assert (got[dropped] == 9).all() and (got[:rim] == 9).all() and (got[rim + R:] == 9).all()
