@@ -490,3 +490,26 @@ def test_ckpt_permute_leaves_out_rows_out_of_range(T, d, E, k):
     differ = (got != want).any(dim=1).nonzero().flatten().tolist()
     assert differ == sorted(dropped)
     assert (got[dropped] == 9).all() and (got[:rim] == 9).all() and (got[rim + R:] == 9).all()
+
+
+@pytest.mark.parametrize("kw", [{"gather": True}, {"fused_combine": True}])
+@pytest.mark.parametrize("T,d,E,k,F,masked", [(300, 256, 8, 2, 256, 0), (1021, 512, 32, 4, 384, 6)])
+def test_balance_loss_in_the_other_forms_of_the_layer(T, d, E, k, F, masked, kw):
+    """Gathered dispatch and fused combine with a balance loss: losses and gradients of the default form, bit for bit
+    (y too, but for the order of the fused combine's sums)."""
+    inp, o, mask, z = _layer_inputs(T, d, E, k, F, masked)
+    g = {n: v.cuda() for n, v in inp.items()}
+    m = None if mask is None else torch.from_numpy(mask).cuda()
+    off = torch.tensor([0, T // 3, T - 5], dtype=I32, device="cuda")
+    got = []
+    for form in ({}, kw):
+        b = layer.MoELayerBuffers(layer.LayerShape(T, d, E, k, F), "cuda", balance_seqs=2, **form)
+        b.dw_gate_up.zero_()
+        b.dw_down.zero_()
+        out = _step(b, g, m, torch.from_numpy(z).cuda(), layer.BalanceLoss(20.0 * T, 0.3 * T, seq_offsets=off))
+        got.append([t.clone() for t in out] + [b.loss, b.balance_counts, b.balance_prob, b.y.clone()])
+    for n, (u, v) in enumerate(zip(*got)):
+        if n == 7 and "fused_combine" in kw:
+            assert_close("y", to_np(v), to_np(u))
+        else:
+            assert torch.equal(u, v), n
