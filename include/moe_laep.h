@@ -628,9 +628,10 @@ int moe_route_bwd_dense(const uint16_t *x, const int32_t *topk_idx, const float 
  * moe_route_dx - a dense logit gradient's share of the layer input's gradient:
  *   dx[t,:] = dx_in[t,:] + sum_e dz[t,e] * w_router[:,e]   (one bf16 rounding)
  * dz [T,E] fp32; w_router [d,E] fp32; dx_in [T,d] bf16 or NULL (zeros), may be dx itself; dx [T,d]
- * bf16 (out); both 16-byte aligned. The product's factors are rounded to 11 significant bits (half precision, a
- * power of two taken out of each row of dz and of w_router), its sums are fp32. An infinity or NaN in
- * a row of dz or w_router stays in that row or column of dx (an entry of w_router from 2^118 on counts as one). k: the layer's (for the workspace's layout). Limits:
+ * bf16 (out); both 16-byte aligned. The product's factors keep 22 significant bits (two half-precision terms, a
+ * power of two taken out of each row of dz and of w_router), its sums are fp32: it is within (E/5 + 10) 2^-23 of
+ * sum_e |dz| |w_router| before the rounding (factors below 2^-18 of their row's largest: within 2^-39 of that). An infinity or NaN in a row of dz or w_router leaves no finite value in
+ * that row or column of dx, and others as they are (an entry of w_router from 2^118 on counts as one). k: the layer's (for the workspace's layout). Limits:
  * 1 <= E <= 256, 1 <= k <= 8, d % 8 == 0, T >= 0; ws as in moe_route_bwd.
  */
 int moe_route_dx(const float *dz, const float *w_router, const uint16_t *dx_in, int T, int d, int E,

@@ -1001,28 +1001,28 @@ __global__ void zero_f32_kernel(float *p, int n) {
 
 // ---- dx = bf16(dx_in + dz W^T) on the tensor cores ------------------------------
 // Both factors in half precision: a row of dz [T, E] and a row of W [d, E] (one output column) are each
-// scaled by the power of two that brings their largest value into [2^14, 2^15), so that a value keeps 11
-// significant bits down to 2^-29 of its row's largest and has an absolute step below. The products are
-// exact, their sum is fp32, and the two powers of two are taken out of it exactly: what is lost is 2^-11 per
-// factor, beside the 2^-8 with which the result is rounded to bf16 (2-norm error of the result against
-// 64 bits: 1.01 times that of the rounding alone). One product instead of the six of bf16 pairs
-// or half the rate of tf32, and half the operand bytes.
+// scaled by the power of two that brings their largest value into [2^14, 2^15), and split into two terms: 22
+// significant bits down to 2^-18 of the row's largest value, an absolute step of 2^-39 of it below. Three products are
+// summed, z1 w1 + z2 w1 + z1 w2 (the fourth is 2^-22 of the first); each product is exact, the sum is fp32, and the two
+// powers of two are taken out of it exactly. What is lost is ~2^-21 of sum |dz| |W| and the accumulation's truncation,
+// where one term of each lost 2^-11 per factor, which shows wherever dx_in and the product cancel. (As good with
+// bf16 terms takes six products; tf32 has the bits of one half-precision term.)
 //
-// HBM-bound (dx_in read, dx written: 4 bytes per 2 E operations). A persistent CTA pair takes
+// HBM-bound up to 64 experts (dx_in read, dx written: 4 bytes per 6 E operations), above by the tensor cores
+// beside it. A persistent CTA pair takes
 // consecutive 256-token x 256-column tiles, columns first, so that a token block's operand stays in shared memory
 // for its whole row of tiles and W's (a few MB) comes from L2, half to each CTA. Warp 0 of each CTA
 // issues its operand loads, one thread of the even CTA the MMAs, into two accumulators; warps 2..17 add dx_in. Each
-// of those has its own ring of three 32-row x 32-column pieces of dx: a piece is loaded by TMA two pieces
-// ahead, gets the products added in place, and is stored by TMA from there. No piece is touched by two warps, so
-// dx_in may be dx.
-// T=65536, d=7168, in and out of place: 307 us at 171 experts (6.1 TB/s; a copy of dx takes 275), 306 at
-// 32, 332 at 256. Single SMs, which load all of W's operand through two 32 KB stages: 317, 299, 400. Eight
-// adding warps with pieces of 64 columns: 318, 315, 340; 128-column tiles: 416 at 171; four pieces a warp
-// and a shorter operand ring: 315, 307, 399.
+// of those has its own ring of 32-row x 32-column pieces of dx: a piece is loaded by TMA, two pieces
+// ahead where there are three, gets the products added in place, and is stored by TMA from there. No piece is touched by
+// two warps, so dx_in may be dx.
+// T=65536, d=7168: 307 us at up to 64 experts (6.1 TB/s; a copy of dx takes 275), 351 at 128, 389 at 171, 499 at
+// 256. One product: 311 / 313 / 317 / 341. MMAs alone take 247 us at 192 experts, 140 clocks each. Tried with one product:
+// single SMs, which load all of W's operand, 317 at 171 experts and 400 at 256; eight
+// adding warps with pieces of 64 columns 318 and 340; 128-column tiles 416 at 171.
 constexpr int kDxBN = 256;
 constexpr int kDxEpiWarps = 16;
 constexpr int kDxThreads = 64 + 32 * kDxEpiWarps;
-constexpr int kDxSlots = 3;
 constexpr uint32_t kDxABlock = kRtBM * kRtBK * 2, kDxBStage = kDxBN / 2 * kRtBK * 2, kDxSlotBytes = 32 * 32 * 2;
 
 struct RouteDxParams {
@@ -1033,16 +1033,19 @@ struct RouteDxParams {
   const float *row_scale, *col_scale;  // what the factors' rows were divided by (col_scale padded to 64)
 };
 
-int route_dx_stages(int nkb) {
-  const int64_t rest = kRtMaxSmem - 2048 - int64_t(nkb) * kDxABlock - int64_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes;
-  return int(std::min<int64_t>(6, rest / kDxBStage));  // 4 with four k-blocks
+// Pieces of a warp's ring: three up to 128 experts; above, the operands leave room for one beside four to six stages (two
+// and two stages at 256 experts: 669 us instead of 499).
+int route_dx_slots(int nkb) { return nkb <= 2 ? 3 : 1; }
+int route_dx_stages(int nkb, int slots) {
+  const int64_t rest = kRtMaxSmem - 2048 - int64_t(2 * nkb) * kDxABlock - int64_t(kDxEpiWarps) * slots * kDxSlotBytes;
+  return int(std::min<int64_t>(6, rest / kDxBStage));  // 4 with two or four k-blocks
 }
-size_t route_dx_smem(int nkb, int stages) {
-  return 1024 + size_t(nkb) * kDxABlock + size_t(stages) * kDxBStage + size_t(kDxEpiWarps) * kDxSlots * kDxSlotBytes +
-         size_t(2 * stages + 8 + kDxEpiWarps * kDxSlots) * 8 + 16;
+size_t route_dx_smem(int nkb, int stages, int slots) {
+  return 1024 + size_t(2 * nkb) * kDxABlock + size_t(stages) * kDxBStage + size_t(kDxEpiWarps) * slots * kDxSlotBytes +
+         size_t(2 * stages + 8 + kDxEpiWarps * slots) * 8 + 16;
 }
 
-// Rows of W, then rows of dz (E fp32 values each) -> half precision [rows][NP] and their scales.
+// Rows of W, then rows of dz (E fp32 values each) -> two half-precision terms each [rows][2][NP] and their scales.
 __global__ void __launch_bounds__(256) route_dx_split_kernel(const float *__restrict__ w, const float *__restrict__ dz,
                                                              int d, int d_pad, int T, int E, int NP,
                                                              __half *__restrict__ w16, float *__restrict__ col_scale,
@@ -1070,16 +1073,22 @@ __global__ void __launch_bounds__(256) route_dx_split_kernel(const float *__rest
     int e = int(m >> 23);
     e = e == 255 ? 141 : max(e, 16);
     const float up = __uint_as_float(uint32_t(268 - e) << 23);  // 2^(14 - (e - 127))
-    __half *dst = (is_w ? w16 : z16) + size_t(i) * NP;
+    __half *dst = (is_w ? w16 : z16) + size_t(i) * (2 * NP);
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (lane + 32 * u < NP) dst[lane + 32 * u] = __float2half_rn(v[u] * up);
+      if (lane + 32 * u < NP) {
+        const float y = v[u] * up;
+        const __half hi = __float2half_rn(y);
+        dst[lane + 32 * u] = hi;
+        dst[NP + lane + 32 * u] = __float2half_rn(y - __half2float(hi));
+      }
     // (2^24 from one scale to the other: a sum, below 2^38, times dz's alone then stays finite for any dz; a row of W
     // from 2^118 on gets an infinite scale)
     if (lane == 0) (is_w ? col_scale : row_scale)[i] = __uint_as_float(uint32_t(e - 14) << 23) * (is_w ? 0x1p24f : 0x1p-24f);
   }
 }
 
+template <int SLOTS>
 __global__ void __launch_bounds__(kDxThreads, 1)
     route_dx_kernel(const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmW,
                     const __grid_constant__ CUtensorMap tmIn, const __grid_constant__ CUtensorMap tmOut,
@@ -1088,10 +1097,10 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   const uint32_t raw = tc::smem_u32(smem_raw);
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
   const int S = p.stages;
-  const uint32_t sA = raw + pad, sB = sA + uint32_t(p.nkb) * kDxABlock, sSlots = sB + uint32_t(S) * kDxBStage;
-  const uint32_t bars_off = pad + uint32_t(p.nkb) * kDxABlock + uint32_t(S) * kDxBStage + kDxEpiWarps * kDxSlots * kDxSlotBytes;
+  const uint32_t sA = raw + pad, sB = sA + uint32_t(2 * p.nkb) * kDxABlock, sSlots = sB + uint32_t(S) * kDxBStage;
+  const uint32_t bars_off = pad + uint32_t(2 * p.nkb) * kDxABlock + uint32_t(S) * kDxBStage + kDxEpiWarps * SLOTS * kDxSlotBytes;
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem_raw + bars_off);
-  int *misc = reinterpret_cast<int *>(bars + 2 * S + 8 + kDxEpiWarps * kDxSlots);
+  int *misc = reinterpret_cast<int *>(bars + 2 * S + 8 + kDxEpiWarps * SLOTS);
   volatile int *abort_flag = misc + 1;
   volatile int no_abort = 0;
   const uint32_t bar0 = tc::smem_u32(bars);
@@ -1101,7 +1110,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * S + 2 + a); };
   const uint32_t afull_bar = bar0 + 8u * (2 * S + 4), aempty_bar = bar0 + 8u * (2 * S + 5);
   const uint32_t drain_bar = bar0 + 8u * (2 * S + 6);
-  auto slot_bar = [&](int w, int s) { return bar0 + 8u * (2 * S + 8 + w * kDxSlots + s); };
+  auto slot_bar = [&](int w, int s) { return bar0 + 8u * (2 * S + 8 + w * SLOTS + s); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr uint32_t IDESC = tc::idesc_f16_f32(2 * kRtBM, kDxBN);
   const uint32_t rank = tc::cluster_ctarank();
@@ -1120,7 +1129,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     tc::mbar_init(aempty_bar, 1);
     tc::mbar_init(drain_bar, 1);
     for (int w = 0; w < kDxEpiWarps; ++w)
-      for (int s = 0; s < kDxSlots; ++s) tc::mbar_init(slot_bar(w, s), 1);
+      for (int s = 0; s < SLOTS; ++s) tc::mbar_init(slot_bar(w, s), 1);
     tc::fence_mbar_init();
     misc[1] = 0;
   }
@@ -1144,24 +1153,30 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   if (warp == 0) {
     if (lane == 0) {
       const uint32_t full_leader = tc::mapa(full_bar(0), 0), afull_leader = tc::mapa(afull_bar, 0);
-      uint32_t it = 0, blocks = 0;
+      uint32_t it = 0, blocks = 0, s = 0, phase = 1;  // (s = it % S, phase = parity of the round before)
       int m_now = -1;
       bool ok = true;
       for (int tile = tile0; tile < tile1 && ok; ++tile) {
         const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
         if (m != m_now) {
           if (blocks > 0 && !tc::mbar_wait(aempty_bar, (blocks - 1) & 1u, kRtWaitNs, abort_flag)) { fail(); break; }
-          if (leader) tc::mbar_arrive_expect_tx(afull_bar, 2 * uint32_t(p.nkb) * kDxABlock);
+          if (leader) tc::mbar_arrive_expect_tx(afull_bar, 4 * uint32_t(p.nkb) * kDxABlock);
           for (int kb = 0; kb < p.nkb; ++kb)
-            tc::tma_load_2d_pair(sA + kb * kDxABlock, &tmZ, afull_leader, kb * kRtBK, (2 * m + int(rank)) * kRtBM);
+            for (int term = 0; term < 2; ++term)
+              tc::tma_load_2d_pair(sA + (2 * kb + term) * kDxABlock, &tmZ, afull_leader, term * p.NP + kb * kRtBK,
+                                   (2 * m + int(rank)) * kRtBM);
           ++blocks;
           m_now = m;
         }
-        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
-          const int s = it % S;
-          if (!tc::mbar_wait(empty_bar(s), ((it / S) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
+        for (int b = 0; b < 2 * p.nkb; ++b, ++it) {  // a k-block's first term, then its second
+          if (!tc::mbar_wait(empty_bar(s), phase, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
           if (leader) tc::mbar_arrive_expect_tx(full_bar(s), 2 * kDxBStage);
-          tc::tma_load_2d_pair(sB + s * kDxBStage, &tmW, full_leader + 8u * s, kb * kRtBK, n * kDxBN + int(rank) * (kDxBN / 2));
+          tc::tma_load_2d_pair(sB + s * kDxBStage, &tmW, full_leader + 8u * s, (b & 1) * p.NP + (b >> 1) * kRtBK,
+                               n * kDxBN + int(rank) * (kDxBN / 2));
+          if (++s == uint32_t(S)) {
+            s = 0;
+            phase ^= 1u;
+          }
         }
       }
       // every issued load lands before the CTAs may exit (the even CTA's barriers count both CTAs')
@@ -1173,7 +1188,9 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     }
   } else if (warp == 1) {
     if (leader && lane == 0) {
-      uint32_t it = 0, blocks = 0, tcount = 0;
+      uint32_t blocks = 0, tcount = 0, s = 0, phase = 0;
+      const uint64_t a_desc = tc::smem_desc_sw128(sA, 16, 1024), b_desc = tc::smem_desc_sw128(sB, 16, 1024);
+      const int last_steps = (p.NP - (p.nkb - 1) * kRtBK) / 16;
       int m_now = -1;
       bool ok = true, issued = false;
       for (int tile = tile0; tile < tile1 && ok; ++tile, ++tcount) {
@@ -1185,16 +1202,31 @@ __global__ void __launch_bounds__(kDxThreads, 1)
           m_now = m;
         }
         if (!tc::mbar_wait(tempty_bar(a), ((tcount >> 1) & 1u) ^ 1u, kRtWaitNs, abort_flag)) { fail(); break; }
-        for (int kb = 0; kb < p.nkb; ++kb, ++it) {
-          const int s = it % S;
-          if (!tc::mbar_wait(full_bar(s), (it / S) & 1u, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
-          tc::fence_after_sync();
-          const uint64_t ad = tc::smem_desc_sw128(sA + kb * kDxABlock, 16, 1024), bd = tc::smem_desc_sw128(sB + s * kDxBStage, 16, 1024);
-          const int steps = min(4, (p.NP - kb * kRtBK) / 16);
-          for (int kk = 0; kk < steps; ++kk)  // (a descriptor's address counts 16 bytes)
-            tc::mma_bf16_pair(tmem_base + a * kDxBN, ad + uint64_t(2 * kk), bd + uint64_t(2 * kk), IDESC, (kb | kk) != 0);
-          tc::mma_commit_pair_mc(empty_bar(s), 0x3);
-          issued = true;
+        const uint32_t d = tmem_base + a * kDxBN;
+        for (int kb = 0; kb < p.nkb && ok; ++kb) {
+          const int steps = kb + 1 < p.nkb ? 4 : last_steps;
+          // (descriptors' addresses count 16 bytes; straight code: with the stage from a division and a loop over the
+          // steps, issuing took longer than the products)
+          const uint64_t ad = a_desc + uint64_t(2 * kb) * (kDxABlock >> 4);
+#pragma unroll
+          for (int term = 0; term < 2; ++term) {
+            if (!tc::mbar_wait(full_bar(s), phase, kRtWaitNs, abort_flag)) { fail(); ok = false; break; }
+            tc::fence_after_sync();
+            const uint64_t bd = b_desc + uint64_t(s) * (kDxBStage >> 4);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              if (kk >= steps) break;
+              tc::mma_bf16_pair(d, ad + uint64_t(2 * kk), bd + uint64_t(2 * kk), IDESC, term != 0 || kk != 0 || kb != 0);
+              if (term == 0)  // dz's second term
+                tc::mma_bf16_pair(d, ad + uint64_t((kDxABlock >> 4) + 2 * kk), bd + uint64_t(2 * kk), IDESC, 1u);
+            }
+            tc::mma_commit_pair_mc(empty_bar(s), 0x3);
+            issued = true;
+            if (++s == uint32_t(S)) {
+              s = 0;
+              phase ^= 1u;
+            }
+          }
         }
         if (!ok) break;
         tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
@@ -1208,9 +1240,9 @@ __global__ void __launch_bounds__(kDxThreads, 1)
   } else {
     const int w = warp - 2, q = warp & 3, part = w / 4;
     const uint32_t tempty_leader = tc::mapa(tempty_bar(0), 0);
-    const uint32_t slots = sSlots + uint32_t(w) * (kDxSlots * kDxSlotBytes);
+    const uint32_t slots = sSlots + uint32_t(w) * (SLOTS * kDxSlotBytes);
     // This warp's pieces: (tile, c), c = 0 or 1, column c * 32 of its quarter of the tile; those that lie
-    // wholly past dx are left out. Piece n is in slot n % 3.
+    // wholly past dx are left out. Piece n is in slot n % SLOTS.
     struct Piece {
       int tile, c;
     };
@@ -1228,7 +1260,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     uint32_t loads = 0, done = 0;
     auto load = [&]() {  // lane 0: the next piece's dx_in into its slot, which its last store has left
       if (p.has_in && ahead.tile < tile1) {
-        const uint32_t s = loads % kDxSlots;
+        const uint32_t s = loads % SLOTS;
         tc::mbar_arrive_expect_tx(slot_bar(w, s), kDxSlotBytes);
         tc::tma_load_2d(slots + s * kDxSlotBytes, &tmIn, slot_bar(w, s), col_of(ahead), row_of(ahead));
         next(ahead);
@@ -1237,7 +1269,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     };
     if (lane == 0) {
       load();
-      load();
+      if (SLOTS > 1) load();
     }
     bool ok = true;
     uint32_t tcount = 0;
@@ -1251,15 +1283,15 @@ __global__ void __launch_bounds__(kDxThreads, 1)
       for (int c = 0; c < 2; ++c) {
         const Piece x{tile, c};
         if (!inside(x)) continue;
-        const uint32_t s = done % kDxSlots, slot = slots + s * kDxSlotBytes;
+        const uint32_t s = done % SLOTS, slot = slots + s * kDxSlotBytes;
         uint32_t r[32];
         tc::tmem_ld_32x32b_x32(tmem_base + (uint32_t(q * 32) << 16) + a * kDxBN + part * 64 + c * 32, r);
         tc::tmem_ld_wait();
         if (p.has_in) {
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(slot_bar(w, s), (done / kDxSlots) & 1u, kRtWaitNs, abort_flag));
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(slot_bar(w, s), (done / SLOTS) & 1u, kRtWaitNs, abort_flag));
           if (!ok) { fail(); break; }
         } else {
-          if (lane == 0) tc::bulk_wait_read<kDxSlots - 1>();  // the slot's last store has read it
+          if (lane == 0) tc::bulk_wait_read<SLOTS - 1>();  // the slot's last store has read it
           __syncwarp();
         }
         const float *cs = p.col_scale + col_of(x);
@@ -1286,7 +1318,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
           tc::tma_store_2d(&tmOut, slot, col_of(x), row_of(x));
           tc::bulk_commit();
           if (p.has_in) {
-            tc::bulk_wait_read<1>();  // the store before this one, from the slot that is loaded now
+            tc::bulk_wait_read<(SLOTS > 1 ? 1 : 0)>();  // the store before this one (with one slot: this one) has left its slot
             load();
           }
         }
@@ -1298,7 +1330,7 @@ __global__ void __launch_bounds__(kDxThreads, 1)
     }
     if (lane == 0) {
       for (uint32_t n = done; n < loads; ++n)  // (after an abort: loads nothing read)
-        if (!tc::mbar_wait(slot_bar(w, n % kDxSlots), (n / kDxSlots) & 1u, kRtWaitNs, &no_abort)) fail();
+        if (!tc::mbar_wait(slot_bar(w, n % SLOTS), (n / SLOTS) & 1u, kRtWaitNs, &no_abort)) fail();
       tc::bulk_wait0();
     }
     __syncwarp();
@@ -1316,8 +1348,8 @@ __global__ void __launch_bounds__(kDxThreads, 1)
 int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int T, int d, int E, uint16_t *dx, char *ws,
                     cudaStream_t s) {
   const int NP = route_tc_np(E), d_pad = (d + 63) / 64 * 64;
-  __half *w16 = reinterpret_cast<__half *>(ws), *z16 = w16 + size_t(d_pad) * NP;
-  float *col_scale = reinterpret_cast<float *>(z16 + size_t(T) * NP), *row_scale = col_scale + d_pad;
+  __half *w16 = reinterpret_cast<__half *>(ws), *z16 = w16 + size_t(d_pad) * (2 * NP);
+  float *col_scale = reinterpret_cast<float *>(z16 + size_t(T) * (2 * NP)), *row_scale = col_scale + d_pad;
   const char *what = "moe_route_dx: factors";
   const int64_t rows = int64_t(d_pad) + T;
   const int grid0 = int(std::min<int64_t>((rows + 7) / 8, int64_t(moe::num_sms()) * 32));
@@ -1332,14 +1364,15 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
   p.nkb = (NP + kRtBK - 1) / kRtBK;
   p.n_tiles = (d + kDxBN - 1) / kDxBN;
   p.tiles = (T + 2 * kRtBM - 1) / (2 * kRtBM) * p.n_tiles;
-  p.stages = route_dx_stages(p.nkb);
+  const int slots = route_dx_slots(p.nkb);
+  p.stages = route_dx_stages(p.nkb, slots);
   p.has_in = dx_in != nullptr;
   p.row_scale = row_scale;
   p.col_scale = col_scale;
   CUtensorMap mz, mw, mi, mo;
   int st;
-  if ((st = moe::make_map(&mz, z16, uint64_t(T), uint64_t(NP), kRtBK, kRtBM, "router dx dz"))) return st;
-  if ((st = moe::make_map(&mw, w16, uint64_t(d), uint64_t(NP), kRtBK, kDxBN / 2, "router dx w"))) return st;
+  if ((st = moe::make_map(&mz, z16, uint64_t(T), uint64_t(2 * NP), kRtBK, kRtBM, "router dx dz"))) return st;
+  if ((st = moe::make_map(&mw, w16, uint64_t(d), uint64_t(2 * NP), kRtBK, kDxBN / 2, "router dx w"))) return st;
   if ((st = moe::make_map(&mo, dx, uint64_t(T), uint64_t(d), 32, 32, "router dx", CU_TENSOR_MAP_SWIZZLE_64B))) return st;
   mi = mo;
   if (dx_in != nullptr &&
@@ -1356,24 +1389,25 @@ int launch_route_dx(const float *dz, const float *w, const uint16_t *dx_in, int 
   cfg.blockDim = dim3(kDxThreads);
   cfg.stream = s;
   cfg.attrs = at;
-  static int fit[64] = {};  // pairs at once on each device (one CTA per SM, whatever the sizes)
-  int &pairs = fit[moe::device_slot()];
+  auto kern = slots == 3 ? route_dx_kernel<3> : route_dx_kernel<1>;
+  static int fit[2][64] = {};  // pairs at once on each device (one CTA per SM, whatever the sizes)
+  int &pairs = fit[slots == 3][moe::device_slot()];
   if (!pairs) {
-    cudaError_t e = cudaFuncSetAttribute(route_dx_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRtMaxSmem);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
     cfg.gridDim = dim3(2 * (moe::num_sms() / 2));
     cfg.dynamicSmemBytes = kRtMaxSmem;
     cfg.numAttrs = 1;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, route_dx_kernel, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
     if (e != cudaSuccess) return moe::cuda_status(e, what);
     if (n <= 0) return moe::set_error(MOE_ERR_CUDA, "%s: no co-resident CTA pair fits", what);
     pairs = n;
   }
   cfg.gridDim = dim3(2 * std::min(p.tiles, pairs));
-  cfg.dynamicSmemBytes = route_dx_smem(p.nkb, p.stages);
+  cfg.dynamicSmemBytes = route_dx_smem(p.nkb, p.stages, slots);
   cfg.numAttrs = 2;
-  MOE_LAUNCH("route_dx", s, cudaLaunchKernelEx(&cfg, route_dx_kernel, mz, mw, mi, mo, p));
+  MOE_LAUNCH("route_dx", s, cudaLaunchKernelEx(&cfg, kern, mz, mw, mi, mo, p));
   return moe::launch_status(what);
 }
 
@@ -1473,7 +1507,7 @@ size_t route_dz3_bytes(int T, int E) {
 }
 size_t route_dx_bytes(int T, int d, int E) {
   const size_t rows = size_t(std::max(T, 0)) + size_t((d + 63) / 64 * 64);
-  return rows * (size_t(route_tc_np(E)) * 2 + 4);
+  return rows * (size_t(route_tc_np(E)) * 4 + 4);
 }
 size_t route_dw_partial_bytes(int T, int d, int E) {
   if (T <= 0) return 0;

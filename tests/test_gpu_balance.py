@@ -637,3 +637,23 @@ def test_dense_router_backward_of_many_tokens_of_one_sign(T, d, E):
     chain = -(-(-(-kb // 64)) // 4)
     tol = (1 + 2 * 48 + chain + 2 + 64) * 2 ** -24
     assert ((dw.double() - ref).abs() <= tol * ref).all(), float(((dw.double() - ref).abs() / ref).max())
+
+
+def _dx_bound_cancelled(ref, size, E, dz, w):
+    # the result's rounding to bf16 (2^-8); factors of two half-precision terms (2^-22 of a value, or 2^-39 of its row's
+    # largest), the product of both second terms left out (2^-22), three fp32 additions per 16 experts that truncate (2^-23)
+    small = 2.0 ** -39 * E * 2 * np.abs(dz).max(1, keepdims=True) * np.abs(w).max(1)
+    return 2 ** -8 * np.abs(ref) + (1 + 2 ** -8) * ((3 * 2 ** -22 + 3 * -(-E // 16) * 2 ** -23) * size + small) + 1e-37
+
+
+@pytest.mark.parametrize("T,d,E,k", ROUTER + [(700, 296, 192, 4), (300, 520, 240, 4)])
+def test_route_dx_carries_more_bits_than_its_result(T, d, E, k):
+    """dx_in cancels the product but for bf16's rounding: what is left of the product's own error shows."""
+    _, w, _, _, _, dz, _ = _router_inputs(T, d, E, k, T + E + 3)
+    z64, w64 = dz.double().numpy(), w.double().numpy()
+    prod, size = z64 @ w64.T, np.abs(z64) @ np.abs(w64).T
+    dx_in = torch.from_numpy(-prod).to(torch.bfloat16)
+    ref = prod + dx_in.double().numpy()
+    got = _dx(dz, w, dx_in.cuda(), k).double().cpu().numpy()
+    bound = _dx_bound_cancelled(ref, size, E, z64, w64)
+    assert (np.abs(got - ref) <= bound).all(), (np.abs(got - ref) / bound).max()
