@@ -164,6 +164,9 @@ int moe_load_stats(const int32_t *topk_idx, int T, int k, int E, int32_t *counts
  *   loss[1]     = z_coef / M * sum_t lse[t]^2               (both 0 without valid tokens)
  *   lse[t]      = log sum_e exp(logits[t,e])                (-inf for tokens that are not valid)
  *   n_tokens    = n_0 .. n_{n_seq-1}, M, N
+ * Published coefficients: Mixtral's batch loss, as commonly computed, is alpha E sum_e (counts[e] / T) prob[e], not divided by
+ * k: coef = k alpha. DeepSeek-V3's sequence loss divides by k as here, coef = alpha, but its mean is over normalised
+ * sigmoid affinities; prob here is always the softmax's, the probability that this router's gates are made of.
  * logits [T,E] fp32 (logits_out of moe_route); topk_idx [T,k] int32; active_mask [E] uint8 or NULL
  * (all live); token_mask [T] uint8 or NULL (all); seq_offsets [n_seq+1] int32, ascending, inside [0, T]
  * (else MOE_DEV_BAD_OFFSETS, and the results are undefined), or NULL; loss [2] fp32; counts, prob
@@ -520,8 +523,8 @@ int moe_grouped_ffn_bwd_wgrad_gather(const uint16_t *d_out_perm, const uint16_t 
 /*
  * Activation checkpoints in 8 bits (no counterpart in the paper). What a layer keeps from its forward
  * to its backward pass, besides the routing: its input x and the pre-activations [A|B]. X_perm and H, the
- * other operands of the backward, are made again from them. At T=65536, d=7168, F=2048, top-8 that is 2.8 GB a layer
- * instead of 15.5 GB.
+ * other operands of the backward, are made again from them. At T=65536, d=7168, F=2048, top-8, 171 experts: x, X_perm, [A|B]
+ * and H are 15.5 GB a layer in bf16, x and [A|B] alone 5.4 GB, and 2.8 GB in 8 bits.
  * Format: 32 consecutive values of a row (a row's last block may be shorter) share the scale 2^(s - 127),
  * the smallest power of two with which the largest of them is at most 448 (s >= 1); each value is
  * the E4M3 code nearest to value / scale, ties to even: off by at most 2^-4 of itself, or by 2^-10 scales
@@ -553,7 +556,8 @@ int moe_ckpt_permute(const uint8_t *q, const uint8_t *scale, const int32_t *row_
 
 /*
  * moe_grouped_ffn_fwd_ckpt - moe_grouped_ffn_fwd that keeps [A|B] in 8 bits instead of ab_saved:
- * the gate/up GEMM's epilogue packs its fp32 accumulators. h and out_perm are moe_grouped_ffn_fwd's, bit for bit.
+ * the gate/up GEMM's epilogue packs its fp32 accumulators, those that h is made from (so a product near the border of two
+ * codes can go to the one that the exact sum would not). h and out_perm are moe_grouped_ffn_fwd's, bit for bit.
  * ab_q: rows_cap*2F bytes, codes of the [rows, 2F] matrix [A|B] in 32-row blocks, element (r, c) at
  * ((r/32)*(2F/16) + c/16)*512 + (r%32)*16 + c%16; ab_scale: rows_cap*2F/32 bytes, the s of row r and
  * columns 32 b .. 32 b + 31 at ((r/32)*(2F/32) + b)*32 + r%32; both 16-byte aligned. Other arguments and

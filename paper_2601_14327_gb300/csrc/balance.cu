@@ -1,8 +1,8 @@
 // Balance loss and z-loss of the router, with their gradient with respect to the logits.
 //
 // The auxiliary losses that LAEP is compared with: the load share of every expert times the
-// router's mean probability of it, over the whole batch (the Mixtral form) or sequence by sequence
-// (the DeepSeek-V3 form). Per sequence s with n_s valid tokens, c[s,e] assignments of them to
+// router's mean probability of it, over the whole batch (as Mixtral's) or sequence by sequence
+// (as DeepSeek-V3's; moe_laep.h says how their coefficients carry over). Per sequence s with n_s valid tokens, c[s,e] assignments of them to
 // expert e, and E' live experts:
 //   p[t,:] = softmax over the live experts of z[t,:],  P[s,e] = mean of p[t,e] over the sequence
 //   f[s,e] = c[s,e] E' / (k n_s)                        (1 where the load is even)
@@ -656,9 +656,14 @@ __global__ void __launch_bounds__(32 * kMaxWarps, 1) balance_bwd_kernel(
 // Warps of a block: enough for its tokens at once, up to what an SM holds.
 int block_warps(int tokens, int E) { return std::min(kMaxWarps, (tokens + warp_tokens(E) - 1) / warp_tokens(E)); }
 // The forward in one block, a launch less than the two kernels: up to four rounds of its warps' tokens, and three
-// sequences, which it takes one after another (~1.4 us each). Forward and backward, two kernels / one block: 13.7 /
-// 11.6 us at 37 tokens of 64 experts, 14.2 / 11.8 in 3 sequences, 14.2 / 15.3 at 200 tokens in 4; 13.7 / 12.9 at 200
-// tokens of 256 experts, 14.1 / 16.1 at 400.
+// sequences, which it takes one after another (~2 us each, where the two kernels take them side by side). Forward and
+// backward replayed from a graph, us, two kernels / one block, at 16, 37, 100, 200 tokens of 64 experts:
+//   1 sequence   10.4 / 5.9    11.3 / 6.3    11.9 / 7.5    11.9 / 8.0
+//   3 sequences  12.9 / 10.5   13.2 / 10.8   13.7 / 12.0   14.1 / 12.6
+//   4 sequences  13.3 / 12.4   12.6 / 12.4   12.8 / 14.1   13.8 / 15.3
+//   6 sequences  15.8 / 17.0   13.3 / 16.0   13.6 / 18.1   14.2 / 19.2
+// and with 256 experts 16.7 / 15.5 for 37 tokens in 3 sequences, 16.9 / 17.8 in 4. In the tokens the two meet at four
+// rounds: 11.8 / 9.4 at 384 of 64 experts in 1 sequence, 11.9 / 13.6 in 3.
 bool one_block(int T, int E, int n_seq) { return T <= 4 * kMaxWarps * warp_tokens(E) && n_seq <= 3; }
 // Lanes per token and logits per lane for E experts; whether a row of logits is whole 16-byte vectors.
 template <typename F> void with_lanes(int E, bool vec, F f) {

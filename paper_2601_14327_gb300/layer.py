@@ -271,7 +271,8 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
     and running those memory-bound kernels beside the GEMMs slowed the GEMMs by more
     than it hid (96.1-96.7 against 97.0-97.3 ms per step).
 
-    After a forward with balance, dw_router and dx hold the auxiliary losses' gradient too; d_loss [2]
+    After a forward with balance, dw_router and dx hold the auxiliary losses' gradient too (dx is then rounded to bf16
+    once more, where the losses' share is added); d_loss [2]
     fp32 on the device: the gradient of the losses (None: ones).
     ckpt: the layer's checkpoint, as in forward(): X_perm, x and H come from its 8 bits.
     Returns (dx, dw_gate_up, dw_down, dw_router)."""
@@ -325,6 +326,9 @@ def backward(b: MoELayerBuffers, dy, w_router, w_gate_up, w_down, stream=None,
     L.moe_permute_bwd(b.dx_perm, kept.row_of_assignment, kept.topk_idx, None, None, s.T, s.d, s.E,
                       s.k, b.dx, b.ws, b.ws_bytes, side)
     if bal is not None:
+        # dx is rounded to bf16 by the call above and again by this one: half a step more, as much as each of the
+        # k rows of dx_perm has. An fp32 sum in between would be 2 T d more bytes written and read (~280 us at T=65536,
+        # d_model=7168, beside ~1,500 for the two calls).
         L.moe_route_dx(b.dz, w_router, b.dx, s.T, s.d, s.E, s.k, b.dx, b.ws, b.ws_bytes, side)
     if b.gather:
         L.moe_grouped_ffn_bwd_wgrad_gather(b.d_out_perm, b.x, b.token_of_row, s.T, b.h, b.d_ab,
