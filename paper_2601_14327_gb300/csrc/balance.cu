@@ -43,9 +43,9 @@ int warp_tokens(int E) { return E <= 16 ? 8 : E <= 64 ? 4 : 2; }
 // block's warps: a lane adds fp32 numbers one after another, and addends that are nearly equal round the same
 // way each time (2,300 rounds of equal tokens, T = 2^26: 3.4e-5 off).
 constexpr int kMaxRounds = 80;
-int even_chunk(int T) { return std::max(8, (T + 151) / 152); }
+int even_chunk(int T) { return std::max(8, T / 152 + (T % 152 != 0)); }
 int chunk_tokens(int T, int E) { return std::min(even_chunk(T), kMaxRounds * kMaxWarps * warp_tokens(E)); }
-int chunk_count(int T, int chunk) { return (T + chunk - 1) / chunk; }
+int chunk_count(int T, int chunk) { return T / chunk + (T % chunk != 0); }
 int expert_groups(int E) { return (E + 31) / 32; }
 
 // Workspace: the ticket of the last block, then the partial sums.

@@ -145,3 +145,11 @@ def test_dense_router_backward_refusals(call, bad, status):
     with pytest.raises(L.MoEError) as e:
         call(**bad)
     assert e.value.status == status
+
+
+@pytest.mark.parametrize("E,n_seq", [(1, 1), (64, 3), (256, 1 << 20)])
+def test_balance_workspace_size_of_any_number_of_tokens(E, n_seq):
+    """Ascending in T up to the largest int, also where the entry points refuse T."""
+    sizes = [L.moe_balance_workspace_size(T, E, n_seq) for T in (0, 1, 1000, 1 << 20, 1 << 30, 2 ** 31 - 200, 2 ** 31 - 1)]
+    assert sizes == sorted(sizes) and sizes[-1] < 1 << 40, sizes
+    assert L.moe_balance_workspace_size(-1, E, n_seq) == 0
