@@ -646,7 +646,7 @@ def _dx_bound_cancelled(ref, size, E, dz, w):
     return 2 ** -8 * np.abs(ref) + (1 + 2 ** -8) * ((3 * 2 ** -22 + 3 * -(-E // 16) * 2 ** -23) * size + small) + 1e-37
 
 
-@pytest.mark.parametrize("T,d,E,k", ROUTER + [(700, 296, 192, 4), (300, 520, 240, 4)])
+@pytest.mark.parametrize("T,d,E,k", ROUTER + [(700, 296, 192, 4), (300, 520, 240, 4), (130, 264, 65, 2), (300, 72, 130, 2), (200, 2872, 225, 8)])
 def test_route_dx_carries_more_bits_than_its_result(T, d, E, k):
     """dx_in cancels the product but for bf16's rounding: what is left of the product's own error shows."""
     _, w, _, _, _, dz, _ = _router_inputs(T, d, E, k, T + E + 3)
