@@ -513,3 +513,21 @@ def test_balance_loss_in_the_other_forms_of_the_layer(T, d, E, k, F, masked, kw)
             assert_close("y", to_np(v), to_np(u))
         else:
             assert torch.equal(u, v), n
+
+
+def test_kept_logits_beside_a_checkpoint():
+    """keep_logits with a checkpoint and a balance loss: the same logits in the buffers, and the same step."""
+    T, d, E, k, F = 333, 128, 12, 3, 128
+    inp, o, mask, z = _layer_inputs(T, d, E, k, F, 2)
+    g, m = {n: v.cuda() for n, v in inp.items()}, torch.from_numpy(mask).cuda()
+    s = layer.LayerShape(T, d, E, k, F)
+    got = []
+    for keep in (False, True):
+        b, c = layer.MoELayerBuffers(s, "cuda", balance_seqs=1, ckpt=True), layer.MoECheckpoint(s, "cuda", 1)
+        b.logits.fill_(7.0)
+        y = layer.forward(b, g["x"], g["w_router"], g["bias"], g["w_gate_up"], g["w_down"], m, keep_logits=keep,
+                          balance=layer.BalanceLoss(0.3, 0.1), ckpt=c)
+        got.append([y, c.loss, c.topk_idx, c.topk_gate, c.counts, c.logits])
+        assert torch.equal(b.logits, c.logits) if keep else (b.logits == 7).all()
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
