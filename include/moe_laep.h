@@ -71,7 +71,8 @@ enum {
   MOE_DEV_COUNT_MISMATCH = 3,/* counts disagree with the routing */
   MOE_DEV_WAIT_TIMEOUT = 4,  /* a pipeline wait in a GEMM kernel gave up */
   MOE_DEV_ROWS_OVERFLOW = 5, /* grouped layout would exceed R rows */
-  MOE_DEV_BAD_OFFSETS = 6    /* seq_offsets descend or leave [0, T] */
+  MOE_DEV_BAD_OFFSETS = 6,   /* seq_offsets descend or leave [0, T] */
+  MOE_DEV_BAD_TARGET = 7     /* a target at or above V */
 };
 
 /* Library version (major*10000 + minor*100 + patch). */
@@ -199,6 +200,93 @@ int moe_balance_loss_bwd(const float *logits, const uint8_t *active_mask, const 
                          int n_seq, int T, int E, int k, float coef, float z_coef,
                          const int32_t *counts, const int32_t *n_tokens, const float *lse,
                          const float *d_loss, float *dz, moe_stream_t stream);
+
+/*
+ * moe_vocab_loss - the language-modelling loss at the end of the model: softmax cross entropy of the hidden
+ * states' logits over the vocabulary, and the z-loss of their normaliser. The paper names the pre-training
+ * loss (its figures plot it) and prints no formula; this is the usual one.
+ *   z[t,v]  = sum_i hidden[t,i] * w_vocab[v,i]                       (fp32 accumulation; never in memory)
+ *   lse[t]  = log sum_v exp(z[t,v])                                  (every token)
+ *   nll[t]  = lse[t] - z[t,target[t]]                                (0 for tokens without a target)
+ *   loss[0] = 1/M * sum_t nll[t],  loss[1] = z_coef/M * sum_t lse[t]^2   over the M tokens with a target
+ *                                                                    (both 0 when M is 0)
+ * A token whose target is negative has none: it is left out (padding, prompts). A target at or above V is
+ * left out too and sets MOE_DEV_BAD_TARGET.
+ * hidden [T,d], w_vocab [V,d] bf16, 16-byte aligned; target [T] int32; loss [2], nll [T], lse [T] fp32,
+ * n_valid [1] int32 = M (all overwritten). piece >= 1: tokens that are worked on at a time (min(piece, T) sets
+ * the workspace: V/16 bytes a token here). ws: of moe_vocab_loss_workspace_size(T, d, V, piece, 0) bytes,
+ * 16-byte aligned, used until the call's kernels end. All sums run in a fixed order: bitwise reproducible, and
+ * independent of piece. A NaN or +inf among a token's logits makes its lse and nll NaN, and loss with them
+ * when it has a target.
+ * Limits: d % 8 == 0, 8 <= d <= 2^20, 0 <= T <= 2^24, 1 <= V <= 2^24, T*d, V*d and min(piece,T)*V at most 2^38.
+ */
+int moe_vocab_loss(const uint16_t *hidden, const uint16_t *w_vocab, const int32_t *target, int T, int d, int V,
+                   int piece, float z_coef, float *loss, float *nll, float *lse, int32_t *n_valid, void *ws,
+                   size_t ws_bytes, moe_stream_t stream);
+
+/* Bytes of `ws` for moe_vocab_loss (grad 0) or moe_vocab_loss_grad (grad 1); 0 for sizes outside the limits.
+ * With grad, min(piece, T) * (2 V + V/16) bytes, the partial sums of d_hidden when that has few tiles, and
+ * 4 V d bytes when piece < T. */
+size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad);
+
+/*
+ * moe_vocab_loss_grad - moe_vocab_loss and its gradient in one call (the logits are not made twice):
+ *   dz[t,v]  = d_loss[0]/M * (p[t,v] - [v == target[t]]) + d_loss[1] * 2 z_coef/M * lse[t] * p[t,v],
+ *              p = exp(z - lse);  0 for tokens without a target
+ *   d_hidden[t,:] = sum_v dz[t,v] * w_vocab[v,:],   d_w[v,:] = sum_t dz[t,v] * hidden[t,:]
+ * Arguments as in moe_vocab_loss; d_loss [2] fp32 (device) or NULL (ones); d_hidden [T,d], d_w [V,d] bf16
+ * (overwritten; either may be NULL: not computed; not both). dz is held in bf16, a piece of `piece` tokens at a
+ * time (the exponentials it is made from in half precision, relative to the largest of 128 columns; p - 1 at the
+ * target is exact to fp32 however sure the token is); the products accumulate in fp32. d_w's sum over pieces is
+ * kept in fp32 in ws and rounded once. Results are bitwise reproducible; d_w's last bits depend on piece, d_hidden's on
+ * it where its reduction is split (few tokens). `hidden` has to be finite also for tokens without a target: their rows
+ * enter d_w times 0.
+ */
+int moe_vocab_loss_grad(const uint16_t *hidden, const uint16_t *w_vocab, const int32_t *target, int T, int d, int V,
+                        int piece, float z_coef, const float *d_loss, float *loss, float *nll, float *lse,
+                        int32_t *n_valid, uint16_t *d_hidden, uint16_t *d_w, void *ws, size_t ws_bytes,
+                        moe_stream_t stream);
+
+/*
+ * moe_orthogonalize - the update direction of the Muon optimiser for a stack of matrices: `steps`
+ * Newton-Schulz products that take a matrix towards the orthogonal factor of its polar decomposition
+ * (Jordan et al. 2024; for the experts' gradients as moe_grouped_ffn_bwd_wgrad leaves them).
+ *   X = g / (|g|_F + eps);  for each step's (a, b, c):  A = X X^T;  X = a X + (b A + c A A) X;   out = X
+ * (with X^T X from the right where rows > cols: the same polynomial of g's singular values.)
+ * g, out [n_mats, rows, cols] bf16, 16-byte aligned (out may be g). Matrix i belongs to expert
+ * i / mats_per_expert: dw_gate_up [E,2F,d] is 2E matrices [F,d] with mats_per_expert 2, dw_down [E,d,F] is E matrices.
+ * active_mask [n_mats / mats_per_expert] uint8 or NULL (all): matrices of pruned experts (0) are neither read nor written.
+ * coef: HOST, 3 * steps floats (a, b, c of each step) or NULL (3.4445, -4.7750, 2.0315 each); 1 <= steps <= 16;
+ * eps > 0. ws: of moe_orthogonalize_workspace_size bytes, 16-byte aligned, used until the call's kernels end; as many
+ * matrices are worked on at a time as it holds (at least 1; the results do not depend on it).
+ * Products of half-precision operands with fp32 accumulation; X is kept to 22 bits between the steps. Components
+ * more than ~2^-24 / sqrt(max(rows, cols)) below g's norm are lost. With coefficients whose polynomials stay within
+ * [0, 4] on [0, 1] nothing overflows. Bitwise reproducible. An infinity or NaN in a matrix makes its result NaN, a
+ * zero matrix gives zeros.
+ * Limits: 1 <= rows, cols <= 16384, n_mats <= 2^20.
+ */
+int moe_orthogonalize(const uint16_t *g, const uint8_t *active_mask, int n_mats, int mats_per_expert, int rows,
+                      int cols, const float *coef, int steps, float eps, uint16_t *out, void *ws, size_t ws_bytes,
+                      moe_stream_t stream);
+
+/* Bytes of `ws` for moe_orthogonalize and moe_muon_step with min(batch, n_mats) matrices at a time (~6 bytes an
+ * element and 4 a square of the short side); 0 for sizes outside the limits or batch < 1. */
+size_t moe_orthogonalize_workspace_size(int n_mats, int rows, int cols, int batch);
+
+/*
+ * moe_muon_step - one step of the Muon optimiser on a stack of matrices: momentum, its orthogonalised
+ * update, new weights.
+ *   momentum = mu * momentum + grad;  u = nesterov ? grad + mu * momentum : momentum
+ *   w = (1 - lr * weight_decay) * w - lr * scale * moe_orthogonalize(u)
+ * grad [n_mats, rows, cols] bf16, momentum fp32 (in, out), w bf16 (in, out); master fp32 (in, out) or NULL: with it the
+ * step is taken on master and w is its rounding (w is then not read). All 16-byte aligned, none overlapping another.
+ * nesterov 0 or 1. `scale` is the caller's factor for the shape, e.g. 0.2 * sqrt(max(rows, cols)).
+ * Matrices of pruned experts keep their w, master and momentum. Other arguments and limits as in moe_orthogonalize.
+ */
+int moe_muon_step(uint16_t *w, float *master, const uint16_t *grad, float *momentum, const uint8_t *active_mask,
+                  int n_mats, int mats_per_expert, int rows, int cols, float lr, float weight_decay, float mu,
+                  int nesterov, float scale, const float *coef, int steps, float eps, void *ws, size_t ws_bytes,
+                  moe_stream_t stream);
 
 /*
  * laep_prune_mask - LAEP expert-pruning decision for one layer (HOST call).

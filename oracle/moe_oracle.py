@@ -606,3 +606,48 @@ def ckpt_round(x):
     v = np.ldexp(np.round(y / step) * step, e[:, :, None])
     v[bad] = np.nan
     return v.reshape(rows, -1)[:, :cols], np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def vocab_loss(hidden, w_vocab, target, z_coef=0.0, d_loss=(1.0, 1.0)):
+    """Softmax cross entropy over a vocabulary with a z-loss, and its gradients.
+
+    loss = (1/M sum nll, z_coef/M sum lse^2) over the M tokens with a target in [0, V); nll is 0 elsewhere.
+    """
+    h, w, t = np.asarray(hidden, np.float64), np.asarray(w_vocab, np.float64), np.asarray(target)
+    T, V = h.shape[0], w.shape[0]
+    z = h @ w.T
+    m = z.max(axis=1, keepdims=True) if T else np.zeros((0, 1))
+    lse = (m + np.log(np.exp(z - m).sum(axis=1, keepdims=True)))[:, 0]
+    ok = (t >= 0) & (t < V)
+    rows = np.flatnonzero(ok)
+    M = len(rows)
+    nll = np.zeros(T)
+    nll[rows] = lse[rows] - z[rows, t[rows]]
+    n = max(M, 1)
+    p = np.exp(z - lse[:, None])
+    dz = p * (d_loss[0] / n + d_loss[1] * 2 * z_coef / n * lse)[:, None]
+    # p - 1 = expm1(-nll): no cancellation at a sure token
+    dz[rows, t[rows]] = (d_loss[0] / n * np.expm1(-nll[rows])
+                         + d_loss[1] * 2 * z_coef / n * lse[rows] * p[rows, t[rows]])
+    dz[~ok] = 0
+    return {"loss": np.array([nll.sum() / n, z_coef * (lse[rows] ** 2).sum() / n]), "nll": nll, "lse": lse,
+            "n_valid": M, "dz": dz, "d_hidden": dz @ w, "d_w": dz.T @ h, "z": z}
+
+
+def newton_schulz(g, coef=(3.4445, -4.7750, 2.0315), steps=5, eps=1e-7):
+    """Newton-Schulz products of one matrix; coef: one (a, b, c) or one per step."""
+    x = np.asarray(g, np.float64)
+    x = x / (np.sqrt((x * x).sum()) + eps)
+    rows = [coef] * steps if np.isscalar(coef[0]) else coef
+    for a, b, c in rows:
+        s = x @ x.T
+        x = a * x + (b * s + c * s @ s) @ x
+    return x
+
+
+def muon_step(w, grad, momentum, lr, weight_decay=0.0, mu=0.95, nesterov=True, scale=1.0, **ns):
+    """(w, momentum) after one step of the Muon optimiser on one matrix."""
+    g, m = np.asarray(grad, np.float64), np.asarray(momentum, np.float64)
+    m = mu * m + g
+    u = g + mu * m if nesterov else m
+    return np.asarray(w, np.float64) * (1 - lr * weight_decay) - lr * scale * newton_schulz(u, **ns), m

@@ -21,7 +21,7 @@ STATUS_NAMES = {0: "MOE_OK", -1: "MOE_ERR_ARG", -2: "MOE_ERR_UNSUPPORTED", -3: "
                 -4: "MOE_ERR_INVARIANT", -5: "MOE_ERR_TIMEOUT", -6: "MOE_ERR_WORKSPACE"}
 DEV_NAMES = {0: "MOE_DEV_OK", 1: "MOE_DEV_BAD_EXPERT", 2: "MOE_DEV_TOO_FEW_LIVE",
              3: "MOE_DEV_COUNT_MISMATCH", 4: "MOE_DEV_WAIT_TIMEOUT", 5: "MOE_DEV_ROWS_OVERFLOW",
-             6: "MOE_DEV_BAD_OFFSETS"}
+             6: "MOE_DEV_BAD_OFFSETS", 7: "MOE_DEV_BAD_TARGET"}
 
 
 class MoEError(RuntimeError):
@@ -81,6 +81,12 @@ _SIGS = {
     "moe_balance_workspace_size": (SZ, [I, I, I]),
     "moe_balance_loss": (I, [P, P, P, P, P, I, I, I, I, F32, F32, P, P, P, P, P, P, SZ, P]),
     "moe_balance_loss_bwd": (I, [P, P, P, I, I, I, I, F32, F32, P, P, P, P, P, P]),
+    "moe_vocab_loss": (I, [P, P, P, I, I, I, I, F32, P, P, P, P, P, SZ, P]),
+    "moe_vocab_loss_workspace_size": (SZ, [I, I, I, I, I]),
+    "moe_vocab_loss_grad": (I, [P, P, P, I, I, I, I, F32, P, P, P, P, P, P, P, P, SZ, P]),
+    "moe_orthogonalize": (I, [P, P, I, I, I, I, P, I, F32, P, P, SZ, P]),
+    "moe_orthogonalize_workspace_size": (SZ, [I, I, I, I]),
+    "moe_muon_step": (I, [P, P, P, P, P, I, I, I, I, F32, F32, F32, I, F32, P, I, F32, P, SZ, P]),
 }
 
 
@@ -427,6 +433,56 @@ def moe_balance_loss_bwd(logits, active_mask, seq_offsets, n_seq, T, E, k, coef,
     _check("moe_balance_loss_bwd", load().moe_balance_loss_bwd(
         _ptr(logits), _ptr(active_mask), _ptr(seq_offsets), n_seq, T, E, k, coef, z_coef,
         _ptr(counts), _ptr(n_tokens), _ptr(lse), _ptr(d_loss), _ptr(dz), _stream(stream)))
+
+
+def moe_vocab_loss_workspace_size(T, d, V, piece, grad):
+    return int(load().moe_vocab_loss_workspace_size(T, d, V, piece, int(grad)))
+
+
+def moe_vocab_loss(hidden, w_vocab, target, T, d, V, piece, z_coef, loss, nll, lse, n_valid, ws, ws_bytes,
+                   stream=None):
+    _check("moe_vocab_loss", load().moe_vocab_loss(
+        _ptr(hidden), _ptr(w_vocab), _ptr(target), T, d, V, piece, z_coef, _ptr(loss), _ptr(nll),
+        _ptr(lse), _ptr(n_valid), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_vocab_loss_grad(hidden, w_vocab, target, T, d, V, piece, z_coef, d_loss, loss, nll, lse, n_valid,
+                        d_hidden, d_w, ws, ws_bytes, stream=None):
+    _check("moe_vocab_loss_grad", load().moe_vocab_loss_grad(
+        _ptr(hidden), _ptr(w_vocab), _ptr(target), T, d, V, piece, z_coef, _ptr(d_loss), _ptr(loss),
+        _ptr(nll), _ptr(lse), _ptr(n_valid), _ptr(d_hidden), _ptr(d_w), _ptr(ws), ws_bytes,
+        _stream(stream)))
+
+
+def _coef(coef, steps):
+    """(a, b, c), or one such triple per step, as the C entry points take them (host floats)."""
+    if coef is None:
+        return None
+    rows = [coef] * steps if isinstance(coef[0], (int, float)) else list(coef)
+    if len(rows) != steps or any(len(r) != 3 for r in rows):
+        raise ValueError(f"coef: (a, b, c), or {steps} such triples")
+    return (F32 * (3 * steps))(*(float(v) for r in rows for v in r))
+
+
+def moe_orthogonalize_workspace_size(n_mats, rows, cols, batch):
+    return int(load().moe_orthogonalize_workspace_size(n_mats, rows, cols, batch))
+
+
+def moe_orthogonalize(g, active_mask, n_mats, mats_per_expert, rows, cols, coef, steps, eps, out, ws,
+                      ws_bytes, stream=None):
+    """coef: None, (a, b, c), or `steps` such triples."""
+    _check("moe_orthogonalize", load().moe_orthogonalize(
+        _ptr(g), _ptr(active_mask), n_mats, mats_per_expert, rows, cols, _coef(coef, steps), steps, eps,
+        _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_muon_step(w, master, grad, momentum, active_mask, n_mats, mats_per_expert, rows, cols, lr,
+                  weight_decay, mu, nesterov, scale, coef, steps, eps, ws, ws_bytes, stream=None):
+    """coef: as in moe_orthogonalize."""
+    _check("moe_muon_step", load().moe_muon_step(
+        _ptr(w), _ptr(master), _ptr(grad), _ptr(momentum), _ptr(active_mask), n_mats, mats_per_expert,
+        rows, cols, lr, weight_decay, mu, int(nesterov), scale, _coef(coef, steps), steps, eps, _ptr(ws),
+        ws_bytes, _stream(stream)))
 
 
 def moe_selftest_wait_timeout(limit_ns, stream=None):

@@ -17,8 +17,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libmoe_laep.so")
-SOURCES = ["api.cu", "laep.cu", "route.cu", "permute.cu", "gemm.cu", "balance.cu", "ckpt.cu"]
-HEADERS = ["ckpt.cuh", "common.cuh", "tc_ptx.cuh", "tmap.cuh"]
+SOURCES = ["api.cu", "laep.cu", "route.cu", "permute.cu", "gemm.cu", "balance.cu", "ckpt.cu", "vocab.cu",
+           "muon.cu"]
+HEADERS = ["ckpt.cuh", "common.cuh", "dense_gemm.cuh", "tc_ptx.cuh", "tmap.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

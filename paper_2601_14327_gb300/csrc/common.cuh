@@ -67,6 +67,8 @@ int route_dev_error(int clear, int *code);
 int permute_dev_error(int clear, int *code);
 int gemm_dev_error(int clear, int *code);
 int balance_dev_error(int clear, int *code);
+int vocab_dev_error(int clear, int *code);
+int muon_dev_error(int clear, int *code);
 
 }  // namespace moe
 

@@ -1,0 +1,383 @@
+// Products of dense matrices, and of stacks of them, on CTA pairs (sm_103a): what the vocabulary loss and
+// the orthogonalised update are made of. C[z] = A[z] B[z]^T with fp32 accumulation in tensor memory and an
+// epilogue of the caller's.
+//
+// The pipeline is that of the grouped GEMMs' CTA-pair kernel: a cluster of two CTAs on two SMs computes a
+// 256 x BN tile; each CTA stages its own 128 rows of A and half of B per 128-deep k-block by TMA (128-byte
+// swizzle, 3 stages of 64 KB at BN = 256, 4 of 48 KB at BN = 128); one thread of the even CTA issues
+// tcgen05.mma.cta_group::2 (M = 256); eight epilogue warps per CTA read the accumulator, double-buffered in
+// TMEM, so that the epilogue of a tile runs under the products of the next. Operands are read as they lie in
+// memory: "K" = rows of the operand along the reduction (K-major), "MN" = reduction over its rows.
+// Rows and columns past a matrix's ends are read as zeros by TMA, so any size works without padding.
+// A file that includes this one has said MOE_DEV_ERR_DECL before.
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+#include "tc_ptx.cuh"
+#include "tmap.cuh"
+
+namespace dg {
+
+constexpr int BM = 128;        // rows of a CTA's share of a tile (TMEM lanes)
+constexpr int kTileRows = 256; // rows of a pair's tile
+constexpr int KB = 128;        // k-block of a ring stage
+constexpr int UMMA_K = 16;
+constexpr int kEpiWarps = 8;   // two per TMEM lane quarter, each half of the tile's columns
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr uint64_t kWaitLimitNs = 2000000000ull;
+constexpr uint32_t kStageBytes = 32 * 64;  // an epilogue warp's 32 x 32 chunk of 16-bit values
+
+template <int BN> struct Shape {
+  static constexpr int BNH = BN / 2;
+  static constexpr int STAGES = BN == 256 ? 3 : 4;
+  static constexpr uint32_t A_BYTES = BM * KB * 2;
+  static constexpr uint32_t B_BYTES = BNH * KB * 2;
+  static constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int NBARS = 2 * STAGES + 5;
+  static constexpr size_t SMEM = 1024 + size_t(STAGES) * STAGE_BYTES + NBARS * 8 + 4 * 4 + 1024 + kEpiWarps * kStageBytes;
+  static constexpr uint32_t TMEM_COLS = 2 * BN;
+};
+
+// The tile list. Every CTA works it out from these numbers; a pair takes every `pairs`-th tile.
+struct Tiles {
+  int mats;              // matrices of the stack ...
+  const int *live;       // ... or, where not null: max(0, min(mats, *live - first))
+  int first;
+  int mt, nt;            // 256-row and BN-column tiles of a matrix
+  int nkb;               // k-blocks of 128
+  int splits;            // the reduction in so many ranges, each a tile of its own
+  int sym;               // only tiles at or above the diagonal (mt == columns / 256 rounded up)
+  int group;             // row tiles that take turns before the next column tile (tiles in flight share both operands in L2)
+};
+
+struct Tile {
+  int z, split, mp, nt, kb0, kb1;
+};
+
+__device__ __forceinline__ int tiles_of_matrix(const Tiles &t, int bn) {
+  return t.sym ? t.mt * (t.mt + 1) / 2 * (kTileRows / bn) : t.mt * t.nt;
+}
+
+__device__ __forceinline__ Tile tile_at(const Tiles &t, int per, int u, int bn) {
+  Tile r;
+  r.z = u / (per * t.splits);
+  int q = u - r.z * per * t.splits;
+  r.split = q / per;
+  q -= r.split * per;
+  if (t.sym) {
+    const int sub = kTileRows / bn;
+    const int c = q / sub;  // c-th block of the upper triangle, column by column: block column j has j + 1
+    int j = int((sqrtf(8.f * float(c) + 1.f) - 1.f) * 0.5f);
+    while (j * (j + 1) / 2 > c) --j;
+    while ((j + 1) * (j + 2) / 2 <= c) ++j;
+    r.mp = c - j * (j + 1) / 2;
+    r.nt = j * sub + (q - c * sub);
+  } else {
+    const int band = t.group * t.nt;
+    const int b = q / band, rows = min(t.group, t.mt - b * t.group);
+    q -= b * band;
+    r.nt = q / rows;
+    r.mp = b * t.group + (q - r.nt * rows);
+  }
+  r.kb0 = int((long long)t.nkb * r.split / t.splits);
+  r.kb1 = int((long long)t.nkb * (r.split + 1) / t.splits);
+  return r;
+}
+
+__device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
+}
+
+// Writes this lane's 32 16-bit values (row `lane` of a 32 x 32 chunk) to the warp's staging buffer, in the
+// 64-byte-swizzle layout of a TMA tile, and stores the chunk at (col, row, z) of tensor map `tm`.
+__device__ __forceinline__ void stage_and_store(const CUtensorMap *tm, uint32_t stage, int lane,
+                                                const uint4 (&v)[4], int col, int row, int z) {
+  if (lane == 0) tc::bulk_wait_read0();  // the previous chunk has left the buffer
+  __syncwarp();
+  const uint32_t rowbase = stage + uint32_t(lane) * 64u;
+  const uint32_t sw = (uint32_t(lane) >> 1) & 3u;
+#pragma unroll
+  for (uint32_t c = 0; c < 4; ++c) tc::st_shared_v4(rowbase + ((c ^ sw) << 4), v[c]);
+  tc::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tc::tma_store_3d(tm, stage, col, row, z);
+    tc::bulk_commit();
+  }
+}
+
+// The same chunk transposed: stored at (row, col), so that the lane's row becomes a column.
+__device__ __forceinline__ void stage_and_store_t(const CUtensorMap *tm, uint32_t stage, int lane,
+                                                  const uint4 (&v)[4], int col, int row, int z) {
+  if (lane == 0) tc::bulk_wait_read0();
+  __syncwarp();
+  const uint32_t *w = reinterpret_cast<const uint32_t *>(v);
+  const uint32_t c16 = uint32_t(lane) >> 3, in = (uint32_t(lane) & 7u) * 2u;
+#pragma unroll
+  for (uint32_t c = 0; c < 32; ++c)
+    st_shared_u16(stage + c * 64u + ((c16 ^ ((c >> 1) & 3u)) << 4) + in, uint16_t(w[c >> 1] >> ((c & 1u) * 16u)));
+  tc::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tc::tma_store_3d(tm, stage, row, col, z);
+    tc::bulk_commit();
+  }
+}
+
+// What an epilogue gets of a tile: this thread's accumulator row `row` of matrix z is lane `lane` of the
+// warp's TMEM quarter at `tb`; the warp owns columns [col0 + c0, col0 + c0 + BN / 2) of it.
+struct Warp {
+  int lane, row;       // row of this thread in its matrix
+  int col;             // first column of the warp's half tile
+  int z, split;
+  uint32_t tb;         // TMEM address of the half tile's first column
+  uint32_t stage;      // the warp's staging buffer
+};
+
+// Epi: struct passed to the kernel by value, with the tensor maps it stores through, and
+//   template <int BN> __device__ void run(const Warp &w) const: reads the accumulator and writes the results.
+template <int BN, bool A_MN, bool B_MN, bool HALF, class Epi>
+__global__ void __launch_bounds__(kThreads, 1)
+    dense_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                      const __grid_constant__ Epi epi, const Tiles t) {
+  using Sh = Shape<BN>;
+  constexpr int STAGES = Sh::STAGES, BNH = Sh::BNH;
+  constexpr uint32_t IDESC = HALF ? tc::idesc_f16_f32(2 * BM, BN, A_MN, B_MN) : tc::idesc_bf16_f32(2 * BM, BN, A_MN, B_MN);
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = tc::smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+  uint8_t *smem = smem_raw + pad;
+  const uint32_t sA0 = raw + pad;
+  const uint32_t sB0 = sA0 + STAGES * Sh::A_BYTES;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + STAGES * Sh::STAGE_BYTES);
+  int *misc = reinterpret_cast<int *>(bars + Sh::NBARS);
+  const uint32_t stage_base = (tc::smem_u32(misc + 4) + 1023u) & ~1023u;
+  volatile int *abort_flag = misc + 1;
+  volatile int no_abort = 0;
+
+  const uint32_t bar0 = tc::smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
+  auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
+  auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
+  const uint32_t drain_bar = bar0 + 8u * (2 * STAGES + 4);
+  auto fail = [&]() {
+    dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
+    *abort_flag = 1;
+  };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_ctarank();
+  const bool leader = rank == 0;
+  const int cluster = int(tc::cluster_id_x()), nclusters = int(tc::cluster_count_x());
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      tc::mbar_init(full_bar(s), 1);
+      tc::mbar_init(empty_bar(s), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      tc::mbar_init(tfull_bar(a), 1);
+      tc::mbar_init(tempty_bar(a), 2 * kEpiWarps);  // the epilogue warps of both CTAs
+    }
+    tc::mbar_init(drain_bar, 1);
+    tc::fence_mbar_init();
+    misc[1] = 0;
+  }
+  if (warp == 0 && lane == 0) {
+    tc::tma_prefetch_desc(&tmA);
+    tc::tma_prefetch_desc(&tmB);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc_pair(tc::smem_u32(misc), Sh::TMEM_COLS);
+    tc::tmem_relinquish_pair();
+  }
+  pdl_wait();  // barriers and TMEM are set up while the previous kernel ends
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync();
+  tc::fence_after_sync();
+  const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(misc);
+
+  const int mats = t.live != nullptr ? max(0, min(t.mats, *t.live - t.first)) : t.mats;
+  const int per = tiles_of_matrix(t, BN);
+  const int total = mats * t.splits * per;
+
+  if (warp == 0) {
+    // ============ TMA producer (one thread in each CTA) ============
+    if (lane == 0) {
+      const uint32_t full_leader = tc::mapa(full_bar(0), 0);
+      uint32_t it = 0;
+      bool ok = true;
+      for (int u = cluster; u < total && ok; u += nclusters) {
+        const Tile x = tile_at(t, per, u, BN);
+        const int arow = x.mp * kTileRows + int(rank) * BM, brow = x.nt * BN + int(rank) * BNH;
+        for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
+          const int s = it % STAGES;
+          const uint32_t ph = (it / STAGES) & 1u;
+          if (!tc::mbar_wait(empty_bar(s), ph ^ 1u, kWaitLimitNs, abort_flag)) { fail(); ok = false; break; }
+          if (leader) tc::mbar_arrive_expect_tx(full_bar(s), 2 * Sh::STAGE_BYTES);
+          const uint32_t a_dst = sA0 + s * Sh::A_BYTES, b_dst = sB0 + s * Sh::B_BYTES;
+          const uint32_t fb = full_leader + 8u * s;
+          const int k0 = kb * KB;
+          // K-major: one box per 64-deep half, half h at h * rows * 128 bytes; MN-major: one box of 64
+          // columns x KB rows per 64 columns
+          if (A_MN) {
+#pragma unroll
+            for (int i = 0; i < BM / 64; ++i)
+              tc::tma_load_3d_pair(a_dst + i * (KB * 128), &tmA, fb, arow + i * 64, k0, x.z);
+          } else {
+#pragma unroll
+            for (int h = 0; h < KB / 64; ++h)
+              tc::tma_load_3d_pair(a_dst + h * (BM * 128), &tmA, fb, k0 + h * 64, arow, x.z);
+          }
+          if (B_MN) {
+#pragma unroll
+            for (int i = 0; i < BNH / 64; ++i)
+              tc::tma_load_3d_pair(b_dst + i * (KB * 128), &tmB, fb, brow + i * 64, k0, x.z);
+          } else {
+#pragma unroll
+            for (int h = 0; h < KB / 64; ++h)
+              tc::tma_load_3d_pair(b_dst + h * (BNH * 128), &tmB, fb, k0 + h * 64, brow, x.z);
+          }
+        }
+      }
+      // Drain (even CTA): its full barriers count the loads of both CTAs.
+      if (leader) {
+        for (int s = 0; s < STAGES; ++s) {
+          if (it > uint32_t(s)) {
+            const uint32_t n = (it - 1 - s) / STAGES;
+            if (!tc::mbar_wait(full_bar(s), n & 1u, kWaitLimitNs, &no_abort)) fail();
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ============ MMA issuer (one thread of the even CTA) ============
+    if (leader && lane == 0) {
+      uint32_t it = 0, done = 0;  // tiles issued: tile i accumulates in buffer i % 2
+      bool ok = true, issued = false;
+      for (int u = cluster; u < total && ok; u += nclusters, ++done) {
+        const Tile x = tile_at(t, per, u, BN);
+        const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
+        if (!tc::mbar_wait(tempty_bar(a), aph ^ 1u, kWaitLimitNs, abort_flag)) { fail(); break; }
+        tc::fence_after_sync();
+        const uint32_t d_tmem = tmem_base + a * BN;
+        for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
+          const int s = it % STAGES;
+          const uint32_t ph = (it / STAGES) & 1u;
+          if (!tc::mbar_wait(full_bar(s), ph, kWaitLimitNs, abort_flag)) { fail(); ok = false; break; }
+          tc::fence_after_sync();
+          const uint32_t a_s = sA0 + s * Sh::A_BYTES, b_s = sB0 + s * Sh::B_BYTES;
+#pragma unroll
+          for (int kk = 0; kk < KB / UMMA_K; ++kk) {
+            // K-major: K-half kk / 4 of the stage, 16-wide step kk % 4 inside it (32 bytes along the
+            // swizzled row). MN-major: k-rows 16 kk .. 16 kk + 15 of every 64-column block.
+            const uint32_t ha = uint32_t(kk >> 2) * (BM * 128), hb = uint32_t(kk >> 2) * (BNH * 128);
+            const int q = kk & 3;
+            const uint64_t ad = A_MN ? tc::smem_desc_sw128(a_s + kk * 2048, KB * 128, 1024)
+                                     : tc::smem_desc_sw128(a_s + ha + q * 32, 16, 1024);
+            const uint64_t bd = B_MN ? tc::smem_desc_sw128(b_s + kk * 2048, KB * 128, 1024)
+                                     : tc::smem_desc_sw128(b_s + hb + q * 32, 16, 1024);
+            tc::mma_bf16_pair(d_tmem, ad, bd, IDESC, (kb > x.kb0 || kk > 0) ? 1u : 0u);
+          }
+          tc::mma_commit_pair_mc(empty_bar(s), 0x3);  // frees the stage in both CTAs
+          issued = true;
+        }
+        if (!ok) break;
+        tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
+      }
+      if (issued) {
+        tc::mma_commit_pair(drain_bar);
+        if (!tc::mbar_wait(drain_bar, 0, kWaitLimitNs, &no_abort)) fail();
+      }
+    }
+  } else {
+    // ============ epilogue (warps 2..9 of each CTA) ============
+    const int q = warp & 3, half = (warp - 2) / 4;
+    Warp w;
+    w.lane = lane;
+    w.stage = stage_base + uint32_t(warp - 2) * kStageBytes;
+    const uint32_t tempty_leader = tc::mapa(tempty_bar(0), 0);
+    uint32_t done = 0;
+    for (int u = cluster; u < total; u += nclusters, ++done) {
+      const Tile x = tile_at(t, per, u, BN);
+      const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
+      const bool ok = tc::mbar_wait(tfull_bar(a), aph, kWaitLimitNs, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) { fail(); break; }
+      tc::fence_after_sync();
+      w.row = x.mp * kTileRows + int(rank) * BM + q * 32 + lane;
+      w.col = x.nt * BN + half * BNH;
+      w.z = x.z;
+      w.split = x.split;
+      w.tb = tmem_base + (uint32_t(q * 32) << 16) + a * BN + uint32_t(half * BNH);
+      epi.template run<BN>(w);
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * a);
+    }
+    if (lane == 0) tc::bulk_wait0();  // this warp's output stores are complete
+    __syncwarp();
+  }
+
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync();  // no CTA leaves while its peer may still signal it
+  if (warp == 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc_pair(tmem_base, Sh::TMEM_COLS);
+  }
+}
+
+// Launches the product over `most` tiles at most (the list may be shorter: Tiles::live).
+template <int BN, bool A_MN, bool B_MN, bool HALF, class Epi>
+int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const Epi &epi, const Tiles &t, long long most,
+           cudaStream_t s, const char *what) {
+  using Sh = Shape<BN>;
+  auto kern = dense_pair_kernel<BN, A_MN, B_MN, HALF, Epi>;
+  if (most > 0x3fffffff) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: too many tiles", what);
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see moe::launch_dep
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Sh::SMEM;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  static int fit[64] = {};  // co-resident pairs on each device
+  int &n = fit[moe::device_slot()];
+  if (!n) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(Sh::SMEM));
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    cfg.gridDim = dim3(2 * (moe::num_sms() / 2));
+    int k = 0;
+    e = cudaOccupancyMaxActiveClusters(&k, kern, &cfg);
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    if (k <= 0) return moe::set_error(MOE_ERR_CUDA, "%s: no co-resident CTA pair fits", what);
+    n = k;
+  }
+  cfg.gridDim = dim3(2 * unsigned(std::max(1ll, std::min<long long>(n, most))));
+  cfg.numAttrs = 2;
+  MOE_LAUNCH(name, s, cudaLaunchKernelEx(&cfg, kern, a, b, epi, t));
+  return moe::launch_status(what);
+}
+
+// Tensor map of an operand: K-major boxes of 64 x box_rows, MN-major boxes of 64 x KB.
+inline int operand_map(CUtensorMap *m, const void *base, bool half, bool mn, int64_t mats, int64_t rows, int64_t cols,
+                       int64_t pitch, int64_t step, int box_rows, const char *what) {
+  return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 64, mn ? KB : box_rows, what);
+}
+inline int store_map(CUtensorMap *m, const void *base, bool half, int64_t mats, int64_t rows, int64_t cols,
+                     int64_t pitch, int64_t step, const char *what) {
+  return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 32, 32, what, CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+}  // namespace dg

@@ -2191,4 +2191,20 @@ int make_map(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uin
   if (r != CUDA_SUCCESS) return moe::set_error(MOE_ERR_CUDA, "tensor map for %s: CUresult %d", what, int(r));
   return MOE_OK;
 }
+
+int make_map_stack(CUtensorMap *m, const void *base, bool half, uint64_t mats, uint64_t rows, uint64_t cols,
+                   uint64_t pitch, uint64_t step, uint32_t box_cols, uint32_t box_rows, const char *what,
+                   CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return moe::set_error(MOE_ERR_CUDA, "cuTensorMapEncodeTiled unavailable");
+  cuuint64_t dims[3] = {cols, rows, mats};
+  cuuint64_t strides[2] = {pitch * 2, step * 2};
+  cuuint32_t box[3] = {box_cols, box_rows, 1};
+  cuuint32_t es[3] = {1, 1, 1};
+  CUresult r = fn(m, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                  const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return moe::set_error(MOE_ERR_CUDA, "tensor map for %s: CUresult %d", what, int(r));
+  return MOE_OK;
+}
 }  // namespace moe

@@ -1,0 +1,486 @@
+// Softmax cross entropy over a large vocabulary, and its gradient, without keeping the logits (sm_103a).
+//
+//   z = h W^T, lse = log sum exp z, nll = lse - z[target]
+//   dz = a (p - 1[target]) + b p with a = d_loss[0] / M, b = 2 d_loss[1] z_coef lse / M;  dh = dz W,  dW = dz^T h
+//
+// The logits' product runs over 256 x 256 tiles; a tile's epilogue reduces each row's 128 columns to their
+// maximum and the sum of exp(z - maximum) in fp32, and picks the target's logit out in fp32. Those pairs
+// (a 64th of the logits' bytes) are all that the loss needs.
+// The gradient needs every exp(z - lse) once more, after the row's last tile. Making the logits again would be 2 T V d
+// operations beside the 6 T V d of the three products. Instead the epilogue also keeps exp(z - block maximum)
+// in half precision (values up to 1, 11 bits) for one piece of the tokens, and vocab_dz turns them into dz in place
+// once the row's lse is known: 2 bytes written, read and written a logit, ~0.9 ps, against d / 0.9e15 s for the
+// product. The one number that this would spoil, p - 1 at a target that is almost sure, is taken from the fp32 logit.
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+MOE_DEV_ERR_DECL
+
+#include "dense_gemm.cuh"
+
+namespace {
+
+constexpr int kBlk = 128;    // columns that share a maximum
+constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
+
+struct Sizes {
+  int64_t np, pitch;   // (maximum, sum) pairs of a row; halves from row to row of the kept exponentials
+};
+Sizes sizes(int V) { return {(int64_t(V) + kBlk - 1) / kBlk, (int64_t(V) + 63) / 64 * 64}; }
+
+// ---------------------------------------------------------------- epilogues
+
+// Rows of the logits: see the top of the file. KEEP: the exponentials go to memory through `kept`.
+template <bool KEEP> struct LogitsEpi {
+  CUtensorMap kept;
+  float2 *part;            // [rows, np]
+  float *zt;               // [rows] the target's logit
+  const int32_t *target;
+  int rows, V, np;
+
+  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+    static_assert(BN / 2 == kBlk, "a warp's half tile is a block");
+    const int nv = min(kBlk, V - w.col);
+    if (nv <= 0 || w.row - w.lane >= rows) return;
+    float z[kBlk];
+#pragma unroll
+    for (int c = 0; c < kBlk; c += 32)
+      tc::tmem_ld_32x32b_x32(w.tb + c, *reinterpret_cast<uint32_t(*)[32]>(&z[c]));
+    tc::tmem_ld_wait();
+    const int tgt = w.row < rows ? target[w.row] - w.col : -1;
+    if (nv < kBlk) {
+#pragma unroll
+      for (int c = 0; c < kBlk; ++c)
+        if (c >= nv) z[c] = -INFINITY;
+    }
+    if (tgt >= 0 && tgt < nv) {
+      float v = 0.f;
+#pragma unroll
+      for (int c = 0; c < kBlk; ++c) v = c == tgt ? z[c] : v;
+      zt[w.row] = v;
+    }
+    float m4[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+    for (int c = 4; c < kBlk; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
+    const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+    const float base = m == -INFINITY ? 0.f : m;  // (a block of -inf alone: exponentials of 0)
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < kBlk; ++c) {
+      z[c] = __expf(z[c] - base);
+      s4[c & 3] += z[c];
+    }
+    if (w.row < rows)
+      part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, (s4[0] + s4[1]) + (s4[2] + s4[3]));
+    if (KEEP) {
+#pragma unroll
+      for (int c = 0; c < kBlk; c += 32) {
+        if (c >= nv) break;
+        uint4 v[4];
+        uint32_t *p = reinterpret_cast<uint32_t *>(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const __half2 h = __floats2half2_rn(z[c + 2 * i], z[c + 2 * i + 1]);
+          p[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        dg::stage_and_store(&kept, w.stage, w.lane, v, w.col + c, w.row - w.lane, 0);
+      }
+    }
+  }
+};
+
+// A product's result: fp32 sums from before added where `add` is not null; to fp32 `sum` where that is not
+// null ([splits, rows, cols]), else rounded to bf16 through `out`. cols % 8 == 0.
+struct OutEpi {
+  CUtensorMap out;
+  const float *add;
+  float *sum;
+  int rows, cols;
+
+  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+    if (w.row - w.lane >= rows) return;
+    const bool mine = w.row < rows;
+    const size_t at = (size_t(w.split) * rows + w.row) * cols;
+#pragma unroll 1
+    for (int c = 0; c < BN / 2; c += 32) {
+      const int col = w.col + c;
+      if (col >= cols) break;
+      uint32_t r[32];
+      tc::tmem_ld_32x32b_x32(w.tb + c, r);
+      tc::tmem_ld_wait();
+      if (add != nullptr && mine) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          if (col + i < cols) {
+            const float4 v = *reinterpret_cast<const float4 *>(add + at + col + i);
+            r[i] = __float_as_uint(__uint_as_float(r[i]) + v.x);
+            r[i + 1] = __float_as_uint(__uint_as_float(r[i + 1]) + v.y);
+            r[i + 2] = __float_as_uint(__uint_as_float(r[i + 2]) + v.z);
+            r[i + 3] = __float_as_uint(__uint_as_float(r[i + 3]) + v.w);
+          }
+        }
+      }
+      if (sum != nullptr) {
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            if (col + i < cols) stg_v4(sum + at + col + i, make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]));
+        }
+      } else {
+        uint4 v[4];
+        uint32_t *p = reinterpret_cast<uint32_t *>(v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+        dg::stage_and_store(&out, w.stage, w.lane, v, col, w.row - w.lane, 0);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------- small kernels
+
+constexpr int kSumThreads = 1024;
+
+// Sum over a block of 1,024 threads in a fixed order; valid in thread 0.
+template <class T> __device__ __forceinline__ T block_sum(T v, T *s) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
+  if (lane == 0) s[warp] = v;
+  __syncthreads();
+  if (warp == 0) {
+    v = s[lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
+  }
+  __syncthreads();
+  return v;
+}
+
+// n_valid = tokens with a target.
+__global__ void __launch_bounds__(kSumThreads) vocab_count(const int32_t *__restrict__ target, int T, int V,
+                                                           int32_t *__restrict__ n_valid) {
+  __shared__ int s[32];
+  pdl_start();
+  int n = 0;
+  bool bad = false;
+  for (int t = threadIdx.x; t < T; t += kSumThreads) {
+    const int v = target[t];
+    n += v >= 0 && v < V;
+    bad |= v >= V;
+  }
+  if (bad) dev_flag(&g_dev_err, MOE_DEV_BAD_TARGET);
+  n = block_sum(n, s);
+  if (threadIdx.x == 0) *n_valid = n;
+}
+
+struct Coefs {
+  const float *d_loss;
+  const int32_t *n_valid;
+  float z_coef;
+  __device__ __forceinline__ void get(float &a, float &b) const {
+    const float d0 = d_loss != nullptr ? d_loss[0] : 1.f, d1 = d_loss != nullptr ? d_loss[1] : 1.f;
+    const float m = float(max(1, *n_valid));
+    a = d0 / m;
+    b = 2.f * d1 * z_coef / m;
+  }
+};
+
+// A warp per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
+// block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target.
+__global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, const float *__restrict__ zt,
+                                                 const int32_t *__restrict__ target, int rows, int V, int np, int grad,
+                                                 const Coefs k, float *__restrict__ lse, float *__restrict__ nll) {
+  pdl_start();
+  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (row >= rows) return;
+  float2 *p = part + size_t(row) * np;
+  float m = -INFINITY;
+  for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float s = 0.f;
+  for (int i = lane; i < np; i += 32) {
+    const float2 v = p[i];
+    s += v.y * __expf(v.x - m);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const float l = m + logf(s);
+  const int tgt = target[row];
+  const bool ok = tgt >= 0 && tgt < V;
+  if (lane == 0) {
+    lse[row] = l;
+    nll[row] = ok ? l - zt[row] : 0.f;
+  }
+  if (grad) {
+    float a, b;
+    k.get(a, b);
+    const float f = ok ? fmaf(b, l, a) : 0.f;
+    for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
+  }
+}
+
+// dz in place of the kept exponentials: half precision in, bf16 out. Blocks of 256 threads over (row, 2,048 columns).
+constexpr int kDzCols = 2048;
+__global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
+                                                const float *__restrict__ lse, const float *__restrict__ nll,
+                                                const int32_t *__restrict__ target, int V, int np, const Coefs k) {
+  pdl_start();
+  const int row = blockIdx.y, col = blockIdx.x * kDzCols + threadIdx.x * 8;
+  if (col >= V) return;
+  const float f = part[size_t(row) * np + col / kBlk].y;
+  uint4 *at = e + (size_t(row) * pitch + col) / 8;
+  const uint4 v = *at;
+  float o[8];
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+    o[2 * i] = f * x.x;
+    o[2 * i + 1] = f * x.y;
+  }
+  const int tgt = target[row];
+  if (tgt < 0 || tgt >= V) {  // (a padding token's logits may be anything)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+  } else if (tgt >= col && tgt < col + 8) {
+    float a, b;
+    k.get(a, b);
+    const float x = nll[row];
+    const float d = a * expm1f(-x) + b * lse[row] * expf(-x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = col + i == tgt ? d : o[i];
+  }
+  *at = pack8(o);
+}
+
+// dh = sum of the splits' products, in their order.
+__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int64_t n,
+                                                    uint16_t *__restrict__ out) {
+  pdl_start();
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  float s[8] = {};
+  for (int k = 0; k < splits; ++k) {
+    const float4 *p = reinterpret_cast<const float4 *>(part + k * n + i);
+    const float4 x = p[0], y = p[1];
+    s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+    s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+  }
+  stg_v4(out + i, pack8(s));
+}
+
+// loss = (sum nll, z_coef sum lse^2) / M. Chains of at most 32 additions on either of two levels up to 2^20 tokens.
+__global__ void __launch_bounds__(kSumThreads) vocab_loss_sum(const float *__restrict__ lse, const float *__restrict__ nll,
+                                                              const int32_t *__restrict__ target, int T, int V, float z_coef,
+                                                              const int32_t *__restrict__ n_valid, float *__restrict__ loss) {
+  __shared__ float s[32];
+  pdl_start();
+  float a = 0.f, b = 0.f;
+  for (int t0 = threadIdx.x; t0 < T; t0 += 32 * kSumThreads) {
+    float x = 0.f, y = 0.f;
+    for (int i = 0, t = t0; i < 32 && t < T; ++i, t += kSumThreads) {
+      const int v = target[t];
+      if (v >= 0 && v < V) {
+        x += nll[t];
+        y = fmaf(lse[t], lse[t], y);
+      }
+    }
+    a += x;
+    b += y;
+  }
+  a = block_sum(a, s);
+  b = block_sum(b, s);
+  if (threadIdx.x == 0) {
+    const float m = float(max(1, *n_valid));
+    loss[0] = a / m;
+    loss[1] = z_coef != 0.f ? z_coef * (b / m) : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+inline int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
+
+// Ranges of the vocabulary that dh's reduction is split into. A product of few rows has few tiles (2 at 256 x 512)
+// for 76 CTA pairs. Estimated in k-blocks of 128, which take ~0.57 us: the waves of tiles, 3 for a tile's start and
+// end, and the fp32 sums' way through memory and a launch more.
+int dh_splits(int64_t rows, int d, int V) {
+  const int64_t tiles = ((rows + 255) / 256) * ((int64_t(d) + 255) / 256), nkb = (int64_t(V) + dg::KB - 1) / dg::KB;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 64 && s <= nkb; ++s) {
+    double t = double((tiles * s + kPairs - 1) / kPairs) * double((nkb + s - 1) / s + 3);
+    if (s > 1) t += double(s) * double(rows) * d * 8 / 6.7e12 / 0.57e-6 + 6;
+    if (s == 1 || t < least) {
+      best = s;
+      least = t;
+    }
+  }
+  return best;
+}
+
+struct Layout {
+  int64_t zt, part, kept, dh, dw, total;
+};
+Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
+  const Sizes z = sizes(V);
+  const int64_t rows = std::min(piece, T), last = rows > 0 ? T % rows : 0;
+  Layout l{};
+  int64_t off = 0;
+  l.zt = off;
+  off += up256(rows * 4);
+  l.part = off;
+  off += up256(rows * z.np * 8);
+  if (grad) {
+    l.kept = off;
+    off += up256(rows * z.pitch * 2);
+    int64_t n = 0;
+    for (int64_t r : {rows, last}) {
+      const int s = r > 0 ? dh_splits(r, d, V) : 1;
+      if (s > 1) n = std::max(n, s * r * d * 4);
+    }
+    l.dh = off;
+    off += up256(n);
+    l.dw = off;
+    if (T > rows) off += up256(int64_t(V) * d * 4);
+  }
+  l.total = std::max<int64_t>(off, 256);
+  return l;
+}
+
+bool sizes_ok(int T, int d, int V, int piece) {
+  return T >= 0 && T <= (1 << 24) && d >= 8 && d <= (1 << 20) && d % 8 == 0 && V >= 1 && V <= (1 << 24) && piece >= 1;
+}
+
+int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *target, int T, int d, int V, int piece,
+        float z_coef, const float *d_loss, float *loss, float *nll, float *lse, int32_t *n_valid, uint16_t *d_hidden,
+        uint16_t *d_w, bool grad, void *ws, size_t ws_bytes, cudaStream_t s) {
+  if (!sizes_ok(T, d, V, piece))
+    return moe::set_error(MOE_ERR_ARG, "%s: need 0 <= T <= 2^24, 1 <= V <= 2^24, 8 <= d <= 2^20 with d %% 8 == 0, piece >= 1",
+                          fn);
+  if (!w || !loss || !n_valid || (T > 0 && (!h || !target || !nll || !lse)))
+    return moe::set_error(MOE_ERR_ARG, "%s: null pointer", fn);
+  if (grad && !d_hidden && !d_w) return moe::set_error(MOE_ERR_ARG, "%s: neither d_hidden nor d_w", fn);
+  for (const void *p : {static_cast<const void *>(h), static_cast<const void *>(w), static_cast<const void *>(d_hidden),
+                        static_cast<const void *>(d_w)})
+    if (!moe::aligned16(p)) return moe::set_error(MOE_ERR_ARG, "%s: bf16 tensors must be 16-byte aligned", fn);
+  if (std::max(int64_t(T), int64_t(V)) * d > (int64_t(1) << 38) ||
+      int64_t(std::min(T, piece)) * sizes(V).pitch > (int64_t(1) << 38))
+    return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: more than 2^38 elements in a matrix", fn);
+  const Layout l = layout(T, d, V, piece, grad);
+  if (!ws || !moe::aligned16(ws) || ws_bytes < size_t(l.total))
+    return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace of %lld bytes, 16-byte aligned, needed", fn, (long long)l.total);
+  const Sizes z = sizes(V);
+  uint8_t *base = static_cast<uint8_t *>(ws);
+  float *zt = reinterpret_cast<float *>(base + l.zt);
+  float2 *part = reinterpret_cast<float2 *>(base + l.part);
+  uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept);
+  float *dhp = reinterpret_cast<float *>(base + l.dh), *dwp = reinterpret_cast<float *>(base + l.dw);
+  const Coefs k = {d_loss, n_valid, z_coef};
+  int st;
+  MOE_LAUNCH("vocab_count", s, moe::launch_dep(vocab_count, 1, kSumThreads, 0, s, target, T, V, n_valid));
+  if ((st = moe::launch_status(fn))) return st;
+  if (T == 0 && d_w) {
+    if ((st = moe::cuda_status(cudaMemsetAsync(d_w, 0, size_t(V) * d * 2, s), fn))) return st;
+  }
+  CUtensorMap mw, mw_mn;
+  if ((st = dg::operand_map(&mw, w, false, false, 1, V, d, d, int64_t(V) * d, 128, fn))) return st;
+  if ((st = dg::operand_map(&mw_mn, w, false, true, 1, V, d, d, int64_t(V) * d, 128, fn))) return st;
+  for (int64_t t0 = 0; t0 < T; t0 += piece) {
+    const int rows = int(std::min<int64_t>(piece, T - t0));
+    const uint16_t *hp = h + t0 * d;
+    CUtensorMap mh;
+    if ((st = dg::operand_map(&mh, hp, false, false, 1, rows, d, d, int64_t(rows) * d, 128, fn))) return st;
+    dg::Tiles t = {1, nullptr, 0, (rows + 255) / 256, (V + 255) / 256, (d + dg::KB - 1) / dg::KB, 1, 0, 8};
+    const long long most = (long long)t.mt * t.nt;
+    if (grad) {
+      LogitsEpi<true> e;
+      e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
+      if ((st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn))) return st;
+      st = dg::launch<256, false, false, false>("vocab_logits", mh, mw, e, t, most, s, fn);
+    } else {
+      LogitsEpi<false> e = {};
+      e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
+      st = dg::launch<256, false, false, false>("vocab_logits", mh, mw, e, t, most, s, fn);
+    }
+    if (st) return st;
+    MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
+                                               grad ? 1 : 0, k, lse + t0, nll + t0));
+    if ((st = moe::launch_status(fn))) return st;
+    if (!grad) continue;
+    // (grid.y holds 65,535 rows at most)
+    for (int r0 = 0; r0 < rows; r0 += 65535) {
+      const int n = std::min(65535, rows - r0);
+      MOE_LAUNCH("vocab_dz", s, moe::launch_dep(vocab_dz, dim3((V + kDzCols - 1) / kDzCols, n), 256, 0, s,
+                                                reinterpret_cast<uint4 *>(kept + int64_t(r0) * z.pitch), z.pitch,
+                                                part + int64_t(r0) * z.np, lse + t0 + r0, nll + t0 + r0, target + t0 + r0, V,
+                                                int(z.np), k));
+      if ((st = moe::launch_status(fn))) return st;
+    }
+    if (d_hidden) {
+      CUtensorMap mz;
+      if ((st = dg::operand_map(&mz, kept, false, false, 1, rows, V, z.pitch, rows * z.pitch, 128, fn))) return st;
+      OutEpi e = {};
+      e.rows = rows; e.cols = d;
+      const int splits = dh_splits(rows, d, V);
+      uint16_t *out = d_hidden + t0 * d;
+      if ((st = dg::store_map(&e.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
+      if (splits > 1) e.sum = dhp;
+      dg::Tiles x = {1, nullptr, 0, (rows + 255) / 256, (d + 255) / 256, (V + dg::KB - 1) / dg::KB, splits, 0, 8};
+      if ((st = dg::launch<256, false, true, false>("vocab_dh", mz, mw_mn, e, x, (long long)x.mt * x.nt * splits, s, fn)))
+        return st;
+      if (splits > 1) {
+        const int64_t n = int64_t(rows) * d;
+        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((n / 8 + 255) / 256), 256, 0, s, dhp, splits, n, out));
+        if ((st = moe::launch_status(fn))) return st;
+      }
+    }
+    if (d_w) {
+      CUtensorMap mz, mh_mn;
+      if ((st = dg::operand_map(&mz, kept, false, true, 1, rows, V, z.pitch, rows * z.pitch, 128, fn))) return st;
+      if ((st = dg::operand_map(&mh_mn, hp, false, true, 1, rows, d, d, int64_t(rows) * d, 128, fn))) return st;
+      OutEpi e = {};
+      e.rows = V; e.cols = d;
+      if ((st = dg::store_map(&e.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
+      if (t0 > 0) e.add = dwp;
+      if (t0 + rows < T) e.sum = dwp;
+      dg::Tiles x = {1, nullptr, 0, (V + 255) / 256, (d + 255) / 256, (rows + dg::KB - 1) / dg::KB, 1, 0, 8};
+      if ((st = dg::launch<256, true, true, false>("vocab_dw", mz, mh_mn, e, x, (long long)x.mt * x.nt, s, fn))) return st;
+    }
+  }
+  MOE_LAUNCH("vocab_loss_sum", s, moe::launch_dep(vocab_loss_sum, 1, kSumThreads, 0, s, lse, nll, target, T, V, z_coef, n_valid, loss));
+  return moe::launch_status(fn);
+}
+
+}  // namespace
+
+namespace moe {
+MOE_DEV_ERR_DEFINE_READER(vocab_dev_error)
+}  // namespace moe
+
+extern "C" {
+
+size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad) {
+  if (!sizes_ok(T, d, V, piece)) return 0;
+  return size_t(layout(T, d, V, piece, grad != 0).total);
+}
+
+int moe_vocab_loss(const uint16_t *hidden, const uint16_t *w_vocab, const int32_t *target, int T, int d, int V, int piece,
+                   float z_coef, float *loss, float *nll, float *lse, int32_t *n_valid, void *ws, size_t ws_bytes,
+                   moe_stream_t stream) {
+  return run("moe_vocab_loss", hidden, w_vocab, target, T, d, V, piece, z_coef, nullptr, loss, nll, lse, n_valid, nullptr,
+             nullptr, false, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int moe_vocab_loss_grad(const uint16_t *hidden, const uint16_t *w_vocab, const int32_t *target, int T, int d, int V,
+                        int piece, float z_coef, const float *d_loss, float *loss, float *nll, float *lse,
+                        int32_t *n_valid, uint16_t *d_hidden, uint16_t *d_w, void *ws, size_t ws_bytes,
+                        moe_stream_t stream) {
+  return run("moe_vocab_loss_grad", hidden, w_vocab, target, T, d, V, piece, z_coef, d_loss, loss, nll, lse, n_valid,
+             d_hidden, d_w, true, ws, ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

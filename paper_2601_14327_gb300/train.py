@@ -1,0 +1,140 @@
+"""The two ends of a training step around the expert layer: the vocabulary loss that the layer's output
+gradient comes from, and the Muon step that the experts' gradients go into.
+
+PyTorch only allocates device memory and provides the stream; the work runs in the library's kernels
+(moe_vocab_loss, moe_vocab_loss_grad, moe_orthogonalize, moe_muon_step; see _lib.py and include/moe_laep.h).
+"""
+from __future__ import annotations
+
+import math
+from typing import Optional
+
+import torch
+
+from . import _lib as L
+
+
+def _check(name, t, shape, dtype, dev):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name}: a contiguous {str(dtype)[6:]} tensor {list(shape)} on {dev}")
+
+
+class VocabLossBuffers:
+    """Device buffers of the vocabulary loss of T tokens: loss [2] (cross entropy, z), nll [T], lse [T],
+    n_valid [1]; with backward also d_hidden [T, d] and d_w [V, d].
+
+    piece: tokens worked on at a time. With backward a piece's exponentials take 2 bytes a logit; the default
+    keeps them within 4 GB (and at least 1,024 tokens)."""
+
+    def __init__(self, T: int, d: int, V: int, device="cuda", backward: bool = True, piece: Optional[int] = None):
+        self.T, self.d, self.V, self.backward = T, d, V, backward
+        if piece is None:
+            piece = max(1024, (1 << 31) // max(V, 1) // 256 * 256) if backward else 16384
+        self.piece = max(1, min(piece, T))
+        self.ws_bytes = L.moe_vocab_loss_workspace_size(T, d, V, self.piece, backward)
+        if not self.ws_bytes:
+            raise ValueError(f"vocabulary loss: T={T}, d={d}, V={V}, piece={piece} are outside the limits")
+        dev = torch.device(device)
+        f32, bf16 = torch.float32, torch.bfloat16
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        self.loss = torch.empty(2, dtype=f32, device=dev)
+        self.nll = torch.empty(T, dtype=f32, device=dev)
+        self.lse = torch.empty(T, dtype=f32, device=dev)
+        self.n_valid = torch.empty(1, dtype=torch.int32, device=dev)
+        self.d_hidden = torch.empty(T, d, dtype=bf16, device=dev) if backward else None
+        self.d_w = torch.empty(V, d, dtype=bf16, device=dev) if backward else None
+
+
+def _check_vocab(b, hidden, w_vocab, target):
+    dev = b.loss.device
+    _check("hidden", hidden, (b.T, b.d), torch.bfloat16, dev)
+    _check("w_vocab", w_vocab, (b.V, b.d), torch.bfloat16, dev)
+    _check("target", target, (b.T,), torch.int32, dev)
+
+
+def vocab_loss(b: VocabLossBuffers, hidden, w_vocab, target, z_coef: float = 0.0, stream=None):
+    """Cross entropy of hidden [T, d] over the vocabulary w_vocab [V, d] (both bf16) at target [T] int32
+    (negative: no target), and z_coef times the mean squared log-normaliser. Returns b.loss; b.nll, b.lse and
+    b.n_valid are filled too."""
+    _check_vocab(b, hidden, w_vocab, target)
+    L.moe_vocab_loss(hidden, w_vocab, target, b.T, b.d, b.V, b.piece, z_coef, b.loss, b.nll, b.lse,
+                     b.n_valid, b.ws, b.ws_bytes, stream)
+    return b.loss
+
+
+def vocab_loss_grad(b: VocabLossBuffers, hidden, w_vocab, target, z_coef: float = 0.0, d_loss=None,
+                    stream=None, need_hidden: bool = True, need_w: bool = True):
+    """vocab_loss with its gradient for d_loss [2] fp32 on the device (None: ones). Returns
+    (b.loss, b.d_hidden, b.d_w); need_hidden or need_w False leaves that gradient out (None)."""
+    if not b.backward:
+        raise ValueError("buffers made with backward=False have no gradients")
+    _check_vocab(b, hidden, w_vocab, target)
+    if d_loss is not None:
+        _check("d_loss", d_loss, (2,), torch.float32, b.loss.device)
+    dh, dw = b.d_hidden if need_hidden else None, b.d_w if need_w else None
+    L.moe_vocab_loss_grad(hidden, w_vocab, target, b.T, b.d, b.V, b.piece, z_coef, d_loss, b.loss, b.nll,
+                          b.lse, b.n_valid, dh, dw, b.ws, b.ws_bytes, stream)
+    return b.loss, dh, dw
+
+
+class MuonBuffers:
+    """Workspace for orthogonalize() and muon_step() on stacks of n_mats matrices rows x cols. batch: matrices
+    worked on at a time (~6 bytes an element and 4 a square of the short side each); the default keeps the workspace
+    within 4 GB. One object serves any number of stacks of these sizes, one after another on a stream."""
+
+    def __init__(self, n_mats: int, rows: int, cols: int, device="cuda", batch: Optional[int] = None):
+        self.n_mats, self.rows, self.cols = n_mats, rows, cols
+        if batch is None:
+            one = L.moe_orthogonalize_workspace_size(1, rows, cols, 1)
+            batch = max(1, min(n_mats, (1 << 32) // max(one, 1)))
+        self.ws_bytes = L.moe_orthogonalize_workspace_size(n_mats, rows, cols, batch)
+        if not self.ws_bytes:
+            raise ValueError(f"orthogonalised update: {n_mats} matrices {rows} x {cols} are outside the limits")
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=torch.device(device))
+
+
+def _per_expert(b, active_mask):
+    """Matrices that share an entry of the mask."""
+    if active_mask is None:
+        return 1
+    E = active_mask.numel()
+    if (active_mask.dtype not in (torch.uint8, torch.bool) or not active_mask.is_contiguous()
+            or active_mask.device != b.ws.device or E == 0 or b.n_mats % E):
+        raise ValueError("active_mask: a contiguous uint8 or bool tensor on the buffers' device, of a number of experts "
+                         "that divides the matrices")
+    return b.n_mats // E
+
+
+def _check_stack(b, name, t, dtype=torch.bfloat16):
+    if (t.dtype != dtype or t.numel() != b.n_mats * b.rows * b.cols or t.shape[-1] != b.cols
+            or not t.is_contiguous() or t.device != b.ws.device):
+        raise ValueError(f"{name}: a contiguous {str(dtype)[6:]} stack of {b.n_mats} matrices {b.rows} x {b.cols} on "
+                         f"{b.ws.device}")
+
+
+def orthogonalize(b: MuonBuffers, g, out, active_mask=None, coef=None, steps: int = 5, eps: float = 1e-7, stream=None):
+    """Newton-Schulz products of every matrix of g (bf16, in any leading shape: dw_gate_up [E, 2F, d] is 2E
+    matrices [F, d]) into out (may be g). active_mask [E]: 0 for pruned experts, whose matrices stay as they are.
+    coef: (a, b, c) or one such triple per step. Returns out."""
+    _check_stack(b, "g", g)
+    _check_stack(b, "out", out)
+    L.moe_orthogonalize(g, active_mask, b.n_mats, _per_expert(b, active_mask), b.rows, b.cols, coef, steps, eps, out,
+                        b.ws, b.ws_bytes, stream)
+    return out
+
+
+def muon_step(b: MuonBuffers, w, grad, momentum, lr: float, weight_decay: float = 0.0, mu: float = 0.95,
+              nesterov: bool = True, scale: Optional[float] = None, active_mask=None, coef=None, steps: int = 5,
+              eps: float = 1e-7, master=None, stream=None):
+    """momentum <- mu momentum + grad; w <- (1 - lr weight_decay) w - lr scale orthogonalised(grad + mu momentum)
+    (of momentum without nesterov). w, grad bf16, momentum fp32; master (fp32): the weights that the step is taken on,
+    w their rounding. scale None: 0.2 sqrt(max(rows, cols)), whose update has about the size of AdamW's."""
+    _check_stack(b, "w", w)
+    _check_stack(b, "grad", grad)
+    _check_stack(b, "momentum", momentum, torch.float32)
+    if master is not None:
+        _check_stack(b, "master", master, torch.float32)
+    if scale is None:
+        scale = 0.2 * math.sqrt(max(b.rows, b.cols))
+    L.moe_muon_step(w, master, grad, momentum, active_mask, b.n_mats, _per_expert(b, active_mask), b.rows, b.cols, lr,
+                    weight_decay, mu, nesterov, scale, coef, steps, eps, b.ws, b.ws_bytes, stream)
