@@ -3,8 +3,8 @@
 // epilogue of the caller's.
 //
 // The pipeline is that of the grouped GEMMs' CTA-pair kernel: a cluster of two CTAs on two SMs computes a
-// 256 x BN tile; each CTA stages its own 128 rows of A and half of B per 128-deep k-block by TMA (128-byte
-// swizzle, 3 stages of 64 KB at BN = 256, 4 of 48 KB at BN = 128); one thread of the even CTA issues
+// 256 x BN tile; each CTA stages its own 128 rows of A and half of B per k-block by TMA (128-byte swizzle; see
+// Shape); one thread of the even CTA issues
 // tcgen05.mma.cta_group::2 (M = 256); eight epilogue warps per CTA read the accumulator, double-buffered in
 // TMEM, so that the epilogue of a tile runs under the products of the next. Operands are read as they lie in
 // memory: "K" = rows of the operand along the reduction (K-major), "MN" = reduction over its rows.
@@ -22,23 +22,31 @@ namespace dg {
 
 constexpr int BM = 128;        // rows of a CTA's share of a tile (TMEM lanes)
 constexpr int kTileRows = 256; // rows of a pair's tile
-constexpr int KB = 128;        // k-block of a ring stage
 constexpr int UMMA_K = 16;
 constexpr int kEpiWarps = 8;   // two per TMEM lane quarter, each half of the tile's columns
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr uint32_t kStageBytes = 32 * 64;  // an epilogue warp's 32 x 32 chunk of 16-bit values
 
-template <int BN> struct Shape {
+// Tile width, depth of a k-block, ring stages and staging buffers of an epilogue warp. 128-deep k-blocks halve the
+// barrier waits and commits per operation; 64-deep ones leave room for staging buffers.
+template <int BN_, int KB_, int STAGES_, int BUFS_> struct Shape {
+  static constexpr int BN = BN_, KB = KB_, STAGES = STAGES_, BUFS = BUFS_;
   static constexpr int BNH = BN / 2;
-  static constexpr int STAGES = BN == 256 ? 3 : 4;
   static constexpr uint32_t A_BYTES = BM * KB * 2;
   static constexpr uint32_t B_BYTES = BNH * KB * 2;
   static constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int NBARS = 2 * STAGES + 5;
-  static constexpr size_t SMEM = 1024 + size_t(STAGES) * STAGE_BYTES + NBARS * 8 + 4 * 4 + 1024 + kEpiWarps * kStageBytes;
+  static constexpr int kSlots = BUFS / 2;  // pairs of buffers that an epilogue can have loads in flight for
+  static constexpr int NBARS = 2 * STAGES + 5 + kEpiWarps * kSlots;
+  static constexpr size_t SMEM =
+      1024 + size_t(STAGES) * STAGE_BYTES + size_t(kEpiWarps) * BUFS * kStageBytes + NBARS * 8 + 4 * 4;
   static constexpr uint32_t TMEM_COLS = 2 * BN;
+  static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
 };
+using Wide = Shape<256, 128, 3, 2>;
+using WideIO = Shape<256, 64, 4, 6>;    // epilogues that also load
+using Small = Shape<128, 64, 5, 2>;
+using SmallIO = Shape<128, 64, 5, 6>;
 
 // The tile list. Every CTA works it out from these numbers; a pair takes every `pairs`-th tile.
 struct Tiles {
@@ -46,7 +54,7 @@ struct Tiles {
   const int *live;       // ... or, where not null: max(0, min(mats, *live - first))
   int first;
   int mt, nt;            // 256-row and BN-column tiles of a matrix
-  int nkb;               // k-blocks of 128
+  int k;                 // length of the reduction
   int splits;            // the reduction in so many ranges, each a tile of its own
   int sym;               // only tiles at or above the diagonal (mt == columns / 256 rounded up)
   int group;             // row tiles that take turns before the next column tile (tiles in flight share both operands in L2)
@@ -60,8 +68,9 @@ __device__ __forceinline__ int tiles_of_matrix(const Tiles &t, int bn) {
   return t.sym ? t.mt * (t.mt + 1) / 2 * (kTileRows / bn) : t.mt * t.nt;
 }
 
-__device__ __forceinline__ Tile tile_at(const Tiles &t, int per, int u, int bn) {
+__device__ __forceinline__ Tile tile_at(const Tiles &t, int per, int u, int bn, int kb) {
   Tile r;
+  const int nkb = (t.k + kb - 1) / kb;
   r.z = u / (per * t.splits);
   int q = u - r.z * per * t.splits;
   r.split = q / per;
@@ -81,8 +90,8 @@ __device__ __forceinline__ Tile tile_at(const Tiles &t, int per, int u, int bn) 
     r.nt = q / rows;
     r.mp = b * t.group + (q - r.nt * rows);
   }
-  r.kb0 = int((long long)t.nkb * r.split / t.splits);
-  r.kb1 = int((long long)t.nkb * (r.split + 1) / t.splits);
+  r.kb0 = int((long long)nkb * r.split / t.splits);
+  r.kb1 = int((long long)nkb * (r.split + 1) / t.splits);
   return r;
 }
 
@@ -90,16 +99,29 @@ __device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
 }
 
-// Writes this lane's 32 16-bit values (row `lane` of a 32 x 32 chunk) to the warp's staging buffer, in the
-// 64-byte-swizzle layout of a TMA tile, and stores the chunk at (col, row, z) of tensor map `tm`.
-__device__ __forceinline__ void stage_and_store(const CUtensorMap *tm, uint32_t stage, int lane,
-                                                const uint4 (&v)[4], int col, int row, int z) {
-  if (lane == 0) tc::bulk_wait_read0();  // the previous chunk has left the buffer
-  __syncwarp();
-  const uint32_t rowbase = stage + uint32_t(lane) * 64u;
-  const uint32_t sw = (uint32_t(lane) >> 1) & 3u;
-#pragma unroll
-  for (uint32_t c = 0; c < 4; ++c) tc::st_shared_v4(rowbase + ((c ^ sw) << 4), v[c]);
+// An epilogue warp's staging buffers: two taken in turns, or pairs (slots) that an epilogue with loads fills, changes in
+// place and stores, with a barrier each.
+struct Stager {
+  uint32_t base;
+  uint32_t turn;       // buffers, or slots, handed out so far
+  uint32_t bar;        // the slots' barriers
+  // The next buffer, free of the store that read it last.
+  __device__ __forceinline__ uint32_t next(int lane) {
+    if (lane == 0) tc::bulk_wait_read<1>();
+    __syncwarp();
+    const uint32_t b = base + (turn & 1u) * kStageBytes;
+    ++turn;
+    return b;
+  }
+};
+
+// Where this lane's c-th 16 bytes (of four) lie in a staging buffer: row `lane` of a 32 x 32 chunk of 16-bit values in
+// the 64-byte-swizzle layout of a TMA tile.
+__device__ __forceinline__ uint32_t stage_at(uint32_t stage, int lane, uint32_t c) {
+  return stage + uint32_t(lane) * 64u + ((c ^ ((uint32_t(lane) >> 1) & 3u)) << 4);
+}
+// Stores a filled staging buffer as the chunk at (col, row, z) of tensor map `tm`.
+__device__ __forceinline__ void store_chunk(const CUtensorMap *tm, uint32_t stage, int lane, int col, int row, int z) {
   tc::fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0) {
@@ -107,43 +129,48 @@ __device__ __forceinline__ void stage_and_store(const CUtensorMap *tm, uint32_t 
     tc::bulk_commit();
   }
 }
-
+__device__ __forceinline__ void stage_and_store(const CUtensorMap *tm, Stager &st, int lane, const uint4 (&v)[4], int col,
+                                                int row, int z) {
+  const uint32_t stage = st.next(lane);
+#pragma unroll
+  for (uint32_t c = 0; c < 4; ++c) tc::st_shared_v4(stage_at(stage, lane, c), v[c]);
+  store_chunk(tm, stage, lane, col, row, z);
+}
 // The same chunk transposed: stored at (row, col), so that the lane's row becomes a column.
-__device__ __forceinline__ void stage_and_store_t(const CUtensorMap *tm, uint32_t stage, int lane,
-                                                  const uint4 (&v)[4], int col, int row, int z) {
-  if (lane == 0) tc::bulk_wait_read0();
-  __syncwarp();
+__device__ __forceinline__ void stage_and_store_t(const CUtensorMap *tm, Stager &st, int lane, const uint4 (&v)[4],
+                                                  int col, int row, int z) {
+  const uint32_t stage = st.next(lane);
   const uint32_t *w = reinterpret_cast<const uint32_t *>(v);
   const uint32_t c16 = uint32_t(lane) >> 3, in = (uint32_t(lane) & 7u) * 2u;
 #pragma unroll
   for (uint32_t c = 0; c < 32; ++c)
     st_shared_u16(stage + c * 64u + ((c16 ^ ((c >> 1) & 3u)) << 4) + in, uint16_t(w[c >> 1] >> ((c & 1u) * 16u)));
-  tc::fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    tc::tma_store_3d(tm, stage, row, col, z);
-    tc::bulk_commit();
-  }
+  store_chunk(tm, stage, lane, row, col, z);
 }
 
 // What an epilogue gets of a tile: this thread's accumulator row `row` of matrix z is lane `lane` of the
-// warp's TMEM quarter at `tb`; the warp owns columns [col0 + c0, col0 + c0 + BN / 2) of it.
+// warp's TMEM quarter at `tb`; the warp owns columns [col, col + BN / 2).
 struct Warp {
   int lane, row;       // row of this thread in its matrix
   int col;             // first column of the warp's half tile
   int z, split;
   uint32_t tb;         // TMEM address of the half tile's first column
-  uint32_t stage;      // the warp's staging buffer
+  Stager st;
 };
 
-// Epi: struct passed to the kernel by value, with the tensor maps it stores through, and
-//   template <int BN> __device__ void run(const Warp &w) const: reads the accumulator and writes the results.
-template <int BN, bool A_MN, bool B_MN, bool HALF, class Epi>
+// Epi: struct passed to the kernel by value, with the tensor maps it stores through.
+//   kChunk == 0:  template <int BN, int kSlots> run(warp, ready): reads the accumulator and writes the results; calls ready() before
+//                 the first read, after whatever it can load meanwhile, and returns at once if that is false.
+//                 (kSlots: pairs of staging buffers)
+//   kChunk > 0:   template <int BN> run(warp, z): z [BN / 2] is the row's result in fp32. The tensor cores' accumulator is
+//                 cut short in every 16-wide step (no rounding to nearest: errors of a long sum add up), so that
+//                 the sum is taken out of it every kChunk values of the reduction and added up in registers.
+template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
 __global__ void __launch_bounds__(kThreads, 1)
     dense_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                       const __grid_constant__ Epi epi, const Tiles t) {
-  using Sh = Shape<BN>;
-  constexpr int STAGES = Sh::STAGES, BNH = Sh::BNH;
+  constexpr int STAGES = Sh::STAGES, BN = Sh::BN, BNH = Sh::BNH, KB = Sh::KB;
+  constexpr int kChunkBlocks = Epi::kChunk / KB;  // 0: the whole reduction
   constexpr uint32_t IDESC = HALF ? tc::idesc_f16_f32(2 * BM, BN, A_MN, B_MN) : tc::idesc_bf16_f32(2 * BM, BN, A_MN, B_MN);
 
   extern __shared__ uint8_t smem_raw[];
@@ -152,9 +179,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t *smem = smem_raw + pad;
   const uint32_t sA0 = raw + pad;
   const uint32_t sB0 = sA0 + STAGES * Sh::A_BYTES;
-  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + STAGES * Sh::STAGE_BYTES);
+  const uint32_t stage_base = sA0 + STAGES * Sh::STAGE_BYTES;
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + STAGES * Sh::STAGE_BYTES + kEpiWarps * Sh::BUFS * kStageBytes);
   int *misc = reinterpret_cast<int *>(bars + Sh::NBARS);
-  const uint32_t stage_base = (tc::smem_u32(misc + 4) + 1023u) & ~1023u;
   volatile int *abort_flag = misc + 1;
   volatile int no_abort = 0;
 
@@ -184,6 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::mbar_init(tempty_bar(a), 2 * kEpiWarps);  // the epilogue warps of both CTAs
     }
     tc::mbar_init(drain_bar, 1);
+    for (int i = 0; i < kEpiWarps * Sh::kSlots; ++i) tc::mbar_init(drain_bar + 8u * (1 + i), 1);
     tc::fence_mbar_init();
     misc[1] = 0;
   }
@@ -213,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t it = 0;
       bool ok = true;
       for (int u = cluster; u < total && ok; u += nclusters) {
-        const Tile x = tile_at(t, per, u, BN);
+        const Tile x = tile_at(t, per, u, BN, KB);
         const int arow = x.mp * kTileRows + int(rank) * BM, brow = x.nt * BN + int(rank) * BNH;
         for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
           const int s = it % STAGES;
@@ -258,37 +286,41 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     // ============ MMA issuer (one thread of the even CTA) ============
     if (leader && lane == 0) {
-      uint32_t it = 0, done = 0;  // tiles issued: tile i accumulates in buffer i % 2
+      uint32_t it = 0, done = 0;  // accumulators issued: number i is in buffer i % 2
       bool ok = true, issued = false;
-      for (int u = cluster; u < total && ok; u += nclusters, ++done) {
-        const Tile x = tile_at(t, per, u, BN);
-        const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
-        if (!tc::mbar_wait(tempty_bar(a), aph ^ 1u, kWaitLimitNs, abort_flag)) { fail(); break; }
-        tc::fence_after_sync();
-        const uint32_t d_tmem = tmem_base + a * BN;
-        for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
-          const int s = it % STAGES;
-          const uint32_t ph = (it / STAGES) & 1u;
-          if (!tc::mbar_wait(full_bar(s), ph, kWaitLimitNs, abort_flag)) { fail(); ok = false; break; }
+      for (int u = cluster; u < total && ok; u += nclusters) {
+        const Tile x = tile_at(t, per, u, BN, KB);
+        for (int c0 = x.kb0; c0 < x.kb1 && ok; ++done) {
+          const int c1 = kChunkBlocks > 0 ? min(x.kb1, c0 + kChunkBlocks) : x.kb1;
+          const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
+          if (!tc::mbar_wait(tempty_bar(a), aph ^ 1u, kWaitLimitNs, abort_flag)) { fail(); ok = false; break; }
           tc::fence_after_sync();
-          const uint32_t a_s = sA0 + s * Sh::A_BYTES, b_s = sB0 + s * Sh::B_BYTES;
+          const uint32_t d_tmem = tmem_base + a * BN;
+          for (int kb = c0; kb < c1; ++kb, ++it) {
+            const int s = it % STAGES;
+            const uint32_t ph = (it / STAGES) & 1u;
+            if (!tc::mbar_wait(full_bar(s), ph, kWaitLimitNs, abort_flag)) { fail(); ok = false; break; }
+            tc::fence_after_sync();
+            const uint32_t a_s = sA0 + s * Sh::A_BYTES, b_s = sB0 + s * Sh::B_BYTES;
 #pragma unroll
-          for (int kk = 0; kk < KB / UMMA_K; ++kk) {
-            // K-major: K-half kk / 4 of the stage, 16-wide step kk % 4 inside it (32 bytes along the
-            // swizzled row). MN-major: k-rows 16 kk .. 16 kk + 15 of every 64-column block.
-            const uint32_t ha = uint32_t(kk >> 2) * (BM * 128), hb = uint32_t(kk >> 2) * (BNH * 128);
-            const int q = kk & 3;
-            const uint64_t ad = A_MN ? tc::smem_desc_sw128(a_s + kk * 2048, KB * 128, 1024)
-                                     : tc::smem_desc_sw128(a_s + ha + q * 32, 16, 1024);
-            const uint64_t bd = B_MN ? tc::smem_desc_sw128(b_s + kk * 2048, KB * 128, 1024)
-                                     : tc::smem_desc_sw128(b_s + hb + q * 32, 16, 1024);
-            tc::mma_bf16_pair(d_tmem, ad, bd, IDESC, (kb > x.kb0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < KB / UMMA_K; ++kk) {
+              // K-major: K-half kk / 4 of the stage, 16-wide step kk % 4 inside it (32 bytes along the
+              // swizzled row). MN-major: k-rows 16 kk .. 16 kk + 15 of every 64-column block.
+              const uint32_t ha = uint32_t(kk >> 2) * (BM * 128), hb = uint32_t(kk >> 2) * (BNH * 128);
+              const int q = kk & 3;
+              const uint64_t ad = A_MN ? tc::smem_desc_sw128(a_s + kk * 2048, KB * 128, 1024)
+                                       : tc::smem_desc_sw128(a_s + ha + q * 32, 16, 1024);
+              const uint64_t bd = B_MN ? tc::smem_desc_sw128(b_s + kk * 2048, KB * 128, 1024)
+                                       : tc::smem_desc_sw128(b_s + hb + q * 32, 16, 1024);
+              tc::mma_bf16_pair(d_tmem, ad, bd, IDESC, (kb > c0 || kk > 0) ? 1u : 0u);
+            }
+            tc::mma_commit_pair_mc(empty_bar(s), 0x3);  // frees the stage in both CTAs
+            issued = true;
           }
-          tc::mma_commit_pair_mc(empty_bar(s), 0x3);  // frees the stage in both CTAs
-          issued = true;
+          if (!ok) break;
+          tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
+          c0 = c1;
         }
-        if (!ok) break;
-        tc::mma_commit_pair_mc(tfull_bar(a), 0x3);
       }
       if (issued) {
         tc::mma_commit_pair(drain_bar);
@@ -300,24 +332,65 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q = warp & 3, half = (warp - 2) / 4;
     Warp w;
     w.lane = lane;
-    w.stage = stage_base + uint32_t(warp - 2) * kStageBytes;
+    w.st.base = stage_base + uint32_t(warp - 2) * (Sh::BUFS * kStageBytes);
+    w.st.turn = 0;
+    w.st.bar = drain_bar + 8u * (1 + (warp - 2) * Sh::kSlots);
     const uint32_t tempty_leader = tc::mapa(tempty_bar(0), 0);
+    const uint32_t tb0 = tmem_base + (uint32_t(q * 32) << 16) + uint32_t(half * BNH);
     uint32_t done = 0;
-    for (int u = cluster; u < total; u += nclusters, ++done) {
-      const Tile x = tile_at(t, per, u, BN);
-      const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
-      const bool ok = tc::mbar_wait(tfull_bar(a), aph, kWaitLimitNs, abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) { fail(); break; }
+    bool ok = true;
+    bool waited = false;
+    auto ready = [&]() -> bool {
+      waited = true;
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(tfull_bar(done & 1u), (done >> 1) & 1u, kWaitLimitNs, abort_flag));
+      if (!ok) fail();
       tc::fence_after_sync();
+      return ok;
+    };
+    auto release = [&]() {
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * (done & 1u));
+      ++done;
+    };
+    for (int u = cluster; u < total; u += nclusters) {
+      const Tile x = tile_at(t, per, u, BN, KB);
       w.row = x.mp * kTileRows + int(rank) * BM + q * 32 + lane;
       w.col = x.nt * BN + half * BNH;
       w.z = x.z;
       w.split = x.split;
-      w.tb = tmem_base + (uint32_t(q * 32) << 16) + a * BN + uint32_t(half * BNH);
-      epi.template run<BN>(w);
-      tc::fence_before_sync();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * a);
+      if constexpr (kChunkBlocks > 0) {
+        float z[BNH];
+        for (int c0 = x.kb0; c0 < x.kb1 && ok; c0 += kChunkBlocks) {
+          if (!ready()) break;
+          const uint32_t tb = tb0 + (done & 1u) * BN;
+          if (c0 == x.kb0) {
+#pragma unroll
+            for (int c = 0; c < BNH; c += 32)
+              tc::tmem_ld_32x32b_x32(tb + c, *reinterpret_cast<uint32_t(*)[32]>(&z[c]));
+            tc::tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int c = 0; c < BNH; c += 16) {
+              uint32_t r[16];
+              tc::tmem_ld_32x32b_x16(tb + c, r);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) z[c + i] += __uint_as_float(r[i]);
+            }
+          }
+          release();
+        }
+        if (!ok) break;
+        epi.template run<BN>(w, z);
+      } else {
+        w.tb = tb0 + (done & 1u) * BN;
+        waited = false;
+        epi.template run<BN, Sh::kSlots>(w, ready);
+        if (!waited) ready();  // (a part of the tile past the matrix: nothing to read, but in step with the others)
+        if (!ok) break;
+        release();
+      }
     }
     if (lane == 0) tc::bulk_wait0();  // this warp's output stores are complete
     __syncwarp();
@@ -333,11 +406,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Launches the product over `most` tiles at most (the list may be shorter: Tiles::live).
-template <int BN, bool A_MN, bool B_MN, bool HALF, class Epi>
+template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
 int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const Epi &epi, const Tiles &t, long long most,
            cudaStream_t s, const char *what) {
-  using Sh = Shape<BN>;
-  auto kern = dense_pair_kernel<BN, A_MN, B_MN, HALF, Epi>;
+  auto kern = dense_pair_kernel<Sh, A_MN, B_MN, HALF, Epi>;
   if (most > 0x3fffffff) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: too many tiles", what);
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -370,11 +442,30 @@ int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const E
   return moe::launch_status(what);
 }
 
-// Tensor map of an operand: K-major boxes of 64 x box_rows, MN-major boxes of 64 x KB.
-inline int operand_map(CUtensorMap *m, const void *base, bool half, bool mn, int64_t mats, int64_t rows, int64_t cols,
-                       int64_t pitch, int64_t step, int box_rows, const char *what) {
-  return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 64, mn ? KB : box_rows, what);
+// A stack of row-major matrices of 16-bit values.
+struct Matrix {
+  const void *p;
+  int64_t mats, rows, cols, pitch, step;
+};
+
+// C[z] = A[z] B[z]^T for kernels of shape Sh; t.mt, t.nt and t.k are set here. A_MN, B_MN: the operand's rows are
+// the reduction.
+template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
+int product(const char *name, const Matrix &a, const Matrix &b, const Epi &epi, Tiles t, cudaStream_t s, const char *what) {
+  CUtensorMap ma, mb;
+  int st;
+  if ((st = moe::make_map_stack(&ma, a.p, HALF, a.mats, a.rows, a.cols, a.pitch, a.step, 64, A_MN ? Sh::KB : BM, what)))
+    return st;
+  if ((st = moe::make_map_stack(&mb, b.p, HALF, b.mats, b.rows, b.cols, b.pitch, b.step, 64, B_MN ? Sh::KB : Sh::BNH, what)))
+    return st;
+  const int64_t M = A_MN ? a.cols : a.rows, N = B_MN ? b.cols : b.rows;
+  t.mt = int((M + kTileRows - 1) / kTileRows);
+  t.nt = int((N + Sh::BN - 1) / Sh::BN);
+  t.k = int(A_MN ? a.rows : a.cols);
+  const long long per = t.sym ? (long long)t.mt * (t.mt + 1) / 2 * (kTileRows / Sh::BN) : (long long)t.mt * t.nt;
+  return launch<Sh, A_MN, B_MN, HALF>(name, ma, mb, epi, t, per * t.splits * t.mats, s, what);
 }
+
 inline int store_map(CUtensorMap *m, const void *base, bool half, int64_t mats, int64_t rows, int64_t cols,
                      int64_t pitch, int64_t step, const char *what) {
   return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 32, 32, what, CU_TENSOR_MAP_SWIZZLE_64B);

@@ -16,6 +16,7 @@
 #include <cuda_fp16.h>
 
 #include <math.h>
+#include <stdlib.h>
 
 #include "common.cuh"
 
@@ -44,9 +45,11 @@ struct GramEpi {
   float scale;
   int n;
 
-  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+  static constexpr int kChunk = 0;
+
+  template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
-    if (row0 >= n) return;
+    if (row0 >= n || !ready()) return;
     const bool mirror = row0 / dg::kTileRows != w.col / dg::kTileRows;
 #pragma unroll 1
     for (int c = 0; c < BN / 2; c += 32) {
@@ -60,8 +63,8 @@ struct GramEpi {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         p[i] = pack_half2(__uint_as_float(r[2 * i]) * scale, __uint_as_float(r[2 * i + 1]) * scale);
-      dg::stage_and_store(&out, w.stage, w.lane, v, col, row0, w.z);
-      if (mirror) dg::stage_and_store_t(&out, w.stage, w.lane, v, col, row0, w.z);
+      dg::stage_and_store(&out, w.st, w.lane, v, col, row0, w.z);
+      if (mirror) dg::stage_and_store_t(&out, w.st, w.lane, v, col, row0, w.z);
     }
   }
 };
@@ -74,18 +77,29 @@ struct PolyEpi {
   float b, c;
   int n, pitch;
 
-  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+  static constexpr int kChunk = 0;
+
+  template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
-    if (row0 >= n) return;
+    if (row0 >= n || w.col >= n) return;
     const bool mirror = row0 / dg::kTileRows != w.col / dg::kTileRows;
     const uint16_t *arow = a + (size_t(w.z) * n + min(w.row, n - 1)) * pitch;
+    // A's values of a chunk are loaded a chunk ahead, the first while the products still run
+    // (pitch is a multiple of 64: 32 columns never leave the row)
+    uint4 x[4], nx[4];
+    auto load = [&](int col) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nx[i] = *reinterpret_cast<const uint4 *>(arow + col + 8 * i);
+    };
+    load(w.col);
+    if (!ready()) return;
 #pragma unroll 1
     for (int cc = 0; cc < BN / 2; cc += 32) {
       const int col = w.col + cc;
       if (col >= n) break;
-      uint4 x[4];  // (pitch is a multiple of 64: 32 columns never leave the row)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4 *>(arow + col + 8 * i);
+      for (int i = 0; i < 4; ++i) x[i] = nx[i];
+      if (cc + 32 < BN / 2 && col + 32 < n) load(col + 32);
       uint32_t r[32];
       tc::tmem_ld_32x32b_x32(w.tb + cc, r);
       tc::tmem_ld_wait();
@@ -103,8 +117,8 @@ struct PolyEpi {
         if (col + 2 * i + 1 == w.row) diag = y1 - back.y;
       }
       if (w.row >= col && w.row < col + 32 && w.row < n) resid[size_t(w.z) * n + w.row] = diag * (1.f / kScaleA);
-      dg::stage_and_store(&out, w.stage, w.lane, v, col, row0, w.z);
-      if (mirror) dg::stage_and_store_t(&out, w.stage, w.lane, v, col, row0, w.z);
+      dg::stage_and_store(&out, w.st, w.lane, v, col, row0, w.z);
+      if (mirror) dg::stage_and_store_t(&out, w.st, w.lane, v, col, row0, w.z);
     }
   }
 };
@@ -121,99 +135,144 @@ struct Target {
 };
 
 template <bool LAST> struct StepEpi {
-  CUtensorMap hi_out, lo_out;
-  const uint16_t *hi, *lo;    // [mats, rows, pitch]
+  CUtensorMap hi, lo;         // X's terms; lo is replaced in place
+  CUtensorMap next;           // the new hi, or with LAST and to.vec the caller's bf16 tensor
   const float *resid;         // [mats, rows or cols]
   float a;
-  int rows, cols, pitch, tall;
+  int rows, cols, tall;
   Target to;
 
-  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+  static constexpr int kChunk = 0;
+
+  // A chunk of 32 columns at a time: TMA brings its hi and lo into a slot's two buffers (up to kSlots chunks ahead, the
+  // first ones while the products still run), every lane changes its row in place, and TMA stores them.
+  template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
-    if (row0 >= rows) return;
-    const size_t at = (size_t(w.z) * rows + min(w.row, rows - 1)) * pitch;
+    if (row0 >= rows || w.col >= cols) return;
+    static_assert(kSlots >= 2, "a slot's store is waited for a chunk later");
+    const int chunks = min(BN / 64, (cols - w.col + 31) / 32);
+    volatile int never = 0;
     const float *res = resid + size_t(w.z) * (tall ? cols : rows);
     const float ar = tall ? a : a + res[min(w.row, rows - 1)];
+    auto slot = [&](int c) { return (w.st.turn + uint32_t(c)) % kSlots; };
+    auto load = [&](int c) {
+      const uint32_t s = slot(c), buf = w.st.base + s * (2 * dg::kStageBytes), bar = w.st.bar + 8u * s;
+      tc::mbar_arrive_expect_tx(bar, 2 * dg::kStageBytes);
+      tc::tma_load_3d(buf, &hi, bar, w.col + 32 * c, row0, w.z);
+      tc::tma_load_3d(buf + dg::kStageBytes, &lo, bar, w.col + 32 * c, row0, w.z);
+    };
+    // arrival of chunk c (a slot's n-th use is the phase of parity n % 2)
+    auto arrived = [&](int c) {
+      return tc::mbar_wait(w.st.bar + 8u * slot(c), ((w.st.turn + uint32_t(c)) / kSlots) & 1u, dg::kWaitLimitNs, &never);
+    };
+    __syncwarp();
+    if (w.lane == 0) {
+      tc::bulk_wait_read<0>();  // the last tile's stores have left the slots
+      for (int c = 0; c < min(chunks, kSlots); ++c) load(c);
+    }
+    if (!ready()) {  // (the loads in flight end before the CTA does)
+      if (w.lane == 0)
+        for (int c = 0; c < min(chunks, kSlots); ++c)
+          if (!arrived(c)) dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
+      return;
+    }
 #pragma unroll 1
-    for (int c = 0; c < BN / 2; c += 32) {
-      const int col = w.col + c;
-      if (col >= cols) break;
-      uint4 xh[4], xl[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        xh[i] = *reinterpret_cast<const uint4 *>(hi + at + col + 8 * i);
-        xl[i] = *reinterpret_cast<const uint4 *>(lo + at + col + 8 * i);
-      }
+    for (int c = 0; c < chunks; ++c) {
+      const int col = w.col + 32 * c;
+      const uint32_t sh = w.st.base + slot(c) * (2 * dg::kStageBytes), sl = sh + dg::kStageBytes;
       const float rc = tall ? a + res[min(col + w.lane, cols - 1)] : 0.f;
       uint32_t r[32];
-      tc::tmem_ld_32x32b_x32(w.tb + c, r);
+      tc::tmem_ld_32x32b_x32(w.tb + 32 * c, r);
+      if (!arrived(c)) dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
       tc::tmem_ld_wait();
-      const uint32_t *ph = reinterpret_cast<const uint32_t *>(xh), *pl = reinterpret_cast<const uint32_t *>(xl);
       float x[32];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float2 h = unpack_half2(ph[i]), l = unpack_half2(pl[i]);
-        const float a0 = tall ? __shfl_sync(0xffffffffu, rc, 2 * i) : ar;
-        const float a1 = tall ? __shfl_sync(0xffffffffu, rc, 2 * i + 1) : ar;
-        x[2 * i] = fmaf(a0, fmaf(l.x, 1.f / kLo, h.x), __uint_as_float(r[2 * i]) * (1.f / kScaleA));
-        x[2 * i + 1] = fmaf(a1, fmaf(l.y, 1.f / kLo, h.y), __uint_as_float(r[2 * i + 1]) * (1.f / kScaleA));
+      for (int q = 0; q < 4; ++q) {
+        const uint4 vh = tc::ld_shared_v4(dg::stage_at(sh, w.lane, q)), vl = tc::ld_shared_v4(dg::stage_at(sl, w.lane, q));
+        const uint32_t ph[4] = {vh.x, vh.y, vh.z, vh.w}, pl[4] = {vl.x, vl.y, vl.z, vl.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 8 * q + 2 * i;
+          const float2 h = unpack_half2(ph[i]), l = unpack_half2(pl[i]);
+          const float a0 = tall ? __shfl_sync(0xffffffffu, rc, j) : ar;
+          const float a1 = tall ? __shfl_sync(0xffffffffu, rc, j + 1) : ar;
+          x[j] = fmaf(a0, fmaf(l.x, 1.f / kLo, h.x), __uint_as_float(r[j]) * (1.f / kScaleA));
+          x[j + 1] = fmaf(a1, fmaf(l.y, 1.f / kLo, h.y), __uint_as_float(r[j + 1]) * (1.f / kScaleA));
+        }
       }
       if (!LAST) {
-        uint4 vh[4], vl[4];
-        uint32_t *oh = reinterpret_cast<uint32_t *>(vh), *ol = reinterpret_cast<uint32_t *>(vl);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          oh[i] = pack_half2(x[2 * i], x[2 * i + 1]);
-          const float2 h = unpack_half2(oh[i]);
-          ol[i] = pack_half2((x[2 * i] - h.x) * kLo, (x[2 * i + 1] - h.y) * kLo);
+        for (int q = 0; q < 4; ++q) {
+          uint32_t oh[4], ol[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = 8 * q + 2 * i;
+            oh[i] = pack_half2(x[j], x[j + 1]);
+            const float2 h = unpack_half2(oh[i]);
+            ol[i] = pack_half2((x[j] - h.x) * kLo, (x[j + 1] - h.y) * kLo);
+          }
+          tc::st_shared_v4(dg::stage_at(sh, w.lane, q), make_uint4(oh[0], oh[1], oh[2], oh[3]));
+          tc::st_shared_v4(dg::stage_at(sl, w.lane, q), make_uint4(ol[0], ol[1], ol[2], ol[3]));
         }
-        dg::stage_and_store(&hi_out, w.stage, w.lane, vh, col, row0, w.z);
-        dg::stage_and_store(&lo_out, w.stage, w.lane, vl, col, row0, w.z);
-      } else if (w.row < rows) {
-        finish(w, col, x);
+      } else {
+        finish(w, col, x, sh);
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (w.lane == 0) {
+        if (!LAST) {
+          tc::tma_store_3d(&next, sh, col, row0, w.z);
+          tc::tma_store_3d(&lo, sl, col, row0, w.z);
+        } else if (to.vec) {
+          tc::tma_store_3d(&next, sh, col, row0, to.live[w.z]);
+        }
+        tc::bulk_commit();
+        // the chunk after this one's store in the same slot: loaded once the store has read it, a chunk later
+        if (c >= 1 && c - 1 + kSlots < chunks) {
+          tc::bulk_wait_read<1>();
+          load(c - 1 + kSlots);
+        }
       }
     }
+    w.st.turn += uint32_t(chunks);
   }
 
-  __device__ __forceinline__ void finish(const dg::Warp &w, int col, float (&x)[32]) const {
-    const size_t o = (size_t(to.live[w.z]) * rows + w.row) * cols + col;
+  // The last step's result: to the caller's tensor, by way of the staging buffer at `stage` where TMA can store it.
+  __device__ __forceinline__ void finish(const dg::Warp &w, int col, float (&x)[32], uint32_t stage) const {
+    const size_t o = (size_t(to.live[w.z]) * rows + min(w.row, rows - 1)) * cols + col;
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] *= to.inv;
     if (to.vec) {
 #pragma unroll
       for (int g = 0; g < 32; g += 8) {
-        if (col + g >= cols) break;
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[g + i];
-        if (to.out != nullptr) {
-          stg_v4(to.out + o + g, pack8(y));
-          continue;
-        }
-        float v[8];
-        if (to.master != nullptr) {
-          const float4 p = *reinterpret_cast<const float4 *>(to.master + o + g), q = *reinterpret_cast<const float4 *>(to.master + o + g + 4);
-          v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w;
-          v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
-        } else {
-          unpack8(*reinterpret_cast<const uint4 *>(to.w + o + g), v);
-        }
+        if (to.out == nullptr && col + g < cols && w.row < rows) {
+          float v[8];
+          if (to.master != nullptr) {
+            const float4 p = *reinterpret_cast<const float4 *>(to.master + o + g), q = *reinterpret_cast<const float4 *>(to.master + o + g + 4);
+            v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w;
+            v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
+          } else {
+            unpack8(*reinterpret_cast<const uint4 *>(to.w + o + g), v);
+          }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(to.keep, v[i], -to.step * y[i]);
-        if (to.master != nullptr) {
-          *reinterpret_cast<float4 *>(to.master + o + g) = make_float4(v[0], v[1], v[2], v[3]);
-          *reinterpret_cast<float4 *>(to.master + o + g + 4) = make_float4(v[4], v[5], v[6], v[7]);
+          for (int i = 0; i < 8; ++i) y[i] = fmaf(to.keep, v[i], -to.step * y[i]);
+          if (to.master != nullptr) {
+            *reinterpret_cast<float4 *>(to.master + o + g) = make_float4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<float4 *>(to.master + o + g + 4) = make_float4(y[4], y[5], y[6], y[7]);
+          }
         }
-        stg_v4(to.w + o + g, pack8(v));
+        tc::st_shared_v4(dg::stage_at(stage, w.lane, g / 8), pack8(y));
       }
       return;
     }
-#pragma unroll 1
+    if (w.row >= rows) return;
+#pragma unroll
     for (int i = 0; i < 32; ++i) {
       if (col + i >= cols) break;
-      float y = 0.f;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) y = j == i ? x[j] : y;
+      float y = x[i];
       if (to.out == nullptr) {
         const float v = to.master != nullptr ? to.master[o + i] : __uint_as_float(uint32_t(to.w[o + i]) << 16);
         y = fmaf(to.keep, v, -to.step * y);
@@ -412,6 +471,16 @@ bool sizes_ok(int n_mats, int rows, int cols) {
 
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
+// Whether a product of so many 256 x 256 tiles at most runs in 256 x 128 tiles (dg::Small).
+// MOE_DENSE_SMALL=0 or 1 forces either form (tests and A/B measurements).
+bool small_tiles(long long tiles) {
+  static const int forced = [] {
+    const char *e = getenv("MOE_DENSE_SMALL");
+    return e && (e[0] == '0' || e[0] == '1') && e[1] == 0 ? e[0] - '0' : -1;
+  }();
+  return forced >= 0 ? forced == 1 : tiles <= 76;
+}
+
 const float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
 
 int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int per, Target to, const float *coef, int steps,
@@ -453,19 +522,17 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
   to.vec = u.vec;
   to.inv = 1.f / scale;
   int st;
-  // tensor maps: X as an operand of both products, for its new values; A, B as operands and results
-  CUtensorMap gx[2], px[2], xo[2], lom, am, ao, bm, bo;
   const int64_t xstep = int64_t(rows) * l.pitch, astep = int64_t(n) * l.npitch;
-  for (int i = 0; i < 2; ++i) {
-    if ((st = dg::operand_map(&gx[i], x[i], true, tall, batch, rows, cols, l.pitch, xstep, 128, fn))) return st;
-    if ((st = dg::operand_map(&px[i], x[i], true, !tall, batch, rows, cols, l.pitch, xstep, 128, fn))) return st;
+  CUtensorMap xo[2], lom, ao, bo;
+  for (int i = 0; i < 2; ++i)
     if ((st = dg::store_map(&xo[i], x[i], true, batch, rows, cols, l.pitch, xstep, fn))) return st;
-  }
   if ((st = dg::store_map(&lom, lo, true, batch, rows, cols, l.pitch, xstep, fn))) return st;
-  if ((st = dg::operand_map(&am, ma, true, false, batch, n, n, l.npitch, astep, 128, fn))) return st;
   if ((st = dg::store_map(&ao, ma, true, batch, n, n, l.npitch, astep, fn))) return st;
-  if ((st = dg::operand_map(&bm, mb, true, false, batch, n, n, l.npitch, astep, 128, fn))) return st;
   if ((st = dg::store_map(&bo, mb, true, batch, n, n, l.npitch, astep, fn))) return st;
+  CUtensorMap om = lom;
+  if (to.vec && (st = dg::store_map(&om, to.out ? to.out : to.w, false, n_mats, rows, cols, cols, int64_t(rows) * cols, fn)))
+    return st;
+  const dg::Matrix A = {ma, batch, n, n, l.npitch, astep}, B = {mb, batch, n, n, l.npitch, astep};
 
   const int64_t units = int64_t(rows) * ((cols + 7) / 8);
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(kParts, units / 512)));
@@ -485,33 +552,36 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
                                                   lo + f * xstep));
       if ((st = moe::launch_status(fn))) return st;
     }
+    const int nt = ceil_div(n, 256);
+    const bool small_sq = small_tiles((long long)mats * nt * (nt + 1) / 2), small_x = small_tiles((long long)mats * nt * ceil_div(k, 256));
+    dg::Tiles t = {};
+    t.mats = mats; t.live = live; t.first = first; t.splits = 1; t.group = 8;
     for (int i = 0; i < steps; ++i) {
       const float *cf = coef ? coef + 3 * i : kCoef;
-      const int nt = ceil_div(n, 256);
-      {
-        GramEpi e;
-        e.out = ao; e.scale = kScaleA / (scale * scale); e.n = n;
-        const dg::Tiles t = {mats, live, first, nt, nt, ceil_div(k, dg::KB), 1, 1, 8};
-        const long long most = (long long)mats * nt * (nt + 1) / 2;
-        st = tall ? dg::launch<256, true, true, true>("muon_gram", gx[i & 1], gx[i & 1], e, t, most, s, fn)
-                  : dg::launch<256, false, false, true>("muon_gram", gx[i & 1], gx[i & 1], e, t, most, s, fn);
-        if (st) return st;
-      }
-      {
-        PolyEpi e;
-        e.out = bo; e.a = ma; e.resid = resid; e.b = cf[1]; e.c = cf[2] / kScaleA; e.n = n; e.pitch = l.npitch;
-        const dg::Tiles t = {mats, live, first, nt, nt, ceil_div(n, dg::KB), 1, 1, 8};
-        if ((st = dg::launch<256, false, false, true>("muon_poly", am, am, e, t, (long long)mats * nt * (nt + 1) / 2, s, fn)))
-          return st;
-      }
-      const dg::Tiles t = {mats, live, first, ceil_div(rows, 256), ceil_div(cols, 256), ceil_div(n, dg::KB), 1, 0, 8};
-      const long long most = (long long)mats * t.mt * t.nt;
+      const dg::Matrix X = {x[i & 1], batch, rows, cols, l.pitch, xstep};
+      t.sym = 1;
+      GramEpi g;
+      g.out = ao; g.scale = kScaleA / (scale * scale); g.n = n;
+      if (tall) st = small_sq ? dg::product<dg::Small, true, true, true>("muon_gram", X, X, g, t, s, fn)
+                              : dg::product<dg::Wide, true, true, true>("muon_gram", X, X, g, t, s, fn);
+      else st = small_sq ? dg::product<dg::Small, false, false, true>("muon_gram", X, X, g, t, s, fn)
+                         : dg::product<dg::Wide, false, false, true>("muon_gram", X, X, g, t, s, fn);
+      if (st) return st;
+      PolyEpi p;
+      p.out = bo; p.a = ma; p.resid = resid; p.b = cf[1]; p.c = cf[2] / kScaleA; p.n = n; p.pitch = l.npitch;
+      st = small_sq ? dg::product<dg::Small, false, false, true>("muon_poly", A, A, p, t, s, fn)
+                    : dg::product<dg::Wide, false, false, true>("muon_poly", A, A, p, t, s, fn);
+      if (st) return st;
+      t.sym = 0;
       auto step = [&](auto e) -> int {
-        e.hi_out = xo[(i + 1) & 1]; e.lo_out = lom; e.hi = x[i & 1]; e.lo = lo; e.resid = resid; e.a = cf[0];
-        e.rows = rows; e.cols = cols; e.pitch = l.pitch; e.tall = tall; e.to = to;
+        e.hi = xo[i & 1]; e.lo = lom; e.next = i + 1 < steps ? xo[(i + 1) & 1] : om; e.resid = resid; e.a = cf[0];
+        e.rows = rows; e.cols = cols; e.tall = tall; e.to = to;
         e.to.live = live + 1 + first;
-        return tall ? dg::launch<256, false, false, true>("muon_step", px[i & 1], bm, e, t, most, s, fn)
-                    : dg::launch<256, false, true, true>("muon_step", bm, px[i & 1], e, t, most, s, fn);
+        if (tall)
+          return small_x ? dg::product<dg::SmallIO, false, false, true>("muon_step", X, B, e, t, s, fn)
+                         : dg::product<dg::WideIO, false, false, true>("muon_step", X, B, e, t, s, fn);
+        return small_x ? dg::product<dg::SmallIO, false, true, true>("muon_step", B, X, e, t, s, fn)
+                       : dg::product<dg::WideIO, false, true, true>("muon_step", B, X, e, t, s, fn);
       };
       if ((st = i + 1 < steps ? step(StepEpi<false>()) : step(StepEpi<true>()))) return st;
     }

@@ -38,16 +38,13 @@ template <bool KEEP> struct LogitsEpi {
   float *zt;               // [rows] the target's logit
   const int32_t *target;
   int rows, V, np;
+  // lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum, whose errors point one way
+  static constexpr int kChunk = 512;
 
-  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+  template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     static_assert(BN / 2 == kBlk, "a warp's half tile is a block");
     const int nv = min(kBlk, V - w.col);
     if (nv <= 0 || w.row - w.lane >= rows) return;
-    float z[kBlk];
-#pragma unroll
-    for (int c = 0; c < kBlk; c += 32)
-      tc::tmem_ld_32x32b_x32(w.tb + c, *reinterpret_cast<uint32_t(*)[32]>(&z[c]));
-    tc::tmem_ld_wait();
     const int tgt = w.row < rows ? target[w.row] - w.col : -1;
     if (nv < kBlk) {
 #pragma unroll
@@ -84,40 +81,40 @@ template <bool KEEP> struct LogitsEpi {
           const __half2 h = __floats2half2_rn(z[c + 2 * i], z[c + 2 * i + 1]);
           p[i] = *reinterpret_cast<const uint32_t *>(&h);
         }
-        dg::stage_and_store(&kept, w.stage, w.lane, v, w.col + c, w.row - w.lane, 0);
+        dg::stage_and_store(&kept, w.st, w.lane, v, w.col + c, w.row - w.lane, 0);
       }
     }
   }
 };
 
-// A product's result: fp32 sums from before added where `add` is not null; to fp32 `sum` where that is not
-// null ([splits, rows, cols]), else rounded to bf16 through `out`. cols % 8 == 0.
+// A product's result times `factor`: fp32 sums from before added where `add` is not null; to fp32 `sum` where that is
+// not null ([splits, rows, cols]), else rounded to bf16 through `out`. cols % 8 == 0.
 struct OutEpi {
   CUtensorMap out;
   const float *add;
   float *sum;
+  const float *factor;
   int rows, cols;
+  static constexpr int kChunk = 4096;  // (reductions over a vocabulary of 131,072)
 
-  template <int BN> __device__ __forceinline__ void run(const dg::Warp &w) const {
+  template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     if (w.row - w.lane >= rows) return;
     const bool mine = w.row < rows;
     const size_t at = (size_t(w.split) * rows + w.row) * cols;
-#pragma unroll 1
+    const float f = *factor;
+#pragma unroll
     for (int c = 0; c < BN / 2; c += 32) {
       const int col = w.col + c;
       if (col >= cols) break;
-      uint32_t r[32];
-      tc::tmem_ld_32x32b_x32(w.tb + c, r);
-      tc::tmem_ld_wait();
       if (add != nullptr && mine) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
           if (col + i < cols) {
             const float4 v = *reinterpret_cast<const float4 *>(add + at + col + i);
-            r[i] = __float_as_uint(__uint_as_float(r[i]) + v.x);
-            r[i + 1] = __float_as_uint(__uint_as_float(r[i + 1]) + v.y);
-            r[i + 2] = __float_as_uint(__uint_as_float(r[i + 2]) + v.z);
-            r[i + 3] = __float_as_uint(__uint_as_float(r[i + 3]) + v.w);
+            z[c + i] += v.x;
+            z[c + i + 1] += v.y;
+            z[c + i + 2] += v.z;
+            z[c + i + 3] += v.w;
           }
         }
       }
@@ -125,14 +122,15 @@ struct OutEpi {
         if (mine) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
-            if (col + i < cols) stg_v4(sum + at + col + i, make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]));
+            if (col + i < cols)
+              *reinterpret_cast<float4 *>(sum + at + col + i) = make_float4(z[c + i], z[c + i + 1], z[c + i + 2], z[c + i + 3]);
         }
       } else {
         uint4 v[4];
         uint32_t *p = reinterpret_cast<uint32_t *>(v);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-        dg::stage_and_store(&out, w.stage, w.lane, v, col, w.row - w.lane, 0);
+        for (int i = 0; i < 16; ++i) p[i] = pack_bf16x2(f * z[c + 2 * i], f * z[c + 2 * i + 1]);
+        dg::stage_and_store(&out, w.st, w.lane, v, col, w.row - w.lane, 0);
       }
     }
   }
@@ -175,15 +173,24 @@ __global__ void __launch_bounds__(kSumThreads) vocab_count(const int32_t *__rest
   if (threadIdx.x == 0) *n_valid = n;
 }
 
+// dz = factor (a (p - 1[target]) + b lse p). The factor, the larger of |d_loss[0]| / M and 2 |d_loss[1] z_coef| / M, is taken
+// out of dz and given to the products' results in fp32: an unsure token's target then has -1, which bf16 holds, where
+// rounding d_loss[0] / M itself would put all targets' share off by the same up to 2^-8.
 struct Coefs {
   const float *d_loss;
   const int32_t *n_valid;
   float z_coef;
-  __device__ __forceinline__ void get(float &a, float &b) const {
+  __device__ __forceinline__ void get(float &a, float &b, float &factor) const {
     const float d0 = d_loss != nullptr ? d_loss[0] : 1.f, d1 = d_loss != nullptr ? d_loss[1] : 1.f;
     const float m = float(max(1, *n_valid));
     a = d0 / m;
     b = 2.f * d1 * z_coef / m;
+    factor = fmaxf(fabsf(a), fabsf(b));
+    if (factor > 0.f) {
+      a /= factor;
+      b /= factor;
+    }
+    if (a != a || b != b) factor = a + b;  // (NaN or infinite d_loss: NaN results)
   }
 };
 
@@ -191,7 +198,8 @@ struct Coefs {
 // block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target.
 __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, const float *__restrict__ zt,
                                                  const int32_t *__restrict__ target, int rows, int V, int np, int grad,
-                                                 const Coefs k, float *__restrict__ lse, float *__restrict__ nll) {
+                                                 const Coefs k, float *__restrict__ factor, float *__restrict__ lse,
+                                                 float *__restrict__ nll) {
   pdl_start();
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= rows) return;
@@ -215,8 +223,9 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
     nll[row] = ok ? l - zt[row] : 0.f;
   }
   if (grad) {
-    float a, b;
-    k.get(a, b);
+    float a, b, s0;
+    k.get(a, b, s0);
+    if (row == 0 && lane == 0) *factor = s0;
     const float f = ok ? fmaf(b, l, a) : 0.f;
     for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
   }
@@ -246,8 +255,8 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
   } else if (tgt >= col && tgt < col + 8) {
-    float a, b;
-    k.get(a, b);
+    float a, b, s0;
+    k.get(a, b, s0);
     const float x = nll[row];
     const float d = a * expm1f(-x) + b * lse[row] * expf(-x);
 #pragma unroll
@@ -258,7 +267,7 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 
 // dh = sum of the splits' products, in their order.
 __global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int64_t n,
-                                                    uint16_t *__restrict__ out) {
+                                                    const float *__restrict__ factor, uint16_t *__restrict__ out) {
   pdl_start();
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
   if (i >= n) return;
@@ -269,6 +278,9 @@ __global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ pa
     s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
     s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
   }
+  const float f = *factor;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] *= f;
   stg_v4(out + i, pack8(s));
 }
 
@@ -308,7 +320,7 @@ inline int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
 // for 76 CTA pairs. Estimated in k-blocks of 128, which take ~0.57 us: the waves of tiles, 3 for a tile's start and
 // end, and the fp32 sums' way through memory and a launch more.
 int dh_splits(int64_t rows, int d, int V) {
-  const int64_t tiles = ((rows + 255) / 256) * ((int64_t(d) + 255) / 256), nkb = (int64_t(V) + dg::KB - 1) / dg::KB;
+  const int64_t tiles = ((rows + 255) / 256) * ((int64_t(d) + 255) / 256), nkb = (int64_t(V) + dg::Wide::KB - 1) / dg::Wide::KB;
   int best = 1;
   double least = 0;
   for (int s = 1; s <= 64 && s <= nkb; ++s) {
@@ -323,13 +335,15 @@ int dh_splits(int64_t rows, int d, int V) {
 }
 
 struct Layout {
-  int64_t zt, part, kept, dh, dw, total;
+  int64_t factor, zt, part, kept, dh, dw, total;
 };
 Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
   const Sizes z = sizes(V);
   const int64_t rows = std::min(piece, T), last = rows > 0 ? T % rows : 0;
   Layout l{};
   int64_t off = 0;
+  l.factor = off;
+  off += 256;
   l.zt = off;
   off += up256(rows * 4);
   l.part = off;
@@ -347,7 +361,7 @@ Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
     l.dw = off;
     if (T > rows) off += up256(int64_t(V) * d * 4);
   }
-  l.total = std::max<int64_t>(off, 256);
+  l.total = off;
   return l;
 }
 
@@ -375,7 +389,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace of %lld bytes, 16-byte aligned, needed", fn, (long long)l.total);
   const Sizes z = sizes(V);
   uint8_t *base = static_cast<uint8_t *>(ws);
-  float *zt = reinterpret_cast<float *>(base + l.zt);
+  float *factor = reinterpret_cast<float *>(base + l.factor), *zt = reinterpret_cast<float *>(base + l.zt);
   float2 *part = reinterpret_cast<float2 *>(base + l.part);
   uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept);
   float *dhp = reinterpret_cast<float *>(base + l.dh), *dwp = reinterpret_cast<float *>(base + l.dw);
@@ -386,29 +400,25 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
   if (T == 0 && d_w) {
     if ((st = moe::cuda_status(cudaMemsetAsync(d_w, 0, size_t(V) * d * 2, s), fn))) return st;
   }
-  CUtensorMap mw, mw_mn;
-  if ((st = dg::operand_map(&mw, w, false, false, 1, V, d, d, int64_t(V) * d, 128, fn))) return st;
-  if ((st = dg::operand_map(&mw_mn, w, false, true, 1, V, d, d, int64_t(V) * d, 128, fn))) return st;
+  const dg::Matrix mw = {w, 1, V, d, d, int64_t(V) * d};
   for (int64_t t0 = 0; t0 < T; t0 += piece) {
     const int rows = int(std::min<int64_t>(piece, T - t0));
-    const uint16_t *hp = h + t0 * d;
-    CUtensorMap mh;
-    if ((st = dg::operand_map(&mh, hp, false, false, 1, rows, d, d, int64_t(rows) * d, 128, fn))) return st;
-    dg::Tiles t = {1, nullptr, 0, (rows + 255) / 256, (V + 255) / 256, (d + dg::KB - 1) / dg::KB, 1, 0, 8};
-    const long long most = (long long)t.mt * t.nt;
-    if (grad) {
-      LogitsEpi<true> e;
+    const dg::Matrix mh = {h + t0 * d, 1, rows, d, d, int64_t(rows) * d};
+    const dg::Matrix mz = {kept, 1, rows, V, z.pitch, rows * z.pitch};
+    dg::Tiles t = {};
+    t.mats = t.splits = 1;
+    t.group = 8;
+    auto logits = [&](auto e) {
       e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
-      if ((st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn))) return st;
-      st = dg::launch<256, false, false, false>("vocab_logits", mh, mw, e, t, most, s, fn);
-    } else {
-      LogitsEpi<false> e = {};
-      e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
-      st = dg::launch<256, false, false, false>("vocab_logits", mh, mw, e, t, most, s, fn);
-    }
-    if (st) return st;
+      if (grad) {
+        const int st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
+        if (st) return st;
+      }
+      return dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
+    };
+    if ((st = grad ? logits(LogitsEpi<true>{}) : logits(LogitsEpi<false>{}))) return st;
     MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
-                                               grad ? 1 : 0, k, lse + t0, nll + t0));
+                                               grad ? 1 : 0, k, factor, lse + t0, nll + t0));
     if ((st = moe::launch_status(fn))) return st;
     if (!grad) continue;
     // (grid.y holds 65,535 rows at most)
@@ -421,34 +431,28 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       if ((st = moe::launch_status(fn))) return st;
     }
     if (d_hidden) {
-      CUtensorMap mz;
-      if ((st = dg::operand_map(&mz, kept, false, false, 1, rows, V, z.pitch, rows * z.pitch, 128, fn))) return st;
       OutEpi e = {};
-      e.rows = rows; e.cols = d;
-      const int splits = dh_splits(rows, d, V);
+      e.rows = rows; e.cols = d; e.factor = factor;
+      t.splits = dh_splits(rows, d, V);
       uint16_t *out = d_hidden + t0 * d;
       if ((st = dg::store_map(&e.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
-      if (splits > 1) e.sum = dhp;
-      dg::Tiles x = {1, nullptr, 0, (rows + 255) / 256, (d + 255) / 256, (V + dg::KB - 1) / dg::KB, splits, 0, 8};
-      if ((st = dg::launch<256, false, true, false>("vocab_dh", mz, mw_mn, e, x, (long long)x.mt * x.nt * splits, s, fn)))
-        return st;
-      if (splits > 1) {
+      if (t.splits > 1) e.sum = dhp;
+      if ((st = dg::product<dg::Wide, false, true, false>("vocab_dh", mz, mw, e, t, s, fn))) return st;
+      if (t.splits > 1) {
         const int64_t n = int64_t(rows) * d;
-        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((n / 8 + 255) / 256), 256, 0, s, dhp, splits, n, out));
+        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((n / 8 + 255) / 256), 256, 0, s, dhp, t.splits, n,
+                                                      factor, out));
         if ((st = moe::launch_status(fn))) return st;
       }
+      t.splits = 1;
     }
     if (d_w) {
-      CUtensorMap mz, mh_mn;
-      if ((st = dg::operand_map(&mz, kept, false, true, 1, rows, V, z.pitch, rows * z.pitch, 128, fn))) return st;
-      if ((st = dg::operand_map(&mh_mn, hp, false, true, 1, rows, d, d, int64_t(rows) * d, 128, fn))) return st;
       OutEpi e = {};
-      e.rows = V; e.cols = d;
+      e.rows = V; e.cols = d; e.factor = factor;
       if ((st = dg::store_map(&e.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
       if (t0 > 0) e.add = dwp;
       if (t0 + rows < T) e.sum = dwp;
-      dg::Tiles x = {1, nullptr, 0, (V + 255) / 256, (d + 255) / 256, (rows + dg::KB - 1) / dg::KB, 1, 0, 8};
-      if ((st = dg::launch<256, true, true, false>("vocab_dw", mz, mh_mn, e, x, (long long)x.mt * x.nt, s, fn))) return st;
+      if ((st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, e, t, s, fn))) return st;
     }
   }
   MOE_LAUNCH("vocab_loss_sum", s, moe::launch_dep(vocab_loss_sum, 1, kSumThreads, 0, s, lse, nll, target, T, V, z_coef, n_valid, loss));
