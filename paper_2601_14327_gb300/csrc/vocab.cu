@@ -22,6 +22,7 @@ MOE_DEV_ERR_DECL
 namespace {
 
 constexpr int kBlk = 128;    // columns that share a maximum
+constexpr int kWholeTokens = 2048;  // tokens up to which vocab_lse counts the targets and sums the losses itself
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
 struct Sizes {
@@ -37,6 +38,8 @@ template <bool KEEP> struct LogitsEpi {
   float2 *part;            // [rows, np]
   float *zt;               // [rows] the target's logit
   const int32_t *target;
+  int *left;               // vocab_lse's block counter, set by one thread
+  int blocks;
   int rows, V, np;
   // lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum, whose errors point one way
   static constexpr int kChunk = 512;
@@ -45,6 +48,7 @@ template <bool KEEP> struct LogitsEpi {
     static_assert(BN / 2 == kBlk, "a warp's half tile is a block");
     const int nv = min(kBlk, V - w.col);
     if (nv <= 0 || w.row - w.lane >= rows) return;
+    if (w.row == 0 && w.col == 0) *left = blocks;
     const int tgt = w.row < rows ? target[w.row] - w.col : -1;
     if (nv < kBlk) {
 #pragma unroll
@@ -87,8 +91,15 @@ template <bool KEEP> struct LogitsEpi {
   }
 };
 
+// fp32 sums between launches lie as the epilogue's warps hold them: blocks of 32 x 32, a column's 32 rows together (with
+// rows together instead, every lane of a store writes to another line). First value of the block at (row, col).
+__host__ __device__ __forceinline__ size_t frag_index(int split, int row, int col, int rows, int cols) {
+  const size_t rb = (size_t(rows) + 31) / 32, cb = (size_t(cols) + 31) / 32;
+  return ((size_t(split) * rb + row / 32) * cb + col / 32) * 1024;
+}
+
 // A product's result times `factor`: fp32 sums from before added where `add` is not null; to fp32 `sum` where that is
-// not null ([splits, rows, cols]), else rounded to bf16 through `out`. cols % 8 == 0.
+// not null (frag_index), else rounded to bf16 through `out`. cols % 8 == 0.
 struct OutEpi {
   CUtensorMap out;
   const float *add;
@@ -99,32 +110,19 @@ struct OutEpi {
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     if (w.row - w.lane >= rows) return;
-    const bool mine = w.row < rows;
-    const size_t at = (size_t(w.split) * rows + w.row) * cols;
     const float f = *factor;
 #pragma unroll
     for (int c = 0; c < BN / 2; c += 32) {
       const int col = w.col + c;
       if (col >= cols) break;
-      if (add != nullptr && mine) {
+      const size_t at = frag_index(w.split, w.row - w.lane, col, rows, cols) + w.lane;
+      if (add != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          if (col + i < cols) {
-            const float4 v = *reinterpret_cast<const float4 *>(add + at + col + i);
-            z[c + i] += v.x;
-            z[c + i + 1] += v.y;
-            z[c + i + 2] += v.z;
-            z[c + i + 3] += v.w;
-          }
-        }
+        for (int i = 0; i < 32; ++i) z[c + i] += add[at + 32 * i];
       }
       if (sum != nullptr) {
-        if (mine) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            if (col + i < cols)
-              *reinterpret_cast<float4 *>(sum + at + col + i) = make_float4(z[c + i], z[c + i + 1], z[c + i + 2], z[c + i + 3]);
-        }
+        for (int i = 0; i < 32; ++i) sum[at + 32 * i] = z[c + i];
       } else {
         uint4 v[4];
         uint32_t *p = reinterpret_cast<uint32_t *>(v);
@@ -140,36 +138,30 @@ struct OutEpi {
 
 constexpr int kSumThreads = 1024;
 
-// Sum over a block of 1,024 threads in a fixed order; valid in thread 0.
-template <class T> __device__ __forceinline__ T block_sum(T v, T *s) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
-  if (lane == 0) s[warp] = v;
-  __syncthreads();
-  if (warp == 0) {
-    v = s[lane];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
-  }
-  __syncthreads();
-  return v;
-}
-
-// n_valid = tokens with a target.
-__global__ void __launch_bounds__(kSumThreads) vocab_count(const int32_t *__restrict__ target, int T, int V,
-                                                           int32_t *__restrict__ n_valid) {
-  __shared__ int s[32];
-  pdl_start();
+// Tokens with a target, by a block of any number of warps up to 32 (`s`: 32 ints); for every thread.
+__device__ __forceinline__ int count_targets(const int32_t *__restrict__ target, int T, int V, int *s) {
   int n = 0;
   bool bad = false;
-  for (int t = threadIdx.x; t < T; t += kSumThreads) {
+  for (int t = threadIdx.x; t < T; t += blockDim.x) {
     const int v = target[t];
     n += v >= 0 && v < V;
     bad |= v >= V;
   }
   if (bad) dev_flag(&g_dev_err, MOE_DEV_BAD_TARGET);
-  n = block_sum(n, s);
+  n = __reduce_add_sync(0xffffffffu, n);
+  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = n;
+  __syncthreads();
+  n = 0;
+  for (int i = 0; i < int(blockDim.x >> 5); ++i) n += s[i];
+  __syncthreads();
+  return n;
+}
+
+__global__ void __launch_bounds__(kSumThreads) vocab_count(const int32_t *__restrict__ target, int T, int V,
+                                                           int32_t *__restrict__ n_valid) {
+  __shared__ int s[32];
+  pdl_start();
+  const int n = count_targets(target, T, V, s);
   if (threadIdx.x == 0) *n_valid = n;
 }
 
@@ -180,9 +172,9 @@ struct Coefs {
   const float *d_loss;
   const int32_t *n_valid;
   float z_coef;
-  __device__ __forceinline__ void get(float &a, float &b, float &factor) const {
+  __device__ __forceinline__ void get(int n, float &a, float &b, float &factor) const {
     const float d0 = d_loss != nullptr ? d_loss[0] : 1.f, d1 = d_loss != nullptr ? d_loss[1] : 1.f;
-    const float m = float(max(1, *n_valid));
+    const float m = float(max(1, n));
     a = d0 / m;
     b = 2.f * d1 * z_coef / m;
     factor = fmaxf(fabsf(a), fabsf(b));
@@ -194,41 +186,104 @@ struct Coefs {
   }
 };
 
+// loss = (sum nll, z_coef sum lse^2) / M by one block. Sums of 1,024 strands of tokens, which the block's threads take
+// in turns (the same sums for any block), in chains of at most 32 additions on either of two levels up to 2^20 tokens.
+// `s`: 64 floats.
+__device__ __forceinline__ void sum_losses(const float *lse, const float *nll, const int32_t *__restrict__ target, int T,
+                                           int V, float z_coef, int n_valid, float *__restrict__ loss, float *s) {
+  float a, b;
+  for (int strand = threadIdx.x; strand < kSumThreads; strand += blockDim.x) {
+    a = b = 0.f;
+    for (int t0 = strand; t0 < T; t0 += 32 * kSumThreads) {
+      float x = 0.f, y = 0.f;
+      for (int i = 0, t = t0; i < 32 && t < T; ++i, t += kSumThreads) {
+        const int v = target[t];
+        if (v >= 0 && v < V) {
+          const float l = __ldcg(lse + t);
+          x += __ldcg(nll + t);
+          y = fmaf(l, l, y);
+        }
+      }
+      a += x;
+      b += y;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      a += __shfl_down_sync(0xffffffffu, a, o);
+      b += __shfl_down_sync(0xffffffffu, b, o);
+    }
+    if ((threadIdx.x & 31) == 0) {
+      s[strand >> 5] = a;
+      s[32 + (strand >> 5)] = b;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a = b = 0.f;
+    for (int i = 0; i < 32; ++i) {
+      a += s[i];
+      b += s[32 + i];
+    }
+    const float m = float(max(1, n_valid));
+    loss[0] = a / m;
+    loss[1] = z_coef != 0.f ? z_coef * (b / m) : 0.f;
+  }
+}
+
 // A warp per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
 // block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target.
+// whole (few tokens, one piece): every block counts the targets itself, and the block that ends last
+// (`left`: blocks still at work) sums the losses; a launch each before and after, 7 us of a loss of 37 tokens.
 __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, const float *__restrict__ zt,
                                                  const int32_t *__restrict__ target, int rows, int V, int np, int grad,
                                                  const Coefs k, float *__restrict__ factor, float *__restrict__ lse,
-                                                 float *__restrict__ nll) {
+                                                 float *__restrict__ nll, int whole, int *__restrict__ left,
+                                                 int32_t *__restrict__ n_valid, float *__restrict__ loss) {
+  __shared__ float sh[64];
+  __shared__ int last;
   pdl_start();
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (row >= rows) return;
-  float2 *p = part + size_t(row) * np;
-  float m = -INFINITY;
-  for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
+  int n = 0;
+  if (whole) {
+    n = count_targets(target, rows, V, reinterpret_cast<int *>(sh));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *n_valid = n;
+  }
+  if (row < rows) {
+    float2 *p = part + size_t(row) * np;
+    float m = -INFINITY;
+    for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float s = 0.f;
-  for (int i = lane; i < np; i += 32) {
-    const float2 v = p[i];
-    s += v.y * __expf(v.x - m);
-  }
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float s = 0.f;
+    for (int i = lane; i < np; i += 32) {
+      const float2 v = p[i];
+      s += v.y * __expf(v.x - m);
+    }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const float l = m + logf(s);
-  const int tgt = target[row];
-  const bool ok = tgt >= 0 && tgt < V;
-  if (lane == 0) {
-    lse[row] = l;
-    nll[row] = ok ? l - zt[row] : 0.f;
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const float l = m + logf(s);
+    const int tgt = target[row];
+    const bool ok = tgt >= 0 && tgt < V;
+    if (lane == 0) {
+      lse[row] = l;
+      nll[row] = ok ? l - zt[row] : 0.f;
+    }
+    if (grad) {
+      float a, b, s0;
+      k.get(whole ? n : *k.n_valid, a, b, s0);
+      if (row == 0 && lane == 0) *factor = s0;
+      const float f = ok ? fmaf(b, l, a) : 0.f;
+      for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
+    }
   }
-  if (grad) {
-    float a, b, s0;
-    k.get(a, b, s0);
-    if (row == 0 && lane == 0) *factor = s0;
-    const float f = ok ? fmaf(b, l, a) : 0.f;
-    for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
-  }
+  if (!whole) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicSub(left, 1) == 1;
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  sum_losses(lse, nll, target, rows, V, k.z_coef, n, loss, sh);
 }
 
 // dz in place of the kept exponentials: half precision in, bf16 out. Blocks of 256 threads over (row, 2,048 columns).
@@ -256,7 +311,7 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
   } else if (tgt >= col && tgt < col + 8) {
     float a, b, s0;
-    k.get(a, b, s0);
+    k.get(*k.n_valid, a, b, s0);
     const float x = nll[row];
     const float d = a * expm1f(-x) + b * lse[row] * expf(-x);
 #pragma unroll
@@ -265,51 +320,34 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
   *at = pack8(o);
 }
 
-// dh = sum of the splits' products, in their order.
-__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int64_t n,
+// dh = sum of the splits' products, in their order: a warp per 32 x 8 values, a lane a row.
+__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int rows, int cols,
                                                     const float *__restrict__ factor, uint16_t *__restrict__ out) {
   pdl_start();
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
-  if (i >= n) return;
+  const int lane = threadIdx.x & 31, groups = cols / 8;
+  const int64_t i = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int row = int(i / groups) * 32, col = int(i % groups) * 8;
+  if (row >= rows) return;
   float s[8] = {};
-  for (int k = 0; k < splits; ++k) {
-    const float4 *p = reinterpret_cast<const float4 *>(part + k * n + i);
-    const float4 x = p[0], y = p[1];
-    s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
-    s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+  const float *p = part + frag_index(0, row, col, rows, cols) + (col % 32) * 32 + lane;
+  const size_t step = frag_index(1, 0, 0, rows, cols);
+#pragma unroll 2
+  for (int k = 0; k < splits; ++k, p += step) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] += p[32 * j];
   }
   const float f = *factor;
 #pragma unroll
   for (int j = 0; j < 8; ++j) s[j] *= f;
-  stg_v4(out + i, pack8(s));
+  if (row + lane < rows) stg_v4(out + size_t(row + lane) * cols + col, pack8(s));
 }
 
-// loss = (sum nll, z_coef sum lse^2) / M. Chains of at most 32 additions on either of two levels up to 2^20 tokens.
 __global__ void __launch_bounds__(kSumThreads) vocab_loss_sum(const float *__restrict__ lse, const float *__restrict__ nll,
                                                               const int32_t *__restrict__ target, int T, int V, float z_coef,
                                                               const int32_t *__restrict__ n_valid, float *__restrict__ loss) {
-  __shared__ float s[32];
+  __shared__ float s[64];
   pdl_start();
-  float a = 0.f, b = 0.f;
-  for (int t0 = threadIdx.x; t0 < T; t0 += 32 * kSumThreads) {
-    float x = 0.f, y = 0.f;
-    for (int i = 0, t = t0; i < 32 && t < T; ++i, t += kSumThreads) {
-      const int v = target[t];
-      if (v >= 0 && v < V) {
-        x += nll[t];
-        y = fmaf(lse[t], lse[t], y);
-      }
-    }
-    a += x;
-    b += y;
-  }
-  a = block_sum(a, s);
-  b = block_sum(b, s);
-  if (threadIdx.x == 0) {
-    const float m = float(max(1, *n_valid));
-    loss[0] = a / m;
-    loss[1] = z_coef != 0.f ? z_coef * (b / m) : 0.f;
-  }
+  sum_losses(lse, nll, target, T, V, z_coef, *n_valid, loss, s);
 }
 
 // ---------------------------------------------------------------- host side
@@ -354,12 +392,12 @@ Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
     int64_t n = 0;
     for (int64_t r : {rows, last}) {
       const int s = r > 0 ? dh_splits(r, d, V) : 1;
-      if (s > 1) n = std::max(n, s * r * d * 4);
+      if (s > 1) n = std::max(n, int64_t(frag_index(s, 0, 0, int(r), d)) * 4);
     }
     l.dh = off;
     off += up256(n);
     l.dw = off;
-    if (T > rows) off += up256(int64_t(V) * d * 4);
+    if (T > rows) off += up256(int64_t(frag_index(1, 0, 0, V, d)) * 4);
   }
   l.total = off;
   return l;
@@ -389,14 +427,19 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace of %lld bytes, 16-byte aligned, needed", fn, (long long)l.total);
   const Sizes z = sizes(V);
   uint8_t *base = static_cast<uint8_t *>(ws);
-  float *factor = reinterpret_cast<float *>(base + l.factor), *zt = reinterpret_cast<float *>(base + l.zt);
+  float *factor = reinterpret_cast<float *>(base + l.factor);
+  int *left = reinterpret_cast<int *>(base + l.factor) + 1;
+  float *zt = reinterpret_cast<float *>(base + l.zt);
   float2 *part = reinterpret_cast<float2 *>(base + l.part);
   uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept);
   float *dhp = reinterpret_cast<float *>(base + l.dh), *dwp = reinterpret_cast<float *>(base + l.dw);
   const Coefs k = {d_loss, n_valid, z_coef};
   int st;
-  MOE_LAUNCH("vocab_count", s, moe::launch_dep(vocab_count, 1, kSumThreads, 0, s, target, T, V, n_valid));
-  if ((st = moe::launch_status(fn))) return st;
+  const bool whole = T > 0 && T <= kWholeTokens && T <= piece;
+  if (!whole) {
+    MOE_LAUNCH("vocab_count", s, moe::launch_dep(vocab_count, 1, kSumThreads, 0, s, target, T, V, n_valid));
+    if ((st = moe::launch_status(fn))) return st;
+  }
   if (T == 0 && d_w) {
     if ((st = moe::cuda_status(cudaMemsetAsync(d_w, 0, size_t(V) * d * 2, s), fn))) return st;
   }
@@ -410,6 +453,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     t.group = 8;
     auto logits = [&](auto e) {
       e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
+      e.left = left; e.blocks = (rows + 7) / 8;
       if (grad) {
         const int st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
         if (st) return st;
@@ -418,7 +462,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     };
     if ((st = grad ? logits(LogitsEpi<true>{}) : logits(LogitsEpi<false>{}))) return st;
     MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
-                                               grad ? 1 : 0, k, factor, lse + t0, nll + t0));
+                                               grad ? 1 : 0, k, factor, lse + t0, nll + t0, whole ? 1 : 0, left, n_valid, loss));
     if ((st = moe::launch_status(fn))) return st;
     if (!grad) continue;
     // (grid.y holds 65,535 rows at most)
@@ -439,8 +483,8 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       if (t.splits > 1) e.sum = dhp;
       if ((st = dg::product<dg::Wide, false, true, false>("vocab_dh", mz, mw, e, t, s, fn))) return st;
       if (t.splits > 1) {
-        const int64_t n = int64_t(rows) * d;
-        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((n / 8 + 255) / 256), 256, 0, s, dhp, t.splits, n,
+        const int64_t warps = int64_t((rows + 31) / 32) * (d / 8);
+        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((warps + 7) / 8), 256, 0, s, dhp, t.splits, rows, d,
                                                       factor, out));
         if ((st = moe::launch_status(fn))) return st;
       }
@@ -455,6 +499,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       if ((st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, e, t, s, fn))) return st;
     }
   }
+  if (whole) return MOE_OK;
   MOE_LAUNCH("vocab_loss_sum", s, moe::launch_dep(vocab_loss_sum, 1, kSumThreads, 0, s, lse, nll, target, T, V, z_coef, n_valid, loss));
   return moe::launch_status(fn);
 }
