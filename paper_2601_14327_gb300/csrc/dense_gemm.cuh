@@ -64,36 +64,62 @@ struct Tile {
   int z, split, mp, nt, kb0, kb1;
 };
 
+// Floor of a / b for 0 <= a < 2^30 from b's reciprocal: a tile's numbers cost a dozen dependent integer divisions otherwise,
+// ~1,000 cycles of every role (the compiler's division is ~100), which products with short reductions feel.
+__device__ __forceinline__ int quot(int a, int b, float inv) {
+  int q = int(float(a) * inv);    // off by at most 2^30 2^-22 = 256 b-ths: corrected
+  q += (a - q * b) >= 0 ? int(float(a - q * b) * inv) : -int(float(q * b - a) * inv) - 1;
+  if (a - q * b < 0) --q;
+  if (a - q * b >= b) ++q;
+  return q;
+}
+
 __device__ __forceinline__ int tiles_of_matrix(const Tiles &t, int bn) {
   return t.sym ? t.mt * (t.mt + 1) / 2 * (kTileRows / bn) : t.mt * t.nt;
 }
 
-__device__ __forceinline__ Tile tile_at(const Tiles &t, int per, int u, int bn, int kb) {
-  Tile r;
-  const int nkb = (t.k + kb - 1) / kb;
-  r.z = u / (per * t.splits);
-  int q = u - r.z * per * t.splits;
-  r.split = q / per;
-  q -= r.split * per;
-  if (t.sym) {
-    const int sub = kTileRows / bn;
-    const int c = q / sub;  // c-th block of the upper triangle, column by column: block column j has j + 1
-    int j = int((sqrtf(8.f * float(c) + 1.f) - 1.f) * 0.5f);
-    while (j * (j + 1) / 2 > c) --j;
-    while ((j + 1) * (j + 2) / 2 <= c) ++j;
-    r.mp = c - j * (j + 1) / 2;
-    r.nt = j * sub + (q - c * sub);
-  } else {
-    const int band = t.group * t.nt;
-    const int b = q / band, rows = min(t.group, t.mt - b * t.group);
-    q -= b * band;
-    r.nt = q / rows;
-    r.mp = b * t.group + (q - r.nt * rows);
+// A role's walk through the list.
+struct Walk {
+  int per, band, nkb;
+  float i_all, i_per, i_band, i_group;
+  __device__ __forceinline__ Walk(const Tiles &t, int bn, int kb) {
+    per = tiles_of_matrix(t, bn);
+    band = t.group * t.nt;
+    nkb = (t.k + kb - 1) / kb;
+    i_all = 1.f / float(per * t.splits);
+    i_per = 1.f / float(per);
+    i_band = 1.f / float(band);
+    i_group = 1.f / float(t.group);
   }
-  r.kb0 = int((long long)nkb * r.split / t.splits);
-  r.kb1 = int((long long)nkb * (r.split + 1) / t.splits);
-  return r;
-}
+  __device__ __forceinline__ Tile at(const Tiles &t, int u, int bn) const {
+    Tile r;
+    r.z = t.mats == 1 ? 0 : quot(u, per * t.splits, i_all);
+    int q = u - r.z * per * t.splits;
+    r.split = t.splits == 1 ? 0 : quot(q, per, i_per);
+    q -= r.split * per;
+    if (t.sym) {
+      const int sub = kTileRows / bn;
+      const int c = q / sub;  // c-th block of the upper triangle, column by column: block column j has j + 1
+      int j = int((sqrtf(8.f * float(c) + 1.f) - 1.f) * 0.5f);
+      while (j * (j + 1) / 2 > c) --j;
+      while ((j + 1) * (j + 2) / 2 <= c) ++j;
+      r.mp = c - j * (j + 1) / 2;
+      r.nt = j * sub + (q - c * sub);
+    } else {
+      const int b = quot(q, band, i_band), rows = min(t.group, t.mt - b * t.group);
+      q -= b * band;
+      r.nt = rows == t.group ? quot(q, rows, i_group) : q / rows;
+      r.mp = b * t.group + (q - r.nt * rows);
+    }
+    r.kb0 = 0;
+    r.kb1 = nkb;
+    if (t.splits > 1) {
+      r.kb0 = int((long long)nkb * r.split / t.splits);
+      r.kb1 = int((long long)nkb * (r.split + 1) / t.splits);
+    }
+    return r;
+  }
+};
 
 __device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
@@ -231,8 +257,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(misc);
 
   const int mats = t.live != nullptr ? max(0, min(t.mats, *t.live - t.first)) : t.mats;
-  const int per = tiles_of_matrix(t, BN);
-  const int total = mats * t.splits * per;
+  const Walk walk(t, BN, KB);
+  const int total = mats * t.splits * walk.per;
 
   if (warp == 0) {
     // ============ TMA producer (one thread in each CTA) ============
@@ -241,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t it = 0;
       bool ok = true;
       for (int u = cluster; u < total && ok; u += nclusters) {
-        const Tile x = tile_at(t, per, u, BN, KB);
+        const Tile x = walk.at(t, u, BN);
         const int arow = x.mp * kTileRows + int(rank) * BM, brow = x.nt * BN + int(rank) * BNH;
         for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
           const int s = it % STAGES;
@@ -289,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t it = 0, done = 0;  // accumulators issued: number i is in buffer i % 2
       bool ok = true, issued = false;
       for (int u = cluster; u < total && ok; u += nclusters) {
-        const Tile x = tile_at(t, per, u, BN, KB);
+        const Tile x = walk.at(t, u, BN);
         for (int c0 = x.kb0; c0 < x.kb1 && ok; ++done) {
           const int c1 = kChunkBlocks > 0 ? min(x.kb1, c0 + kChunkBlocks) : x.kb1;
           const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
@@ -354,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++done;
     };
     for (int u = cluster; u < total; u += nclusters) {
-      const Tile x = tile_at(t, per, u, BN, KB);
+      const Tile x = walk.at(t, u, BN);
       w.row = x.mp * kTileRows + int(rank) * BM + q * 32 + lane;
       w.col = x.nt * BN + half * BNH;
       w.z = x.z;

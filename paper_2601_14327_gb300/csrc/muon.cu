@@ -37,6 +37,15 @@ __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // ---------------------------------------------------------------- epilogues of the products
 
 // A = acc * scale, both halves of the symmetric matrix.
@@ -125,7 +134,8 @@ struct PolyEpi {
 
 // X <- (a + resid) X + acc: to the next hi and lo, or with LAST to the caller's tensors.
 struct Target {
-  const int *live;            // the stack's matrices among the caller's
+  const int *live;            // the stack's matrices among the caller's; null: first, first + 1, ...
+  int first;
   int vec;                    // rows of 16-byte multiples, 16-byte aligned tensors
   float inv;                  // 1 / X's scale
   uint16_t *out;              // orthogonalised [n_mats, rows, cols], or null: weights
@@ -149,37 +159,41 @@ template <bool LAST> struct StepEpi {
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
     if (row0 >= rows || w.col >= cols) return;
-    static_assert(kSlots >= 2, "a slot's store is waited for a chunk later");
+    static_assert(kSlots >= 3, "a slot's store is waited for a chunk later");
     const int chunks = min(BN / 64, (cols - w.col + 31) / 32);
     volatile int never = 0;
     const float *res = resid + size_t(w.z) * (tall ? cols : rows);
     const float ar = tall ? a : a + res[min(w.row, rows - 1)];
-    auto slot = [&](int c) { return (w.st.turn + uint32_t(c)) % kSlots; };
+    // a slot: hi, lo and, where w goes through it, w
+    const bool with_w = LAST && to.vec && to.w != nullptr && to.master == nullptr;
+    const uint32_t bufs = with_w ? 3 : 2, slots = 2 * kSlots / bufs;
+    auto slot = [&](int c) { return (w.st.turn + uint32_t(c)) % slots; };
     auto load = [&](int c) {
-      const uint32_t s = slot(c), buf = w.st.base + s * (2 * dg::kStageBytes), bar = w.st.bar + 8u * s;
-      tc::mbar_arrive_expect_tx(bar, 2 * dg::kStageBytes);
+      const uint32_t s = slot(c), buf = w.st.base + s * (bufs * dg::kStageBytes), bar = w.st.bar + 8u * s;
+      tc::mbar_arrive_expect_tx(bar, bufs * dg::kStageBytes);
+      if (with_w) tc::tma_load_3d(buf + 2 * dg::kStageBytes, &next, bar, w.col + 32 * c, row0, caller(w.z));
       tc::tma_load_3d(buf, &hi, bar, w.col + 32 * c, row0, w.z);
       tc::tma_load_3d(buf + dg::kStageBytes, &lo, bar, w.col + 32 * c, row0, w.z);
     };
     // arrival of chunk c (a slot's n-th use is the phase of parity n % 2)
     auto arrived = [&](int c) {
-      return tc::mbar_wait(w.st.bar + 8u * slot(c), ((w.st.turn + uint32_t(c)) / kSlots) & 1u, dg::kWaitLimitNs, &never);
+      return tc::mbar_wait(w.st.bar + 8u * slot(c), ((w.st.turn + uint32_t(c)) / slots) & 1u, dg::kWaitLimitNs, &never);
     };
     __syncwarp();
     if (w.lane == 0) {
       tc::bulk_wait_read<0>();  // the last tile's stores have left the slots
-      for (int c = 0; c < min(chunks, kSlots); ++c) load(c);
+      for (int c = 0; c < min(chunks, int(slots)); ++c) load(c);
     }
     if (!ready()) {  // (the loads in flight end before the CTA does)
       if (w.lane == 0)
-        for (int c = 0; c < min(chunks, kSlots); ++c)
+        for (int c = 0; c < min(chunks, int(slots)); ++c)
           if (!arrived(c)) dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
       return;
     }
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
       const int col = w.col + 32 * c;
-      const uint32_t sh = w.st.base + slot(c) * (2 * dg::kStageBytes), sl = sh + dg::kStageBytes;
+      const uint32_t sh = w.st.base + slot(c) * (bufs * dg::kStageBytes), sl = sh + dg::kStageBytes;
       const float rc = tall ? a + res[min(col + w.lane, cols - 1)] : 0.f;
       uint32_t r[32];
       tc::tmem_ld_32x32b_x32(w.tb + 32 * c, r);
@@ -224,76 +238,92 @@ template <bool LAST> struct StepEpi {
           tc::tma_store_3d(&next, sh, col, row0, w.z);
           tc::tma_store_3d(&lo, sl, col, row0, w.z);
         } else if (to.vec) {
-          tc::tma_store_3d(&next, sh, col, row0, to.live[w.z]);
+          tc::tma_store_3d(&next, with_w ? sh + 2 * dg::kStageBytes : sh, col, row0, caller(w.z));
         }
         tc::bulk_commit();
         // the chunk after this one's store in the same slot: loaded once the store has read it, a chunk later
-        if (c >= 1 && c - 1 + kSlots < chunks) {
+        if (c >= 1 && c - 1 + int(slots) < chunks) {
           tc::bulk_wait_read<1>();
-          load(c - 1 + kSlots);
+          load(c - 1 + int(slots));
         }
       }
     }
     w.st.turn += uint32_t(chunks);
   }
 
-  // The last step's result: to the caller's tensor, by way of the staging buffer at `stage` where TMA can store it.
+  __device__ __forceinline__ int caller(int z) const { return to.live != nullptr ? to.live[z] : to.first + z; }
+
+  // The last step's result: to the caller's tensor, by way of the slot at `stage`.
   __device__ __forceinline__ void finish(const dg::Warp &w, int col, float (&x)[32], uint32_t stage) const {
-    const size_t o = (size_t(to.live[w.z]) * rows + min(w.row, rows - 1)) * cols + col;
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] *= to.inv;
-    if (to.vec) {
+    if (to.vec) {  // rows of 16-byte multiples
+      // out, or w without master: in the slot's first or third buffer, which TMA stores (and filled with w); with master the
+      // row's fp32 values come straight from memory, 128 bytes a lane
+      const uint32_t buf = to.out != nullptr ? stage : stage + 2 * dg::kStageBytes;
+      float *m = to.master;
+      if (m != nullptr) m += (size_t(caller(w.z)) * rows + min(w.row, rows - 1)) * cols + col;
 #pragma unroll
-      for (int g = 0; g < 32; g += 8) {
+      for (int g = 0; g < 4; ++g) {
         float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[g + i];
-        if (to.out == nullptr && col + g < cols && w.row < rows) {
-          float v[8];
-          if (to.master != nullptr) {
-            const float4 p = *reinterpret_cast<const float4 *>(to.master + o + g), q = *reinterpret_cast<const float4 *>(to.master + o + g + 4);
-            v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w;
-            v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
-          } else {
-            unpack8(*reinterpret_cast<const uint4 *>(to.w + o + g), v);
-          }
+        for (int i = 0; i < 8; ++i) y[i] = x[8 * g + i];
+        const uint32_t at = dg::stage_at(m != nullptr ? stage : buf, w.lane, g);
+        if (m != nullptr) {
+          if (col + 8 * g < cols && w.row < rows) {
+            float4 *q = reinterpret_cast<float4 *>(m + 8 * g);
+            const float4 u = q[0], v = q[1];
+            const float o[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = fmaf(to.keep, v[i], -to.step * y[i]);
-          if (to.master != nullptr) {
-            *reinterpret_cast<float4 *>(to.master + o + g) = make_float4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<float4 *>(to.master + o + g + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(to.keep, o[i], -to.step * y[i]);
+            q[0] = make_float4(y[0], y[1], y[2], y[3]);
+            q[1] = make_float4(y[4], y[5], y[6], y[7]);
           }
+        } else if (to.out == nullptr) {
+          float o[8];
+          unpack8(tc::ld_shared_v4(at), o);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = fmaf(to.keep, o[i], -to.step * y[i]);
         }
-        tc::st_shared_v4(dg::stage_at(stage, w.lane, g / 8), pack8(y));
+        tc::st_shared_v4(at, pack8(y));
       }
       return;
     }
-    if (w.row >= rows) return;
+    // Rows of odd length: a lane a column, so that a warp's accesses to memory lie together (a row a lane: ~5,400 cycles a chunk
+    // in the place of ~1,300), through 32 x 32 fp32 values, column c of row r at c ^ r: no bank twice in either direction.
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (col + i >= cols) break;
-      float y = x[i];
-      if (to.out == nullptr) {
-        const float v = to.master != nullptr ? to.master[o + i] : __uint_as_float(uint32_t(to.w[o + i]) << 16);
-        y = fmaf(to.keep, v, -to.step * y);
-        if (to.master != nullptr) to.master[o + i] = y;
+    for (int i = 0; i < 32; ++i) st_shared_f32(stage + uint32_t(w.lane * 32 + (i ^ w.lane)) * 4u, x[i]);
+    __syncwarp();
+    const size_t o0 = (size_t(caller(w.z)) * rows + (w.row - w.lane)) * cols + col + w.lane;
+    const int here = min(32, rows - (w.row - w.lane));
+    if (col + w.lane < cols) {
+#pragma unroll 4
+      for (int r = 0; r < here; ++r) {
+        const size_t at = o0 + size_t(r) * cols;
+        float y = ld_shared_f32(stage + uint32_t(r * 32 + (w.lane ^ r)) * 4u);
+        if (to.out == nullptr) {
+          const float v = to.master != nullptr ? to.master[at] : __uint_as_float(uint32_t(to.w[at]) << 16);
+          y = fmaf(to.keep, v, -to.step * y);
+          if (to.master != nullptr) to.master[at] = y;
+        }
+        (to.out != nullptr ? to.out : to.w)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
       }
-      const uint16_t b = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-      (to.out != nullptr ? to.out : to.w)[o + i] = b;
     }
+    __syncwarp();
   }
 };
 
 // ---------------------------------------------------------------- small kernels
 
-// live[0] = number of matrices that are updated, then their indices in ascending order.
+// With a mask: live[0] = number of matrices that are updated, then their indices in ascending order.
 __global__ void muon_live(const uint8_t *__restrict__ mask, int n_mats, int per, int *__restrict__ live) {
   pdl_start();
   const int lane = threadIdx.x;
   int n = 0;
   for (int i0 = 0; i0 < n_mats; i0 += 32) {
     const int i = i0 + lane;
-    const bool on = i < n_mats && (mask == nullptr || mask[i / per] != 0);
+    const bool on = i < n_mats && mask[i / per] != 0;
     const uint32_t b = __ballot_sync(0xffffffffu, on);
     if (on) live[1 + n + __popc(b & ((1u << lane) - 1u))] = i;
     n += __popc(b);
@@ -352,8 +382,8 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
   __shared__ float sh[3][8];
   pdl_start();
   const int slot = blockIdx.y;
-  if (first + slot >= live[0]) return;
-  const size_t mrow = size_t(live[1 + first + slot]) * s.rows;
+  if (live != nullptr && first + slot >= live[0]) return;
+  const size_t mrow = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows;
   const int cpr = (s.cols + 7) / 8;
   const int64_t units = int64_t(s.rows) * cpr;
   float t[3] = {};
@@ -392,7 +422,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
   __shared__ float sh[2];
   pdl_start();
   const int slot = blockIdx.y;
-  if (first + slot >= live[0]) return;
+  if (live != nullptr && first + slot >= live[0]) return;
   if (threadIdx.x < 32) {
     float t[3] = {};
     for (int i = threadIdx.x; i < parts; i += 32)
@@ -413,7 +443,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
   }
   __syncthreads();
   const float pre = sh[0], norm = sh[1];
-  const size_t mrow = size_t(live[1 + first + slot]) * s.rows;
+  const size_t mrow = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows;
   const int cpr = (s.cols + 7) / 8;
   const int64_t units = int64_t(s.rows) * cpr;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < units; i += int64_t(gridDim.x) * 256) {
@@ -537,8 +567,12 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
   const int64_t units = int64_t(rows) * ((cols + 7) / 8);
   const int parts = int(std::max<int64_t>(1, std::min<int64_t>(kParts, units / 512)));
   const int blocks = int(std::max<int64_t>(1, std::min<int64_t>(1024, units / 512)));
-  MOE_LAUNCH("muon_live", s, moe::launch_dep(muon_live, 1, 32, 0, s, mask, n_mats, per, live));
-  if ((st = moe::launch_status(fn))) return st;
+  if (mask) {
+    MOE_LAUNCH("muon_live", s, moe::launch_dep(muon_live, 1, 32, 0, s, mask, n_mats, per, live));
+    if ((st = moe::launch_status(fn))) return st;
+  } else {
+    live = nullptr;
+  }
   for (int first = 0; first < n_mats; first += batch) {
     const int mats = std::min(batch, n_mats - first);
     // (grid.y holds 65,535 matrices at most)
@@ -576,7 +610,7 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
       auto step = [&](auto e) -> int {
         e.hi = xo[i & 1]; e.lo = lom; e.next = i + 1 < steps ? xo[(i + 1) & 1] : om; e.resid = resid; e.a = cf[0];
         e.rows = rows; e.cols = cols; e.tall = tall; e.to = to;
-        e.to.live = live + 1 + first;
+        e.to.live = live ? live + 1 + first : nullptr; e.to.first = first;
         if (tall)
           return small_x ? dg::product<dg::SmallIO, false, false, true>("muon_step", X, B, e, t, s, fn)
                          : dg::product<dg::WideIO, false, false, true>("muon_step", X, B, e, t, s, fn);
