@@ -55,6 +55,7 @@ struct GramEpi {
   int n;
 
   static constexpr int kChunk = 0;
+  static constexpr bool kTrigger = true;
 
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
@@ -87,6 +88,7 @@ struct PolyEpi {
   int n, pitch;
 
   static constexpr int kChunk = 0;
+  static constexpr bool kTrigger = true;
 
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
@@ -153,6 +155,7 @@ template <bool LAST> struct StepEpi {
   Target to;
 
   static constexpr int kChunk = 0;
+  static constexpr bool kTrigger = true;
 
   // A chunk of 32 columns at a time: TMA brings its hi and lo into a slot's two buffers (up to kSlots chunks ahead, the
   // first ones while the products still run), every lane changes its row in place, and TMA stores them.
