@@ -185,10 +185,6 @@ struct Warp {
 };
 
 // Epi: struct passed to the kernel by value, with the tensor maps it stores through.
-//   kTrigger:     whether the next kernel on the stream may become resident while this one's last stores end. Chains of dense
-//                 products gain by it (17 launches at 16 matrices 256 x 512: 117 -> 110 us, as a graph 115 -> 102); in the
-//                 vocabulary loss, where row kernels of thousands of blocks follow, it cost 15% (91 -> 105 us at 512 tokens,
-//                 d 512, 32,000 entries).
 //   kChunk == 0:  template <int BN, int kSlots> run(warp, ready): reads the accumulator and writes the results; calls ready() before
 //                 the first read, after whatever it can load meanwhile, and returns at once if that is false.
 //                 (kSlots: pairs of staging buffers)
@@ -424,7 +420,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   }
 
-  if (Epi::kTrigger) pdl_launch();
   tc::fence_before_sync();
   __syncthreads();
   tc::cluster_sync();  // no CTA leaves while its peer may still signal it

@@ -55,7 +55,6 @@ struct GramEpi {
   int n;
 
   static constexpr int kChunk = 0;
-  static constexpr bool kTrigger = true;
 
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
@@ -88,7 +87,6 @@ struct PolyEpi {
   int n, pitch;
 
   static constexpr int kChunk = 0;
-  static constexpr bool kTrigger = true;
 
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
@@ -155,7 +153,6 @@ template <bool LAST> struct StepEpi {
   Target to;
 
   static constexpr int kChunk = 0;
-  static constexpr bool kTrigger = true;
 
   // A chunk of 32 columns at a time: TMA brings its hi and lo into a slot's two buffers (up to kSlots chunks ahead, the
   // first ones while the products still run), every lane changes its row in place, and TMA stores them.
@@ -380,6 +377,15 @@ __device__ __forceinline__ void load_u(const Source &s, size_t row, int col, flo
 // Sums of squares of a matrix's U in three scales, so that any fp32 values have a norm: squares of values
 // around 1, of small ones times 2^80, of large ones times 2^-80. Block (part, slot).
 constexpr float kUp = 1.2089258196146292e24f, kDown = 8.271806125530277e-25f;  // 2^80, 2^-80
+
+// |U|_F + eps times a power of two, `pre`, from those sums: the plain one unless it lost squares below (then it is small) or
+// above fp32's range (where the norm itself may lie: U and eps are divided as they are scaled).
+__device__ __forceinline__ void scaled_norm(const float (&t)[3], float eps, float &pre, float &norm) {
+  const int j = t[0] > 1e30f ? 2 : t[0] < 1e-18f ? 1 : 0;
+  pre = j == 2 ? kDown : j == 1 ? kUp : 1.f;
+  norm = sqrtf(j == 2 ? t[2] : j == 1 ? t[1] : t[0]) + eps * pre;
+}
+
 __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__restrict__ live, int first, int parts,
                                                  float *__restrict__ sums) {
   __shared__ float sh[3][8];
@@ -436,16 +442,11 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) t[j] += __shfl_down_sync(0xffffffffu, t[j], o);
     if (threadIdx.x == 0) {
-      // the plain sum unless it lost squares below (then it is small) or above fp32's range; the norm itself may
-      // lie above it, so U and eps are divided as they are scaled
-      const int j = t[0] > 1e30f ? 2 : t[0] < 1e-18f ? 1 : 0;
-      const float pre = j == 2 ? kDown : j == 1 ? kUp : 1.f;
-      sh[0] = pre;
-      sh[1] = sqrtf(j == 2 ? t[2] : j == 1 ? t[1] : t[0]) + eps * pre;
+      scaled_norm(t, eps, sh[0], sh[1]);
     }
   }
   __syncthreads();
-  const float pre = sh[0], norm = sh[1];
+  const float pre = sh[0], factor = scale / sh[1];  // (a division each value was slower than the memory)
   const size_t mrow = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows;
   const int cpr = (s.cols + 7) / 8;
   const int64_t units = int64_t(s.rows) * cpr;
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
     uint32_t h[4], l[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float x = u[2 * j] * pre / norm * scale, y = u[2 * j + 1] * pre / norm * scale;
+      const float x = u[2 * j] * pre * factor, y = u[2 * j + 1] * pre * factor;
       h[j] = pack_half2(x, y);
       const float2 b = unpack_half2(h[j]);
       l[j] = pack_half2((x - b.x) * kLo, (y - b.y) * kLo);
@@ -465,6 +466,393 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
     const size_t o = (size_t(slot) * s.rows + r) * pitch + col;
     stg_v4(hi + o, make_uint4(h[0], h[1], h[2], h[3]));
     stg_v4(lo + o, make_uint4(l[0], l[1], l[2], l[3]));
+  }
+}
+
+// ---------------------------------------------------------------- matrices of a short side up to 128: on the chip
+//
+// A cluster of up to eight CTAs takes a matrix through momentum, norm, all steps and the update. A CTA owns all n <= 128
+// rows of `cols` <= 384 columns of X (of X^T where rows > cols): X itself as fp32 accumulator in TMEM (128 lanes x cols), its
+// half-precision rounding in shared memory, where one copy serves both products: its 64-column blocks of 128-byte rows are a K-major
+// operand for X X^T (the reduction along the columns) and an MN-major one for B X (along the rows). Per step: the CTA's share of
+// X X^T into 128 TMEM columns; the shares summed over the cluster (each CTA adds up 128 / CTAs rows, fp32, in the order of
+// the ranks, and gives A's rows to all); A A and B in every CTA; B X added by the tensor cores onto a X in TMEM.
+// As launches the 3 * steps products took 85-145 us whatever the size, which is latency; nothing here leaves the cluster. X is kept
+// in fp32 (22 bits in the launches' form), and roundings to half precision are theirs.
+constexpr int kN = 128;           // rows, zero past n
+constexpr int kMaxCols = 384;     // of a CTA: with the 128 columns of the products all of TMEM's 512
+constexpr int kMaxCluster = 8;
+constexpr int kSms = 152;
+constexpr int kSmallThreads = 512;   // four warps a TMEM lane quarter take 32-column chunks in turns
+constexpr uint32_t kBlkBytes = kN * 128;                                  // 128 rows of 64 halves
+constexpr uint32_t kOffA = kMaxCols / 64 * kBlkBytes, kOffB = kOffA + 2 * kBlkBytes, kOffRecv = kOffB + 2 * kBlkBytes;
+constexpr uint32_t kOffMisc = kOffRecv + kN * kN * 4;
+constexpr size_t kSmallSmem = 1024 + kOffMisc + 1024;
+
+struct SmallArgs {
+  Source s;
+  Target to;
+  const uint8_t *mask;
+  int per, n, k, tall, steps, ctas, cols;
+  float scale, eps;
+  float coef[3 * kMaxSteps];
+};
+
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster_v2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// 16-byte chunk q of row r in a block of 128-byte rows with the tensor cores' 128-byte swizzle.
+__device__ __forceinline__ uint32_t sw128(uint32_t block, int r, int q) {
+  return block + uint32_t(r) * 128u + (uint32_t(q ^ (r & 7)) << 4);
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  const int mat = int(blockIdx.x) / p.ctas;
+  pdl_start();
+  if (p.mask != nullptr && p.mask[mat / p.per] == 0) return;  // (the whole cluster)
+  const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t sX = base, sA = base + kOffA, sB = base + kOffB, recv = base + kOffRecv, misc = base + kOffMisc;
+  // misc: TMEM address, barrier, sums of the cluster's CTAs [8][3], of the warps [16][3], what B's diagonal lost [128]
+  const uint32_t bar = misc + 8, sums = misc + 16, wsums = misc + 128, delta = misc + 384;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = int(tc::cluster_ctarank()), ctas = p.ctas;
+  const int row0 = (warp & 3) * 32, row = row0 + lane, group = warp >> 2;
+  const int blocks = p.cols / 64, chunks = p.cols / 32;
+  const int col_cta = rank * p.cols;
+  if (tid == 0) {
+    tc::mbar_init(bar, 1);
+    tc::fence_mbar_init();
+  }
+  if (warp == 0) {
+    tc::tmem_alloc(misc, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::cluster_sync();  // (the peers' shared memory is written to from here on)
+  tc::fence_after_sync();
+  uint32_t tmem;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(misc) : "memory");
+  const uint32_t t_x = tmem + (uint32_t(row0) << 16), t_acc = tmem + kMaxCols;
+  const uint32_t t_acc_w = t_acc + (uint32_t(row0) << 16) + uint32_t(group * 32);  // this warp's 32 of 128 columns
+  uint32_t phase = 0;
+  auto mma_wait = [&]() {
+    volatile int never = 0;
+    if (!tc::mbar_wait(bar, phase & 1u, dg::kWaitLimitNs, &never)) dev_flag(&g_dev_err, MOE_DEV_WAIT_TIMEOUT);
+    ++phase;
+    tc::fence_after_sync();
+  };
+  // Everyone's shared memory and TMEM writes before the tensor cores' next reads.
+  auto publish = [&]() {
+    tc::fence_proxy_async_smem();
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+  };
+  // 32 x 32 fp32 a warp, where A and B are or will be
+  const uint32_t scratch = sA + uint32_t(warp) * 4096u;
+  const size_t m0 = size_t(mat) * p.s.rows * p.s.cols;
+  // In memory, X's columns lie together (a lane a column, turned round through scratch), or with `tall` its rows (a lane a row).
+
+  // ---- momentum, U into TMEM, sums of squares
+  float q0 = 0.f, q1 = 0.f, q2 = 0.f;
+  for (int c = group; c < chunks; c += 4) {
+    const int j0 = col_cta + 32 * c;  // first of 32 columns of X
+    float u[32];
+    // row of X (wide) or column (tall) i of the chunk, this lane the other index
+    const int other = p.tall ? row : j0 + lane;
+    const int end_i = p.tall ? p.k - j0 : p.n - row0;
+    const bool in = other < (p.tall ? p.n : p.k);
+    const size_t o = m0 + (p.tall ? size_t(j0) * p.s.cols + row : size_t(row0) * p.s.cols + j0 + lane);
+    float m[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      u[i] = m[i] = 0.f;
+      if (in && i < end_i) {
+        u[i] = __uint_as_float(uint32_t(p.s.g[o + size_t(i) * p.s.cols]) << 16);
+        if (p.s.m != nullptr) m[i] = p.s.m[o + size_t(i) * p.s.cols];
+      }
+    }
+    if (p.s.m != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        m[i] = fmaf(p.s.mu, m[i], u[i]);
+        if (in && i < end_i) p.s.m[o + size_t(i) * p.s.cols] = m[i];
+        u[i] = p.s.nesterov ? fmaf(p.s.mu, m[i], u[i]) : m[i];
+      }
+    }
+    float r0 = 0.f, r1 = 0.f, r2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float up = u[i] * kUp, down = u[i] * kDown;
+      r0 = fmaf(u[i], u[i], r0);
+      r1 = fmaf(up, up, r1);
+      r2 = fmaf(down, down, r2);
+    }
+    q0 += r0;
+    q1 += r1;
+    q2 += r2;
+    if (!p.tall) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) st_shared_f32(scratch + uint32_t(i * 32 + (lane ^ i)) * 4u, u[i]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) u[i] = ld_shared_f32(scratch + uint32_t(lane * 32 + (i ^ lane)) * 4u);
+      __syncwarp();
+    }
+    tc::tmem_st_32x32b_x32(t_x + 32 * c, reinterpret_cast<const uint32_t(&)[32]>(u));
+  }
+  tc::tmem_st_wait();
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    q0 += __shfl_down_sync(0xffffffffu, q0, o);
+    q1 += __shfl_down_sync(0xffffffffu, q1, o);
+    q2 += __shfl_down_sync(0xffffffffu, q2, o);
+  }
+  if (lane == 0) {
+    st_shared_f32(wsums + 12u * warp, q0);
+    st_shared_f32(wsums + 12u * warp + 4, q1);
+    st_shared_f32(wsums + 12u * warp + 8, q2);
+  }
+  __syncthreads();
+  if (tid < 3) {
+    float v = 0.f;
+    for (int i = 0; i < kSmallThreads / 32; ++i) v += ld_shared_f32(wsums + 12u * i + 4u * tid);
+    for (int r = 0; r < ctas; ++r) st_cluster_f32(tc::mapa(sums + 12u * rank + 4u * tid, r), v);
+  }
+  tc::cluster_sync();
+  float norm, pre;
+  {
+    float t[3] = {0.f, 0.f, 0.f};
+    for (int r = 0; r < ctas; ++r)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) t[i] += ld_shared_f32(sums + 12u * r + 4u * i);
+    scaled_norm(t, p.eps, pre, norm);
+  }
+  const float factor = p.scale / norm;
+
+  // X's row chunk in S units: its rounding to shared memory, kScaleA * a * x to TMEM for the next step's sum.
+  auto keep = [&](int c, float (&x)[32], float a) {
+    const int col = 32 * c;
+    const uint32_t blk = sX + uint32_t(col / 64) * kBlkBytes;
+    const int q0_ = (col & 63) / 8;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      tc::st_shared_v4(sw128(blk, row, q0_ + g),
+                       make_uint4(pack_half2(x[8 * g], x[8 * g + 1]), pack_half2(x[8 * g + 2], x[8 * g + 3]),
+                                  pack_half2(x[8 * g + 4], x[8 * g + 5]), pack_half2(x[8 * g + 6], x[8 * g + 7])));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] *= a * kScaleA;
+    tc::tmem_st_32x32b_x32(t_x + 32 * c, reinterpret_cast<const uint32_t(&)[32]>(x));
+  };
+  for (int c = group; c < chunks; c += 4) {
+    float x[32];
+    tc::tmem_ld_32x32b_x32(t_x + 32 * c, reinterpret_cast<uint32_t(&)[32]>(x));
+    tc::tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = x[i] * pre * factor;
+    keep(c, x, p.coef[0]);
+  }
+  tc::tmem_st_wait();
+  __syncthreads();  // (the scratch of all warps is done with)
+  for (int i = tid; i < int(2 * kBlkBytes / 16); i += kSmallThreads) tc::st_shared_v4(sA + 16u * i, make_uint4(0, 0, 0, 0));
+  if (ctas > 1) tc::cluster_sync();  // before a peer's rows of A come
+
+  constexpr uint32_t kSquare = tc::idesc_f16_f32(kN, kN), kTimesX = tc::idesc_f16_f32(kN, 64, false, true);
+  const float gram_scale = kScaleA / (p.scale * p.scale);
+  const int mine = kN / ctas;  // rows of A that this CTA adds up
+  for (int step = 0; step < p.steps; ++step) {
+    // ---- this CTA's share of X X^T
+    publish();
+    if (tid == 0) {
+      for (int b = 0; b < blocks; ++b)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const uint64_t d = tc::smem_desc_sw128(sX + b * kBlkBytes + kk * 32, 16, 1024);
+          tc::mma_bf16(t_acc, d, d, kSquare, (b | kk) != 0 ? 1u : 0u);
+        }
+      tc::mma_commit(bar);
+    }
+    mma_wait();
+    const bool in_a = row0 < p.n && group * 32 < p.n;  // A is n x n; the rest of it stays zero
+    if (ctas == 1) {
+      if (in_a) {
+        uint32_t r[32];
+        tc::tmem_ld_32x32b_x32(t_acc_w, r);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint32_t v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] = pack_half2(__uint_as_float(r[8 * g + 2 * i]) * gram_scale, __uint_as_float(r[8 * g + 2 * i + 1]) * gram_scale);
+          tc::st_shared_v4(sw128(sA + (group / 2) * kBlkBytes, row, (group & 1) * 4 + g), make_uint4(v[0], v[1], v[2], v[3]));
+        }
+      }
+    } else {
+      // rows to the CTA that adds them up: [source][row][128 values], 16-byte chunks at q ^ (row % 32)
+      const int local = row / ctas;  // (rows are dealt out: all CTAs have some of few)
+      const uint32_t to = tc::mapa(recv, uint32_t(row % ctas)) + uint32_t(rank * mine + local) * (kN * 4u);
+      if (in_a) {
+        uint32_t r[32];
+        tc::tmem_ld_32x32b_x32(t_acc_w, r);
+        tc::tmem_ld_wait();
+        if (row < p.n) {
+#pragma unroll
+          for (int g = 0; g < 8; ++g)
+            if (group * 32 + 4 * g < p.n)
+              st_cluster_v4(to + (uint32_t((group * 8 + g) ^ (local & 31)) << 4),
+                            make_float4(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]), __uint_as_float(r[4 * g + 2]),
+                                        __uint_as_float(r[4 * g + 3])));
+        }
+      }
+      tc::fence_before_sync();
+      tc::cluster_sync();
+      const int quads = (p.n + 3) / 4;
+      for (int i = tid; i < mine * 32; i += kSmallThreads) {
+        const int local_i = i / 32, q = i % 32, a_row = local_i * ctas + rank;
+        if (q >= quads || a_row >= p.n) continue;
+        const uint32_t from = recv + uint32_t(local_i) * (kN * 4u) + (uint32_t(q ^ (local_i & 31)) << 4);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int r = 0; r < ctas; ++r) {
+          const float4 w = ld_shared_f4(from + uint32_t(r * mine) * (kN * 4u));
+          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        const uint32_t lo = pack_half2(v.x * gram_scale, v.y * gram_scale), hi = pack_half2(v.z * gram_scale, v.w * gram_scale);
+        const uint32_t at = sw128(sA + uint32_t(q / 16) * kBlkBytes, a_row, (q % 16) / 2) + uint32_t(q & 1) * 8u;
+        for (int r = 0; r < ctas; ++r) st_cluster_v2(tc::mapa(at, r), lo, hi);
+      }
+      asm volatile("fence.proxy.async;" ::: "memory");
+      tc::cluster_sync();
+    }
+    // ---- A A, B = b A + c A A
+    publish();
+    if (tid == 0) {
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const uint64_t d = tc::smem_desc_sw128(sA + (kk >> 2) * kBlkBytes + (kk & 3) * 32, 16, 1024);
+        tc::mma_bf16(t_acc, d, d, kSquare, kk != 0 ? 1u : 0u);
+      }
+      tc::mma_commit(bar);
+    }
+    mma_wait();
+    const float cb = p.coef[3 * step + 1], cc = p.coef[3 * step + 2] * (1.f / kScaleA);
+    {
+      uint32_t r[32];
+      tc::tmem_ld_32x32b_x32(t_acc_w, r);
+      tc::tmem_ld_wait();
+      const uint32_t blk_a = sA + (group / 2) * kBlkBytes, blk_b = sB + (group / 2) * kBlkBytes;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint4 av = tc::ld_shared_v4(sw128(blk_a, row, (group & 1) * 4 + g));
+        const uint32_t pa[4] = {av.x, av.y, av.z, av.w};
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 8 * g + 2 * i;
+          const float2 ai = unpack_half2(pa[i]);
+          const float y0 = fmaf(cb, ai.x, cc * __uint_as_float(r[j])), y1 = fmaf(cb, ai.y, cc * __uint_as_float(r[j + 1]));
+          v[i] = pack_half2(y0, y1);
+          const float2 back = unpack_half2(v[i]);
+          const int col = group * 32 + j;
+          if (col == row) st_shared_f32(delta + 4u * row, (y0 - back.x) * (1.f / kScaleA));
+          if (col + 1 == row) st_shared_f32(delta + 4u * row, (y1 - back.y) * (1.f / kScaleA));
+        }
+        tc::st_shared_v4(sw128(blk_b, row, (group & 1) * 4 + g), make_uint4(v[0], v[1], v[2], v[3]));
+      }
+    }
+    // ---- B X onto a X
+    publish();
+    if (tid == 0) {
+      for (int b = 0; b < blocks; ++b)
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+          tc::mma_bf16(tmem + b * 64, tc::smem_desc_sw128(sB + (kk >> 2) * kBlkBytes + (kk & 3) * 32, 16, 1024),
+                       tc::smem_desc_sw128(sX + b * kBlkBytes + kk * 2048, kBlkBytes, 1024), kTimesX, 1u);
+      tc::mma_commit(bar);
+    }
+    const float dr = ld_shared_f32(delta + 4u * row);
+    mma_wait();
+    const bool last = step + 1 == p.steps;
+    const float next_a = last ? 0.f : p.coef[3 * step + 3];
+#pragma unroll 1
+    for (int c = group; c < chunks; c += 4) {
+      const int col = 32 * c;
+      const uint32_t blk = sX + uint32_t(col / 64) * kBlkBytes;
+      float x[32];
+      tc::tmem_ld_32x32b_x32(t_x + 32 * c, reinterpret_cast<uint32_t(&)[32]>(x));
+      tc::tmem_ld_wait();
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const uint4 xv = tc::ld_shared_v4(sw128(blk, row, (col & 63) / 8 + g));
+        const uint32_t px[4] = {xv.x, xv.y, xv.z, xv.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 h = unpack_half2(px[i]);
+          x[8 * g + 2 * i] = fmaf(dr, h.x, x[8 * g + 2 * i] * (1.f / kScaleA));
+          x[8 * g + 2 * i + 1] = fmaf(dr, h.y, x[8 * g + 2 * i + 1] * (1.f / kScaleA));
+        }
+      }
+      if (!last) {
+        keep(c, x, next_a);
+        continue;
+      }
+      // ---- the result (A and B are no longer needed: their place is scratch)
+      const int j0 = col_cta + col;
+      if (!p.tall) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) st_shared_f32(scratch + uint32_t(lane * 32 + (i ^ lane)) * 4u, x[i]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = ld_shared_f32(scratch + uint32_t(i * 32 + (lane ^ i)) * 4u);
+        __syncwarp();
+      }
+      const int other = p.tall ? row : j0 + lane;
+      const int end_i = other < (p.tall ? p.n : p.k) ? (p.tall ? p.k - j0 : p.n - row0) : 0;
+      const size_t o = m0 + (p.tall ? size_t(j0) * p.s.cols + row : size_t(row0) * p.s.cols + j0 + lane);
+      float v[32];
+      if (p.to.out == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          v[i] = 0.f;
+          if (i < end_i) {
+            const size_t at = o + size_t(i) * p.s.cols;
+            v[i] = p.to.master != nullptr ? p.to.master[at] : __uint_as_float(uint32_t(p.to.w[at]) << 16);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (i >= end_i) continue;
+        const size_t at = o + size_t(i) * p.s.cols;
+        float y = x[i] * p.to.inv;
+        if (p.to.out == nullptr) {
+          y = fmaf(p.to.keep, v[i], -p.to.step * y);
+          if (p.to.master != nullptr) p.to.master[at] = y;
+        }
+        (p.to.out != nullptr ? p.to.out : p.to.w)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+      }
+    }
+    tc::tmem_st_wait();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (ctas > 1) tc::cluster_sync();  // no CTA leaves while a peer may still write to it
+  if (warp == 0) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem, 512);
   }
 }
 
@@ -516,6 +904,66 @@ bool small_tiles(long long tiles) {
 
 const float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
 
+// CTAs for the columns of a matrix in the form on the chip: as few as hold them, and more while there are SMs without one.
+int small_cols(int k, int ctas) { return ceil_div(ceil_div(k, ctas), 64) * 64; }
+int small_ctas(int n_mats, int k) {
+  int ctas = 1;
+  while (ctas < kMaxCluster && (small_cols(k, ctas) > kMaxCols || (small_cols(k, ctas) > 64 && 2ll * ctas * n_mats <= kSms))) ctas *= 2;
+  return ctas;
+}
+// The form on the chip takes its phases one after another, an SM to a CTA: up to two CTAs an SM; the launches
+// of more matrices overlap better.
+// MOE_MUON_SMALL=0 or 1 takes the launches, or wherever it fits the other form (tests and A/B measurements).
+bool small_form(int n_mats, int n, int k) {
+  static const int forced = [] {
+    const char *e = getenv("MOE_MUON_SMALL");
+    return e && (e[0] == '0' || e[0] == '1') && e[1] == 0 ? e[0] - '0' : -1;
+  }();
+  if (n > kN || k > kMaxCluster * kMaxCols || forced == 0) return false;
+  return forced == 1 || (long long)n_mats * small_ctas(n_mats, k) <= 2 * kSms;
+}
+
+int run_small(const Source &u, const Target &to, const uint8_t *mask, int n_mats, int per, const float *coef, int steps, float eps,
+              float scale, cudaStream_t s, const char *what) {
+  SmallArgs a = {};
+  a.s = u;
+  a.to = to;
+  a.mask = mask;
+  a.per = per;
+  a.n = std::min(u.rows, u.cols);
+  a.k = std::max(u.rows, u.cols);
+  a.tall = u.rows > u.cols;
+  a.steps = steps;
+  a.scale = scale;
+  a.eps = eps;
+  for (int i = 0; i < 3 * steps; ++i) a.coef[i] = coef ? coef[i] : kCoef[i % 3];
+  a.ctas = small_ctas(n_mats, a.k);
+  a.cols = small_cols(a.k, a.ctas);
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = unsigned(a.ctas);
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see moe::launch_dep
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(n_mats) * unsigned(a.ctas));
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = kSmallSmem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  static bool attr[64] = {};  // of each device
+  bool &set = attr[moe::device_slot()];
+  if (!set) {
+    cudaError_t e = cudaFuncSetAttribute(muon_small, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem));
+    if (e != cudaSuccess) return moe::cuda_status(e, what);
+    set = true;
+  }
+  MOE_LAUNCH("muon_small", s, cudaLaunchKernelEx(&cfg, muon_small, a));
+  return moe::launch_status(what);
+}
+
 int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int per, Target to, const float *coef, int steps,
         float eps, void *ws, size_t ws_bytes, cudaStream_t s) {
   const int rows = src.rows, cols = src.cols;
@@ -555,6 +1003,7 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
   to.vec = u.vec;
   to.inv = 1.f / scale;
   int st;
+  if (small_form(n_mats, n, k)) return run_small(u, to, mask, n_mats, per, coef, steps, eps, scale, s, fn);
   const int64_t xstep = int64_t(rows) * l.pitch, astep = int64_t(n) * l.npitch;
   CUtensorMap xo[2], lom, ao, bo;
   for (int i = 0; i < 2; ++i)

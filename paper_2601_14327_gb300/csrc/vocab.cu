@@ -43,7 +43,6 @@ template <bool KEEP> struct LogitsEpi {
   int rows, V, np;
   // lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum, whose errors point one way
   static constexpr int kChunk = 512;
-  static constexpr bool kTrigger = false;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     static_assert(BN / 2 == kBlk, "a warp's half tile is a block");
@@ -108,7 +107,6 @@ struct OutEpi {
   const float *factor;
   int rows, cols;
   static constexpr int kChunk = 4096;  // (reductions over a vocabulary of 131,072)
-  static constexpr bool kTrigger = false;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     if (w.row - w.lane >= rows) return;
