@@ -139,6 +139,13 @@ struct Stager {
     ++turn;
     return b;
   }
+  // Both buffers, free of the stores before.
+  __device__ __forceinline__ void both(int lane, uint32_t &a, uint32_t &b) {
+    if (lane == 0) tc::bulk_wait_read<0>();
+    __syncwarp();
+    a = base;
+    b = base + kStageBytes;
+  }
 };
 
 // Where this lane's c-th 16 bytes (of four) lie in a staging buffer: row `lane` of a 32 x 32 chunk of 16-bit values in
@@ -394,13 +401,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               tc::tmem_ld_32x32b_x32(tb + c, *reinterpret_cast<uint32_t(*)[32]>(&z[c]));
             tc::tmem_ld_wait();
           } else {
+            // two loads in flight: the second while the first is added
+            uint32_t r[2][16];
+            tc::tmem_ld_32x32b_x16(tb, r[0]);
 #pragma unroll
             for (int c = 0; c < BNH; c += 16) {
-              uint32_t r[16];
-              tc::tmem_ld_32x32b_x16(tb + c, r);
+              const int i = (c / 16) & 1;
               tc::tmem_ld_wait();
+              if (c + 16 < BNH) tc::tmem_ld_32x32b_x16(tb + c + 16, r[i ^ 1]);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) z[c + i] += __uint_as_float(r[i]);
+              for (int j = 0; j < 16; ++j) z[c + j] += __uint_as_float(r[i][j]);
             }
           }
           release();

@@ -30,6 +30,34 @@ struct Sizes {
 };
 Sizes sizes(int V) { return {(int64_t(V) + kBlk - 1) / kBlk, (int64_t(V) + 63) / 64 * 64}; }
 
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Two fp32 values in a 64-bit register, and arithmetic on both.
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float &a, float &b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+// 2^x to 2 ulp; results below the normal range are 0.
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // ---------------------------------------------------------------- epilogues
 
 // Rows of the logits: see the top of the file. KEEP: the exponentials go to memory through `kept`.
@@ -65,27 +93,47 @@ template <bool KEEP> struct LogitsEpi {
 #pragma unroll
     for (int c = 4; c < kBlk; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
     const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-    const float base = m == -INFINITY ? 0.f : m;  // (a block of -inf alone: exponentials of 0)
-    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+    // exp(z - m) = 2^(z log2 e - m log2 e), two values an instruction (a block of -inf alone: exponentials of 0)
+    const float shift = m == -INFINITY ? 0.f : m * -kLog2e;
+    const uint64_t scale2 = pack_f32x2(kLog2e, kLog2e), shift2 = pack_f32x2(shift, shift);
+    uint64_t sum2[2] = {0, 0};
 #pragma unroll
-    for (int c = 0; c < kBlk; ++c) {
-      z[c] = __expf(z[c] - base);
-      s4[c & 3] += z[c];
+    for (int c = 0; c < kBlk; c += 2) {
+      float a, b;
+      unpack_f32x2(fma_f32x2(pack_f32x2(z[c], z[c + 1]), scale2, shift2), a, b);
+      z[c] = exp2_approx(a);
+      z[c + 1] = exp2_approx(b);
+      sum2[(c >> 1) & 1] = add_f32x2(sum2[(c >> 1) & 1], pack_f32x2(z[c], z[c + 1]));
     }
-    if (w.row < rows)
-      part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, (s4[0] + s4[1]) + (s4[2] + s4[3]));
+    float s0, s1;
+    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+    if (w.row < rows) part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, s0 + s1);
     if (KEEP) {
 #pragma unroll
-      for (int c = 0; c < kBlk; c += 32) {
+      for (int c = 0; c < kBlk; c += 64) {  // both staging buffers with one fence
         if (c >= nv) break;
-        uint4 v[4];
-        uint32_t *p = reinterpret_cast<uint32_t *>(v);
+        uint32_t buf[2];
+        w.st.both(w.lane, buf[0], buf[1]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const __half2 h = __floats2half2_rn(z[c + 2 * i], z[c + 2 * i + 1]);
-          p[i] = *reinterpret_cast<const uint32_t *>(&h);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int j = c + 32 * h + 8 * q + 2 * i;
+              const __half2 x = __floats2half2_rn(z[j], z[j + 1]);
+              v[i] = *reinterpret_cast<const uint32_t *>(&x);
+            }
+            tc::st_shared_v4(dg::stage_at(buf[h], w.lane, q), make_uint4(v[0], v[1], v[2], v[3]));
+          }
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (w.lane == 0) {
+          tc::tma_store_3d(&kept, buf[0], w.col + c, w.row - w.lane, 0);
+          if (c + 32 < nv) tc::tma_store_3d(&kept, buf[1], w.col + c + 32, w.row - w.lane, 0);
+          tc::bulk_commit();
         }
-        dg::stage_and_store(&kept, w.st, w.lane, v, w.col + c, w.row - w.lane, 0);
       }
     }
   }
