@@ -14,6 +14,8 @@
 
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "tc_ptx.cuh"
 #include "tmap.cuh"
@@ -198,10 +200,40 @@ struct Warp {
 //   kChunk > 0:   template <int BN> run(warp, z): z [BN / 2] is the row's result in fp32. The tensor cores' accumulator is
 //                 cut short in every 16-wide step (no rounding to nearest: errors of a long sum add up), so that
 //                 the sum is taken out of it every kChunk values of the reduction and added up in registers.
-template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
+// A second product in the same launch (DUAL), with its reduction along A's rows: its tiles follow the first one's. Where those
+// leave a last wave unfilled, the pairs without a tile in it take `head` tiles of the second meanwhile.
+template <class Epi> struct Second {
+  CUtensorMap a, b;
+  Epi epi;
+  Tiles t;
+  int head;   // what a tile of the first product costs, in tiles of the second
+};
+struct NoSecond {};
+
+// The j-th tile of this pair; false: no more. job: 0, or 1 of the second product.
+struct Items {
+  int cluster, nclusters;
+  int total, total2, mine, rem, head;
+  __device__ __forceinline__ bool at(int j, int &job, int &u) const {
+    job = 0;
+    u = cluster + j * nclusters;
+    if (u < total) return true;
+    if (total2 == 0) return false;
+    job = 1;
+    const int i = j - mine;
+    const int free = nclusters - rem;  // pairs with one tile of the first product less (rem > 0)
+    const int early = rem > 0 ? free * head : 0;
+    if (rem > 0 && cluster >= rem) u = i < head ? (cluster - rem) + free * i : early + (i - head) * nclusters + cluster;
+    else u = early + i * nclusters + cluster;
+    return u < total2;
+  }
+};
+
+template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi, class Extra>
 __global__ void __launch_bounds__(kThreads, 1)
     dense_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                      const __grid_constant__ Epi epi, const Tiles t) {
+                      const __grid_constant__ Epi epi, const Tiles t, const __grid_constant__ Extra second) {
+  constexpr bool DUAL = !std::is_same<Extra, NoSecond>::value;
   constexpr int STAGES = Sh::STAGES, BN = Sh::BN, BNH = Sh::BNH, KB = Sh::KB;
   constexpr int kChunkBlocks = Epi::kChunk / KB;  // 0: the whole reduction
   constexpr uint32_t IDESC = HALF ? tc::idesc_f16_f32(2 * BM, BN, A_MN, B_MN) : tc::idesc_bf16_f32(2 * BM, BN, A_MN, B_MN);
@@ -257,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::tmem_relinquish_pair();
   }
   const Walk walk(t, BN, KB);
-  Tile x = walk.at(t, cluster, BN);  // this pair's first tile
+  Tile x = walk.at(t, cluster, BN);  // this pair's first tile (DUAL: of the first product)
   pdl_wait();  // (barriers, TMEM and the first tile's numbers while the previous kernel ends)
   tc::fence_before_sync();
   __syncthreads();
@@ -266,7 +298,32 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(misc);
 
   const int mats = t.live != nullptr ? max(0, min(t.mats, *t.live - t.first)) : t.mats;
-  const int total = mats * t.splits * walk.per;
+  Items items;
+  items.cluster = cluster;
+  items.nclusters = nclusters;
+  items.total = mats * t.splits * walk.per;
+  items.total2 = 0;
+  Walk walk2 = walk;
+  if constexpr (DUAL) {
+    walk2 = Walk(second.t, BN, KB);
+    items.total2 = second.t.mats * second.t.splits * walk2.per;
+    items.rem = items.total % nclusters;
+    items.mine = items.total / nclusters + (cluster < items.rem ? 1 : 0);
+    items.head = second.head;
+    if (cluster >= items.total) x = walk2.at(second.t, min(cluster - items.rem, items.total2 - 1), BN);
+  }
+  int job = 0, u = 0;
+  // the tile after this pair's j-th
+  auto next = [&](int j) {
+    if (!items.at(j + 1, job, u)) return;
+    if constexpr (DUAL) {
+      if (job != 0) {
+        x = walk2.at(second.t, u, BN);
+        return;
+      }
+    }
+    x = walk.at(t, u, BN);
+  };
 
   if (warp == 0) {
     // ============ TMA producer (one thread in each CTA) ============
@@ -274,7 +331,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t full_leader = tc::mapa(full_bar(0), 0);
       uint32_t it = 0;
       bool ok = true;
-      for (int u = cluster; u < total && ok; u += nclusters, x = walk.at(t, u, BN)) {
+      for (int j = 0; ok && items.at(j, job, u); next(j), ++j) {
+        const bool a_mn = A_MN || (DUAL && job != 0);
+        const CUtensorMap *ma = &tmA, *mb = &tmB;
+        if constexpr (DUAL) {
+          if (job != 0) {
+            ma = &second.a;
+            mb = &second.b;
+          }
+        }
         const int arow = x.mp * kTileRows + int(rank) * BM, brow = x.nt * BN + int(rank) * BNH;
         for (int kb = x.kb0; kb < x.kb1; ++kb, ++it) {
           const int s = it % STAGES;
@@ -286,23 +351,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int k0 = kb * KB;
           // K-major: one box per 64-deep half, half h at h * rows * 128 bytes; MN-major: one box of 64
           // columns x KB rows per 64 columns
-          if (A_MN) {
+          if (a_mn) {
 #pragma unroll
             for (int i = 0; i < BM / 64; ++i)
-              tc::tma_load_3d_pair(a_dst + i * (KB * 128), &tmA, fb, arow + i * 64, k0, x.z);
+              tc::tma_load_3d_pair(a_dst + i * (KB * 128), ma, fb, arow + i * 64, k0, x.z);
           } else {
 #pragma unroll
             for (int h = 0; h < KB / 64; ++h)
-              tc::tma_load_3d_pair(a_dst + h * (BM * 128), &tmA, fb, k0 + h * 64, arow, x.z);
+              tc::tma_load_3d_pair(a_dst + h * (BM * 128), ma, fb, k0 + h * 64, arow, x.z);
           }
           if (B_MN) {
 #pragma unroll
             for (int i = 0; i < BNH / 64; ++i)
-              tc::tma_load_3d_pair(b_dst + i * (KB * 128), &tmB, fb, brow + i * 64, k0, x.z);
+              tc::tma_load_3d_pair(b_dst + i * (KB * 128), mb, fb, brow + i * 64, k0, x.z);
           } else {
 #pragma unroll
             for (int h = 0; h < KB / 64; ++h)
-              tc::tma_load_3d_pair(b_dst + h * (BNH * 128), &tmB, fb, k0 + h * 64, brow, x.z);
+              tc::tma_load_3d_pair(b_dst + h * (BNH * 128), mb, fb, k0 + h * 64, brow, x.z);
           }
         }
       }
@@ -321,7 +386,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (leader && lane == 0) {
       uint32_t it = 0, done = 0;  // accumulators issued: number i is in buffer i % 2
       bool ok = true, issued = false;
-      for (int u = cluster; u < total && ok; u += nclusters, x = walk.at(t, u, BN)) {
+      for (int j = 0; ok && items.at(j, job, u); next(j), ++j) {
+        const bool a_mn = A_MN || (DUAL && job != 0);
+        const uint32_t idesc = IDESC | (uint32_t(a_mn) << 15);
         for (int c0 = x.kb0; c0 < x.kb1 && ok; ++done) {
           const int c1 = kChunkBlocks > 0 ? min(x.kb1, c0 + kChunkBlocks) : x.kb1;
           const uint32_t a = done & 1u, aph = (done >> 1) & 1u;
@@ -340,11 +407,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               // swizzled row). MN-major: k-rows 16 kk .. 16 kk + 15 of every 64-column block.
               const uint32_t ha = uint32_t(kk >> 2) * (BM * 128), hb = uint32_t(kk >> 2) * (BNH * 128);
               const int q = kk & 3;
-              const uint64_t ad = A_MN ? tc::smem_desc_sw128(a_s + kk * 2048, KB * 128, 1024)
+              const uint64_t ad = a_mn ? tc::smem_desc_sw128(a_s + kk * 2048, KB * 128, 1024)
                                        : tc::smem_desc_sw128(a_s + ha + q * 32, 16, 1024);
               const uint64_t bd = B_MN ? tc::smem_desc_sw128(b_s + kk * 2048, KB * 128, 1024)
                                        : tc::smem_desc_sw128(b_s + hb + q * 32, 16, 1024);
-              tc::mma_bf16_pair(d_tmem, ad, bd, IDESC, (kb > c0 || kk > 0) ? 1u : 0u);
+              tc::mma_bf16_pair(d_tmem, ad, bd, idesc, (kb > c0 || kk > 0) ? 1u : 0u);
             }
             tc::mma_commit_pair_mc(empty_bar(s), 0x3);  // frees the stage in both CTAs
             issued = true;
@@ -385,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) tc::mbar_arrive_remote(tempty_leader + 8u * (done & 1u));
       ++done;
     };
-    for (int u = cluster; u < total; u += nclusters, x = walk.at(t, u, BN)) {
+    for (int j = 0; items.at(j, job, u); next(j), ++j) {
       w.row = x.mp * kTileRows + int(rank) * BM + q * 32 + lane;
       w.col = x.nt * BN + half * BNH;
       w.z = x.z;
@@ -402,21 +469,25 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tmem_ld_wait();
           } else {
             // two loads in flight: the second while the first is added
-            uint32_t r[2][16];
-            tc::tmem_ld_32x32b_x16(tb, r[0]);
+            uint32_t r[2][8];
+            tc::tmem_ld_32x32b_x8(tb, r[0]);
 #pragma unroll
-            for (int c = 0; c < BNH; c += 16) {
-              const int i = (c / 16) & 1;
+            for (int c = 0; c < BNH; c += 8) {
+              const int i = (c / 8) & 1;
               tc::tmem_ld_wait();
-              if (c + 16 < BNH) tc::tmem_ld_32x32b_x16(tb + c + 16, r[i ^ 1]);
+              if (c + 8 < BNH) tc::tmem_ld_32x32b_x8(tb + c + 8, r[i ^ 1]);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) z[c + j] += __uint_as_float(r[i][j]);
+              for (int j = 0; j < 8; ++j) z[c + j] += __uint_as_float(r[i][j]);
             }
           }
           release();
         }
         if (!ok) break;
-        epi.template run<BN>(w, z);
+        const Epi *e = &epi;
+        if constexpr (DUAL) {
+          if (job != 0) e = &second.epi;
+        }
+        e->template run<BN>(w, z);
       } else {
         w.tb = tb0 + (done & 1u) * BN;
         waited = false;
@@ -440,10 +511,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Launches the product over `most` tiles at most (the list may be shorter: Tiles::live).
-template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
-int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const Epi &epi, const Tiles &t, long long most,
-           cudaStream_t s, const char *what) {
-  auto kern = dense_pair_kernel<Sh, A_MN, B_MN, HALF, Epi>;
+template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi, class Extra>
+int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const Epi &epi, const Tiles &t, const Extra &second,
+           long long most, cudaStream_t s, const char *what) {
+  auto kern = dense_pair_kernel<Sh, A_MN, B_MN, HALF, Epi, Extra>;
   if (most > 0x3fffffff) return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: too many tiles", what);
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -472,7 +543,7 @@ int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const E
   }
   cfg.gridDim = dim3(2 * unsigned(std::max(1ll, std::min<long long>(n, most))));
   cfg.numAttrs = 2;
-  MOE_LAUNCH(name, s, cudaLaunchKernelEx(&cfg, kern, a, b, epi, t));
+  MOE_LAUNCH(name, s, cudaLaunchKernelEx(&cfg, kern, a, b, epi, t, second));
   return moe::launch_status(what);
 }
 
@@ -482,22 +553,46 @@ struct Matrix {
   int64_t mats, rows, cols, pitch, step;
 };
 
-// C[z] = A[z] B[z]^T for kernels of shape Sh; t.mt, t.nt and t.k are set here. A_MN, B_MN: the operand's rows are
-// the reduction.
+// Operand maps and tile numbers (t.mt, t.nt, t.k) of C[z] = A[z] B[z]^T; `most`: tiles at most.
+template <class Sh>
+int plan(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, bool half, Tiles &t, CUtensorMap *ma, CUtensorMap *mb,
+         long long *most, const char *what) {
+  int st;
+  if ((st = moe::make_map_stack(ma, a.p, half, a.mats, a.rows, a.cols, a.pitch, a.step, 64, a_mn ? Sh::KB : BM, what))) return st;
+  if ((st = moe::make_map_stack(mb, b.p, half, b.mats, b.rows, b.cols, b.pitch, b.step, 64, b_mn ? Sh::KB : Sh::BNH, what)))
+    return st;
+  const int64_t M = a_mn ? a.cols : a.rows, N = b_mn ? b.cols : b.rows;
+  t.mt = int((M + kTileRows - 1) / kTileRows);
+  t.nt = int((N + Sh::BN - 1) / Sh::BN);
+  t.k = int(a_mn ? a.rows : a.cols);
+  *most = (t.sym ? (long long)t.mt * (t.mt + 1) / 2 * (kTileRows / Sh::BN) : (long long)t.mt * t.nt) * t.splits * t.mats;
+  return MOE_OK;
+}
+
+// C[z] = A[z] B[z]^T for kernels of shape Sh. A_MN, B_MN: the operand's rows are the reduction.
 template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi>
 int product(const char *name, const Matrix &a, const Matrix &b, const Epi &epi, Tiles t, cudaStream_t s, const char *what) {
   CUtensorMap ma, mb;
-  int st;
-  if ((st = moe::make_map_stack(&ma, a.p, HALF, a.mats, a.rows, a.cols, a.pitch, a.step, 64, A_MN ? Sh::KB : BM, what)))
-    return st;
-  if ((st = moe::make_map_stack(&mb, b.p, HALF, b.mats, b.rows, b.cols, b.pitch, b.step, 64, B_MN ? Sh::KB : Sh::BNH, what)))
-    return st;
-  const int64_t M = A_MN ? a.cols : a.rows, N = B_MN ? b.cols : b.rows;
-  t.mt = int((M + kTileRows - 1) / kTileRows);
-  t.nt = int((N + Sh::BN - 1) / Sh::BN);
-  t.k = int(A_MN ? a.rows : a.cols);
-  const long long per = t.sym ? (long long)t.mt * (t.mt + 1) / 2 * (kTileRows / Sh::BN) : (long long)t.mt * t.nt;
-  return launch<Sh, A_MN, B_MN, HALF>(name, ma, mb, epi, t, per * t.splits * t.mats, s, what);
+  long long most;
+  const int st = plan<Sh>(a, A_MN, b, B_MN, HALF, t, &ma, &mb, &most, what);
+  return st ? st : launch<Sh, A_MN, B_MN, HALF>(name, ma, mb, epi, t, NoSecond{}, most, s, what);
+}
+
+// Two products of bf16 matrices in a launch: A B^T with the reduction along B's rows, and A2 B2^T with it along both
+// operands' rows. head: see Second.
+template <class Sh, class Epi>
+int two_products(const char *name, const Matrix &a, const Matrix &b, const Epi &epi, Tiles t, const Matrix &a2, const Matrix &b2,
+                 const Epi &epi2, Tiles t2, int head, cudaStream_t s, const char *what) {
+  CUtensorMap ma, mb;
+  Second<Epi> second;
+  long long most, most2;
+  int st = plan<Sh>(a, false, b, true, false, t, &ma, &mb, &most, what);
+  if (!st) st = plan<Sh>(a2, true, b2, true, false, t2, &second.a, &second.b, &most2, what);
+  if (st) return st;
+  second.epi = epi2;
+  second.t = t2;
+  second.head = head;
+  return launch<Sh, false, true, false>(name, ma, mb, epi, t, second, most + most2, s, what);
 }
 
 inline int store_map(CUtensorMap *m, const void *base, bool half, int64_t mats, int64_t rows, int64_t cols,

@@ -190,8 +190,9 @@ constexpr int kSumThreads = 1024;
 __device__ __forceinline__ int count_targets(const int32_t *__restrict__ target, int T, int V, int *s) {
   int n = 0;
   bool bad = false;
+#pragma unroll 4
   for (int t = threadIdx.x; t < T; t += blockDim.x) {
-    const int v = target[t];
+    const int v = __ldg(target + t);
     n += v >= 0 && v < V;
     bad |= v >= V;
   }
@@ -299,10 +300,12 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
   if (row < rows) {
     float2 *p = part + size_t(row) * np;
     float m = -INFINITY;
+#pragma unroll 4
     for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     float s = 0.f;
+#pragma unroll 4
     for (int i = lane; i < np; i += 32) {
       const float2 v = p[i];
       s += v.y * __expf(v.x - m);
@@ -402,22 +405,29 @@ __global__ void __launch_bounds__(kSumThreads) vocab_loss_sum(const float *__res
 
 inline int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
-// Ranges of the vocabulary that dh's reduction is split into. A product of few rows has few tiles (2 at 256 x 512)
-// for 76 CTA pairs. Estimated in k-blocks of 128, which take ~0.57 us: the waves of tiles, 3 for a tile's start and
-// end, and the fp32 sums' way through memory and a launch more.
-int dh_splits(int64_t rows, int d, int V) {
-  const int64_t tiles = ((rows + 255) / 256) * ((int64_t(d) + 255) / 256), nkb = (int64_t(V) + dg::Wide::KB - 1) / dg::Wide::KB;
-  int best = 1;
+// How dh and dW are computed: ranges of the vocabulary that dh's reduction is split into (a product of few rows has few
+// tiles, 2 at 256 x 512, for 76 CTA pairs), and what one of its tiles costs in tiles of dW, which share its launch. Estimated in
+// k-blocks of 128, ~0.57 us each: a tile's k-blocks and 3 for its start and end; the fp32 sums' way through memory and a launch more.
+struct Plan {
+  int splits, head;
+};
+Plan grad_plan(int64_t rows, int d, int V, bool need_h, bool need_w) {
+  const int64_t wide = (int64_t(d) + 255) / 256, tiles = ((rows + 255) / 256) * wide, tiles_w = ((int64_t(V) + 255) / 256) * wide;
+  const int64_t nkb = (int64_t(V) + dg::Wide::KB - 1) / dg::Wide::KB, nkb_w = (rows + dg::Wide::KB - 1) / dg::Wide::KB;
+  const double cost_w = std::max(double(nkb_w) + 0.5, 4.0);  // (short reductions: the epilogue's time)
+  Plan best = {1, 1};
   double least = 0;
   for (int s = 1; s <= 64 && s <= nkb; ++s) {
-    double t = double((tiles * s + kPairs - 1) / kPairs) * double((nkb + s - 1) / s + 3);
+    const double unit = double((nkb + s - 1) / s) + 3 + (s > 1 ? 5 : 0);
+    double t = double((tiles * s + kPairs - 1) / kPairs) * unit;
+    if (need_w) t = std::max(t, (double(tiles * s) * unit + double(tiles_w) * cost_w) / kPairs);
     if (s > 1) t += double(s) * double(rows) * d * 8 / 6.7e12 / 0.57e-6 + 6;
     if (s == 1 || t < least) {
-      best = s;
+      best = {s, std::max(1, int(unit / cost_w + 0.5))};
       least = t;
     }
   }
-  return best;
+  return need_h ? best : Plan{1, 1};
 }
 
 struct Layout {
@@ -439,8 +449,10 @@ Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
     off += up256(rows * z.pitch * 2);
     int64_t n = 0;
     for (int64_t r : {rows, last}) {
-      const int s = r > 0 ? dh_splits(r, d, V) : 1;
-      if (s > 1) n = std::max(n, int64_t(frag_index(s, 0, 0, int(r), d)) * 4);
+      for (bool need_w : {false, true}) {
+        const int s = r > 0 ? grad_plan(r, d, V, true, need_w).splits : 1;
+        if (s > 1) n = std::max(n, int64_t(frag_index(s, 0, 0, int(r), d)) * 4);
+      }
     }
     l.dh = off;
     off += up256(n);
@@ -522,29 +534,31 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
                                                 int(z.np), k));
       if ((st = moe::launch_status(fn))) return st;
     }
+    const Plan plan = grad_plan(rows, d, V, d_hidden != nullptr, d_w != nullptr);
+    OutEpi eh = {}, ew = {};
+    dg::Tiles th = t;
+    th.splits = plan.splits;
+    uint16_t *out = d_hidden ? d_hidden + t0 * d : nullptr;
     if (d_hidden) {
-      OutEpi e = {};
-      e.rows = rows; e.cols = d; e.factor = factor;
-      t.splits = dh_splits(rows, d, V);
-      uint16_t *out = d_hidden + t0 * d;
-      if ((st = dg::store_map(&e.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
-      if (t.splits > 1) e.sum = dhp;
-      if ((st = dg::product<dg::Wide, false, true, false>("vocab_dh", mz, mw, e, t, s, fn))) return st;
-      if (t.splits > 1) {
-        const int64_t warps = int64_t((rows + 31) / 32) * (d / 8);
-        MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((warps + 7) / 8), 256, 0, s, dhp, t.splits, rows, d,
-                                                      factor, out));
-        if ((st = moe::launch_status(fn))) return st;
-      }
-      t.splits = 1;
+      eh.rows = rows; eh.cols = d; eh.factor = factor;
+      if ((st = dg::store_map(&eh.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
+      if (plan.splits > 1) eh.sum = dhp;
     }
     if (d_w) {
-      OutEpi e = {};
-      e.rows = V; e.cols = d; e.factor = factor;
-      if ((st = dg::store_map(&e.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
-      if (t0 > 0) e.add = dwp;
-      if (t0 + rows < T) e.sum = dwp;
-      if ((st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, e, t, s, fn))) return st;
+      ew.rows = V; ew.cols = d; ew.factor = factor;
+      if ((st = dg::store_map(&ew.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
+      if (t0 > 0) ew.add = dwp;
+      if (t0 + rows < T) ew.sum = dwp;
+    }
+    if (d_hidden && d_w) st = dg::two_products<dg::Wide>("vocab_dh_dw", mz, mw, eh, th, mz, mh, ew, t, plan.head, s, fn);
+    else if (d_hidden) st = dg::product<dg::Wide, false, true, false>("vocab_dh", mz, mw, eh, th, s, fn);
+    else st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, ew, t, s, fn);
+    if (st) return st;
+    if (plan.splits > 1) {
+      const int64_t warps = int64_t((rows + 31) / 32) * (d / 8);
+      MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((warps + 7) / 8), 256, 0, s, dhp, plan.splits, rows, d,
+                                                    factor, out));
+      if ((st = moe::launch_status(fn))) return st;
     }
   }
   if (whole) return MOE_OK;
