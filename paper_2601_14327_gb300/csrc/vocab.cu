@@ -22,7 +22,8 @@ MOE_DEV_ERR_DECL
 namespace {
 
 constexpr int kBlk = 128;    // columns that share a maximum
-constexpr int kWholeTokens = 2048;  // tokens up to which vocab_lse counts the targets and sums the losses itself
+constexpr int kWholeTokens = 2048;  // tokens up to which the last block of vocab_lse(_dz) counts the targets and sums the losses
+constexpr int kFewTokens = 512;     // tokens up to which vocab_lse_dz takes the place of vocab_lse and vocab_dz
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
 struct Sizes {
@@ -214,12 +215,11 @@ __global__ void __launch_bounds__(kSumThreads) vocab_count(const int32_t *__rest
   if (threadIdx.x == 0) *n_valid = n;
 }
 
-// dz = factor (a (p - 1[target]) + b lse p). The factor, the larger of |d_loss[0]| / M and 2 |d_loss[1] z_coef| / M, is taken
+// dz = factor (a (p - 1[target]) + b lse p). (a and b depend on d_loss and z_coef alone.) The factor, the larger of |d_loss[0]| / M and 2 |d_loss[1] z_coef| / M, is taken
 // out of dz and given to the products' results in fp32: an unsure token's target then has -1, which bf16 holds, where
 // rounding d_loss[0] / M itself would put all targets' share off by the same up to 2^-8.
 struct Coefs {
   const float *d_loss;
-  const int32_t *n_valid;
   float z_coef;
   __device__ __forceinline__ void get(int n, float &a, float &b, float &factor) const {
     const float d0 = d_loss != nullptr ? d_loss[0] : 1.f, d1 = d_loss != nullptr ? d_loss[1] : 1.f;
@@ -279,10 +279,51 @@ __device__ __forceinline__ void sum_losses(const float *lse, const float *nll, c
   }
 }
 
+// What is left to do once every token's lse is there, by one block: M, the losses and the factor. `s`: 64 floats.
+__device__ __forceinline__ void finish_losses(const float *lse, const float *nll, const int32_t *__restrict__ target, int T,
+                                              int V, const Coefs &k, int32_t *__restrict__ n_valid, float *__restrict__ loss,
+                                              float *__restrict__ factor, float *s) {
+  const int n = count_targets(target, T, V, reinterpret_cast<int *>(s));
+  sum_losses(lse, nll, target, T, V, k.z_coef, n, loss, s);
+  if (threadIdx.x == 0) {
+    float a, b, f;
+    k.get(n, a, b, f);
+    *n_valid = n;
+    *factor = f;
+  }
+}
+// Whether this block is the last of those that count `left` down to finish (their writes are then visible).
+__device__ __forceinline__ bool last_block(int *left, int *sh) {
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) *sh = atomicSub(left, 1) == 1;
+  __syncthreads();
+  if (*sh) __threadfence();
+  return *sh != 0;
+}
+
+// A row's log-sum-exp from its pairs, by a warp (every lane has it).
+__device__ __forceinline__ float row_lse(const float2 *p, int np, int lane) {
+  float m = -INFINITY;
+#pragma unroll 4
+  for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float s = 0.f;
+#pragma unroll 4
+  for (int i = lane; i < np; i += 32) {
+    const float2 v = p[i];
+    s += v.y * __expf(v.x - m);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return m + logf(s);
+}
+
 // A warp per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
-// block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target.
-// whole (few tokens, one piece): every block counts the targets itself, and the block that ends last
-// (`left`: blocks still at work) sums the losses; a launch each before and after, 7 us of a loss of 37 tokens.
+// block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target. whole (few
+// tokens, one piece): the block that ends last (`left`: blocks still at work) counts the targets and sums the losses, a
+// launch each otherwise, 7 us of a loss of 37 tokens.
 __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, const float *__restrict__ zt,
                                                  const int32_t *__restrict__ target, int rows, int V, int np, int grad,
                                                  const Coefs k, float *__restrict__ factor, float *__restrict__ lse,
@@ -292,27 +333,9 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
   __shared__ int last;
   pdl_start();
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  int n = 0;
-  if (whole) {
-    n = count_targets(target, rows, V, reinterpret_cast<int *>(sh));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *n_valid = n;
-  }
   if (row < rows) {
     float2 *p = part + size_t(row) * np;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float s = 0.f;
-#pragma unroll 4
-    for (int i = lane; i < np; i += 32) {
-      const float2 v = p[i];
-      s += v.y * __expf(v.x - m);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const float l = m + logf(s);
+    const float l = row_lse(p, np, lane);
     const int tgt = target[row];
     const bool ok = tgt >= 0 && tgt < V;
     if (lane == 0) {
@@ -321,23 +344,37 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
     }
     if (grad) {
       float a, b, s0;
-      k.get(whole ? n : *k.n_valid, a, b, s0);
-      if (row == 0 && lane == 0) *factor = s0;
+      k.get(whole ? 1 : *n_valid, a, b, s0);
+      if (!whole && row == 0 && lane == 0) *factor = s0;
       const float f = ok ? fmaf(b, l, a) : 0.f;
       for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
     }
   }
-  if (!whole) return;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicSub(left, 1) == 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  sum_losses(lse, nll, target, rows, V, k.z_coef, n, loss, sh);
+  if (whole && last_block(left, &last)) finish_losses(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
-// dz in place of the kept exponentials: half precision in, bf16 out. Blocks of 256 threads over (row, 2,048 columns).
+// Eight kept exponentials (half precision) as eight of dz (bf16): f = exp(maximum - lse) (a + b lse).
+__device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, int V, float a, float b, float lse, float nll) {
+  float o[8];
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+    o[2 * i] = f * x.x;
+    o[2 * i + 1] = f * x.y;
+  }
+  if (tgt < 0 || tgt >= V) {  // (a padding token's logits may be anything)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+  } else if (tgt >= col && tgt < col + 8) {
+    const float d = a * expm1f(-nll) + b * lse * expf(-nll);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = col + i == tgt ? d : o[i];
+  }
+  return pack8(o);
+}
+
+// dz in place of the kept exponentials. Blocks of 256 threads over (row, 2,048 columns).
 constexpr int kDzCols = 2048;
 __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                 const float *__restrict__ lse, const float *__restrict__ nll,
@@ -347,28 +384,49 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
   if (col >= V) return;
   const float f = part[size_t(row) * np + col / kBlk].y;
   uint4 *at = e + (size_t(row) * pitch + col) / 8;
-  const uint4 v = *at;
-  float o[8];
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-    o[2 * i] = f * x.x;
-    o[2 * i + 1] = f * x.y;
+  float a, b, s0;
+  k.get(1, a, b, s0);
+  *at = dz8(*at, f, target[row], col, V, a, b, lse[row], nll[row]);
+}
+
+// vocab_lse and vocab_dz of few tokens in one launch (512 tokens of 32,000 entries: 77 -> 73 us for the loss with its gradients;
+// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, 16,384 columns), each of which has its
+// first warp work out the row's lse again (lse, nll and the losses: the blocks of the first columns).
+constexpr int kFewCols = 16384;
+__global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
+                                                    const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
+                                                    int V, int np, const Coefs k, float *__restrict__ factor,
+                                                    float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
+                                                    int32_t *__restrict__ n_valid, float *__restrict__ loss) {
+  __shared__ float sh[64];
+  __shared__ float row_l;
+  __shared__ int last;
+  pdl_start();
+  const int row = blockIdx.y;
+  const float2 *p = part + size_t(row) * np;
+  if (threadIdx.x < 32) {
+    const float l = row_lse(p, np, threadIdx.x);
+    if (threadIdx.x == 0) row_l = l;
   }
+  __syncthreads();
+  const float l = row_l;
   const int tgt = target[row];
-  if (tgt < 0 || tgt >= V) {  // (a padding token's logits may be anything)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = 0.f;
-  } else if (tgt >= col && tgt < col + 8) {
-    float a, b, s0;
-    k.get(*k.n_valid, a, b, s0);
-    const float x = nll[row];
-    const float d = a * expm1f(-x) + b * lse[row] * expf(-x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = col + i == tgt ? d : o[i];
+  const bool ok = tgt >= 0 && tgt < V;
+  const float x = ok ? l - zt[row] : 0.f;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    lse[row] = l;
+    nll[row] = x;
   }
-  *at = pack8(o);
+  float a, b, s0;
+  k.get(1, a, b, s0);
+  const float f0 = fmaf(b, l, a);
+  const int first = blockIdx.x * kFewCols, end = min(V, first + kFewCols);
+#pragma unroll 4
+  for (int col = first + threadIdx.x * 8; col < end; col += 256 * 8) {
+    uint4 *at = e + (size_t(row) * pitch + col) / 8;
+    *at = dz8(*at, __expf(p[col / kBlk].x - l) * f0, tgt, col, V, a, b, l, x);
+  }
+  if (blockIdx.x == 0 && last_block(left, &last)) finish_losses(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
 // dh = sum of the splits' products, in their order: a warp per 32 x 8 values, a lane a row.
@@ -493,7 +551,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
   float2 *part = reinterpret_cast<float2 *>(base + l.part);
   uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept);
   float *dhp = reinterpret_cast<float *>(base + l.dh), *dwp = reinterpret_cast<float *>(base + l.dw);
-  const Coefs k = {d_loss, n_valid, z_coef};
+  const Coefs k = {d_loss, z_coef};
   int st;
   const bool whole = T > 0 && T <= kWholeTokens && T <= piece;
   if (!whole) {
@@ -513,7 +571,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     t.group = 8;
     auto logits = [&](auto e) {
       e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
-      e.left = left; e.blocks = (rows + 7) / 8;
+      e.left = left; e.blocks = grad && rows <= kFewTokens ? rows : (rows + 7) / 8;
       if (grad) {
         const int st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
         if (st) return st;
@@ -521,18 +579,25 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       return dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
     };
     if ((st = grad ? logits(LogitsEpi<true>{}) : logits(LogitsEpi<false>{}))) return st;
-    MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
-                                               grad ? 1 : 0, k, factor, lse + t0, nll + t0, whole ? 1 : 0, left, n_valid, loss));
-    if ((st = moe::launch_status(fn))) return st;
-    if (!grad) continue;
-    // (grid.y holds 65,535 rows at most)
-    for (int r0 = 0; r0 < rows; r0 += 65535) {
-      const int n = std::min(65535, rows - r0);
-      MOE_LAUNCH("vocab_dz", s, moe::launch_dep(vocab_dz, dim3((V + kDzCols - 1) / kDzCols, n), 256, 0, s,
-                                                reinterpret_cast<uint4 *>(kept + int64_t(r0) * z.pitch), z.pitch,
-                                                part + int64_t(r0) * z.np, lse + t0 + r0, nll + t0 + r0, target + t0 + r0, V,
-                                                int(z.np), k));
+    if (grad && whole && rows <= kFewTokens) {
+      MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, rows), 256, 0, s,
+                                                    reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
+                                                    k, factor, lse, nll, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
+    } else {
+      MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
+                                                 grad ? 1 : 0, k, factor, lse + t0, nll + t0, whole ? 1 : 0, left, n_valid, loss));
+      if ((st = moe::launch_status(fn))) return st;
+      if (!grad) continue;
+      // (grid.y holds 65,535 rows at most)
+      for (int r0 = 0; r0 < rows; r0 += 65535) {
+        const int n = std::min(65535, rows - r0);
+        MOE_LAUNCH("vocab_dz", s, moe::launch_dep(vocab_dz, dim3((V + kDzCols - 1) / kDzCols, n), 256, 0, s,
+                                                  reinterpret_cast<uint4 *>(kept + int64_t(r0) * z.pitch), z.pitch,
+                                                  part + int64_t(r0) * z.np, lse + t0 + r0, nll + t0 + r0, target + t0 + r0, V,
+                                                  int(z.np), k));
+        if ((st = moe::launch_status(fn))) return st;
+      }
     }
     const Plan plan = grad_plan(rows, d, V, d_hidden != nullptr, d_w != nullptr);
     OutEpi eh = {}, ew = {};
