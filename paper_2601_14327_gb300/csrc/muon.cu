@@ -477,23 +477,28 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
 // operand for X X^T (the reduction along the columns) and an MN-major one for B X (along the rows). Per step: the CTA's share of
 // X X^T into 128 TMEM columns; the shares summed over the cluster (each CTA adds up 128 / CTAs rows, fp32, in the order of
 // the ranks, and gives A's rows to all); A A and B in every CTA; B X added by the tensor cores onto a X in TMEM.
+// Short sides up to 64 leave half of the 128 rows free: X's second half-precision term goes there, and both products take it
+// without an instruction more. Few values do not average over their roundings (17 x 60: 1.8e-3 off before the result's
+// rounding with one term, 8e-4 with two).
 // As launches the 3 * steps products took 85-145 us whatever the size, which is latency; nothing here leaves the cluster. X is kept
 // in fp32 (22 bits in the launches' form), and roundings to half precision are theirs.
 constexpr int kN = 128;           // rows, zero past n
 constexpr int kMaxCols = 384;     // of a CTA: with the 128 columns of the products all of TMEM's 512
 constexpr int kMaxCluster = 8;
-constexpr int kSms = 152;
 constexpr int kSmallThreads = 512;   // four warps a TMEM lane quarter take 32-column chunks in turns
-constexpr uint32_t kBlkBytes = kN * 128;                                  // 128 rows of 64 halves
-constexpr uint32_t kOffA = kMaxCols / 64 * kBlkBytes, kOffB = kOffA + 2 * kBlkBytes, kOffRecv = kOffB + 2 * kBlkBytes;
-constexpr uint32_t kOffMisc = kOffRecv + kN * kN * 4;
-constexpr size_t kSmallSmem = 1024 + kOffMisc + 1024;
+constexpr int kLoN = 64;          // short side up to which X's second half-precision term is kept, in rows 64 to 127
+constexpr uint32_t kBlkBytes = kN * 128; // 128 rows of 64 halves
+// Shared memory: what is used otherwise, A, B, X's blocks, and the peers' shares of A's rows.
+constexpr uint32_t kOffA = 1024, kOffB = kOffA + 2 * kBlkBytes, kOffX = kOffB + 2 * kBlkBytes;
+constexpr uint32_t kOffRecv = kOffX + kMaxCols / 64 * kBlkBytes;
+constexpr size_t kSmallSmem = 1024 + kOffRecv + kN * kN * 4;
 
 struct SmallArgs {
   Source s;
   Target to;
   const uint8_t *mask;
   int per, n, k, tall, steps, ctas, cols;
+  int lo;               // n <= kLoN
   float scale, eps;
   float coef[3 * kMaxSteps];
 };
@@ -523,7 +528,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
   pdl_start();
   if (p.mask != nullptr && p.mask[mat / p.per] == 0) return;  // (the whole cluster)
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t sX = base, sA = base + kOffA, sB = base + kOffB, recv = base + kOffRecv, misc = base + kOffMisc;
+  const uint32_t misc = base, sA = base + kOffA, sB = base + kOffB, sX = base + kOffX, recv = base + kOffRecv;
   // misc: TMEM address, barrier, sums of the cluster's CTAs [8][3], of the warps [16][3], what B's diagonal lost [128]
   const uint32_t bar = misc + 8, sums = misc + 16, wsums = misc + 128, delta = misc + 384;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -649,10 +654,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
     const uint32_t blk = sX + uint32_t(col / 64) * kBlkBytes;
     const int q0_ = (col & 63) / 8;
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      tc::st_shared_v4(sw128(blk, row, q0_ + g),
-                       make_uint4(pack_half2(x[8 * g], x[8 * g + 1]), pack_half2(x[8 * g + 2], x[8 * g + 3]),
-                                  pack_half2(x[8 * g + 4], x[8 * g + 5]), pack_half2(x[8 * g + 6], x[8 * g + 7])));
+    for (int g = 0; g < 4; ++g) {
+      uint32_t h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = pack_half2(x[8 * g + 2 * i], x[8 * g + 2 * i + 1]);
+      if (p.lo && row >= kLoN) break;
+      tc::st_shared_v4(sw128(blk, row, q0_ + g), make_uint4(h[0], h[1], h[2], h[3]));
+      if (p.lo) {  // (not scaled up: what falls below 2^-24 is nothing beside entries around 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 b = unpack_half2(h[i]);
+          h[i] = pack_half2(x[8 * g + 2 * i] - b.x, x[8 * g + 2 * i + 1] - b.y);
+        }
+        tc::st_shared_v4(sw128(blk, row + kLoN, q0_ + g), make_uint4(h[0], h[1], h[2], h[3]));
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] *= a * kScaleA;
     tc::tmem_st_32x32b_x32(t_x + 32 * c, reinterpret_cast<const uint32_t(&)[32]>(x));
@@ -672,7 +688,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
 
   constexpr uint32_t kSquare = tc::idesc_f16_f32(kN, kN), kTimesX = tc::idesc_f16_f32(kN, 64, false, true);
   const float gram_scale = kScaleA / (p.scale * p.scale);
-  const int mine = kN / ctas;  // rows of A that this CTA adds up
+  const int mine = (p.n + ctas - 1) / ctas;  // rows of A that this CTA adds up
+  const uint32_t recv_row = p.n <= kLoN ? kLoN * 4 : kN * 4;
   for (int step = 0; step < p.steps; ++step) {
     // ---- this CTA's share of X X^T
     publish();
@@ -687,7 +704,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
     }
     mma_wait();
     const bool in_a = row0 < p.n && group * 32 < p.n;  // A is n x n; the rest of it stays zero
-    if (ctas == 1) {
+    if (ctas == 1 && !p.lo) {
       if (in_a) {
         uint32_t r[32];
         tc::tmem_ld_32x32b_x32(t_acc_w, r);
@@ -702,36 +719,46 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
         }
       }
     } else {
-      // rows to the CTA that adds them up: [source][row][128 values], 16-byte chunks at q ^ (row % 32)
-      const int local = row / ctas;  // (rows are dealt out: all CTAs have some of few)
-      const uint32_t to = tc::mapa(recv, uint32_t(row % ctas)) + uint32_t(rank * mine + local) * (kN * 4u);
-      if (in_a) {
+      // Rows to the CTA that adds them up: [source][row][128 or 64 values], 16-byte chunks at q ^ (row % 16). With second terms
+      // the tensor cores' result is [hi hi^T, hi lo^T; lo hi^T, lo lo^T]: A's row is the first two's sum (one source) and the
+      // third (another); the fourth is below its roundings.
+      const int a_row = p.lo ? row % kLoN : row, local = a_row / ctas;  // (rows are dealt out: all CTAs have some of few)
+      const bool second = p.lo && row >= kLoN;
+      const uint32_t to = tc::mapa(recv, uint32_t(a_row % ctas)) + uint32_t((rank + (second ? ctas : 0)) * mine + local) * recv_row;
+      if (group * 32 < p.n && (p.lo ? row0 % kLoN : row0) < p.n) {
         uint32_t r[32];
         tc::tmem_ld_32x32b_x32(t_acc_w, r);
         tc::tmem_ld_wait();
-        if (row < p.n) {
+        if (p.lo && !second) {
+          uint32_t r2[32];
+          tc::tmem_ld_32x32b_x32(t_acc_w + kLoN, r2);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(r2[i]));
+        }
+        if (a_row < p.n) {
 #pragma unroll
           for (int g = 0; g < 8; ++g)
             if (group * 32 + 4 * g < p.n)
-              st_cluster_v4(to + (uint32_t((group * 8 + g) ^ (local & 31)) << 4),
+              st_cluster_v4(to + (uint32_t((group * 8 + g) ^ (local & 15)) << 4),
                             make_float4(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]), __uint_as_float(r[4 * g + 2]),
                                         __uint_as_float(r[4 * g + 3])));
         }
       }
       tc::fence_before_sync();
       tc::cluster_sync();
-      const int quads = (p.n + 3) / 4;
+      const int quads = (p.n + 3) / 4, sources = p.lo ? 2 * ctas : ctas;
       for (int i = tid; i < mine * 32; i += kSmallThreads) {
-        const int local_i = i / 32, q = i % 32, a_row = local_i * ctas + rank;
-        if (q >= quads || a_row >= p.n) continue;
-        const uint32_t from = recv + uint32_t(local_i) * (kN * 4u) + (uint32_t(q ^ (local_i & 31)) << 4);
+        const int local_i = i / 32, q = i % 32, r_i = local_i * ctas + rank;
+        if (q >= quads || r_i >= p.n) continue;
+        const uint32_t from = recv + uint32_t(local_i) * recv_row + (uint32_t(q ^ (local_i & 15)) << 4);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int r = 0; r < ctas; ++r) {
-          const float4 w = ld_shared_f4(from + uint32_t(r * mine) * (kN * 4u));
+        for (int r = 0; r < sources; ++r) {
+          const float4 w = ld_shared_f4(from + uint32_t(r * mine) * recv_row);
           v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
         }
         const uint32_t lo = pack_half2(v.x * gram_scale, v.y * gram_scale), hi = pack_half2(v.z * gram_scale, v.w * gram_scale);
-        const uint32_t at = sw128(sA + uint32_t(q / 16) * kBlkBytes, a_row, (q % 16) / 2) + uint32_t(q & 1) * 8u;
+        const uint32_t at = sw128(sA + uint32_t(q / 16) * kBlkBytes, r_i, (q % 16) / 2) + uint32_t(q & 1) * 8u;
         for (int r = 0; r < ctas; ++r) st_cluster_v2(tc::mapa(at, r), lo, hi);
       }
       asm volatile("fence.proxy.async;" ::: "memory");
@@ -770,7 +797,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
           if (col == row) st_shared_f32(delta + 4u * row, (y0 - back.x) * (1.f / kScaleA));
           if (col + 1 == row) st_shared_f32(delta + 4u * row, (y1 - back.y) * (1.f / kScaleA));
         }
+        if (p.lo && group >= 2) break;
         tc::st_shared_v4(sw128(blk_b, row, (group & 1) * 4 + g), make_uint4(v[0], v[1], v[2], v[3]));
+        if (p.lo)  // [B, B] times [hi; lo]
+          tc::st_shared_v4(sw128(blk_b + kBlkBytes, row, (group & 1) * 4 + g), make_uint4(v[0], v[1], v[2], v[3]));
       }
     }
     // ---- B X onto a X
@@ -904,27 +934,56 @@ bool small_tiles(long long tiles) {
 
 const float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
 
-// CTAs for the columns of a matrix in the form on the chip: as few as hold them, and more while there are SMs without one.
-int small_cols(int k, int ctas) { return ceil_div(ceil_div(k, ctas), 64) * 64; }
-int small_ctas(int n_mats, int k) {
-  int ctas = 1;
-  while (ctas < kMaxCluster && (small_cols(k, ctas) > kMaxCols || (small_cols(k, ctas) > 64 && 2ll * ctas * n_mats <= kSms))) ctas *= 2;
-  return ctas;
+// Clusters of so many CTAs that are resident together (GPCs hold a number of SMs that clusters do not always divide), or 0.
+int small_fit(int ctas) {
+  static int fit[64][4] = {};  // of each device
+  int &n = fit[moe::device_slot()][ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3];
+  if (n) return n;
+  if (cudaFuncSetAttribute(muon_small, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem)) != cudaSuccess) return 0;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = unsigned(ctas);
+  at.val.clusterDim.y = 1;
+  at.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(ctas));
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = kSmallSmem;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  int k = 0;
+  if (cudaOccupancyMaxActiveClusters(&k, muon_small, &cfg) != cudaSuccess) return 0;
+  return n = k;
 }
-// The form on the chip takes its phases one after another, an SM to a CTA: up to two CTAs an SM; the launches
-// of more matrices overlap better.
+int small_cols(int k, int ctas) { return ceil_div(ceil_div(k, ctas), 64) * 64; }
+// CTAs a matrix in the form on the chip, 0: launches. The form takes its phases one after another, an SM to a CTA: a wave of
+// clusters takes about 15 us and 0.1 a column; of many waves the launches, which overlap better, are as
+// fast (Muon step of 128 matrices 128 x 2,048: 746 us here in nine waves, 678 as launches; 31 updates of them, three: 190, 233).
 // MOE_MUON_SMALL=0 or 1 takes the launches, or wherever it fits the other form (tests and A/B measurements).
-bool small_form(int n_mats, int n, int k) {
+int small_ctas(int n_mats, int n, int k) {
   static const int forced = [] {
     const char *e = getenv("MOE_MUON_SMALL");
     return e && (e[0] == '0' || e[0] == '1') && e[1] == 0 ? e[0] - '0' : -1;
   }();
-  if (n > kN || k > kMaxCluster * kMaxCols || forced == 0) return false;
-  return forced == 1 || (long long)n_mats * small_ctas(n_mats, k) <= 2 * kSms;
+  if (n > kN || forced == 0) return 0;
+  int best = 0, waves = 0;
+  double least = 0;
+  for (int ctas = 1; ctas <= kMaxCluster; ctas *= 2) {
+    const int cols = small_cols(k, ctas), fit = cols <= kMaxCols ? small_fit(ctas) : 0;
+    if (!fit) continue;
+    const int w = ceil_div(n_mats, fit);
+    const double t = w * (15 + 0.1 * cols);
+    if (!best || t < least) {
+      best = ctas;
+      waves = w;
+      least = t;
+    }
+  }
+  return forced == 1 || waves <= 3 ? best : 0;
 }
 
-int run_small(const Source &u, const Target &to, const uint8_t *mask, int n_mats, int per, const float *coef, int steps, float eps,
-              float scale, cudaStream_t s, const char *what) {
+int run_small(int ctas, const Source &u, const Target &to, const uint8_t *mask, int n_mats, int per, const float *coef, int steps,
+              float eps, float scale, cudaStream_t s, const char *what) {
   SmallArgs a = {};
   a.s = u;
   a.to = to;
@@ -937,7 +996,9 @@ int run_small(const Source &u, const Target &to, const uint8_t *mask, int n_mats
   a.scale = scale;
   a.eps = eps;
   for (int i = 0; i < 3 * steps; ++i) a.coef[i] = coef ? coef[i] : kCoef[i % 3];
-  a.ctas = small_ctas(n_mats, a.k);
+  a.ctas = ctas;
+  a.cols = small_cols(a.k, ctas);
+  a.lo = a.n <= kLoN;
   a.cols = small_cols(a.k, a.ctas);
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -953,13 +1014,6 @@ int run_small(const Source &u, const Target &to, const uint8_t *mask, int n_mats
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  static bool attr[64] = {};  // of each device
-  bool &set = attr[moe::device_slot()];
-  if (!set) {
-    cudaError_t e = cudaFuncSetAttribute(muon_small, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem));
-    if (e != cudaSuccess) return moe::cuda_status(e, what);
-    set = true;
-  }
   MOE_LAUNCH("muon_small", s, cudaLaunchKernelEx(&cfg, muon_small, a));
   return moe::launch_status(what);
 }
@@ -1003,7 +1057,7 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
   to.vec = u.vec;
   to.inv = 1.f / scale;
   int st;
-  if (small_form(n_mats, n, k)) return run_small(u, to, mask, n_mats, per, coef, steps, eps, scale, s, fn);
+  if (const int ctas = small_ctas(n_mats, n, k)) return run_small(ctas, u, to, mask, n_mats, per, coef, steps, eps, scale, s, fn);
   const int64_t xstep = int64_t(rows) * l.pitch, astep = int64_t(n) * l.npitch;
   CUtensorMap xo[2], lom, ao, bo;
   for (int i = 0; i < 2; ++i)

@@ -4,13 +4,13 @@
 //   dz = a (p - 1[target]) + b p with a = d_loss[0] / M, b = 2 d_loss[1] z_coef lse / M;  dh = dz W,  dW = dz^T h
 //
 // The logits' product runs over 256 x 256 tiles; a tile's epilogue reduces each row's 128 columns to their
-// maximum and the sum of exp(z - maximum) in fp32, and picks the target's logit out in fp32. Those pairs
+// maximum and the sum of exp(z - maximum) in fp32, and picks the target's logit out of it in fp32. Those pairs
 // (a 64th of the logits' bytes) are all that the loss needs.
 // The gradient needs every exp(z - lse) once more, after the row's last tile. Making the logits again would be 2 T V d
 // operations beside the 6 T V d of the three products. Instead the epilogue also keeps exp(z - block maximum)
 // in half precision (values up to 1, 11 bits) for one piece of the tokens, and vocab_dz turns them into dz in place
 // once the row's lse is known: 2 bytes written, read and written a logit, ~0.9 ps, against d / 0.9e15 s for the
-// product. The one number that this would spoil, p - 1 at a target that is almost sure, is taken from the fp32 logit.
+// product. The one number that this would spoil, p - 1 at a target that is almost sure, is taken from the fp32 sums of the others.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -84,7 +84,8 @@ template <bool KEEP> struct LogitsEpi {
       for (int c = 0; c < kBlk; ++c)
         if (c >= nv) z[c] = -INFINITY;
     }
-    if (tgt >= 0 && tgt < nv) {
+    const bool hit = tgt >= 0 && tgt < nv;
+    if (hit) {
       float v = 0.f;
 #pragma unroll
       for (int c = 0; c < kBlk; ++c) v = c == tgt ? z[c] : v;
@@ -108,6 +109,14 @@ template <bool KEEP> struct LogitsEpi {
     }
     float s0, s1;
     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+    if (hit) {  // the others' sum (see row_lse): beside a sure token it is below the total's rounding
+      s0 = s1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < kBlk; c += 2) {
+        s0 += c == tgt ? 0.f : z[c];
+        s1 += c + 1 == tgt ? 0.f : z[c + 1];
+      }
+    }
     if (w.row < rows) part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, s0 + s1);
     if (KEEP) {
 #pragma unroll
@@ -302,8 +311,10 @@ __device__ __forceinline__ bool last_block(int *left, int *sh) {
   return *sh != 0;
 }
 
-// A row's log-sum-exp from its pairs, by a warp (every lane has it).
-__device__ __forceinline__ float row_lse(const float2 *p, int np, int lane) {
+// A row's lse and nll from its pairs, by a warp (every lane has them). The pairs leave the target's own logit out: with
+// r = log sum over the others of exp z, nll = log(1 + exp(r - z_t)) and lse = z_t + nll, so that nll and p - 1 = expm1(-nll)
+// keep their digits however sure the token is (lse - z_t has an error of ~1e-6 whatever nll is).
+__device__ __forceinline__ void row_lse(const float2 *p, int np, int lane, bool has_target, float zt, float &lse, float &nll) {
   float m = -INFINITY;
 #pragma unroll 4
   for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
@@ -317,7 +328,13 @@ __device__ __forceinline__ float row_lse(const float2 *p, int np, int lane) {
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return m + logf(s);
+  lse = m + logf(s);
+  nll = 0.f;
+  if (has_target) {
+    const float d = lse - zt;  // (s = 0, -inf: exp underflows as it should)
+    nll = d > 0.f ? d + log1pf(expf(-d)) : log1pf(expf(d));
+    lse = zt + nll;
+  }
 }
 
 // A warp per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
@@ -335,12 +352,13 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row < rows) {
     float2 *p = part + size_t(row) * np;
-    const float l = row_lse(p, np, lane);
     const int tgt = target[row];
     const bool ok = tgt >= 0 && tgt < V;
+    float l, x;
+    row_lse(p, np, lane, ok, ok ? zt[row] : 0.f, l, x);
     if (lane == 0) {
       lse[row] = l;
-      nll[row] = ok ? l - zt[row] : 0.f;
+      nll[row] = x;
     }
     if (grad) {
       float a, b, s0;
@@ -399,20 +417,23 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
                                                     int32_t *__restrict__ n_valid, float *__restrict__ loss) {
   __shared__ float sh[64];
-  __shared__ float row_l;
+  __shared__ float row_l[2];
   __shared__ int last;
   pdl_start();
   const int row = blockIdx.y;
   const float2 *p = part + size_t(row) * np;
+  const int tgt = target[row];
   if (threadIdx.x < 32) {
-    const float l = row_lse(p, np, threadIdx.x);
-    if (threadIdx.x == 0) row_l = l;
+    const bool ok = tgt >= 0 && tgt < V;
+    float l, x;
+    row_lse(p, np, threadIdx.x, ok, ok ? zt[row] : 0.f, l, x);
+    if (threadIdx.x == 0) {
+      row_l[0] = l;
+      row_l[1] = x;
+    }
   }
   __syncthreads();
-  const float l = row_l;
-  const int tgt = target[row];
-  const bool ok = tgt >= 0 && tgt < V;
-  const float x = ok ? l - zt[row] : 0.f;
+  const float l = row_l[0], x = row_l[1];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     lse[row] = l;
     nll[row] = x;

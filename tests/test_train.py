@@ -1,0 +1,219 @@
+"""The vocabulary loss and the orthogonalised update without a GPU: the oracle against autograd, differences and the polar
+factor, and the refusals of the entry points and of the package's calls (nothing is launched)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import moe_oracle as O
+from paper_2601_14327_gb300 import _lib as L
+from paper_2601_14327_gb300 import build as B
+from paper_2601_14327_gb300 import train
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    B.build()
+
+
+# ---------------------------------------------------------------- the oracle
+
+
+@pytest.mark.parametrize("T,d,V,ignored", [(1, 3, 1, False), (7, 5, 11, True), (12, 4, 30, False)])
+def test_oracle_vocab_loss_against_autograd(T, d, V, ignored):
+    rng = np.random.default_rng(T)
+    h, w = rng.standard_normal((T, d)), rng.standard_normal((V, d))
+    t = rng.integers(0, V, T)
+    if ignored:
+        t[::3] = -1
+        t[1] = V + 2
+    ref = O.vocab_loss(h, w, t, 0.3, (0.7, 1.9))
+    ht, wt = torch.tensor(h, requires_grad=True), torch.tensor(w, requires_grad=True)
+    z = ht @ wt.T
+    ok = torch.tensor((t >= 0) & (t < V))
+    lse = torch.logsumexp(z, 1)
+    nll = (lse - z.gather(1, torch.tensor(np.clip(t, 0, V - 1))[:, None])[:, 0])[ok]
+    parts = nll.sum() / ok.sum(), 0.3 * (lse[ok] ** 2).sum() / ok.sum()
+    np.testing.assert_allclose(ref["loss"], [p.item() for p in parts], rtol=1e-12, atol=1e-14)
+    (0.7 * parts[0] + 1.9 * parts[1]).backward()
+    np.testing.assert_allclose(ref["d_hidden"], ht.grad.numpy(), rtol=1e-9, atol=1e-13)
+    np.testing.assert_allclose(ref["d_w"], wt.grad.numpy(), rtol=1e-9, atol=1e-13)
+
+
+def test_oracle_vocab_loss_without_targets():
+    ref = O.vocab_loss(np.ones((3, 2)), np.ones((4, 2)), np.array([-1, -5, 9]), 1.0)
+    assert (ref["loss"] == 0).all() and (ref["d_hidden"] == 0).all() and (ref["d_w"] == 0).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 9), (9, 5), (6, 6)])
+def test_oracle_newton_schulz_acts_on_the_singular_values(rows, cols):
+    g = np.random.default_rng(rows).standard_normal((rows, cols))
+    u, s, v = np.linalg.svd(g, full_matrices=False)
+    s = s / (np.linalg.norm(g) + 1e-7)
+    for _ in range(5):
+        s = 3.4445 * s - 4.7750 * s ** 3 + 2.0315 * s ** 5
+    np.testing.assert_allclose(O.newton_schulz(g), (u * s) @ v, rtol=1e-9, atol=1e-11)
+    # a cubic that converges gives the orthogonal factor of the polar decomposition
+    np.testing.assert_allclose(O.newton_schulz(g, (1.5, -0.5, 0.0), 60), u @ v, atol=1e-9)
+
+
+def test_oracle_muon_step():
+    w, g, m = (np.random.default_rng(i).standard_normal((4, 6)) for i in range(3))
+    for nesterov in (True, False):
+        w1, m1 = O.muon_step(w, g, m, 0.1, 0.2, 0.9, nesterov, 3.0)
+        np.testing.assert_allclose(m1, 0.9 * m + g)
+        u = g + 0.9 * m1 if nesterov else m1
+        np.testing.assert_allclose(w1, w * 0.98 - 0.3 * O.newton_schulz(u))
+
+
+# ---------------------------------------------------------------- refusals of the entry points
+
+
+def _vocab(grad=True, **kw):
+    a = dict(hidden=16, w_vocab=16, target=16, T=10, d=64, V=100, piece=10, z_coef=0.0)
+    if grad:
+        a["d_loss"] = None
+    a.update(loss=16, nll=16, lse=16, n_valid=16)
+    if grad:
+        a.update(d_hidden=16, d_w=16)
+    a.update(ws=16, ws_bytes=1 << 30)
+    a.update(kw)
+    (L.moe_vocab_loss_grad if grad else L.moe_vocab_loss)(*a.values(), stream=0)
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=-1), -1), (dict(d=60), -1), (dict(d=0), -1), (dict(V=0), -1), (dict(piece=0), -1), (dict(V=(1 << 24) + 1), -1),
+    (dict(T=(1 << 24) + 1), -1), (dict(d=(1 << 20) + 8), -1), (dict(T=1 << 24, d=1 << 20), -2), (dict(hidden=None), -1),
+    (dict(w_vocab=None), -1), (dict(target=None), -1), (dict(loss=None), -1), (dict(nll=None), -1), (dict(lse=None), -1),
+    (dict(n_valid=None), -1), (dict(hidden=8), -1), (dict(w_vocab=24), -1), (dict(ws=None), -6), (dict(ws=8), -6),
+    (dict(ws_bytes=100), -6)])
+def test_vocab_loss_refusals(grad, kw, status):
+    with pytest.raises(L.MoEError) as e:
+        _vocab(grad, **kw)
+    assert e.value.status == status
+
+
+def test_vocab_loss_grad_refusals():
+    for kw in (dict(d_hidden=None, d_w=None), dict(d_hidden=8), dict(d_w=40)):
+        with pytest.raises(L.MoEError) as e:
+            _vocab(**kw)
+        assert e.value.status == -1
+
+
+def test_vocab_workspace():
+    ws = L.moe_vocab_loss_workspace_size
+    assert ws(10, 64, 100, 0, 1) == 0 and ws(-1, 64, 100, 1, 1) == 0 and ws(10, 60, 100, 1, 1) == 0
+    # a piece's rows, not all tokens', set it; the gradient's terms are there only with it
+    assert ws(1 << 20, 64, 32000, 256, 0) == ws(256, 64, 32000, 1 << 20, 0)
+    assert ws(1024, 512, 32000, 1024, 1) >= 1024 * 32000 * 2 > ws(1024, 512, 32000, 1024, 0)
+    # fp32 sums of d_w only for several pieces
+    assert ws(2048, 512, 32000, 1024, 1) - ws(1024, 512, 32000, 1024, 1) >= 32000 * 512 * 4
+    need = ws(10, 64, 100, 10, 1)
+    with pytest.raises(L.MoEError) as e:
+        _vocab(ws_bytes=need - 1)
+    assert e.value.status == -6
+    # sizes past 32 bits
+    assert ws(1 << 20, 4096, 1 << 20, 1 << 17, 1) > (1 << 38)
+
+
+def _orth(**kw):
+    a = dict(g=16, active_mask=None, n_mats=6, mats_per_expert=2, rows=40, cols=72, coef=None, steps=5, eps=1e-7, out=16, ws=16,
+             ws_bytes=1 << 30)
+    a.update(kw)
+    L.moe_orthogonalize(*a.values(), stream=0)
+
+
+def _muon(**kw):
+    a = dict(w=16, master=None, grad=16, momentum=16, active_mask=None, n_mats=6, mats_per_expert=2, rows=40, cols=72, lr=0.1,
+             weight_decay=0.0, mu=0.9, nesterov=True, scale=1.0, coef=None, steps=5, eps=1e-7, ws=16, ws_bytes=1 << 30)
+    a.update(kw)
+    L.moe_muon_step(*a.values(), stream=0)
+
+
+@pytest.mark.parametrize("call", [_orth, _muon])
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_mats=-1), -1), (dict(n_mats=5), -1), (dict(mats_per_expert=0), -1), (dict(rows=0), -1), (dict(cols=16385), -1),
+    (dict(steps=0), -1), (dict(steps=17), -1), (dict(eps=0.0), -1), (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1),
+    (dict(ws=None), -6), (dict(ws=8), -6), (dict(ws_bytes=1000), -6)])
+def test_update_refusals(call, kw, status):
+    with pytest.raises(L.MoEError) as e:
+        call(**kw)
+    assert e.value.status == status
+
+
+@pytest.mark.parametrize("kw", [dict(g=None), dict(out=None), dict(g=8), dict(out=8)])
+def test_orthogonalize_refusals(kw):
+    with pytest.raises(L.MoEError) as e:
+        _orth(**kw)
+    assert e.value.status == -1
+
+
+@pytest.mark.parametrize("kw", [dict(w=None), dict(grad=None), dict(momentum=None), dict(w=8), dict(grad=8), dict(momentum=8),
+                                dict(master=8)])
+def test_muon_refusals(kw):
+    with pytest.raises(L.MoEError) as e:
+        _muon(**kw)
+    assert e.value.status == -1
+
+
+def test_no_matrices_and_workspace():
+    _orth(n_mats=0, g=None, out=None, ws=None)
+    _muon(n_mats=0, w=None, grad=None, momentum=None, ws=None)
+    ws = L.moe_orthogonalize_workspace_size
+    assert ws(4, 0, 5, 1) == 0 and ws(4, 5, 5, 0) == 0 and ws(-1, 5, 5, 1) == 0
+    assert ws(4, 300, 500, 100) == ws(4, 300, 500, 4) > ws(4, 300, 500, 2) > ws(4, 300, 500, 1)
+    assert ws(1 << 20, 16384, 16384, 1 << 20) > (1 << 50)
+    with pytest.raises(L.MoEError) as e:
+        _orth(ws_bytes=ws(6, 40, 72, 1) - 1)
+    assert e.value.status == -6
+
+
+@pytest.mark.parametrize("coef", [(1.0, 2.0), [(1.0, 2.0, 3.0)] * 4, [(1.0, 2.0)] * 5])
+def test_coefficients_of_another_number(coef):
+    with pytest.raises(ValueError):
+        _orth(coef=coef)
+
+
+# ---------------------------------------------------------------- refusals of the package's calls
+
+
+def test_vocab_buffers_and_tensors():
+    b = train.VocabLossBuffers(6, 16, 50, "cpu", backward=False)
+    h, w, t = torch.zeros(6, 16, dtype=torch.bfloat16), torch.zeros(50, 16, dtype=torch.bfloat16), torch.zeros(6, dtype=torch.int32)
+    with pytest.raises(ValueError, match="backward"):
+        train.vocab_loss_grad(b, h, w, t)
+    for bad in [(h.float(), w, t), (h[:5], w, t), (h, w.T, t), (h, w[:, ::2], t), (h, w, t.long()), (h, w, t[:, None])]:
+        with pytest.raises(ValueError):
+            train.vocab_loss(b, *bad)
+    with pytest.raises(ValueError):
+        train.VocabLossBuffers(6, 12, 50, "cpu")
+    g = train.VocabLossBuffers(6, 16, 50, "cpu")
+    for d_loss in (torch.ones(1), torch.ones(2).double(), torch.ones(4)[::2]):
+        with pytest.raises(ValueError, match="d_loss"):
+            train.vocab_loss_grad(g, h, w, t, d_loss=d_loss)
+    # the default piece keeps the exponentials within 4 GB
+    big = L.moe_vocab_loss_workspace_size(1 << 20, 64, 131072, max(1024, (1 << 31) // 131072 // 256 * 256), True)
+    assert big < 5 << 30
+
+
+def test_muon_buffers_and_tensors():
+    b = train.MuonBuffers(4, 24, 40, "cpu")
+    g = torch.zeros(4, 24, 40, dtype=torch.bfloat16)
+    m = torch.zeros(4, 24, 40)
+    for bad in (g.float(), g[:3], g.transpose(1, 2), torch.zeros(4, 40, 24, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            train.orthogonalize(b, bad, g)
+        with pytest.raises(ValueError):
+            train.orthogonalize(b, g, bad)
+        with pytest.raises(ValueError):
+            train.muon_step(b, g, bad, m, lr=0.1)
+    for bad in (m.double(), g, m[:2]):
+        with pytest.raises(ValueError):
+            train.muon_step(b, g, g, bad, lr=0.1)
+        with pytest.raises(ValueError):
+            train.muon_step(b, g, g, m, lr=0.1, master=bad)
+    for mask in (torch.ones(3, dtype=torch.uint8), torch.ones(2), torch.ones(0, dtype=torch.uint8), torch.ones(4, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            train.orthogonalize(b, g, g.clone(), active_mask=mask)
+    with pytest.raises(ValueError):
+        train.MuonBuffers(4, 0, 40, "cpu")
