@@ -46,6 +46,7 @@ template <int BN_, int KB_, int STAGES_, int BUFS_> struct Shape {
   static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
 };
 using Wide = Shape<256, 128, 3, 2>;
+using Narrow = Shape<128, 128, 4, 2>;
 using WideIO = Shape<256, 64, 4, 6>;    // epilogues that also load
 using Small = Shape<128, 64, 5, 2>;
 using SmallIO = Shape<128, 64, 5, 6>;

@@ -21,15 +21,22 @@ MOE_DEV_ERR_DECL
 
 namespace {
 
-constexpr int kBlk = 128;    // columns that share a maximum
 constexpr int kWholeTokens = 2048;  // tokens up to which the last block of vocab_lse(_dz) counts the targets and sums the losses
 constexpr int kFewTokens = 512;     // tokens up to which vocab_lse_dz takes the place of vocab_lse and vocab_dz
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
 struct Sizes {
+  int blk;             // columns that share a maximum: half a tile
   int64_t np, pitch;   // (maximum, sum) pairs of a row; halves from row to row of the kept exponentials
 };
-Sizes sizes(int V) { return {(int64_t(V) + kBlk - 1) / kBlk, (int64_t(V) + 63) / 64 * 64}; }
+// Tiles of the logits are 256 columns wide, or 128 where the wide ones are at most half as many as the pairs: each then has half
+// the products (6 tokens of d 856, 2,422 entries, with gradients: 34 -> 29 us). By all tokens, not a piece's:
+// the order of a row's sums follows from it.
+bool narrow(int64_t T, int64_t V) { return ((T + 255) / 256) * ((V + 255) / 256) <= kPairs / 2; }
+Sizes sizes(int64_t T, int V) {
+  const int blk = narrow(T, V) ? 64 : 128;
+  return {blk, (int64_t(V) + blk - 1) / blk, (int64_t(V) + 63) / 64 * 64};
+}
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -74,7 +81,7 @@ template <bool KEEP> struct LogitsEpi {
   static constexpr int kChunk = 512;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
-    static_assert(BN / 2 == kBlk, "a warp's half tile is a block");
+    constexpr int kBlk = BN / 2;  // a warp's half tile is a block
     const int nv = min(kBlk, V - w.col);
     if (nv <= 0 || w.row - w.lane >= rows) return;
     if (w.row == 0 && w.col == 0) *left = blocks;
@@ -396,11 +403,11 @@ __device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, 
 constexpr int kDzCols = 2048;
 __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                 const float *__restrict__ lse, const float *__restrict__ nll,
-                                                const int32_t *__restrict__ target, int V, int np, const Coefs k) {
+                                                const int32_t *__restrict__ target, int V, int np, int blk, const Coefs k) {
   pdl_start();
   const int row = blockIdx.y, col = blockIdx.x * kDzCols + threadIdx.x * 8;
   if (col >= V) return;
-  const float f = part[size_t(row) * np + col / kBlk].y;
+  const float f = part[size_t(row) * np + (blk == 128 ? col / 128 : col / 64)].y;
   uint4 *at = e + (size_t(row) * pitch + col) / 8;
   float a, b, s0;
   k.get(1, a, b, s0);
@@ -413,7 +420,7 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 constexpr int kFewCols = 16384;
 __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                     const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
-                                                    int V, int np, const Coefs k, float *__restrict__ factor,
+                                                    int V, int np, int blk, const Coefs k, float *__restrict__ factor,
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
                                                     int32_t *__restrict__ n_valid, float *__restrict__ loss) {
   __shared__ float sh[64];
@@ -445,31 +452,44 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
 #pragma unroll 4
   for (int col = first + threadIdx.x * 8; col < end; col += 256 * 8) {
     uint4 *at = e + (size_t(row) * pitch + col) / 8;
-    *at = dz8(*at, __expf(p[col / kBlk].x - l) * f0, tgt, col, V, a, b, l, x);
+    *at = dz8(*at, __expf(p[blk == 128 ? col / 128 : col / 64].x - l) * f0, tgt, col, V, a, b, l, x);
   }
   if (blockIdx.x == 0 && last_block(left, &last)) finish_losses(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
-// dh = sum of the splits' products, in their order: a warp per 32 x 8 values, a lane a row.
-__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int rows, int cols,
+// dh = sum of the splits' products: a lane a row of 32 x 8 values, and `team` (1 or 8) warps of a block to them, each adding up
+// every team-th split, the teams' sums in their order (few values of 64 splits were one chain of loads: 15 us at 9 x 168).
+__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int rows, int cols, int team,
                                                     const float *__restrict__ factor, uint16_t *__restrict__ out) {
+  __shared__ float sh[8][8][32];
   pdl_start();
-  const int lane = threadIdx.x & 31, groups = cols / 8;
-  const int64_t i = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = cols / 8;
+  const int64_t i = int64_t(blockIdx.x) * (8 / team) + warp / team;
   const int row = int(i / groups) * 32, col = int(i % groups) * 8;
-  if (row >= rows) return;
+  const bool in = row < rows;
   float s[8] = {};
-  const float *p = part + frag_index(0, row, col, rows, cols) + (col % 32) * 32 + lane;
-  const size_t step = frag_index(1, 0, 0, rows, cols);
+  if (in) {
+    const size_t step = frag_index(1, 0, 0, rows, cols);
+    const float *p = part + frag_index(0, row, col, rows, cols) + (col % 32) * 32 + lane + (warp % team) * step;
 #pragma unroll 2
-  for (int k = 0; k < splits; ++k, p += step) {
+    for (int k = warp % team; k < splits; k += team, p += team * step) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] += p[32 * j];
+      for (int j = 0; j < 8; ++j) s[j] += p[32 * j];
+    }
+  }
+  if (team > 1) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sh[warp][j][lane] = s[j];
+    __syncthreads();
+    if (warp != 0) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      for (int w = 1; w < 8; ++w) s[j] += sh[w][j][lane];
   }
   const float f = *factor;
 #pragma unroll
   for (int j = 0; j < 8; ++j) s[j] *= f;
-  if (row + lane < rows) stg_v4(out + size_t(row + lane) * cols + col, pack8(s));
+  if (in && row + lane < rows) stg_v4(out + size_t(row + lane) * cols + col, pack8(s));
 }
 
 __global__ void __launch_bounds__(kSumThreads) vocab_loss_sum(const float *__restrict__ lse, const float *__restrict__ nll,
@@ -513,7 +533,7 @@ struct Layout {
   int64_t factor, zt, part, kept, dh, dw, total;
 };
 Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
-  const Sizes z = sizes(V);
+  const Sizes z = sizes(T, V);
   const int64_t rows = std::min(piece, T), last = rows > 0 ? T % rows : 0;
   Layout l{};
   int64_t off = 0;
@@ -559,12 +579,12 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
                         static_cast<const void *>(d_w)})
     if (!moe::aligned16(p)) return moe::set_error(MOE_ERR_ARG, "%s: bf16 tensors must be 16-byte aligned", fn);
   if (std::max(int64_t(T), int64_t(V)) * d > (int64_t(1) << 38) ||
-      int64_t(std::min(T, piece)) * sizes(V).pitch > (int64_t(1) << 38))
+      int64_t(std::min(T, piece)) * sizes(T, V).pitch > (int64_t(1) << 38))
     return moe::set_error(MOE_ERR_UNSUPPORTED, "%s: more than 2^38 elements in a matrix", fn);
   const Layout l = layout(T, d, V, piece, grad);
   if (!ws || !moe::aligned16(ws) || ws_bytes < size_t(l.total))
     return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace of %lld bytes, 16-byte aligned, needed", fn, (long long)l.total);
-  const Sizes z = sizes(V);
+  const Sizes z = sizes(T, V);
   uint8_t *base = static_cast<uint8_t *>(ws);
   float *factor = reinterpret_cast<float *>(base + l.factor);
   int *left = reinterpret_cast<int *>(base + l.factor) + 1;
@@ -597,13 +617,14 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
         const int st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
         if (st) return st;
       }
-      return dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
+      return z.blk == 64 ? dg::product<dg::Narrow, false, false, false>("vocab_logits", mh, mw, e, t, s, fn)
+                         : dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
     };
     if ((st = grad ? logits(LogitsEpi<true>{}) : logits(LogitsEpi<false>{}))) return st;
     if (grad && whole && rows <= kFewTokens) {
       MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, rows), 256, 0, s,
                                                     reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
-                                                    k, factor, lse, nll, left, n_valid, loss));
+                                                    z.blk, k, factor, lse, nll, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
     } else {
       MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
@@ -616,7 +637,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
         MOE_LAUNCH("vocab_dz", s, moe::launch_dep(vocab_dz, dim3((V + kDzCols - 1) / kDzCols, n), 256, 0, s,
                                                   reinterpret_cast<uint4 *>(kept + int64_t(r0) * z.pitch), z.pitch,
                                                   part + int64_t(r0) * z.np, lse + t0 + r0, nll + t0 + r0, target + t0 + r0, V,
-                                                  int(z.np), k));
+                                                  int(z.np), z.blk, k));
         if ((st = moe::launch_status(fn))) return st;
       }
     }
@@ -641,9 +662,10 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     else st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, ew, t, s, fn);
     if (st) return st;
     if (plan.splits > 1) {
-      const int64_t warps = int64_t((rows + 31) / 32) * (d / 8);
-      MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((warps + 7) / 8), 256, 0, s, dhp, plan.splits, rows, d,
-                                                    factor, out));
+      const int64_t units = int64_t((rows + 31) / 32) * (d / 8);
+      const int team = units <= 1216 ? 8 : 1, each = 8 / team;  // (eight blocks an SM)
+      MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((units + each - 1) / each), 256, 0, s, dhp, plan.splits,
+                                                    rows, d, team, factor, out));
       if ((st = moe::launch_status(fn))) return st;
     }
   }
