@@ -70,6 +70,7 @@ struct Tile {
 // Floor of a / b for 0 <= a < 2^30 from b's reciprocal: a tile's numbers cost a dozen dependent integer divisions otherwise,
 // ~1,000 cycles of every role (the compiler's division is ~100), which products with short reductions feel.
 __device__ __forceinline__ int quot(int a, int b, float inv) {
+  if (a < b) return 0;
   int q = int(float(a) * inv);    // off by at most 2^30 2^-22 = 256 b-ths: corrected
   q += (a - q * b) >= 0 ? int(float(a - q * b) * inv) : -int(float(q * b - a) * inv) - 1;
   if (a - q * b < 0) --q;
@@ -77,15 +78,16 @@ __device__ __forceinline__ int quot(int a, int b, float inv) {
   return q;
 }
 
-__device__ __forceinline__ int tiles_of_matrix(const Tiles &t, int bn) {
+__host__ __device__ __forceinline__ int tiles_of_matrix(const Tiles &t, int bn) {
   return t.sym ? t.mt * (t.mt + 1) / 2 * (kTileRows / bn) : t.mt * t.nt;
 }
 
-// A role's walk through the list.
+// What the walk through the list needs besides, worked out on the host (in the kernels, with everything cold, it took most of
+// 2,300 cycles of each launch).
 struct Walk {
   int per, band, nkb;
   float i_all, i_per, i_band, i_group;
-  __device__ __forceinline__ Walk(const Tiles &t, int bn, int kb) {
+  Walk(const Tiles &t, int bn, int kb) {
     per = tiles_of_matrix(t, bn);
     band = t.group * t.nt;
     nkb = (t.k + kb - 1) / kb;
@@ -207,6 +209,7 @@ template <class Epi> struct Second {
   CUtensorMap a, b;
   Epi epi;
   Tiles t;
+  Walk walk;
   int head;   // what a tile of the first product costs, in tiles of the second
 };
 struct NoSecond {};
@@ -233,7 +236,8 @@ struct Items {
 template <class Sh, bool A_MN, bool B_MN, bool HALF, class Epi, class Extra>
 __global__ void __launch_bounds__(kThreads, 1)
     dense_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                      const __grid_constant__ Epi epi, const Tiles t, const __grid_constant__ Extra second) {
+                      const __grid_constant__ Epi epi, const Tiles t, const Walk walk,
+                      const __grid_constant__ Extra second) {
   constexpr bool DUAL = !std::is_same<Extra, NoSecond>::value;
   constexpr int STAGES = Sh::STAGES, BN = Sh::BN, BNH = Sh::BNH, KB = Sh::KB;
   constexpr int kChunkBlocks = Epi::kChunk / KB;  // 0: the whole reduction
@@ -289,7 +293,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc::tmem_alloc_pair(tc::smem_u32(misc), Sh::TMEM_COLS);
     tc::tmem_relinquish_pair();
   }
-  const Walk walk(t, BN, KB);
   Tile x = walk.at(t, cluster, BN);  // this pair's first tile (DUAL: of the first product)
   pdl_wait();  // (barriers, TMEM and the first tile's numbers while the previous kernel ends)
   tc::fence_before_sync();
@@ -304,14 +307,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   items.nclusters = nclusters;
   items.total = mats * t.splits * walk.per;
   items.total2 = 0;
-  Walk walk2 = walk;
   if constexpr (DUAL) {
-    walk2 = Walk(second.t, BN, KB);
-    items.total2 = second.t.mats * second.t.splits * walk2.per;
+    items.total2 = second.t.mats * second.t.splits * second.walk.per;
     items.rem = items.total % nclusters;
     items.mine = items.total / nclusters + (cluster < items.rem ? 1 : 0);
     items.head = second.head;
-    if (cluster >= items.total) x = walk2.at(second.t, min(cluster - items.rem, items.total2 - 1), BN);
+    if (cluster >= items.total) x = second.walk.at(second.t, min(cluster - items.rem, items.total2 - 1), BN);
   }
   int job = 0, u = 0;
   // the tile after this pair's j-th
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!items.at(j + 1, job, u)) return;
     if constexpr (DUAL) {
       if (job != 0) {
-        x = walk2.at(second.t, u, BN);
+        x = second.walk.at(second.t, u, BN);
         return;
       }
     }
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         release();
       }
     }
-    if (lane == 0) tc::bulk_wait0();  // this warp's output stores are complete
+    if (lane == 0) tc::bulk_wait_read<0>();  // this warp's stores have read its buffers (they are complete when the kernel is)
     __syncwarp();
   }
 
@@ -544,7 +545,7 @@ int launch(const char *name, const CUtensorMap &a, const CUtensorMap &b, const E
   }
   cfg.gridDim = dim3(2 * unsigned(std::max(1ll, std::min<long long>(n, most))));
   cfg.numAttrs = 2;
-  MOE_LAUNCH(name, s, cudaLaunchKernelEx(&cfg, kern, a, b, epi, t, second));
+  MOE_LAUNCH(name, s, cudaLaunchKernelEx(&cfg, kern, a, b, epi, t, Walk(t, Sh::BN, Sh::KB), second));
   return moe::launch_status(what);
 }
 
@@ -585,14 +586,13 @@ template <class Sh, class Epi>
 int two_products(const char *name, const Matrix &a, const Matrix &b, const Epi &epi, Tiles t, const Matrix &a2, const Matrix &b2,
                  const Epi &epi2, Tiles t2, int head, cudaStream_t s, const char *what) {
   CUtensorMap ma, mb;
-  Second<Epi> second;
+  Second<Epi> second = {{}, {}, epi2, t2, Walk(t2, Sh::BN, Sh::KB), head};
   long long most, most2;
   int st = plan<Sh>(a, false, b, true, false, t, &ma, &mb, &most, what);
   if (!st) st = plan<Sh>(a2, true, b2, true, false, t2, &second.a, &second.b, &most2, what);
   if (st) return st;
-  second.epi = epi2;
   second.t = t2;
-  second.head = head;
+  second.walk = Walk(t2, Sh::BN, Sh::KB);
   return launch<Sh, false, true, false>(name, ma, mb, epi, t, second, most + most2, s, what);
 }
 
