@@ -29,7 +29,7 @@ namespace {
 constexpr float kLo = 2048.f;      // lo = (x - hi) * kLo
 constexpr float kScaleA = 64.f;    // A and B are stored times this: entries up to ~1,000 fit, normal down to 1e-6
 constexpr int kMaxSteps = 16;
-constexpr int kParts = 64;         // blocks that a matrix's sums are taken by, at most
+constexpr int kParts = 256;        // blocks that a matrix's sums are taken by, at most (64 left a third of the memory's rate to 8 of 2048 x 4096)
 
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -159,7 +159,7 @@ template <bool LAST> struct StepEpi {
   template <int BN, int kSlots, class Ready> __device__ __forceinline__ void run(dg::Warp &w, Ready ready) const {
     const int row0 = w.row - w.lane;
     if (row0 >= rows || w.col >= cols) return;
-    static_assert(kSlots >= 3, "a slot's store is waited for a chunk later");
+    static_assert(kSlots >= (LAST ? 3 : 2), "a slot's store is waited for a chunk later; with w, slots are half as many again");
     const int chunks = min(BN / 64, (cols - w.col + 31) / 32);
     volatile int never = 0;
     const float *res = resid + size_t(w.z) * (tall ? cols : rows);
@@ -339,10 +339,9 @@ struct Source {
   int rows, cols, vec;
 };
 
-// U of the 8 columns from `col` of matrix row `row` (0 past the row's end). UPDATE: the momentum is new.
+// U's 8 values from element o on (0 past `left` of them). UPDATE: the momentum is new.
 template <bool UPDATE>
-__device__ __forceinline__ void load_u(const Source &s, size_t row, int col, float (&u)[8]) {
-  const size_t o = row * s.cols + col;
+__device__ __forceinline__ void load_u(const Source &s, size_t o, int left, float (&u)[8]) {
   if (s.vec) {
     unpack8(*reinterpret_cast<const uint4 *>(s.g + o), u);
     if (s.m == nullptr) return;
@@ -362,7 +361,7 @@ __device__ __forceinline__ void load_u(const Source &s, size_t row, int col, flo
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     u[i] = 0.f;
-    if (col + i >= s.cols) continue;
+    if (i >= left) continue;
     u[i] = __uint_as_float(uint32_t(s.g[o + i]) << 16);
     if (s.m == nullptr) continue;
     float m = s.m[o + i];
@@ -392,14 +391,18 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
   pdl_start();
   const int slot = blockIdx.y;
   if (live != nullptr && first + slot >= live[0]) return;
-  const size_t mrow = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows;
-  const int cpr = (s.cols + 7) / 8;
-  const int64_t units = int64_t(s.rows) * cpr;
+  const size_t m0 = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows * s.cols;
+  const int cpr = (s.cols + 7) / 8, units = s.rows * cpr;  // (2^25 at most)
   float t[3] = {};
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < units; i += int64_t(parts) * 256) {
-    const int64_t r = i / cpr;
+#pragma unroll 2
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += parts * 256) {
     float u[8], q[3] = {};
-    load_u<true>(s, mrow + r, int(i - r * cpr) * 8, u);
+    if (s.vec) {
+      load_u<true>(s, m0 + size_t(i) * 8, 8, u);
+    } else {
+      const int r = i / cpr, col = (i - r * cpr) * 8;
+      load_u<true>(s, m0 + size_t(r) * s.cols + col, s.cols - col, u);
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float up = u[j] * kUp, down = u[j] * kDown;
@@ -447,14 +450,13 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
   }
   __syncthreads();
   const float pre = sh[0], factor = scale / sh[1];  // (a division each value was slower than the memory)
-  const size_t mrow = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows;
-  const int cpr = (s.cols + 7) / 8;
-  const int64_t units = int64_t(s.rows) * cpr;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < units; i += int64_t(gridDim.x) * 256) {
-    const int64_t r = i / cpr;
-    const int col = int(i - r * cpr) * 8;
+  const size_t m0 = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows * s.cols;
+  const int cpr = (s.cols + 7) / 8, units = s.rows * cpr;
+#pragma unroll 2
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += gridDim.x * 256) {
+    const int r = i / cpr, col = (i - r * cpr) * 8;
     float u[8];
-    load_u<false>(s, mrow + r, col, u);
+    load_u<false>(s, m0 + size_t(r) * s.cols + col, s.cols - col, u);
     uint32_t h[4], l[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -1117,6 +1119,10 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
         e.hi = xo[i & 1]; e.lo = lom; e.next = i + 1 < steps ? xo[(i + 1) & 1] : om; e.resid = resid; e.a = cf[0];
         e.rows = rows; e.cols = cols; e.tall = tall; e.to = to;
         e.to.live = live ? live + 1 + first : nullptr; e.to.first = first;
+        if constexpr (!std::is_same<decltype(e), StepEpi<true>>::value)
+          if (n >= 1536)
+            return tall ? dg::product<dg::WideLong, false, false, true>("muon_step", X, B, e, t, s, fn)
+                        : dg::product<dg::WideLong, false, true, true>("muon_step", B, X, e, t, s, fn);
         if (tall)
           return small_x ? dg::product<dg::SmallIO, false, false, true>("muon_step", X, B, e, t, s, fn)
                          : dg::product<dg::WideIO, false, false, true>("muon_step", X, B, e, t, s, fn);
