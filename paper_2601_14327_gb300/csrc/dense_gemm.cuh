@@ -145,12 +145,11 @@ struct Stager {
     ++turn;
     return b;
   }
-  // Both buffers, free of the stores before.
-  __device__ __forceinline__ void both(int lane, uint32_t &a, uint32_t &b) {
+  // Both buffers as one of 4 KB, free of the stores before.
+  __device__ __forceinline__ uint32_t both(int lane) {
     if (lane == 0) tc::bulk_wait_read<0>();
     __syncwarp();
-    a = base;
-    b = base + kStageBytes;
+    return base;
   }
 };
 
@@ -174,6 +173,11 @@ __device__ __forceinline__ void stage_and_store(const CUtensorMap *tm, Stager &s
 #pragma unroll
   for (uint32_t c = 0; c < 4; ++c) tc::st_shared_v4(stage_at(stage, lane, c), v[c]);
   store_chunk(tm, stage, lane, col, row, z);
+}
+// Both buffers as one: 32 rows of 64 16-bit values in the 128-byte-swizzle layout, of which this lane writes its own (values
+// 8 q .. 8 q + 7 of its row at stage64_at), and their store as one tile of whole 128-byte lines.
+__device__ __forceinline__ uint32_t stage64_at(uint32_t stage, int lane, uint32_t q) {
+  return stage + uint32_t(lane) * 128u + ((q ^ (uint32_t(lane) & 7u)) << 4);
 }
 // The same chunk transposed: stored at (row, col), so that the lane's row becomes a column.
 __device__ __forceinline__ void stage_and_store_t(const CUtensorMap *tm, Stager &st, int lane, const uint4 (&v)[4],
@@ -597,6 +601,11 @@ int two_products(const char *name, const Matrix &a, const Matrix &b, const Epi &
   return launch<Sh, false, true, false>(name, ma, mb, epi, t, second, most + most2, s, what);
 }
 
+// For stores of 32 rows of 64 values (stage64_at).
+inline int store64_map(CUtensorMap *m, const void *base, bool half, int64_t mats, int64_t rows, int64_t cols, int64_t pitch,
+                       int64_t step, const char *what) {
+  return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 64, 32, what, CU_TENSOR_MAP_SWIZZLE_128B);
+}
 inline int store_map(CUtensorMap *m, const void *base, bool half, int64_t mats, int64_t rows, int64_t cols,
                      int64_t pitch, int64_t step, const char *what) {
   return moe::make_map_stack(m, base, half, mats, rows, cols, pitch, step, 32, 32, what, CU_TENSOR_MAP_SWIZZLE_64B);

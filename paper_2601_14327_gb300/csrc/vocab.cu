@@ -127,30 +127,20 @@ template <bool KEEP> struct LogitsEpi {
     if (w.row < rows) part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, s0 + s1);
     if (KEEP) {
 #pragma unroll
-      for (int c = 0; c < kBlk; c += 64) {  // both staging buffers with one fence
+      for (int c = 0; c < kBlk; c += 64) {
         if (c >= nv) break;
-        uint32_t buf[2];
-        w.st.both(w.lane, buf[0], buf[1]);
+        const uint32_t buf = w.st.both(w.lane);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int q = 0; q < 8; ++q) {
+          uint32_t v[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int j = c + 32 * h + 8 * q + 2 * i;
-              const __half2 x = __floats2half2_rn(z[j], z[j + 1]);
-              v[i] = *reinterpret_cast<const uint32_t *>(&x);
-            }
-            tc::st_shared_v4(dg::stage_at(buf[h], w.lane, q), make_uint4(v[0], v[1], v[2], v[3]));
+          for (int i = 0; i < 4; ++i) {
+            const __half2 x = __floats2half2_rn(z[c + 8 * q + 2 * i], z[c + 8 * q + 2 * i + 1]);
+            v[i] = *reinterpret_cast<const uint32_t *>(&x);
           }
-        tc::fence_proxy_async_smem();
-        __syncwarp();
-        if (w.lane == 0) {
-          tc::tma_store_3d(&kept, buf[0], w.col + c, w.row - w.lane, 0);
-          if (c + 32 < nv) tc::tma_store_3d(&kept, buf[1], w.col + c + 32, w.row - w.lane, 0);
-          tc::bulk_commit();
+          tc::st_shared_v4(dg::stage64_at(buf, w.lane, q), make_uint4(v[0], v[1], v[2], v[3]));
         }
+        dg::store_chunk(&kept, buf, w.lane, w.col + c, w.row - w.lane, 0);
       }
     }
   }
@@ -175,26 +165,36 @@ struct OutEpi {
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     if (w.row - w.lane >= rows) return;
+    if (add != nullptr || sum != nullptr) {
+#pragma unroll
+      for (int c = 0; c < BN / 2; c += 32) {
+        const int col = w.col + c;
+        if (col >= cols) break;
+        const size_t at = frag_index(w.split, w.row - w.lane, col, rows, cols) + w.lane;
+        if (add != nullptr) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) z[c + i] += add[at + 32 * i];
+        }
+        if (sum != nullptr) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sum[at + 32 * i] = z[c + i];
+        }
+      }
+      if (sum != nullptr) return;
+    }
     const float f = *factor;
 #pragma unroll
-    for (int c = 0; c < BN / 2; c += 32) {
-      const int col = w.col + c;
-      if (col >= cols) break;
-      const size_t at = frag_index(w.split, w.row - w.lane, col, rows, cols) + w.lane;
-      if (add != nullptr) {
+    for (int c = 0; c < BN / 2; c += 64) {
+      if (w.col + c >= cols) break;
+      const uint32_t buf = w.st.both(w.lane);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[c + i] += add[at + 32 * i];
+      for (int q = 0; q < 8; ++q) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = f * z[c + 8 * q + i];
+        tc::st_shared_v4(dg::stage64_at(buf, w.lane, q), pack8(v));
       }
-      if (sum != nullptr) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) sum[at + 32 * i] = z[c + i];
-      } else {
-        uint4 v[4];
-        uint32_t *p = reinterpret_cast<uint32_t *>(v);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = pack_bf16x2(f * z[c + 2 * i], f * z[c + 2 * i + 1]);
-        dg::stage_and_store(&out, w.st, w.lane, v, col, w.row - w.lane, 0);
-      }
+      dg::store_chunk(&out, buf, w.lane, w.col + c, w.row - w.lane, 0);
     }
   }
 };
@@ -614,7 +614,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
       e.left = left; e.blocks = grad && rows <= kFewTokens ? rows : (rows + 7) / 8;
       if (grad) {
-        const int st = dg::store_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
+        const int st = dg::store64_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
         if (st) return st;
       }
       return z.blk == 64 ? dg::product<dg::Narrow, false, false, false>("vocab_logits", mh, mw, e, t, s, fn)
@@ -648,12 +648,12 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     uint16_t *out = d_hidden ? d_hidden + t0 * d : nullptr;
     if (d_hidden) {
       eh.rows = rows; eh.cols = d; eh.factor = factor;
-      if ((st = dg::store_map(&eh.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
+      if ((st = dg::store64_map(&eh.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
       if (plan.splits > 1) eh.sum = dhp;
     }
     if (d_w) {
       ew.rows = V; ew.cols = d; ew.factor = factor;
-      if ((st = dg::store_map(&ew.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
+      if ((st = dg::store64_map(&ew.out, d_w, false, 1, V, d, d, int64_t(V) * d, fn))) return st;
       if (t0 > 0) ew.add = dwp;
       if (t0 + rows < T) ew.sum = dwp;
     }
