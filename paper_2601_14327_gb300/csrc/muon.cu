@@ -527,7 +527,7 @@ __device__ __forceinline__ uint32_t sw128(uint32_t block, int r, int q) {
 __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p) {
   extern __shared__ uint8_t smem_raw[];
   const int mat = int(blockIdx.x) / p.ctas;
-  pdl_start();
+  pdl_wait();
   if (p.mask != nullptr && p.mask[mat / p.per] == 0) return;  // (the whole cluster)
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t misc = base, sA = base + kOffA, sB = base + kOffB, sX = base + kOffX, recv = base + kOffRecv;
@@ -549,6 +549,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
   tc::fence_before_sync();
   __syncthreads();
   tc::cluster_sync();  // (the peers' shared memory is written to from here on)
+  pdl_launch();        // only now: a dependent must not take the TMEM columns this kernel waits for
   tc::fence_after_sync();
   uint32_t tmem;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(misc) : "memory");
@@ -1037,9 +1038,10 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
   if (!ws || !moe::aligned16(ws) || ws_bytes < size_t(layout(n_mats, rows, cols, 1).total))
     return moe::set_error(MOE_ERR_WORKSPACE, "%s: workspace of %lld bytes at least, 16-byte aligned, needed", fn,
                           (long long)layout(n_mats, rows, cols, 1).total);
-  // as many matrices at a time as the workspace holds
+  // as many matrices at a time as the workspace holds, and 2^28 tiles of 256 x 128 do
+  const int64_t tiles = int64_t(ceil_div(rows, 256)) * ceil_div(cols, 128) * 2;
   int batch = 1;
-  for (int hi = n_mats; batch < hi;) {
+  for (int hi = int(std::min<int64_t>(n_mats, (int64_t(1) << 28) / tiles)); batch < hi;) {
     const int mid = batch + (hi - batch + 1) / 2;
     if (size_t(layout(n_mats, rows, cols, mid).total) <= ws_bytes) batch = mid;
     else hi = mid - 1;

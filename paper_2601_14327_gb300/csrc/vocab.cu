@@ -251,61 +251,76 @@ struct Coefs {
   }
 };
 
-// loss = (sum nll, z_coef sum lse^2) / M by one block. Sums of 1,024 strands of tokens, which the block's threads take
-// in turns (the same sums for any block), in chains of at most 32 additions on either of two levels up to 2^20 tokens.
-// `s`: 64 floats.
-__device__ __forceinline__ void sum_losses(const float *lse, const float *nll, const int32_t *__restrict__ target, int T,
-                                           int V, float z_coef, int n_valid, float *__restrict__ loss, float *s) {
-  float a, b;
-  for (int strand = threadIdx.x; strand < kSumThreads; strand += blockDim.x) {
-    a = b = 0.f;
-    for (int t0 = strand; t0 < T; t0 += 32 * kSumThreads) {
-      float x = 0.f, y = 0.f;
-      for (int i = 0, t = t0; i < 32 && t < T; ++i, t += kSumThreads) {
-        const int v = target[t];
-        if (v >= 0 && v < V) {
-          const float l = __ldcg(lse + t);
-          x += __ldcg(nll + t);
-          y = fmaf(l, l, y);
-        }
-      }
-      a += x;
-      b += y;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      a += __shfl_down_sync(0xffffffffu, a, o);
-      b += __shfl_down_sync(0xffffffffu, b, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-      s[strand >> 5] = a;
-      s[32 + (strand >> 5)] = b;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    a = b = 0.f;
-    for (int i = 0; i < 32; ++i) {
-      a += s[i];
-      b += s[32 + i];
-    }
-    const float m = float(max(1, n_valid));
-    loss[0] = a / m;
-    loss[1] = z_coef != 0.f ? z_coef * (b / m) : 0.f;
-  }
-}
-
-// What is left to do once every token's lse is there, by one block: M, the losses and the factor. `s`: 64 floats.
+// M, the losses = (sum nll, z_coef sum lse^2) / M, and the factor, by one block of THREADS once every token's lse is there.
+// Sums of 1,024 strands of tokens, each thread some of them (the same sums for any block), in chains of at most 32
+// additions on either of two levels up to 2^20 tokens. `s`: 96 words.
+template <int THREADS>
 __device__ __forceinline__ void finish_losses(const float *lse, const float *nll, const int32_t *__restrict__ target, int T,
                                               int V, const Coefs &k, int32_t *__restrict__ n_valid, float *__restrict__ loss,
                                               float *__restrict__ factor, float *s) {
-  const int n = count_targets(target, T, V, reinterpret_cast<int *>(s));
-  sum_losses(lse, nll, target, T, V, k.z_coef, n, loss, s);
-  if (threadIdx.x == 0) {
-    float a, b, f;
-    k.get(n, a, b, f);
-    *n_valid = n;
-    *factor = f;
+  constexpr int PER = kSumThreads / THREADS;
+  float a[PER] = {}, b[PER] = {};
+  int n = 0;
+  bool bad = false;
+  for (int t0 = threadIdx.x; t0 < T; t0 += 32 * kSumThreads) {
+    float x[PER] = {}, y[PER] = {};
+    for (int i = 0; i < 32 && t0 + i * kSumThreads < T; ++i) {
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int t = t0 + i * kSumThreads + p * THREADS;
+        if (t >= T) continue;
+        const int v = target[t];
+        const float l = __ldcg(lse + t), m = __ldcg(nll + t);
+        const bool ok = v >= 0 && v < V;
+        x[p] += ok ? m : 0.f;
+        y[p] = ok ? fmaf(l, l, y[p]) : y[p];
+        n += ok;
+        bad |= v >= V;
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      a[p] += x[p];
+      b[p] += y[p];
+    }
+  }
+  if (bad) dev_flag(&g_dev_err, MOE_DEV_BAD_TARGET);
+  n = __reduce_add_sync(0xffffffffu, n);
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      a[p] += __shfl_down_sync(0xffffffffu, a[p], o);
+      b[p] += __shfl_down_sync(0xffffffffu, b[p], o);
+    }
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      s[p * (THREADS / 32) + warp] = a[p];
+      s[32 + p * (THREADS / 32) + warp] = b[p];
+    }
+    s[64 + warp] = __int_as_float(n);
+  }
+  __syncthreads();
+  if (warp == 0) {
+    float u = s[lane], v = s[32 + lane];
+    n = __reduce_add_sync(0xffffffffu, lane < THREADS / 32 ? __float_as_int(s[64 + lane]) : 0);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      u += __shfl_down_sync(0xffffffffu, u, o);
+      v += __shfl_down_sync(0xffffffffu, v, o);
+    }
+    if (lane == 0) {
+      const float m = float(max(1, n));
+      loss[0] = u / m;
+      loss[1] = k.z_coef != 0.f ? k.z_coef * (v / m) : 0.f;
+      float fa, fb, f;
+      k.get(n, fa, fb, f);
+      *n_valid = n;
+      *factor = f;
+    }
   }
 }
 // Whether this block is the last of those that count `left` down to finish (their writes are then visible).
@@ -338,9 +353,9 @@ __device__ __forceinline__ void row_lse(const float2 *p, int np, int lane, bool 
   lse = m + logf(s);
   nll = 0.f;
   if (has_target) {
-    const float d = lse - zt;  // (s = 0, -inf: exp underflows as it should)
-    nll = d > 0.f ? d + log1pf(expf(-d)) : log1pf(expf(d));
-    lse = zt + nll;
+    const float d = lse - zt, x = log1pf(expf(-fabsf(d)));  // (r or z_t may be -inf: d infinite, x 0)
+    nll = d > 0.f ? d + x : x;
+    lse = (d > 0.f ? lse : zt) + x;
   }
 }
 
@@ -353,7 +368,7 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
                                                  const Coefs k, float *__restrict__ factor, float *__restrict__ lse,
                                                  float *__restrict__ nll, int whole, int *__restrict__ left,
                                                  int32_t *__restrict__ n_valid, float *__restrict__ loss) {
-  __shared__ float sh[64];
+  __shared__ float sh[96];
   __shared__ int last;
   pdl_start();
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -375,7 +390,7 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
       for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
     }
   }
-  if (whole && last_block(left, &last)) finish_losses(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
+  if (whole && last_block(left, &last)) finish_losses<256>(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
 // Eight kept exponentials (half precision) as eight of dz (bf16): f = exp(maximum - lse) (a + b lse).
@@ -423,7 +438,7 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
                                                     int V, int np, int blk, const Coefs k, float *__restrict__ factor,
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
                                                     int32_t *__restrict__ n_valid, float *__restrict__ loss) {
-  __shared__ float sh[64];
+  __shared__ float sh[96];
   __shared__ float row_l[2];
   __shared__ int last;
   pdl_start();
@@ -454,7 +469,7 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
     uint4 *at = e + (size_t(row) * pitch + col) / 8;
     *at = dz8(*at, __expf(p[blk == 128 ? col / 128 : col / 64].x - l) * f0, tgt, col, V, k, l, x);
   }
-  if (blockIdx.x == 0 && last_block(left, &last)) finish_losses(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
+  if (blockIdx.x == 0 && last_block(left, &last)) finish_losses<256>(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
 // dh = sum of the splits' products: a lane a row of 32 x 8 values, and `team` (1 or 8) warps of a block to them, each adding up
@@ -493,11 +508,12 @@ __global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ pa
 }
 
 __global__ void __launch_bounds__(kSumThreads) vocab_loss_sum(const float *__restrict__ lse, const float *__restrict__ nll,
-                                                              const int32_t *__restrict__ target, int T, int V, float z_coef,
-                                                              const int32_t *__restrict__ n_valid, float *__restrict__ loss) {
-  __shared__ float s[64];
+                                                              const int32_t *__restrict__ target, int T, int V, const Coefs k,
+                                                              int32_t *__restrict__ n_valid, float *__restrict__ loss,
+                                                              float *__restrict__ factor) {
+  __shared__ float s[96];
   pdl_start();
-  sum_losses(lse, nll, target, T, V, z_coef, *n_valid, loss, s);
+  finish_losses<kSumThreads>(lse, nll, target, T, V, k, n_valid, loss, factor, s);
 }
 
 // ---------------------------------------------------------------- host side
@@ -574,7 +590,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
                           fn);
   if (!w || !loss || !n_valid || (T > 0 && (!h || !target || !nll || !lse)))
     return moe::set_error(MOE_ERR_ARG, "%s: null pointer", fn);
-  if (grad && !d_hidden && !d_w) return moe::set_error(MOE_ERR_ARG, "%s: neither d_hidden nor d_w", fn);
+  if (grad && T > 0 && !d_hidden && !d_w) return moe::set_error(MOE_ERR_ARG, "%s: neither d_hidden nor d_w", fn);
   for (const void *p : {static_cast<const void *>(h), static_cast<const void *>(w), static_cast<const void *>(d_hidden),
                         static_cast<const void *>(d_w)})
     if (!moe::aligned16(p)) return moe::set_error(MOE_ERR_ARG, "%s: bf16 tensors must be 16-byte aligned", fn);
@@ -670,7 +686,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     }
   }
   if (whole) return MOE_OK;
-  MOE_LAUNCH("vocab_loss_sum", s, moe::launch_dep(vocab_loss_sum, 1, kSumThreads, 0, s, lse, nll, target, T, V, z_coef, n_valid, loss));
+  MOE_LAUNCH("vocab_loss_sum", s, moe::launch_dep(vocab_loss_sum, 1, kSumThreads, 0, s, lse, nll, target, T, V, k, n_valid, loss, factor));
   return moe::launch_status(fn);
 }
 

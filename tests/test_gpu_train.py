@@ -1,5 +1,9 @@
 """The vocabulary loss and the orthogonalised update on the GPU, through the package's calls, against the oracle
 in 64 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -195,6 +199,39 @@ def test_vocab_nan_stays_with_its_token():
     assert np.isnan(out["lse"][[17, 260]]).all() and (out["nll"][[17, 260]] == 0).all()
     assert np.isfinite(out["loss"]).all()
     dev_ok()
+
+
+def test_vocab_logits_of_minus_infinity():
+    # entries that no token can have: the target's own gives an infinite nll, lse is the others'
+    h = torch.ones(4, 8, dtype=BF16)
+    w = torch.randn(300, 8, generator=torch.Generator().manual_seed(1)).to(BF16)
+    w[[5, 200, 299]] = float("-inf")
+    t = torch.tensor([5, 6, 299, -1], dtype=torch.int32)
+    out = run_vocab(h, w, t, backward=False)
+    keep = [i for i in range(300) if i not in (5, 200, 299)]
+    ref = O.vocab_loss(npf(h), npf(w[keep]), np.array([-1, 5, -1, -1]))
+    np.testing.assert_allclose(out["lse"], ref["lse"], rtol=1e-6)
+    assert np.isposinf(out["nll"][[0, 2]]).all() and out["nll"][3] == 0 and np.isposinf(out["loss"][0])
+    np.testing.assert_allclose(out["nll"][1], ref["nll"][1], rtol=1e-5)
+    dev_ok()
+
+
+def test_vocab_sure_tokens_keep_their_digits():
+    # nll from 4e-6 to 0.9: z_t is off by (d / 16 + 2) 2^-23 sum |h w| as the others are, their difference by twice that, and
+    # nll by as much relative to itself (d nll / d (z_t - z_v) <= nll); exponentials and sums 2^-19 more
+    d, V = 64, 400
+    g = torch.Generator().manual_seed(4)
+    w = (torch.randn(V, d, generator=g) * 0.1).to(BF16)
+    t = torch.arange(24, dtype=torch.int32)
+    u = w[:24].float()
+    h = (u / u.square().sum(1, keepdim=True) * torch.linspace(6, 22, 24)[:, None]).to(BF16)
+    ref = O.vocab_loss(npf(h), npf(w), t.numpy())
+    assert ref["nll"].min() < 1e-5
+    out = run_vocab(h, w, t)
+    dev_ok()
+    tz, _ = loss_tolerance(npf(h), npf(w), ref)
+    assert (np.abs(out["nll"] - ref["nll"]) <= ref["nll"] * (2 * tz + 2.0 ** -19)).all()
+    check_vocab(out, h, w, t, 0.0)
 
 
 def test_vocab_one_gradient_alone():
@@ -425,6 +462,16 @@ def test_muon_captured_and_replayed():
     graph.replay()
     dev_ok()
     assert torch.equal(wd, want_w) and torch.equal(md, want_m)
+
+
+@pytest.mark.parametrize("form", [{"MOE_MUON_SMALL": "0", "MOE_DENSE_SMALL": "0"}, {"MOE_MUON_SMALL": "0", "MOE_DENSE_SMALL": "1"},
+                                  {"MOE_MUON_SMALL": "1"}])
+def test_other_forms_of_the_updates(form):
+    """The tests above with each form of the products forced (the variables are read once, so in a child process)."""
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", "-p", "no:cacheprovider", "-k",
+                        "orthogonalize or muon_step or muon_captured", os.path.abspath(__file__)],
+                       env={**os.environ, **form}, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout[-2000:]
 
 
 # ---------------------------------------------------------------- together
