@@ -214,7 +214,7 @@ int moe_balance_loss_bwd(const float *logits, const uint8_t *active_mask, const 
  * left out too and sets MOE_DEV_BAD_TARGET.
  * hidden [T,d], w_vocab [V,d] bf16, 16-byte aligned; target [T] int32; loss [2], nll [T], lse [T] fp32,
  * n_valid [1] int32 = M (all overwritten). piece >= 1: tokens that are worked on at a time (min(piece, T) sets
- * the workspace: V/16 bytes a token here). ws: of moe_vocab_loss_workspace_size(T, d, V, piece, 0) bytes,
+ * the workspace: V/16 bytes a token here, V/8 of few, V/4 of up to 128). ws: of moe_vocab_loss_workspace_size(T, d, V, piece, 0) bytes,
  * 16-byte aligned, used until the call's kernels end. All sums run in a fixed order: bitwise reproducible, and
  * independent of piece. A NaN or +inf among a token's logits makes its lse and nll NaN, and loss with them
  * when it has a target.
@@ -225,7 +225,7 @@ int moe_vocab_loss(const uint16_t *hidden, const uint16_t *w_vocab, const int32_
                    size_t ws_bytes, moe_stream_t stream);
 
 /* Bytes of `ws` for moe_vocab_loss (grad 0) or moe_vocab_loss_grad (grad 1); 0 for sizes outside the limits.
- * With grad, min(piece, T) * (2 V + V/16) bytes, the partial sums of d_hidden when that has few tiles, and
+ * With grad, min(piece, T) * (2 V + V/16, V/8 or V/4) bytes, the partial sums of d_hidden when that has few tiles, and
  * 4 V d bytes when piece < T. */
 size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad);
 
@@ -236,7 +236,7 @@ size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad);
  *   d_hidden[t,:] = sum_v dz[t,v] * w_vocab[v,:],   d_w[v,:] = sum_t dz[t,v] * hidden[t,:]
  * Arguments as in moe_vocab_loss; d_loss [2] fp32 (device) or NULL (ones); d_hidden [T,d], d_w [V,d] bf16
  * (overwritten; either may be NULL: not computed; not both). dz is held in bf16, a piece of `piece` tokens at a
- * time (the exponentials it is made from in half precision, relative to the largest of 128 columns; p - 1 at the
+ * time (the exponentials it is made from in half precision, relative to the largest of 128, 64 or 32 columns; p - 1 at the
  * target is exact to fp32 however sure the token is); the products accumulate in fp32. d_w's sum over pieces is
  * kept in fp32 in ws and rounded once. Results are bitwise reproducible; d_w's last bits depend on piece, d_hidden's on
  * it where its reduction is split (few tokens). `hidden` has to be finite also for tokens without a target: their rows

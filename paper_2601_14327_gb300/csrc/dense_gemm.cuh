@@ -47,6 +47,7 @@ template <int BN_, int KB_, int STAGES_, int BUFS_> struct Shape {
 };
 using Wide = Shape<256, 128, 3, 2>;
 using Narrow = Shape<128, 128, 4, 2>;
+using Few64 = Shape<64, 128, 4, 2>;
 using WideIO = Shape<256, 64, 4, 6>;    // epilogues that also load: two or three chunks ahead
 using WideLong = Shape<256, 64, 5, 4>;  // under long reductions, where a chunk less and a stage more are faster (4%)
 using Small = Shape<128, 64, 5, 2>;

@@ -28,13 +28,17 @@ constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is 
 struct Sizes {
   int blk;             // columns that share a maximum: half a tile
   int64_t np, pitch;   // (maximum, sum) pairs of a row; halves from row to row of the kept exponentials
+  int shift() const { return blk == 32 ? 5 : blk == 64 ? 6 : 7; }
 };
 // Tiles of the logits are 256 columns wide, or 128 where the wide ones are at most half as many as the pairs: each then has half
 // the products (6 tokens of d 856, 2,422 entries, with gradients: 34 -> 29 us). By all tokens, not a piece's:
 // the order of a row's sums follows from it.
 bool narrow(int64_t T, int64_t V) { return ((T + 255) / 256) * ((V + 255) / 256) <= kPairs / 2; }
+// Up to 128 tokens the logits are computed with the entries as rows (FewEpi), unless that would leave fewer tiles (104
+// tokens of d 416, 7,602 entries: 15 us, 13 in narrow tiles).
+bool entries_as_rows(int64_t T, int64_t V) { return T <= 128 && !narrow(T, V); }
 Sizes sizes(int64_t T, int V) {
-  const int blk = narrow(T, V) ? 64 : 128;
+  const int blk = entries_as_rows(T, V) ? 32 : narrow(T, V) ? 64 : 128;
   return {blk, (int64_t(V) + blk - 1) / blk, (int64_t(V) + 63) / 64 * 64};
 }
 
@@ -66,18 +70,85 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float ld_shared_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // ---------------------------------------------------------------- epilogues
 
-// Rows of the logits: see the top of the file. KEEP: the exponentials go to memory through `kept`.
-template <bool KEEP> struct LogitsEpi {
-  CUtensorMap kept;
+// A block of N logits of a row, `nv` of them entries, `tgt` the target's place among them or outside: z becomes the exponentials
+// relative to the maximum m (those past nv 0); s their sum without the target's, zt the target's logit.
+template <int N>
+__device__ __forceinline__ bool exp_block(float (&z)[N], int nv, int tgt, float &m, float &s, float &zt) {
+  if (nv < N) {
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+      if (c >= nv) z[c] = -INFINITY;
+  }
+  const bool hit = tgt >= 0 && tgt < nv;
+  if (hit) {
+    zt = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) zt = c == tgt ? z[c] : zt;
+  }
+  float m4[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+  for (int c = 4; c < N; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
+  m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+  // exp(z - m) = 2^(z log2 e - m log2 e), two values an instruction (a block of -inf alone: exponentials of 0)
+  const float shift = m == -INFINITY ? 0.f : m * -kLog2e;
+  const uint64_t scale2 = pack_f32x2(kLog2e, kLog2e), shift2 = pack_f32x2(shift, shift);
+  uint64_t sum2[2] = {0, 0};
+#pragma unroll
+  for (int c = 0; c < N; c += 2) {
+    float a, b;
+    unpack_f32x2(fma_f32x2(pack_f32x2(z[c], z[c + 1]), scale2, shift2), a, b);
+    z[c] = exp2_approx(a);
+    z[c + 1] = exp2_approx(b);
+    sum2[(c >> 1) & 1] = add_f32x2(sum2[(c >> 1) & 1], pack_f32x2(z[c], z[c + 1]));
+  }
+  float s0, s1;
+  unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
+  if (hit) {  // the others' sum (see row_lse): beside a sure token it is below the total's rounding
+    s0 = s1 = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; c += 2) {
+      s0 += c == tgt ? 0.f : z[c];
+      s1 += c + 1 == tgt ? 0.f : z[c + 1];
+    }
+  }
+  s = s0 + s1;
+  return hit;
+}
+template <int N> __device__ __forceinline__ uint4 halves8(const float (&z)[N], int c) {
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 x = __floats2half2_rn(z[c + 2 * i], z[c + 2 * i + 1]);
+    v[i] = *reinterpret_cast<const uint32_t *>(&x);
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// Where the logits' epilogues write. lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum
+// over the features, whose errors point one way: hence kChunk.
+struct Logits {
+  CUtensorMap kept;        // the exponentials, with KEEP
   float2 *part;            // [rows, np]
   float *zt;               // [rows] the target's logit
   const int32_t *target;
   int *left;               // vocab_lse's block counter, set by one thread
   int blocks;
   int rows, V, np;
-  // lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum, whose errors point one way
+};
+
+// Rows of the logits (tokens) by columns (entries): see the top of the file.
+template <bool KEEP> struct LogitsEpi : Logits {
   static constexpr int kChunk = 512;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
@@ -86,61 +157,52 @@ template <bool KEEP> struct LogitsEpi {
     if (nv <= 0 || w.row - w.lane >= rows) return;
     if (w.row == 0 && w.col == 0) *left = blocks;
     const int tgt = w.row < rows ? target[w.row] - w.col : -1;
-    if (nv < kBlk) {
-#pragma unroll
-      for (int c = 0; c < kBlk; ++c)
-        if (c >= nv) z[c] = -INFINITY;
-    }
-    const bool hit = tgt >= 0 && tgt < nv;
-    if (hit) {
-      float v = 0.f;
-#pragma unroll
-      for (int c = 0; c < kBlk; ++c) v = c == tgt ? z[c] : v;
-      zt[w.row] = v;
-    }
-    float m4[4] = {z[0], z[1], z[2], z[3]};
-#pragma unroll
-    for (int c = 4; c < kBlk; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
-    const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-    // exp(z - m) = 2^(z log2 e - m log2 e), two values an instruction (a block of -inf alone: exponentials of 0)
-    const float shift = m == -INFINITY ? 0.f : m * -kLog2e;
-    const uint64_t scale2 = pack_f32x2(kLog2e, kLog2e), shift2 = pack_f32x2(shift, shift);
-    uint64_t sum2[2] = {0, 0};
-#pragma unroll
-    for (int c = 0; c < kBlk; c += 2) {
-      float a, b;
-      unpack_f32x2(fma_f32x2(pack_f32x2(z[c], z[c + 1]), scale2, shift2), a, b);
-      z[c] = exp2_approx(a);
-      z[c + 1] = exp2_approx(b);
-      sum2[(c >> 1) & 1] = add_f32x2(sum2[(c >> 1) & 1], pack_f32x2(z[c], z[c + 1]));
-    }
-    float s0, s1;
-    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), s0, s1);
-    if (hit) {  // the others' sum (see row_lse): beside a sure token it is below the total's rounding
-      s0 = s1 = 0.f;
-#pragma unroll
-      for (int c = 0; c < kBlk; c += 2) {
-        s0 += c == tgt ? 0.f : z[c];
-        s1 += c + 1 == tgt ? 0.f : z[c + 1];
-      }
-    }
-    if (w.row < rows) part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, s0 + s1);
+    float m, s, t;
+    if (exp_block(z, nv, tgt, m, s, t)) zt[w.row] = t;
+    if (w.row < rows) part[size_t(w.row) * np + w.col / kBlk] = make_float2(m, s);
     if (KEEP) {
 #pragma unroll
       for (int c = 0; c < kBlk; c += 64) {
         if (c >= nv) break;
         const uint32_t buf = w.st.both(w.lane);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          uint32_t v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const __half2 x = __floats2half2_rn(z[c + 8 * q + 2 * i], z[c + 8 * q + 2 * i + 1]);
-            v[i] = *reinterpret_cast<const uint32_t *>(&x);
-          }
-          tc::st_shared_v4(dg::stage64_at(buf, w.lane, q), make_uint4(v[0], v[1], v[2], v[3]));
-        }
+        for (int q = 0; q < 8; ++q) tc::st_shared_v4(dg::stage64_at(buf, w.lane, q), halves8(z, c + 8 * q));
         dg::store_chunk(&kept, buf, w.lane, w.col + c, w.row - w.lane, 0);
+      }
+    }
+  }
+};
+
+// The same of few tokens, from the product's other side: rows are entries, columns tokens, and the tensor cores take 64 or 128
+// columns instead of the 256 rows that the tokens would leave empty (9 tokens of d 168, 69,881 entries: 25 -> 18 us).
+// 32 x 32 values change places through the staging buffers, so that a lane has 32 entries of a token: blocks of 32.
+template <bool KEEP> struct FewEpi : Logits {
+  static constexpr int kChunk = 512;
+
+  template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
+    const int v0 = w.row - w.lane, nv = min(32, V - v0);
+    if (nv <= 0) return;
+    if (w.row == 0 && w.col == 0) *left = blocks;
+#pragma unroll
+    for (int c = 0; c < BN / 2; c += 32) {
+      if (w.col + c >= rows) break;
+      const uint32_t buf = w.st.both(w.lane);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) st_shared_f32(buf + uint32_t(w.lane * 32 + (i ^ w.lane)) * 4u, z[c + i]);
+      __syncwarp();
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = ld_shared_f32(buf + uint32_t(i * 32 + (w.lane ^ i)) * 4u);
+      __syncwarp();
+      const int t = w.col + c + w.lane;
+      const int tgt = t < rows ? target[t] - v0 : -1;
+      float m, s, at;
+      if (exp_block(x, nv, tgt, m, s, at)) zt[t] = at;
+      if (t < rows) part[size_t(t) * np + v0 / 32] = make_float2(m, s);
+      if (KEEP) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tc::st_shared_v4(dg::stage_at(buf, w.lane, q), halves8(x, 8 * q));
+        dg::store_chunk(&kept, buf, w.lane, v0, w.col + c, 0);
       }
     }
   }
@@ -420,11 +482,11 @@ __device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, 
 constexpr int kDzCols = 2048;
 __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                 const float *__restrict__ lse, const float *__restrict__ nll,
-                                                const int32_t *__restrict__ target, int V, int np, int blk, const Coefs k) {
+                                                const int32_t *__restrict__ target, int V, int np, int shift, const Coefs k) {
   pdl_start();
   const int row = blockIdx.y, col = blockIdx.x * kDzCols + threadIdx.x * 8;
   if (col >= V) return;
-  const float f = part[size_t(row) * np + (blk == 128 ? col / 128 : col / 64)].y;
+  const float f = part[size_t(row) * np + (col >> shift)].y;
   uint4 *at = e + (size_t(row) * pitch + col) / 8;
   *at = dz8(*at, f, target[row], col, V, k, lse[row], nll[row]);
 }
@@ -435,7 +497,7 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 constexpr int kFewCols = 16384;
 __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                     const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
-                                                    int V, int np, int blk, const Coefs k, float *__restrict__ factor,
+                                                    int V, int np, int shift, const Coefs k, float *__restrict__ factor,
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
                                                     int32_t *__restrict__ n_valid, float *__restrict__ loss) {
   __shared__ float sh[96];
@@ -467,7 +529,7 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
 #pragma unroll 4
   for (int col = first + threadIdx.x * 8; col < end; col += 256 * 8) {
     uint4 *at = e + (size_t(row) * pitch + col) / 8;
-    *at = dz8(*at, __expf(p[blk == 128 ? col / 128 : col / 64].x - l) * f0, tgt, col, V, k, l, x);
+    *at = dz8(*at, __expf(p[col >> shift].x - l) * f0, tgt, col, V, k, l, x);
   }
   if (blockIdx.x == 0 && last_block(left, &last)) finish_losses<256>(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
@@ -626,21 +688,29 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     dg::Tiles t = {};
     t.mats = t.splits = 1;
     t.group = 8;
-    auto logits = [&](auto e) {
-      e.part = part; e.zt = zt; e.target = target + t0; e.rows = rows; e.V = V; e.np = int(z.np);
-      e.left = left; e.blocks = grad && rows <= kFewTokens ? rows : (rows + 7) / 8;
-      if (grad) {
-        const int st = dg::store64_map(&e.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn);
-        if (st) return st;
-      }
+    const bool few = entries_as_rows(T, V);
+    Logits l = {};
+    l.part = part; l.zt = zt; l.target = target + t0; l.rows = rows; l.V = V; l.np = int(z.np);
+    l.left = left;
+    l.blocks = grad && rows <= kFewTokens ? rows : (rows + 7) / 8;
+    if (grad && (st = few ? dg::store_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)
+                          : dg::store64_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)))
+      return st;
+    auto tokens = [&](auto e) {
       return z.blk == 64 ? dg::product<dg::Narrow, false, false, false>("vocab_logits", mh, mw, e, t, s, fn)
                          : dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
     };
-    if ((st = grad ? logits(LogitsEpi<true>{}) : logits(LogitsEpi<false>{}))) return st;
+    auto entries = [&](auto e) {
+      return T <= 64 ? dg::product<dg::Few64, false, false, false>("vocab_logits", mw, mh, e, t, s, fn)
+                     : dg::product<dg::Narrow, false, false, false>("vocab_logits", mw, mh, e, t, s, fn);
+    };
+    if (few) st = grad ? entries(FewEpi<true>{l}) : entries(FewEpi<false>{l});
+    else st = grad ? tokens(LogitsEpi<true>{l}) : tokens(LogitsEpi<false>{l});
+    if (st) return st;
     if (grad && whole && rows <= kFewTokens) {
       MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, rows), 256, 0, s,
                                                     reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
-                                                    z.blk, k, factor, lse, nll, left, n_valid, loss));
+                                                    z.shift(), k, factor, lse, nll, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
     } else {
       MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
@@ -653,7 +723,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
         MOE_LAUNCH("vocab_dz", s, moe::launch_dep(vocab_dz, dim3((V + kDzCols - 1) / kDzCols, n), 256, 0, s,
                                                   reinterpret_cast<uint4 *>(kept + int64_t(r0) * z.pitch), z.pitch,
                                                   part + int64_t(r0) * z.np, lse + t0 + r0, nll + t0 + r0, target + t0 + r0, V,
-                                                  int(z.np), z.blk, k));
+                                                  int(z.np), z.shift(), k));
         if ((st = moe::launch_status(fn))) return st;
       }
     }

@@ -112,7 +112,8 @@ def run_vocab(h, w, target, z_coef=0.0, d_loss=None, backward=True, piece=None, 
 
 
 VOCAB_SIZES = [(1, 8, 1), (1, 64, 7), (3, 8, 129), (2, 136, 128), (37, 200, 1000), (129, 256, 256), (257, 136, 513),
-               (300, 520, 4099), (255, 64, 2049), (1021, 72, 300)]
+               (300, 520, 4099), (255, 64, 2049), (1021, 72, 300), (5, 16, 20001), (64, 72, 20001), (65, 600, 20001), (128, 24, 19457),
+               (600, 136, 9000)]
 
 
 @pytest.mark.parametrize("T,d,V", VOCAB_SIZES)
