@@ -395,23 +395,36 @@ __device__ __forceinline__ bool last_block(int *left, int *sh) {
   return *sh != 0;
 }
 
-// A row's lse and nll from its pairs, by a warp (every lane has them). The pairs leave the target's own logit out: with
-// r = log sum over the others of exp z, nll = log(1 + exp(r - z_t)) and lse = z_t + nll, so that nll and p - 1 = expm1(-nll)
-// keep their digits however sure the token is (lse - z_t has an error of ~1e-6 whatever nll is).
-__device__ __forceinline__ void row_lse(const float2 *p, int np, int lane, bool has_target, float zt, float &lse, float &nll) {
+// A row's lse and nll from its pairs, by WARPS warps (every thread has them; `sh`: 2 WARPS floats). The pairs leave the target's
+// own logit out: with r = log sum over the others of exp z, nll = log(1 + exp(r - z_t)) and lse = z_t + nll, so that nll and
+// p - 1 = expm1(-nll) keep their digits however sure the token is (lse - z_t has an error of ~1e-6 whatever nll is).
+template <int WARPS>
+__device__ __forceinline__ void row_lse(const float2 *p, int np, bool has_target, float zt, float *sh, float &lse, float &nll) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = WARPS == 1 ? lane : int(threadIdx.x);
   float m = -INFINITY;
 #pragma unroll 4
-  for (int i = lane; i < np; i += 32) m = fmaxf(m, p[i].x);
+  for (int i = first; i < np; i += 32 * WARPS) m = fmaxf(m, p[i].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (WARPS > 1) {
+    if (lane == 0) sh[warp] = m;
+    __syncthreads();
+    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, sh[w]);
+  }
   float s = 0.f;
 #pragma unroll 4
-  for (int i = lane; i < np; i += 32) {
+  for (int i = first; i < np; i += 32 * WARPS) {
     const float2 v = p[i];
     s += v.y * __expf(v.x - m);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (WARPS > 1) {
+    if (lane == 0) sh[WARPS + warp] = s;
+    __syncthreads();
+    s = 0.f;
+    for (int w = 0; w < WARPS; ++w) s += sh[WARPS + w];
+  }
   lse = m + logf(s);
   nll = 0.f;
   if (has_target) {
@@ -421,10 +434,11 @@ __device__ __forceinline__ void row_lse(const float2 *p, int np, int lane, bool 
   }
 }
 
-// A warp per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
+// A warp (up to 512 tokens in all a block: ROWS 1) per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
 // block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target. whole (few
 // tokens, one piece): the block that ends last (`left`: blocks still at work) counts the targets and sums the losses, a
 // launch each otherwise, 7 us of a loss of 37 tokens.
+template <int ROWS>
 __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, const float *__restrict__ zt,
                                                  const int32_t *__restrict__ target, int rows, int V, int np, int grad,
                                                  const Coefs k, float *__restrict__ factor, float *__restrict__ lse,
@@ -433,23 +447,25 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
   __shared__ float sh[96];
   __shared__ int last;
   pdl_start();
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int row = ROWS == 1 ? int(blockIdx.x) : int(blockIdx.x) * 8 + int(threadIdx.x >> 5);
+  const int at = ROWS == 1 ? int(threadIdx.x) : int(threadIdx.x) & 31, step = 256 / ROWS;
   if (row < rows) {
     float2 *p = part + size_t(row) * np;
     const int tgt = target[row];
     const bool ok = tgt >= 0 && tgt < V;
     float l, x;
-    row_lse(p, np, lane, ok, ok ? zt[row] : 0.f, l, x);
-    if (lane == 0) {
+    row_lse<8 / ROWS>(p, np, ok, ok ? zt[row] : 0.f, sh, l, x);
+    if (at == 0) {
       lse[row] = l;
       nll[row] = x;
     }
     if (grad) {
       float a, b, s0;
       k.get(whole ? 1 : *n_valid, a, b, s0);
-      if (!whole && row == 0 && lane == 0) *factor = s0;
+      if (!whole && row == 0 && at == 0) *factor = s0;
       const float f = ok ? fmaf(b, l, a) : 0.f;
-      for (int i = lane; i < np; i += 32) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
+      if (ROWS == 1) __syncthreads();  // (all have read the sums)
+      for (int i = at; i < np; i += step) p[i].y = ok ? __expf(p[i].x - l) * f : 0.f;
     }
   }
   if (whole && last_block(left, &last)) finish_losses<256>(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
@@ -492,8 +508,8 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 }
 
 // vocab_lse and vocab_dz of few tokens in one launch (512 tokens of 32,000 entries: 77 -> 73 us for the loss with its gradients;
-// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, 16,384 columns), each of which has its
-// first warp work out the row's lse again (lse, nll and the losses: the blocks of the first columns).
+// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, 16,384 columns), each of which works
+// out the row's lse again (lse, nll and the losses: the blocks of the first columns).
 constexpr int kFewCols = 16384;
 __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                     const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
@@ -501,23 +517,14 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
                                                     int32_t *__restrict__ n_valid, float *__restrict__ loss) {
   __shared__ float sh[96];
-  __shared__ float row_l[2];
   __shared__ int last;
   pdl_start();
   const int row = blockIdx.y;
   const float2 *p = part + size_t(row) * np;
   const int tgt = target[row];
-  if (threadIdx.x < 32) {
-    const bool ok = tgt >= 0 && tgt < V;
-    float l, x;
-    row_lse(p, np, threadIdx.x, ok, ok ? zt[row] : 0.f, l, x);
-    if (threadIdx.x == 0) {
-      row_l[0] = l;
-      row_l[1] = x;
-    }
-  }
-  __syncthreads();
-  const float l = row_l[0], x = row_l[1];
+  const bool ok = tgt >= 0 && tgt < V;
+  float l, x;
+  row_lse<8>(p, np, ok, ok ? zt[row] : 0.f, sh, l, x);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     lse[row] = l;
     nll[row] = x;
@@ -692,7 +699,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     Logits l = {};
     l.part = part; l.zt = zt; l.target = target + t0; l.rows = rows; l.V = V; l.np = int(z.np);
     l.left = left;
-    l.blocks = grad && rows <= kFewTokens ? rows : (rows + 7) / 8;
+    l.blocks = T <= kFewTokens ? rows : (rows + 7) / 8;
     if (grad && (st = few ? dg::store_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)
                           : dg::store64_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)))
       return st;
@@ -707,13 +714,13 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     if (few) st = grad ? entries(FewEpi<true>{l}) : entries(FewEpi<false>{l});
     else st = grad ? tokens(LogitsEpi<true>{l}) : tokens(LogitsEpi<false>{l});
     if (st) return st;
-    if (grad && whole && rows <= kFewTokens) {
+    if (grad && whole && T <= kFewTokens) {
       MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, rows), 256, 0, s,
                                                     reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
                                                     z.shift(), k, factor, lse, nll, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
     } else {
-      MOE_LAUNCH("vocab_lse", s, moe::launch_dep(vocab_lse, (rows + 7) / 8, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
+      MOE_LAUNCH("vocab_lse", s, moe::launch_dep(T <= kFewTokens ? vocab_lse<1> : vocab_lse<8>, l.blocks, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
                                                  grad ? 1 : 0, k, factor, lse + t0, nll + t0, whole ? 1 : 0, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
       if (!grad) continue;
