@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kWholeTokens = 2048;  // tokens up to which the last block of vocab_lse(_dz) counts the targets and sums the losses
 constexpr int kFewTokens = 512;     // tokens up to which vocab_lse_dz takes the place of vocab_lse and vocab_dz
+constexpr int kTwoTerms = 32;       // tokens up to which dz has two terms
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
 struct Sizes {
@@ -472,7 +473,9 @@ __global__ void __launch_bounds__(256) vocab_lse(float2 *__restrict__ part, cons
 }
 
 // Eight kept exponentials (half precision) as eight of dz (bf16): f = exp(maximum - lse) (a + b lse).
-__device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, int V, const Coefs &k, float lse, float nll) {
+// `second` (or null): what the rounding leaves, in bf16 too.
+__device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, int V, const Coefs &k, float lse, float nll,
+                                     uint4 *second) {
   float o[8];
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -491,7 +494,15 @@ __device__ __forceinline__ uint4 dz8(const uint4 &v, float f, int tgt, int col, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = col + i == tgt ? d : o[i];
   }
-  return pack8(o);
+  const uint4 r = pack8(o);
+  if (second != nullptr) {
+    float b[8];
+    unpack8(r, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] -= b[i];
+    *second = pack8(o);
+  }
+  return r;
 }
 
 // dz in place of the kept exponentials. Blocks of 256 threads over (row, 2,048 columns).
@@ -504,22 +515,39 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
   if (col >= V) return;
   const float f = part[size_t(row) * np + (col >> shift)].y;
   uint4 *at = e + (size_t(row) * pitch + col) / 8;
-  *at = dz8(*at, f, target[row], col, V, k, lse[row], nll[row]);
+  *at = dz8(*at, f, target[row], col, V, k, lse[row], nll[row], nullptr);
 }
 
 // vocab_lse and vocab_dz of few tokens in one launch (512 tokens of 32,000 entries: 77 -> 73 us for the loss with its gradients;
 // at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, 16,384 columns), each of which works
 // out the row's lse again (lse, nll and the losses: the blocks of the first columns).
+// two (up to kTwoTerms tokens): dz in two bf16 terms, token t's second in row kTwoTerms + t. d_hidden and d_w take both (rows of
+// `hidden` twice in h2): a few tokens' roundings do not average (one token: gradients 2.9e-3 off in the root
+// mean square, now the outputs' own 1.7e-3), and the products' tiles have the room: 45 -> 47 us at 9 x 168 x 69,881. Rows between
+// are zeros.
 constexpr int kFewCols = 16384;
 __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                     const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
                                                     int V, int np, int shift, const Coefs k, float *__restrict__ factor,
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
-                                                    int32_t *__restrict__ n_valid, float *__restrict__ loss) {
+                                                    int32_t *__restrict__ n_valid, float *__restrict__ loss, int two,
+                                                    const uint4 *__restrict__ hidden, uint4 *__restrict__ h2, int d) {
   __shared__ float sh[96];
   __shared__ int last;
   pdl_start();
-  const int row = blockIdx.y;
+  const int row = blockIdx.y, first = blockIdx.x * kFewCols, end = min(V, first + kFewCols);
+  if (two && blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < d / 8; i += 256) {
+      const uint4 v = row < rows ? hidden[size_t(row) * (d / 8) + i] : make_uint4(0, 0, 0, 0);
+      h2[size_t(row) * (d / 8) + i] = v;
+      if (row < rows) h2[size_t(kTwoTerms + row) * (d / 8) + i] = v;
+    }
+  }
+  if (row >= rows) {  // (two)
+    for (int col = first + threadIdx.x * 8; col < end; col += 256 * 8)
+      e[(size_t(row) * pitch + col) / 8] = make_uint4(0, 0, 0, 0);
+    return;
+  }
   const float2 *p = part + size_t(row) * np;
   const int tgt = target[row];
   const bool ok = tgt >= 0 && tgt < V;
@@ -532,19 +560,20 @@ __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64
   float a, b, s0;
   k.get(1, a, b, s0);
   const float f0 = fmaf(b, l, a);
-  const int first = blockIdx.x * kFewCols, end = min(V, first + kFewCols);
 #pragma unroll 4
   for (int col = first + threadIdx.x * 8; col < end; col += 256 * 8) {
     uint4 *at = e + (size_t(row) * pitch + col) / 8;
-    *at = dz8(*at, __expf(p[col >> shift].x - l) * f0, tgt, col, V, k, l, x);
+    *at = dz8(*at, __expf(p[col >> shift].x - l) * f0, tgt, col, V, k, l, x, two ? at + size_t(kTwoTerms) * pitch / 8 : nullptr);
   }
   if (blockIdx.x == 0 && last_block(left, &last)) finish_losses<256>(lse, nll, target, rows, V, k, n_valid, loss, factor, sh);
 }
 
 // dh = sum of the splits' products: a lane a row of 32 x 8 values, and `team` (1 or 8) warps of a block to them, each adding up
 // every team-th split, the teams' sums in their order (few values of 64 splits were one chain of loads: 15 us at 9 x 168).
-__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int rows, int cols, int team,
-                                                    const float *__restrict__ factor, uint16_t *__restrict__ out) {
+// second: blocks of 32 rows further down lie the second terms' shares (0: none); prows rows in all.
+__global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ part, int splits, int rows, int prows, int second,
+                                                    int cols, int team, const float *__restrict__ factor,
+                                                    uint16_t *__restrict__ out) {
   __shared__ float sh[8][8][32];
   pdl_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = cols / 8;
@@ -553,12 +582,16 @@ __global__ void __launch_bounds__(256) vocab_dh_sum(const float *__restrict__ pa
   const bool in = row < rows;
   float s[8] = {};
   if (in) {
-    const size_t step = frag_index(1, 0, 0, rows, cols);
-    const float *p = part + frag_index(0, row, col, rows, cols) + (col % 32) * 32 + lane + (warp % team) * step;
+    const size_t step = frag_index(1, 0, 0, prows, cols), low = frag_index(0, 32 * second, 0, prows, cols);
+    const float *p = part + frag_index(0, row, col, prows, cols) + (col % 32) * 32 + lane + (warp % team) * step;
 #pragma unroll 2
     for (int k = warp % team; k < splits; k += team, p += team * step) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += p[32 * j];
+      if (second) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += p[low + 32 * j];
+      }
     }
   }
   if (team > 1) {
@@ -615,8 +648,9 @@ Plan grad_plan(int64_t rows, int d, int V, bool need_h, bool need_w) {
 }
 
 struct Layout {
-  int64_t factor, zt, part, kept, dh, dw, total;
+  int64_t factor, zt, part, kept, h2, dh, dw, total;
 };
+bool two_terms(int64_t T, int64_t piece) { return T > 0 && T <= kTwoTerms && T <= piece; }
 Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
   const Sizes z = sizes(T, V);
   const int64_t rows = std::min(piece, T), last = rows > 0 ? T % rows : 0;
@@ -629,13 +663,17 @@ Layout layout(int64_t T, int d, int V, int64_t piece, bool grad) {
   l.part = off;
   off += up256(rows * z.np * 8);
   if (grad) {
+    const bool two = two_terms(T, piece);
+    const int64_t rows_z = two ? kTwoTerms + rows : rows;
     l.kept = off;
-    off += up256(rows * z.pitch * 2);
+    off += up256(rows_z * z.pitch * 2);
+    l.h2 = off;
+    if (two) off += up256(rows_z * d * 2);
     int64_t n = 0;
-    for (int64_t r : {rows, last}) {
+    for (int64_t r : {rows_z, last}) {
       for (bool need_w : {false, true}) {
         const int s = r > 0 ? grad_plan(r, d, V, true, need_w).splits : 1;
-        if (s > 1) n = std::max(n, int64_t(frag_index(s, 0, 0, int(r), d)) * 4);
+        if (s > 1 || two) n = std::max(n, int64_t(frag_index(s, 0, 0, int(r), d)) * 4);
       }
     }
     l.dh = off;
@@ -675,11 +713,11 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
   int *left = reinterpret_cast<int *>(base + l.factor) + 1;
   float *zt = reinterpret_cast<float *>(base + l.zt);
   float2 *part = reinterpret_cast<float2 *>(base + l.part);
-  uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept);
+  uint16_t *kept = reinterpret_cast<uint16_t *>(base + l.kept), *h2 = reinterpret_cast<uint16_t *>(base + l.h2);
   float *dhp = reinterpret_cast<float *>(base + l.dh), *dwp = reinterpret_cast<float *>(base + l.dw);
   const Coefs k = {d_loss, z_coef};
   int st;
-  const bool whole = T > 0 && T <= kWholeTokens && T <= piece;
+  const bool whole = T > 0 && T <= kWholeTokens && T <= piece, two = grad && two_terms(T, piece);
   if (!whole) {
     MOE_LAUNCH("vocab_count", s, moe::launch_dep(vocab_count, 1, kSumThreads, 0, s, target, T, V, n_valid));
     if ((st = moe::launch_status(fn))) return st;
@@ -689,9 +727,10 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
   }
   const dg::Matrix mw = {w, 1, V, d, d, int64_t(V) * d};
   for (int64_t t0 = 0; t0 < T; t0 += piece) {
-    const int rows = int(std::min<int64_t>(piece, T - t0));
+    const int rows = int(std::min<int64_t>(piece, T - t0)), rows_z = two ? kTwoTerms + rows : rows;
     const dg::Matrix mh = {h + t0 * d, 1, rows, d, d, int64_t(rows) * d};
-    const dg::Matrix mz = {kept, 1, rows, V, z.pitch, rows * z.pitch};
+    const dg::Matrix mz = {kept, 1, rows_z, V, z.pitch, rows_z * z.pitch};
+    const dg::Matrix mhz = two ? dg::Matrix{h2, 1, rows_z, d, d, int64_t(rows_z) * d} : mh;  // the rows that go with dz's
     dg::Tiles t = {};
     t.mats = t.splits = 1;
     t.group = 8;
@@ -715,9 +754,10 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     else st = grad ? tokens(LogitsEpi<true>{l}) : tokens(LogitsEpi<false>{l});
     if (st) return st;
     if (grad && whole && T <= kFewTokens) {
-      MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, rows), 256, 0, s,
+      MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, two ? kTwoTerms : rows), 256, 0, s,
                                                     reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
-                                                    z.shift(), k, factor, lse, nll, left, n_valid, loss));
+                                                    z.shift(), k, factor, lse, nll, left, n_valid, loss, two ? 1 : 0,
+                                                    reinterpret_cast<const uint4 *>(h), reinterpret_cast<uint4 *>(h2), d));
       if ((st = moe::launch_status(fn))) return st;
     } else {
       MOE_LAUNCH("vocab_lse", s, moe::launch_dep(T <= kFewTokens ? vocab_lse<1> : vocab_lse<8>, l.blocks, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
@@ -734,15 +774,15 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
         if ((st = moe::launch_status(fn))) return st;
       }
     }
-    const Plan plan = grad_plan(rows, d, V, d_hidden != nullptr, d_w != nullptr);
+    const Plan plan = grad_plan(rows_z, d, V, d_hidden != nullptr, d_w != nullptr);
     OutEpi eh = {}, ew = {};
     dg::Tiles th = t;
     th.splits = plan.splits;
     uint16_t *out = d_hidden ? d_hidden + t0 * d : nullptr;
     if (d_hidden) {
-      eh.rows = rows; eh.cols = d; eh.factor = factor;
+      eh.rows = rows_z; eh.cols = d; eh.factor = factor;
       if ((st = dg::store64_map(&eh.out, out, false, 1, rows, d, d, int64_t(rows) * d, fn))) return st;
-      if (plan.splits > 1) eh.sum = dhp;
+      if (plan.splits > 1 || two) eh.sum = dhp;
     }
     if (d_w) {
       ew.rows = V; ew.cols = d; ew.factor = factor;
@@ -750,15 +790,15 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
       if (t0 > 0) ew.add = dwp;
       if (t0 + rows < T) ew.sum = dwp;
     }
-    if (d_hidden && d_w) st = dg::two_products<dg::Wide>("vocab_dh_dw", mz, mw, eh, th, mz, mh, ew, t, plan.head, s, fn);
+    if (d_hidden && d_w) st = dg::two_products<dg::Wide>("vocab_dh_dw", mz, mw, eh, th, mz, mhz, ew, t, plan.head, s, fn);
     else if (d_hidden) st = dg::product<dg::Wide, false, true, false>("vocab_dh", mz, mw, eh, th, s, fn);
-    else st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mh, ew, t, s, fn);
+    else st = dg::product<dg::Wide, true, true, false>("vocab_dw", mz, mhz, ew, t, s, fn);
     if (st) return st;
-    if (plan.splits > 1) {
+    if (eh.sum != nullptr) {
       const int64_t units = int64_t((rows + 31) / 32) * (d / 8);
       const int team = units <= 1216 ? 8 : 1, each = 8 / team;  // (eight blocks an SM)
       MOE_LAUNCH("vocab_dh_sum", s, moe::launch_dep(vocab_dh_sum, unsigned((units + each - 1) / each), 256, 0, s, dhp, plan.splits,
-                                                    rows, d, team, factor, out));
+                                                    rows, rows_z, two ? 1 : 0, d, team, factor, out));
       if ((st = moe::launch_status(fn))) return st;
     }
   }

@@ -132,6 +132,26 @@ def test_vocab_loss_with_gradients(T, d, V):
     check_vocab(out, h, w, t, 0.01, (0.7, 1.9))
 
 
+@pytest.mark.parametrize("T,d,V", [(1, 128, 300), (2, 2048, 77), (3, 264, 5000), (31, 72, 1000), (32, 136, 20001)])
+def test_vocab_gradients_of_few_tokens_are_rounded_once(T, d, V):
+    """Up to 32 tokens: dz in two terms (2^-16 left), so that what remains beside the outputs' half step is the kept
+    exponentials' 2^-11 (2^-25 of their block's maximum), exp's 2^-20 and what lse and the logits are off. The target's
+    own share a (p - 1) comes from nll: 2^-20 of a and the same."""
+    h, w, t = vocab_case(T, d, V, 3 * T + V, sure=0.7)
+    t[1:2] = -1
+    out = run_vocab(h, w, t)
+    dev_ok()
+    ref = O.vocab_loss(npf(h), npf(w), t.numpy(), 0.0, (1.0, 1.0))
+    tz, tl = loss_tolerance(npf(h), npf(w), ref)
+    ok, off = (t.numpy() >= 0), 2 * (tl + tz)
+    ddz = np.abs(ref["dz"]) * (2.0 ** -16 + 2.0 ** -11 + 2.0 ** -20 + off[:, None])
+    ddz[ok] += 2.0 ** -25 / ok.sum()
+    ddz[ok, t.numpy()[ok]] += (2.0 ** -20 + off[ok]) / ok.sum()
+    for name, k, err in [("d_hidden", V, lambda a: a @ np.abs(npf(w))), ("d_w", 64, lambda a: a.T @ np.abs(npf(h)))]:
+        tol = err(ddz) + (k / 16 + 66) * 2.0 ** -23 * err(np.abs(ref["dz"])) + U16 * np.abs(ref[name]) + 1e-38
+        assert (np.abs(out[name] - ref[name]) <= tol).all(), name
+
+
 @pytest.mark.parametrize("piece", [1, 100, 256, 299, 300, 1000])
 def test_vocab_pieces(piece):
     h, w, t = vocab_case(300, 72, 777, 5, ignored=0.3)
