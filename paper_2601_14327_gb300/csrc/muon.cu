@@ -358,18 +358,25 @@ __device__ __forceinline__ void load_u(const Source &s, size_t o, int left, floa
     for (int i = 0; i < 8; ++i) u[i] = s.nesterov ? fmaf(s.mu, m[i], u[i]) : m[i];
     return;
   }
+  // (loads without a condition: all in flight together)
+  uint32_t raw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) raw[i] = s.g[o + min(i, left - 1)];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u[i] = i < left ? __uint_as_float(raw[i] << 16) : 0.f;
+  if (s.m == nullptr) return;
+  float m[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m[i] = s.m[o + min(i, left - 1)];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m[i] = i < left ? m[i] : 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    u[i] = 0.f;
-    if (i >= left) continue;
-    u[i] = __uint_as_float(uint32_t(s.g[o + i]) << 16);
-    if (s.m == nullptr) continue;
-    float m = s.m[o + i];
     if (UPDATE) {
-      m = fmaf(s.mu, m, u[i]);
-      s.m[o + i] = m;
+      m[i] = fmaf(s.mu, m[i], u[i]);
+      if (i < left) s.m[o + i] = m[i];
     }
-    u[i] = s.nesterov ? fmaf(s.mu, m, u[i]) : m;
+    u[i] = s.nesterov ? fmaf(s.mu, m[i], u[i]) : m[i];
   }
 }
 
@@ -473,7 +480,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
 
 // ---------------------------------------------------------------- matrices of a short side up to 128: on the chip
 //
-// A cluster of up to eight CTAs takes a matrix through momentum, norm, all steps and the update. A CTA owns all n <= 128
+// A cluster of up to 16 CTAs takes a matrix through momentum, norm, all steps and the update. A CTA owns all n <= 128
 // rows of `cols` <= 384 columns of X (of X^T where rows > cols): X itself as fp32 accumulator in TMEM (128 lanes x cols), its
 // half-precision rounding in shared memory, where one copy serves both products: its 64-column blocks of 128-byte rows are a K-major
 // operand for X X^T (the reduction along the columns) and an MN-major one for B X (along the rows). Per step: the CTA's share of
@@ -486,7 +493,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
 // in fp32 (22 bits in the launches' form), and roundings to half precision are theirs.
 constexpr int kN = 128;           // rows, zero past n
 constexpr int kMaxCols = 384;     // of a CTA: with the 128 columns of the products all of TMEM's 512
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;   // (more than 8 where the device allows)
 constexpr int kSmallThreads = 512;   // four warps a TMEM lane quarter take 32-column chunks in turns
 constexpr int kLoN = 64;          // short side up to which X's second half-precision term is kept, in rows 64 to 127
 constexpr uint32_t kBlkBytes = kN * 128; // 128 rows of 64 halves
@@ -508,9 +515,6 @@ struct SmallArgs {
 __device__ __forceinline__ void st_cluster_v4(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ void st_cluster_v2(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("st.shared::cluster.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
-}
 __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
@@ -524,6 +528,94 @@ __device__ __forceinline__ uint32_t sw128(uint32_t block, int r, int q) {
   return block + uint32_t(r) * 128u + (uint32_t(q ^ (r & 7)) << 4);
 }
 
+// A warp's tile of 32 x 32 values of a matrix in memory, its first row and column r, c: with `vec` (rows of 16-byte multiples) a lane
+// has a row of 32 values, else a column. All loads are issued before the first is used (with a test beside each one they waited for
+// one another: 13,000 cycles for two tiles a warp of 128 x 2,048, now 4,600; 17,000 for three of 32 x 300, now 10,000).
+struct Tile {
+  int rows, cols, r, c, vec;
+  size_t at;      // this lane's first value
+  int n;          // rows of the tile under this lane (columns with vec: values right of it)
+  __device__ __forceinline__ Tile(int rows_, int cols_, int r_, int c_, int vec_, size_t m0, int lane)
+      : rows(rows_), cols(cols_), r(r_), c(c_), vec(vec_) {
+    const int rl = vec ? r + lane : r, cl = vec ? c : c + lane;
+    at = m0 + size_t(rl) * cols + cl;
+    n = rl < rows && cl < cols ? (vec ? cols - cl : rows - rl) : 0;
+    if (n == 0) at = m0;
+  }
+  // Value i down a column, past the end the last one: loads without a condition, all in flight together.
+  __device__ __forceinline__ size_t down(int i) const { return at + size_t(min(i, max(n - 1, 0))) * cols; }
+  __device__ __forceinline__ void load(const uint16_t *p, float (&v)[32]) const {
+    if (vec) {
+      uint4 q[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) q[g] = 8 * g < n ? *reinterpret_cast<const uint4 *>(p + at + 8 * g) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float o[8];
+        unpack8(q[g], o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * g + i] = o[i];
+      }
+    } else {
+      uint32_t q[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) q[i] = p[down(i)];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = i < n ? __uint_as_float(q[i] << 16) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void load(const float *p, float (&v)[32]) const {
+    if (vec) {
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const float4 q = 4 * g < n ? *reinterpret_cast<const float4 *>(p + at + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[4 * g] = q.x; v[4 * g + 1] = q.y; v[4 * g + 2] = q.z; v[4 * g + 3] = q.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = p[down(i)];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = i < n ? v[i] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void store(float *p, const float (&v)[32]) const {
+    if (vec) {
+#pragma unroll
+      for (int g = 0; g < 8; ++g)
+        if (4 * g < n)
+          *reinterpret_cast<float4 *>(p + at + 4 * g) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < n) p[at + size_t(i) * cols] = v[i];
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t *p, const float (&v)[32]) const {
+    if (vec) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = v[8 * g + i];
+        if (8 * g < n) stg_v4(p + at + 8 * g, pack8(o));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < n) p[at + size_t(i) * cols] = __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+    }
+  }
+};
+// 32 x 32 values of a warp turned round (row i to column i), through 4 KB.
+__device__ __forceinline__ void turn(float (&v)[32], uint32_t scratch, int lane) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) st_shared_f32(scratch + uint32_t(i * 32 + (lane ^ i)) * 4u, v[i]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = ld_shared_f32(scratch + uint32_t(lane * 32 + (i ^ lane)) * 4u);
+  __syncwarp();
+}
+
 __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p) {
   extern __shared__ uint8_t smem_raw[];
   const int mat = int(blockIdx.x) / p.ctas;
@@ -531,8 +623,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
   if (p.mask != nullptr && p.mask[mat / p.per] == 0) return;  // (the whole cluster)
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t misc = base, sA = base + kOffA, sB = base + kOffB, sX = base + kOffX, recv = base + kOffRecv;
-  // misc: TMEM address, barrier, sums of the cluster's CTAs [8][3], of the warps [16][3], what B's diagonal lost [128]
-  const uint32_t bar = misc + 8, sums = misc + 16, wsums = misc + 128, delta = misc + 384;
+  // misc: TMEM address, barrier, sums of the cluster's CTAs [16][3], of the warps [16][3], what B's diagonal lost [128]
+  const uint32_t bar = misc + 8, sums = misc + 16, wsums = misc + 256, delta = misc + 512;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = int(tc::cluster_ctarank()), ctas = p.ctas;
   const int row0 = (warp & 3) * 32, row = row0 + lane, group = warp >> 2;
@@ -572,34 +664,29 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
   // 32 x 32 fp32 a warp, where A and B are or will be
   const uint32_t scratch = sA + uint32_t(warp) * 4096u;
   const size_t m0 = size_t(mat) * p.s.rows * p.s.cols;
-  // In memory, X's columns lie together (a lane a column, turned round through scratch), or with `tall` its rows (a lane a row).
+  // A chunk of X (32 rows, a lane a row, of 32 columns from j0) lies in memory as it is, or with `tall` turned round.
+  const bool turned = (p.tall != 0) == (p.s.vec != 0);
+  auto tile = [&](int c) {
+    const int j0 = col_cta + 32 * c;
+    return Tile(p.s.rows, p.s.cols, p.tall ? j0 : row0, p.tall ? row0 : j0, p.s.vec, m0, lane);
+  };
 
   // ---- momentum, U into TMEM, sums of squares
   float q0 = 0.f, q1 = 0.f, q2 = 0.f;
+#pragma unroll 1
   for (int c = group; c < chunks; c += 4) {
-    const int j0 = col_cta + 32 * c;  // first of 32 columns of X
+    const Tile t = tile(c);
     float u[32];
-    // row of X (wide) or column (tall) i of the chunk, this lane the other index
-    const int other = p.tall ? row : j0 + lane;
-    const int end_i = p.tall ? p.k - j0 : p.n - row0;
-    const bool in = other < (p.tall ? p.n : p.k);
-    const size_t o = m0 + (p.tall ? size_t(j0) * p.s.cols + row : size_t(row0) * p.s.cols + j0 + lane);
-    float m[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      u[i] = m[i] = 0.f;
-      if (in && i < end_i) {
-        u[i] = __uint_as_float(uint32_t(p.s.g[o + size_t(i) * p.s.cols]) << 16);
-        if (p.s.m != nullptr) m[i] = p.s.m[o + size_t(i) * p.s.cols];
-      }
-    }
+    t.load(p.s.g, u);
     if (p.s.m != nullptr) {
+      float m[32];
+      t.load(p.s.m, m);
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         m[i] = fmaf(p.s.mu, m[i], u[i]);
-        if (in && i < end_i) p.s.m[o + size_t(i) * p.s.cols] = m[i];
         u[i] = p.s.nesterov ? fmaf(p.s.mu, m[i], u[i]) : m[i];
       }
+      t.store(p.s.m, m);
     }
     float r0 = 0.f, r1 = 0.f, r2 = 0.f;
 #pragma unroll
@@ -612,14 +699,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
     q0 += r0;
     q1 += r1;
     q2 += r2;
-    if (!p.tall) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) st_shared_f32(scratch + uint32_t(i * 32 + (lane ^ i)) * 4u, u[i]);
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 32; ++i) u[i] = ld_shared_f32(scratch + uint32_t(lane * 32 + (i ^ lane)) * 4u);
-      __syncwarp();
-    }
+    if (turned) turn(u, scratch, lane);
     tc::tmem_st_32x32b_x32(t_x + 32 * c, reinterpret_cast<const uint32_t(&)[32]>(u));
   }
   tc::tmem_st_wait();
@@ -689,7 +769,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
   for (int i = tid; i < int(2 * kBlkBytes / 16); i += kSmallThreads) tc::st_shared_v4(sA + 16u * i, make_uint4(0, 0, 0, 0));
   if (ctas > 1) tc::cluster_sync();  // before a peer's rows of A come
 
-  constexpr uint32_t kSquare = tc::idesc_f16_f32(kN, kN), kTimesX = tc::idesc_f16_f32(kN, 64, false, true);
+  constexpr uint32_t kSquare = tc::idesc_f16_f32(kN, kN);
   const float gram_scale = kScaleA / (p.scale * p.scale);
   const int mine = (p.n + ctas - 1) / ctas;  // rows of A that this CTA adds up
   const uint32_t recv_row = p.n <= kLoN ? kLoN * 4 : kN * 4;
@@ -725,10 +805,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
       // Rows to the CTA that adds them up: [source][row][128 or 64 values], 16-byte chunks at q ^ (row % 16). With second terms
       // the tensor cores' result is [hi hi^T, hi lo^T; lo hi^T, lo lo^T]: A's row is the first two's sum (one source) and the
       // third (another); the fourth is below its roundings.
-      const int a_row = p.lo ? row % kLoN : row, local = a_row / ctas;  // (rows are dealt out: all CTAs have some of few)
-      const bool second = p.lo && row >= kLoN;
-      const uint32_t to = tc::mapa(recv, uint32_t(a_row % ctas)) + uint32_t((rank + (second ? ctas : 0)) * mine + local) * recv_row;
-      if (group * 32 < p.n && (p.lo ? row0 % kLoN : row0) < p.n) {
+      // Through 4 KB a warp, so that eight lanes send 128 bytes of a row (a lane a row: 5,900 cycles for 128 rows among 8 CTAs, now
+      // 4,300).
+      const bool second = p.lo && row0 >= kLoN;
+      const int a_row0 = second ? row0 - kLoN : row0;
+      if (group * 32 < p.n && a_row0 < p.n) {
         uint32_t r[32];
         tc::tmem_ld_32x32b_x32(t_acc_w, r);
         tc::tmem_ld_wait();
@@ -739,30 +820,46 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
 #pragma unroll
           for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(r2[i]));
         }
-        if (a_row < p.n) {
+        const uint32_t stage = p.lo ? sB + uint32_t(warp) * 4096u : scratch;  // (lo: warps 0 to 7. A's place is written anew below)
 #pragma unroll
-          for (int g = 0; g < 8; ++g)
-            if (group * 32 + 4 * g < p.n)
-              st_cluster_v4(to + (uint32_t((group * 8 + g) ^ (local & 15)) << 4),
-                            make_float4(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]), __uint_as_float(r[4 * g + 2]),
-                                        __uint_as_float(r[4 * g + 3])));
+        for (int q = 0; q < 8; ++q)
+          tc::st_shared_v4(stage + uint32_t(lane) * 128u + (uint32_t(q ^ (lane & 7)) << 4), make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]));
+        __syncwarp();
+        const int q = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int rw = i + 8 * (lane >> 3), a_row = a_row0 + rw, local = a_row / ctas;  // (rows are dealt out: all CTAs have some of few)
+          const uint32_t to = tc::mapa(recv, uint32_t(a_row % ctas)) + uint32_t((rank + (second ? ctas : 0)) * mine + local) * recv_row;
+          const float4 v = ld_shared_f4(stage + uint32_t(rw) * 128u + (uint32_t(q ^ (rw & 7)) << 4));
+          if (a_row < p.n && group * 32 + 4 * q < p.n) st_cluster_v4(to + (uint32_t((group * 8 + q) ^ (local & 15)) << 4), v);
         }
       }
       tc::fence_before_sync();
       tc::cluster_sync();
-      const int quads = (p.n + 3) / 4, sources = p.lo ? 2 * ctas : ctas;
-      for (int i = tid; i < mine * 32; i += kSmallThreads) {
-        const int local_i = i / 32, q = i % 32, r_i = local_i * ctas + rank;
-        if (q >= quads || r_i >= p.n) continue;
-        const uint32_t from = recv + uint32_t(local_i) * recv_row + (uint32_t(q ^ (local_i & 15)) << 4);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int r = 0; r < sources; ++r) {
-          const float4 w = ld_shared_f4(from + uint32_t(r * mine) * recv_row);
-          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+      // Rows and columns past n are zeros: with second terms from the start, else written each time.
+      const int quads = (p.n + 3) / 4, sources = p.lo ? 2 * ctas : ctas, out_rows = p.lo ? mine : kN / ctas;
+      for (int i = tid; i < out_rows * 16; i += kSmallThreads) {
+        const int local = i / 16, q = i % 16 * 2, r_i = local * ctas + rank;
+        const bool in_row = r_i < p.n;
+        if (p.lo && (!in_row || q >= quads)) continue;
+        float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!in_row || q + h >= quads) continue;
+          const uint32_t from = recv + uint32_t(local) * recv_row + (uint32_t((q + h) ^ (local & 15)) << 4);
+#pragma unroll 4
+          for (int r = 0; r < sources; ++r) {
+            const float4 w = ld_shared_f4(from + uint32_t(r * mine) * recv_row);
+            v[h].x += w.x; v[h].y += w.y; v[h].z += w.z; v[h].w += w.w;
+          }
         }
-        const uint32_t lo = pack_half2(v.x * gram_scale, v.y * gram_scale), hi = pack_half2(v.z * gram_scale, v.w * gram_scale);
-        const uint32_t at = sw128(sA + uint32_t(q / 16) * kBlkBytes, r_i, (q % 16) / 2) + uint32_t(q & 1) * 8u;
-        for (int r = 0; r < ctas; ++r) st_cluster_v2(tc::mapa(at, r), lo, hi);
+        float4 o;
+        o.x = __uint_as_float(pack_half2(v[0].x * gram_scale, v[0].y * gram_scale));
+        o.y = __uint_as_float(pack_half2(v[0].z * gram_scale, v[0].w * gram_scale));
+        o.z = __uint_as_float(pack_half2(v[1].x * gram_scale, v[1].y * gram_scale));
+        o.w = __uint_as_float(pack_half2(v[1].z * gram_scale, v[1].w * gram_scale));
+        const uint32_t at = sw128(sA + uint32_t(q / 16) * kBlkBytes, r_i, (q % 16) / 2);
+        for (int r = 0; r < ctas; ++r) st_cluster_v4(tc::mapa(at, r), o);
       }
       asm volatile("fence.proxy.async;" ::: "memory");
       tc::cluster_sync();
@@ -809,11 +906,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
     // ---- B X onto a X
     publish();
     if (tid == 0) {
-      for (int b = 0; b < blocks; ++b)
+      for (int b = 0; b < blocks; b += 4) {  // up to 256 columns an instruction (256 in 64s: 2,260 cycles, now 1,490)
+        const uint32_t times_x = tc::idesc_f16_f32(kN, 64 * min(4, blocks - b), false, true);
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
           tc::mma_bf16(tmem + b * 64, tc::smem_desc_sw128(sB + (kk >> 2) * kBlkBytes + (kk & 3) * 32, 16, 1024),
-                       tc::smem_desc_sw128(sX + b * kBlkBytes + kk * 2048, kBlkBytes, 1024), kTimesX, 1u);
+                       tc::smem_desc_sw128(sX + b * kBlkBytes + kk * 2048, kBlkBytes, 1024), times_x, 1u);
+      }
       tc::mma_commit(bar);
     }
     const float dr = ld_shared_f32(delta + 4u * row);
@@ -843,40 +942,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small(const SmallArgs p
         continue;
       }
       // ---- the result (A and B are no longer needed: their place is scratch)
-      const int j0 = col_cta + col;
-      if (!p.tall) {
+      if (turned) turn(x, scratch, lane);
+      const Tile t = tile(c);
+      if (p.to.out != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) st_shared_f32(scratch + uint32_t(lane * 32 + (i ^ lane)) * 4u, x[i]);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = ld_shared_f32(scratch + uint32_t(i * 32 + (lane ^ i)) * 4u);
-        __syncwarp();
+        for (int i = 0; i < 32; ++i) x[i] *= p.to.inv;
+        t.store(p.to.out, x);
+        continue;
       }
-      const int other = p.tall ? row : j0 + lane;
-      const int end_i = other < (p.tall ? p.n : p.k) ? (p.tall ? p.k - j0 : p.n - row0) : 0;
-      const size_t o = m0 + (p.tall ? size_t(j0) * p.s.cols + row : size_t(row0) * p.s.cols + j0 + lane);
       float v[32];
-      if (p.to.out == nullptr) {
+      if (p.to.master != nullptr) t.load(p.to.master, v);
+      else t.load(p.to.w, v);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          v[i] = 0.f;
-          if (i < end_i) {
-            const size_t at = o + size_t(i) * p.s.cols;
-            v[i] = p.to.master != nullptr ? p.to.master[at] : __uint_as_float(uint32_t(p.to.w[at]) << 16);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        if (i >= end_i) continue;
-        const size_t at = o + size_t(i) * p.s.cols;
-        float y = x[i] * p.to.inv;
-        if (p.to.out == nullptr) {
-          y = fmaf(p.to.keep, v[i], -p.to.step * y);
-          if (p.to.master != nullptr) p.to.master[at] = y;
-        }
-        (p.to.out != nullptr ? p.to.out : p.to.w)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-      }
+      for (int i = 0; i < 32; ++i) v[i] = fmaf(p.to.keep, v[i], -p.to.step * (x[i] * p.to.inv));
+      if (p.to.master != nullptr) t.store(p.to.master, v);
+      t.store(p.to.w, v);
     }
     tc::tmem_st_wait();
   }
@@ -939,10 +1019,11 @@ const float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
 
 // Clusters of so many CTAs that are resident together (GPCs hold a number of SMs that clusters do not always divide), or 0.
 int small_fit(int ctas) {
-  static int fit[64][4] = {};  // of each device
-  int &n = fit[moe::device_slot()][ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3];
-  if (n) return n;
+  static int fit[64][kMaxCluster + 1] = {};  // of each device
+  int &n = fit[moe::device_slot()][ctas];
+  if (n) return n > 0 ? n : 0;
   if (cudaFuncSetAttribute(muon_small, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmallSmem)) != cudaSuccess) return 0;
+  if (cudaFuncSetAttribute(muon_small, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return 0;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = unsigned(ctas);
@@ -955,34 +1036,37 @@ int small_fit(int ctas) {
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   int k = 0;
-  if (cudaOccupancyMaxActiveClusters(&k, muon_small, &cfg) != cudaSuccess) return 0;
-  return n = k;
+  if (cudaOccupancyMaxActiveClusters(&k, muon_small, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    k = 0;
+  }
+  n = k > 0 ? k : -1;
+  return k;
 }
 int small_cols(int k, int ctas) { return ceil_div(ceil_div(k, ctas), 64) * 64; }
-// CTAs a matrix in the form on the chip, 0: launches. The form takes its phases one after another, an SM to a CTA: a wave of
-// clusters takes about 15 us and 0.1 a column; of many waves the launches, which overlap better, are as
-// fast (Muon step of 128 matrices 128 x 2,048: 746 us here in nine waves, 678 as launches; 31 updates of them, three: 190, 233).
-// MOE_MUON_SMALL=0 or 1 takes the launches, or wherever it fits the other form (tests and A/B measurements).
+// CTAs a matrix in the form on the chip, 0: launches, where it does not fit (the form is faster at every number of matrices: a step
+// of 19 of 29 x 2,132 114 us here, 280 as launches; of 128 of 128 x 2,048, nine waves, 649 and 695; of 300 of 2,048 x 128 1,468
+// and 1,489). The phases of a wave of clusters follow one another: about 33 us, 1 a CTA of the cluster (more to exchange) and
+// 0.065 a column (4 of 128 x 1,024: 48.5 us on 8 CTAs each, 52.5 on 16; 1 of 128 x 2,999: 66 and 61).
+// MOE_MUON_SMALL=0 takes the launches everywhere (tests and A/B measurements).
 int small_ctas(int n_mats, int n, int k) {
-  static const int forced = [] {
+  static const bool off = [] {
     const char *e = getenv("MOE_MUON_SMALL");
-    return e && (e[0] == '0' || e[0] == '1') && e[1] == 0 ? e[0] - '0' : -1;
+    return e && e[0] == '0' && e[1] == 0;
   }();
-  if (n > kN || forced == 0) return 0;
-  int best = 0, waves = 0;
+  if (n > kN || off) return 0;
+  int best = 0;
   double least = 0;
   for (int ctas = 1; ctas <= kMaxCluster; ctas *= 2) {
     const int cols = small_cols(k, ctas), fit = cols <= kMaxCols ? small_fit(ctas) : 0;
     if (!fit) continue;
-    const int w = ceil_div(n_mats, fit);
-    const double t = w * (15 + 0.1 * cols);
+    const double t = ceil_div(n_mats, fit) * (33 + ctas + 0.065 * cols);
     if (!best || t < least) {
       best = ctas;
-      waves = w;
       least = t;
     }
   }
-  return forced == 1 || waves <= 3 ? best : 0;
+  return best;
 }
 
 int run_small(int ctas, const Source &u, const Target &to, const uint8_t *mask, int n_mats, int per, const float *coef, int steps,
