@@ -291,24 +291,32 @@ template <bool LAST> struct StepEpi {
     }
     // Rows of odd length: a lane a column, so that a warp's accesses to memory lie together (a row a lane: ~5,400 cycles a chunk
     // in the place of ~1,300), through 32 x 32 fp32 values, column c of row r at c ^ r: no bank twice in either direction.
+    // What the weights were is loaded without a condition (past the end the last row and column again), all of it
+    // before the first is used: the five steps' products of 2 of 1,568 x 5,151 435 -> 283 us.
+    const bool in = col + w.lane < cols;
+    const int row0 = w.row - w.lane, last = min(32, rows - row0) - 1;
+    const size_t o0 = (size_t(caller(w.z)) * rows + row0) * cols + col + (in ? w.lane : 0);
+    float v[32];
+    if (to.master != nullptr) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) v[r] = to.master[o0 + size_t(min(r, last)) * cols];
+    } else if (to.out == nullptr) {
+#pragma unroll
+      for (int r = 0; r < 32; ++r) v[r] = __uint_as_float(uint32_t(to.w[o0 + size_t(min(r, last)) * cols]) << 16);
+    }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 32; ++i) st_shared_f32(stage + uint32_t(w.lane * 32 + (i ^ w.lane)) * 4u, x[i]);
     __syncwarp();
-    const size_t o0 = (size_t(caller(w.z)) * rows + (w.row - w.lane)) * cols + col + w.lane;
-    const int here = min(32, rows - (w.row - w.lane));
-    if (col + w.lane < cols) {
-#pragma unroll 4
-      for (int r = 0; r < here; ++r) {
-        const size_t at = o0 + size_t(r) * cols;
-        float y = ld_shared_f32(stage + uint32_t(r * 32 + (w.lane ^ r)) * 4u);
-        if (to.out == nullptr) {
-          const float v = to.master != nullptr ? to.master[at] : __uint_as_float(uint32_t(to.w[at]) << 16);
-          y = fmaf(to.keep, v, -to.step * y);
-          if (to.master != nullptr) to.master[at] = y;
-        }
-        (to.out != nullptr ? to.out : to.w)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-      }
+    uint16_t *out = to.out != nullptr ? to.out : to.w;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) {
+      float y = ld_shared_f32(stage + uint32_t(r * 32 + (w.lane ^ r)) * 4u);
+      if (to.out == nullptr) y = fmaf(to.keep, v[r], -to.step * y);
+      if (!in || r > last) continue;
+      const size_t at = o0 + size_t(r) * cols;
+      if (to.master != nullptr) to.master[at] = y;
+      out[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
     }
     __syncwarp();
   }
@@ -399,17 +407,12 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
   const int slot = blockIdx.y;
   if (live != nullptr && first + slot >= live[0]) return;
   const size_t m0 = size_t(live != nullptr ? live[1 + first + slot] : first + slot) * s.rows * s.cols;
-  const int cpr = (s.cols + 7) / 8, units = s.rows * cpr;  // (2^25 at most)
+  // The matrix lies together: eights from the first multiple of 8 on, whatever its rows' length (row by row, an element
+  // a load: 66 us for 2 of 1,568 x 5,151 with momentum, now 37), and what is left at its ends by one thread each.
+  const int total = s.rows * s.cols, head = min(total, int(-m0 & 7)), units = (total - head) / 8, ends = total - 8 * units;
   float t[3] = {};
-#pragma unroll 2
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += parts * 256) {
-    float u[8], q[3] = {};
-    if (s.vec) {
-      load_u<true>(s, m0 + size_t(i) * 8, 8, u);
-    } else {
-      const int r = i / cpr, col = (i - r * cpr) * 8;
-      load_u<true>(s, m0 + size_t(r) * s.cols + col, s.cols - col, u);
-    }
+  auto add = [&](const float (&u)[8]) {
+    float q[3] = {};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float up = u[j] * kUp, down = u[j] * kDown;
@@ -419,6 +422,19 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
     }
 #pragma unroll
     for (int j = 0; j < 3; ++j) t[j] += q[j];
+  };
+  float u[8];
+  Source flat = s;
+  flat.vec = 1;
+#pragma unroll 2
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += parts * 256) {
+    load_u<true>(flat, m0 + head + size_t(i) * 8, 8, u);
+    add(u);
+  }
+  if (blockIdx.x == 0 && int(threadIdx.x) < ends) {
+    flat.vec = 0;
+    load_u<true>(flat, m0 + (int(threadIdx.x) < head ? threadIdx.x : threadIdx.x + 8 * units), 1, u);
+    add(u);
   }
 #pragma unroll
   for (int j = 0; j < 3; ++j) {
@@ -1005,14 +1021,16 @@ bool sizes_ok(int n_mats, int rows, int cols) {
 
 int ceil_div(int64_t a, int64_t b) { return int((a + b - 1) / b); }
 
-// Whether a product of so many 256 x 256 tiles at most runs in 256 x 128 tiles (dg::Small).
+// Whether a product runs in 256 x 128 tiles (dg::Small): where so many of them are one for each pair at most (gram of 16 of 256 x 512,
+// 32 tiles: 11.1 us, in wide ones 12.3; of 2 of 1,568 x 5,151, 112: 55, in 56 wide ones 34).
 // MOE_DENSE_SMALL=0 or 1 forces either form (tests and A/B measurements).
+constexpr int kPairs = 76;   // CTA pairs
 bool small_tiles(long long tiles) {
   static const int forced = [] {
     const char *e = getenv("MOE_DENSE_SMALL");
     return e && (e[0] == '0' || e[0] == '1') && e[1] == 0 ? e[0] - '0' : -1;
   }();
-  return forced >= 0 ? forced == 1 : tiles <= 76;
+  return forced >= 0 ? forced == 1 : tiles <= kPairs;
 }
 
 const float kCoef[3] = {3.4445f, -4.7750f, 2.0315f};
@@ -1181,7 +1199,8 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
       if ((st = moe::launch_status(fn))) return st;
     }
     const int nt = ceil_div(n, 256);
-    const bool small_sq = small_tiles((long long)mats * nt * (nt + 1) / 2), small_x = small_tiles((long long)mats * nt * ceil_div(k, 256));
+    const bool small_sq = small_tiles((long long)mats * nt * (nt + 1)),
+               small_x = small_tiles((long long)mats * ceil_div(rows, 256) * ceil_div(cols, 128));
     dg::Tiles t = {};
     t.mats = mats; t.live = live; t.first = first; t.splits = 1; t.group = 8;
     for (int i = 0; i < steps; ++i) {
