@@ -347,10 +347,10 @@ struct Source {
   int rows, cols, vec;
 };
 
-// U's 8 values from element o on (0 past `left` of them). UPDATE: the momentum is new.
-template <bool UPDATE>
+// U's 8 values from element o on (0 past `left` of them). UPDATE: the momentum is new. VEC: all 8, o a multiple of 8.
+template <bool UPDATE, bool VEC>
 __device__ __forceinline__ void load_u(const Source &s, size_t o, int left, float (&u)[8]) {
-  if (s.vec) {
+  if (VEC) {
     unpack8(*reinterpret_cast<const uint4 *>(s.g + o), u);
     if (s.m == nullptr) return;
     float4 *pm = reinterpret_cast<float4 *>(s.m + o);
@@ -423,17 +423,25 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
 #pragma unroll
     for (int j = 0; j < 3; ++j) t[j] += q[j];
   };
-  float u[8];
-  Source flat = s;
-  flat.vec = 1;
+  int i = blockIdx.x * 256 + threadIdx.x;
+  if (s.m == nullptr) {  // four loads in flight (24 of 4,096 x 2,048: 78 -> 64 us; with momentum the bytes are in flight as it is)
+    for (; i + 3 * parts * 256 < units; i += 4 * parts * 256) {
+      float u[4][8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_u<true, true>(s, m0 + head + size_t(i + j * parts * 256) * 8, 8, u[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add(u[j]);
+    }
+  }
 #pragma unroll 2
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += parts * 256) {
-    load_u<true>(flat, m0 + head + size_t(i) * 8, 8, u);
+  for (; i < units; i += parts * 256) {
+    float u[8];
+    load_u<true, true>(s, m0 + head + size_t(i) * 8, 8, u);
     add(u);
   }
   if (blockIdx.x == 0 && int(threadIdx.x) < ends) {
-    flat.vec = 0;
-    load_u<true>(flat, m0 + (int(threadIdx.x) < head ? threadIdx.x : threadIdx.x + 8 * units), 1, u);
+    float u[8];
+    load_u<true, false>(s, m0 + (int(threadIdx.x) < head ? threadIdx.x : threadIdx.x + 8 * units), 1, u);
     add(u);
   }
 #pragma unroll
@@ -450,7 +458,9 @@ __global__ void __launch_bounds__(256) muon_norm(const Source s, const int *__re
   }
 }
 
-// hi and lo of U * scale / (|U|_F + eps).
+// hi and lo of U * scale / (|U|_F + eps). VEC: rows of 16-byte multiples (a form of its own: 40 registers, with the other's
+// loads 55, and 128 of 1,408 x 2,048 took 731 us in the place of 585).
+template <bool VEC>
 __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__restrict__ live, int first, int parts,
                                                   const float *__restrict__ sums, float scale, float eps, int pitch,
                                                   uint16_t *__restrict__ hi, uint16_t *__restrict__ lo) {
@@ -479,7 +489,7 @@ __global__ void __launch_bounds__(256) muon_split(const Source s, const int *__r
   for (int i = blockIdx.x * 256 + threadIdx.x; i < units; i += gridDim.x * 256) {
     const int r = i / cpr, col = (i - r * cpr) * 8;
     float u[8];
-    load_u<false>(s, m0 + size_t(r) * s.cols + col, s.cols - col, u);
+    load_u<false, VEC>(s, m0 + size_t(r) * s.cols + col, s.cols - col, u);
     uint32_t h[4], l[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -1193,7 +1203,7 @@ int run(const char *fn, const Source &src, const uint8_t *mask, int n_mats, int 
       MOE_LAUNCH("muon_norm", s, moe::launch_dep(muon_norm, dim3(parts, m), 256, 0, s, u, live, first + f, parts,
                                                  sums + size_t(f) * kParts * 3));
       if ((st = moe::launch_status(fn))) return st;
-      MOE_LAUNCH("muon_split", s, moe::launch_dep(muon_split, dim3(blocks, m), 256, 0, s, u, live, first + f, parts,
+      MOE_LAUNCH("muon_split", s, moe::launch_dep(u.vec ? muon_split<true> : muon_split<false>, dim3(blocks, m), 256, 0, s, u, live, first + f, parts,
                                                   sums + size_t(f) * kParts * 3, scale, eps, l.pitch, x[0] + f * xstep,
                                                   lo + f * xstep));
       if ((st = moe::launch_status(fn))) return st;
