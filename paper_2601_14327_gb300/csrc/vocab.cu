@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kWholeTokens = 2048;  // tokens up to which the last block of vocab_lse(_dz) counts the targets and sums the losses
 constexpr int kFewTokens = 512;     // tokens up to which vocab_lse_dz takes the place of vocab_lse and vocab_dz
-constexpr int kTwoTerms = 32;       // tokens up to which dz has two terms
+constexpr int kTwoTerms = 32;       // tokens up to which dz has two terms, and logits are summed more exactly
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
 struct Sizes {
@@ -137,7 +137,9 @@ template <int N> __device__ __forceinline__ uint4 halves8(const float (&z)[N], i
 }
 
 // Where the logits' epilogues write. lse and nll, fp32, were 8.8e-7 off at d = 1024 and 5.8e-6 at 7168 with one sum
-// over the features, whose errors point one way: hence kChunk.
+// over the features, whose errors point one way: hence kChunk. 512 features: 4.5e-7. Up to 32 tokens do not average over what is
+// left, and their products wait for memory: 128, 1.2e-7 (7 x 3,704 x 122,001: 166 -> 170 us; 2 x 5,288 x 1,768: 30 -> 34; the
+// products of 37 x 2,048 x 32,000 would take 2 us more, those of 2,039 x 1,024 x 50,257 149 us in the place of 116).
 struct Logits {
   CUtensorMap kept;        // the exponentials, with KEEP
   float2 *part;            // [rows, np]
@@ -149,8 +151,8 @@ struct Logits {
 };
 
 // Rows of the logits (tokens) by columns (entries): see the top of the file.
-template <bool KEEP> struct LogitsEpi : Logits {
-  static constexpr int kChunk = 512;
+template <bool KEEP, int CHUNK> struct LogitsEpi : Logits {
+  static constexpr int kChunk = CHUNK;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     constexpr int kBlk = BN / 2;  // a warp's half tile is a block
@@ -177,8 +179,8 @@ template <bool KEEP> struct LogitsEpi : Logits {
 // The same of few tokens, from the product's other side: rows are entries, columns tokens, and the tensor cores take 64 or 128
 // columns instead of the 256 rows that the tokens would leave empty (9 tokens of d 168, 69,881 entries: 25 -> 18 us).
 // 32 x 32 values change places through the staging buffers, so that a lane has 32 entries of a token: blocks of 32.
-template <bool KEEP> struct FewEpi : Logits {
-  static constexpr int kChunk = 512;
+template <bool KEEP, int CHUNK> struct FewEpi : Logits {
+  static constexpr int kChunk = CHUNK;
 
   template <int BN> __device__ __forceinline__ void run(dg::Warp &w, float (&z)[BN / 2]) const {
     const int v0 = w.row - w.lane, nv = min(32, V - v0);
@@ -625,6 +627,9 @@ inline int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
 // How dh and dW are computed: ranges of the vocabulary that dh's reduction is split into (a product of few rows has few
 // tiles, 2 at 256 x 512, for 76 CTA pairs), and what one of its tiles costs in tiles of dW, which share its launch. Estimated in
 // k-blocks of 128, ~0.57 us each: a tile's k-blocks and 3 for its start and end; the fp32 sums' way through memory and a launch more.
+// Up to 256 rows and with W and dW larger than L2, dh's k-blocks wait for memory: 0.8 us each, 0.97 where other pairs store
+// dW meanwhile (7 x 3,704 x 122,001, both gradients: 376 us in 5 ranges, 449 in 2, which 0.57 would ask for; 9 x 168 x 69,881 is
+// 3 us slower in more ranges).
 struct Plan {
   int splits, head;
 };
@@ -635,7 +640,8 @@ Plan grad_plan(int64_t rows, int d, int V, bool need_h, bool need_w) {
   Plan best = {1, 1};
   double least = 0;
   for (int s = 1; s <= 64 && s <= nkb; ++s) {
-    const double unit = double((nkb + s - 1) / s) + 3 + (s > 1 ? 5 : 0);
+    const double block = !need_w || rows > 256 || int64_t(V) * d < (int64_t(1) << 25) ? 1 : 10 * tiles * s < 9 * kPairs ? 1.7 : 1.4;
+    const double unit = double((nkb + s - 1) / s) * block + 3 + (s > 1 ? 5 : 0);
     double t = double((tiles * s + kPairs - 1) / kPairs) * unit;
     if (need_w) t = std::max(t, (double(tiles * s) * unit + double(tiles_w) * cost_w) / kPairs);
     if (s > 1) t += double(s) * double(rows) * d * 8 / 6.7e12 / 0.57e-6 + 6;
@@ -742,16 +748,16 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     if (grad && (st = few ? dg::store_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)
                           : dg::store64_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)))
       return st;
-    auto tokens = [&](auto e) {
-      return z.blk == 64 ? dg::product<dg::Narrow, false, false, false>("vocab_logits", mh, mw, e, t, s, fn)
-                         : dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn);
-    };
-    auto entries = [&](auto e) {
-      return T <= 64 ? dg::product<dg::Few64, false, false, false>("vocab_logits", mw, mh, e, t, s, fn)
-                     : dg::product<dg::Narrow, false, false, false>("vocab_logits", mw, mh, e, t, s, fn);
-    };
-    if (few) st = grad ? entries(FewEpi<true>{l}) : entries(FewEpi<false>{l});
-    else st = grad ? tokens(LogitsEpi<true>{l}) : tokens(LogitsEpi<false>{l});
+    auto tokens = [&](auto e) { return dg::product<dg::Wide, false, false, false>("vocab_logits", mh, mw, e, t, s, fn); };
+    auto half = [&](auto e) { return dg::product<dg::Narrow, false, false, false>("vocab_logits", mh, mw, e, t, s, fn); };
+    auto entries = [&](auto e) { return dg::product<dg::Narrow, false, false, false>("vocab_logits", mw, mh, e, t, s, fn); };
+    auto entries64 = [&](auto e) { return dg::product<dg::Few64, false, false, false>("vocab_logits", mw, mh, e, t, s, fn); };
+    if (few && T <= kTwoTerms) st = grad ? entries64(FewEpi<true, 128>{l}) : entries64(FewEpi<false, 128>{l});
+    else if (few && T <= 64) st = grad ? entries64(FewEpi<true, 512>{l}) : entries64(FewEpi<false, 512>{l});
+    else if (few) st = grad ? entries(FewEpi<true, 512>{l}) : entries(FewEpi<false, 512>{l});
+    else if (z.blk == 64 && T <= kTwoTerms) st = grad ? half(LogitsEpi<true, 128>{l}) : half(LogitsEpi<false, 128>{l});
+    else if (z.blk == 64) st = grad ? half(LogitsEpi<true, 512>{l}) : half(LogitsEpi<false, 512>{l});
+    else st = grad ? tokens(LogitsEpi<true, 512>{l}) : tokens(LogitsEpi<false, 512>{l});
     if (st) return st;
     if (grad && whole && T <= kFewTokens) {
       MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, two ? kTwoTerms : rows), 256, 0, s,
