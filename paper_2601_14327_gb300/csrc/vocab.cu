@@ -521,23 +521,23 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
 }
 
 // vocab_lse and vocab_dz of few tokens in one launch (512 tokens of 32,000 entries: 77 -> 73 us for the loss with its gradients;
-// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, 16,384 columns), each of which works
-// out the row's lse again (lse, nll and the losses: the blocks of the first columns).
+// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, `cols` columns), each of which works
+// out the row's lse again (lse, nll and the losses: the blocks of the first columns). cols: 4,096 for few rows (104 of 7,602 entries:
+// 10.4 us, in 16,384 12.6), whole rows for many (512 of 32,000: 18.3, in 4,096 26.5).
 // two (up to kTwoTerms tokens): dz in two bf16 terms, token t's second in row kTwoTerms + t. d_hidden and d_w take both (rows of
 // `hidden` twice in h2): a few tokens' roundings do not average (one token: gradients 2.9e-3 off in the root
 // mean square, now the outputs' own 1.7e-3), and the products' tiles have the room: 45 -> 47 us at 9 x 168 x 69,881. Rows between
 // are zeros.
-constexpr int kFewCols = 16384;
 __global__ void __launch_bounds__(256) vocab_lse_dz(uint4 *__restrict__ e, int64_t pitch, const float2 *__restrict__ part,
                                                     const float *__restrict__ zt, const int32_t *__restrict__ target, int rows,
                                                     int V, int np, int shift, const Coefs k, float *__restrict__ factor,
                                                     float *__restrict__ lse, float *__restrict__ nll, int *__restrict__ left,
-                                                    int32_t *__restrict__ n_valid, float *__restrict__ loss, int two,
+                                                    int32_t *__restrict__ n_valid, float *__restrict__ loss, int cols, int two,
                                                     const uint4 *__restrict__ hidden, uint4 *__restrict__ h2, int d) {
   __shared__ float sh[96];
   __shared__ int last;
   pdl_start();
-  const int row = blockIdx.y, first = blockIdx.x * kFewCols, end = min(V, first + kFewCols);
+  const int row = blockIdx.y, first = blockIdx.x * cols, end = min(V, first + cols);
   if (two && blockIdx.x == 0) {
     for (int i = threadIdx.x; i < d / 8; i += 256) {
       const uint4 v = row < rows ? hidden[size_t(row) * (d / 8) + i] : make_uint4(0, 0, 0, 0);
@@ -760,9 +760,11 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     else st = grad ? tokens(LogitsEpi<true, 512>{l}) : tokens(LogitsEpi<false, 512>{l});
     if (st) return st;
     if (grad && whole && T <= kFewTokens) {
-      MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + kFewCols - 1) / kFewCols, two ? kTwoTerms : rows), 256, 0, s,
+      const int grid_rows = two ? kTwoTerms : rows, per_row = std::max(1, std::min((V + 4095) / 4096, 4 * 152 / grid_rows));
+      const int cols = ((V + per_row - 1) / per_row + 2047) / 2048 * 2048;
+      MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + cols - 1) / cols, grid_rows), 256, 0, s,
                                                     reinterpret_cast<uint4 *>(kept), z.pitch, part, zt, target, rows, V, int(z.np),
-                                                    z.shift(), k, factor, lse, nll, left, n_valid, loss, two ? 1 : 0,
+                                                    z.shift(), k, factor, lse, nll, left, n_valid, loss, cols, two ? 1 : 0,
                                                     reinterpret_cast<const uint4 *>(h), reinterpret_cast<uint4 *>(h2), d));
       if ((st = moe::launch_status(fn))) return st;
     } else {
