@@ -22,7 +22,7 @@ MOE_DEV_ERR_DECL
 namespace {
 
 constexpr int kWholeTokens = 2048;  // tokens up to which the last block of vocab_lse(_dz) counts the targets and sums the losses
-constexpr int kFewTokens = 512;     // tokens up to which vocab_lse_dz takes the place of vocab_lse and vocab_dz
+constexpr int kFewTokens = 512;     // tokens up to which a token's pairs are summed by a block in any case
 constexpr int kTwoTerms = 32;       // tokens up to which dz has two terms, and logits are summed more exactly
 constexpr int kPairs = 76;   // CTA pairs that the split of a long reduction is planned for
 
@@ -38,6 +38,12 @@ bool narrow(int64_t T, int64_t V) { return ((T + 255) / 256) * ((V + 255) / 256)
 // Up to 128 tokens the logits are computed with the entries as rows (FewEpi), unless that would leave fewer tiles (104
 // tokens of d 416, 7,602 entries: 15 us, 13 in narrow tiles).
 bool entries_as_rows(int64_t T, int64_t V) { return T <= 128 && !narrow(T, V); }
+// Whether vocab_lse_dz takes the place of vocab_lse and vocab_dz: while the exponentials and dz stay in L2 (600 tokens of 32,000
+// entries, with gradients: 85 -> 76 us; 1,000 of 50,257: 124, in one launch 136), up to 1,024 tokens (beyond, the loss alone loses the
+// 2 us by the blocks that its gradients gain).
+bool one_pass(int64_t T, int64_t V) { return T <= kTwoTerms || (T <= 1024 && T * V < (int64_t(1) << 25)); }
+// Whether a token's pairs are summed by a block or by a warp: by all tokens again, and the same with and without gradients.
+bool by_block(int64_t T, int64_t V) { return T <= kFewTokens || one_pass(T, V); }
 Sizes sizes(int64_t T, int V) {
   const int blk = entries_as_rows(T, V) ? 32 : narrow(T, V) ? 64 : 128;
   return {blk, (int64_t(V) + blk - 1) / blk, (int64_t(V) + 63) / 64 * 64};
@@ -437,7 +443,7 @@ __device__ __forceinline__ void row_lse(const float2 *p, int np, bool has_target
   }
 }
 
-// A warp (up to 512 tokens in all a block: ROWS 1) per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
+// A warp (by_block: a block, ROWS 1) per token: lse and nll from the row's pairs. grad: the pairs' sums are overwritten by what a
 // block's kept exponentials are multiplied with, exp(maximum - lse) (a + b lse), 0 without a target. whole (few
 // tokens, one piece): the block that ends last (`left`: blocks still at work) counts the targets and sums the losses, a
 // launch each otherwise, 7 us of a loss of 37 tokens.
@@ -520,8 +526,7 @@ __global__ void __launch_bounds__(256) vocab_dz(uint4 *__restrict__ e, int64_t p
   *at = dz8(*at, f, target[row], col, V, k, lse[row], nll[row], nullptr);
 }
 
-// vocab_lse and vocab_dz of few tokens in one launch (512 tokens of 32,000 entries: 77 -> 73 us for the loss with its gradients;
-// at 2,039 of 50,257 the two launches are faster, 85 against 103 us): blocks over (row, `cols` columns), each of which works
+// vocab_lse and vocab_dz in one launch (one_pass): blocks over (row, `cols` columns), each of which works
 // out the row's lse again (lse, nll and the losses: the blocks of the first columns). cols: 4,096 for few rows (104 of 7,602 entries:
 // 10.4 us, in 16,384 12.6), whole rows for many (512 of 32,000: 18.3, in 4,096 26.5).
 // two (up to kTwoTerms tokens): dz in two bf16 terms, token t's second in row kTwoTerms + t. d_hidden and d_w take both (rows of
@@ -744,7 +749,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     Logits l = {};
     l.part = part; l.zt = zt; l.target = target + t0; l.rows = rows; l.V = V; l.np = int(z.np);
     l.left = left;
-    l.blocks = T <= kFewTokens ? rows : (rows + 7) / 8;
+    l.blocks = by_block(T, V) ? rows : (rows + 7) / 8;
     if (grad && (st = few ? dg::store_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)
                           : dg::store64_map(&l.kept, kept, true, 1, rows, V, z.pitch, rows * z.pitch, fn)))
       return st;
@@ -759,7 +764,7 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
     else if (z.blk == 64) st = grad ? half(LogitsEpi<true, 512>{l}) : half(LogitsEpi<false, 512>{l});
     else st = grad ? tokens(LogitsEpi<true, 512>{l}) : tokens(LogitsEpi<false, 512>{l});
     if (st) return st;
-    if (grad && whole && T <= kFewTokens) {
+    if (grad && whole && one_pass(T, V)) {
       const int grid_rows = two ? kTwoTerms : rows, per_row = std::max(1, std::min((V + 4095) / 4096, 4 * 152 / grid_rows));
       const int cols = ((V + per_row - 1) / per_row + 2047) / 2048 * 2048;
       MOE_LAUNCH("vocab_lse_dz", s, moe::launch_dep(vocab_lse_dz, dim3((V + cols - 1) / cols, grid_rows), 256, 0, s,
@@ -768,7 +773,8 @@ int run(const char *fn, const uint16_t *h, const uint16_t *w, const int32_t *tar
                                                     reinterpret_cast<const uint4 *>(h), reinterpret_cast<uint4 *>(h2), d));
       if ((st = moe::launch_status(fn))) return st;
     } else {
-      MOE_LAUNCH("vocab_lse", s, moe::launch_dep(T <= kFewTokens ? vocab_lse<1> : vocab_lse<8>, l.blocks, 256, 0, s, part, zt, target + t0, rows, V, int(z.np),
+      MOE_LAUNCH("vocab_lse", s, moe::launch_dep(by_block(T, V) ? vocab_lse<1> : vocab_lse<8>, l.blocks, 256, 0, s, part, zt,
+                                                 target + t0, rows, V, int(z.np),
                                                  grad ? 1 : 0, k, factor, lse + t0, nll + t0, whole ? 1 : 0, left, n_valid, loss));
       if ((st = moe::launch_status(fn))) return st;
       if (!grad) continue;

@@ -132,6 +132,17 @@ def test_vocab_loss_with_gradients(T, d, V):
     check_vocab(out, h, w, t, 0.01, (0.7, 1.9))
 
 
+@pytest.mark.parametrize("T,d,V", [(300, 16, 115000), (1024, 24, 130), (1500, 72, 300), (2048, 24, 130), (2049, 16, 200), (513, 64, 2000)])
+def test_vocab_either_side_of_the_forms_borders(T, d, V):
+    h, w, t = vocab_case(T, d, V, T + 2 * V, ignored=0.1, sure=0.5)
+    out = run_vocab(h, w, t, z_coef=0.02, d_loss=(1.3, 0.4))
+    alone = run_vocab(h, w, t, z_coef=0.02, backward=False)
+    dev_ok()
+    check_vocab(out, h, w, t, 0.02, (1.3, 0.4))
+    for k in ("loss", "nll", "lse"):
+        assert (out[k] == alone[k]).all(), k  # in the same order with and without gradients
+
+
 @pytest.mark.parametrize("T,d,V", [(1, 128, 300), (2, 2048, 77), (3, 264, 5000), (31, 72, 1000), (32, 136, 20001)])
 def test_vocab_gradients_of_few_tokens_are_rounded_once(T, d, V):
     """Up to 32 tokens: dz in two terms (2^-16 left), so that what remains beside the outputs' half step is the kept
