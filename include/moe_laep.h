@@ -225,8 +225,7 @@ int moe_vocab_loss(const uint16_t *hidden, const uint16_t *w_vocab, const int32_
                    size_t ws_bytes, moe_stream_t stream);
 
 /* Bytes of `ws` for moe_vocab_loss (grad 0) or moe_vocab_loss_grad (grad 1); 0 for sizes outside the limits.
- * With grad, min(piece, T) * (2 V + V/16, V/8 or V/4) bytes, the partial sums of d_hidden when that has few tiles, and
- * 4 V d bytes when piece < T. */
+ * With grad, min(piece, T) * (2 V + V/16, V/8 or V/4) bytes (up to 32 tokens in one piece 64 V + 2 d (32 + T) more), the partial sums of d_hidden when that has few tiles, and 4 V d bytes when piece < T. */
 size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad);
 
 /*
@@ -235,8 +234,8 @@ size_t moe_vocab_loss_workspace_size(int T, int d, int V, int piece, int grad);
  *              p = exp(z - lse);  0 for tokens without a target
  *   d_hidden[t,:] = sum_v dz[t,v] * w_vocab[v,:],   d_w[v,:] = sum_t dz[t,v] * hidden[t,:]
  * Arguments as in moe_vocab_loss; d_loss [2] fp32 (device) or NULL (ones); d_hidden [T,d], d_w [V,d] bf16
- * (overwritten; either may be NULL: not computed; not both). dz is held in bf16, a piece of `piece` tokens at a
- * time (the exponentials it is made from in half precision, relative to the largest of 128, 64 or 32 columns; p - 1 at the
+ * (overwritten; either may be NULL: not computed; not both). dz is held in bf16 (up to 32 tokens in one piece in two such
+ * terms: their roundings do not average), a piece of `piece` tokens at a time (the exponentials it is made from in half precision, relative to the largest of 128, 64 or 32 columns; p - 1 at the
  * target is exact to fp32 however sure the token is); the products accumulate in fp32. d_w's sum over pieces is
  * kept in fp32 in ws and rounded once. Results are bitwise reproducible; d_w's last bits depend on piece, d_hidden's on
  * it where its reduction is split (few tokens). `hidden` has to be finite also for tokens without a target: their rows

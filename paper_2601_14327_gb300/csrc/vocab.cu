@@ -3,9 +3,9 @@
 //   z = h W^T, lse = log sum exp z, nll = lse - z[target]
 //   dz = a (p - 1[target]) + b p with a = d_loss[0] / M, b = 2 d_loss[1] z_coef lse / M;  dh = dz W,  dW = dz^T h
 //
-// The logits' product runs over 256 x 256 tiles; a tile's epilogue reduces each row's 128 columns to their
-// maximum and the sum of exp(z - maximum) in fp32, and picks the target's logit out of it in fp32. Those pairs
-// (a 64th of the logits' bytes) are all that the loss needs.
+// The logits' product runs over 256 x 256 tiles (few tokens or entries: Sizes, FewEpi); a tile's epilogue reduces each row's
+// 128 columns to their maximum and the sum of exp(z - maximum) in fp32, and picks the target's logit out of it in fp32. Those
+// pairs (a 32nd of the bytes of bf16 logits) are all that the loss needs.
 // The gradient needs every exp(z - lse) once more, after the row's last tile. Making the logits again would be 2 T V d
 // operations beside the 6 T V d of the three products. Instead the epilogue also keeps exp(z - block maximum)
 // in half precision (values up to 1, 11 bits) for one piece of the tokens, and vocab_dz turns them into dz in place
